@@ -462,6 +462,130 @@ SN_API sn_status sn_conv2d_wino_noalloc(const void *x_dev, sn_schema schema, con
                                         int32_t c_out, int32_t pad, int32_t act, const float *w_dev,
                                         const float *bias_dev, void *y_dev, void *stream);
 
+/* ---------------- operators of a state-space block -------------------------
+ * The serving form of a state-space language model's block, used directly on
+ * device buffers (they are not layers of a graph): a dense layer with 4-bit
+ * weights, the norms around a block with its gate and residual scale, the short
+ * causal convolution and the selective scan, for prompts and for single tokens.
+ * Common to all of them:
+ *   - dtype is SN_F32, SN_F16 or SN_BF16; sums, statistics and states are fp32,
+ *     and outputs are rounded once (to nearest even);
+ *   - a *_stride is the distance of two rows (tokens) in elements, at least the
+ *     row's length; rows themselves are contiguous;
+ *   - outputs may not overlap inputs unless the call says so;
+ *   - calls are asynchronous on `stream` and allocate nothing; a call with no
+ *     rows, tokens or sequences returns SN_OK and launches nothing;
+ *   - errors: SN_EINVAL (NULL pointer, bad size, stride, dtype or option),
+ *     SN_EUNSUPPORTED (a size beyond the stated limits), SN_ECUDA.
+ * Sequences: `batch` sequences lie one behind the other in the token rows;
+ * offsets (device int32 [batch + 1], ascending from 0; NULL: every sequence has
+ * max_len tokens) says where each begins.  max_len is at least the longest
+ * one's length.  Sequences may be empty.  slots (device int32 [batch], NULL: the
+ * sequence's own index) names the entry of the state and kept buffers that a
+ * sequence uses; entries of two sequences differ; a slot outside [0, n_slots)
+ * stands for none: nothing is read from or written to the buffers for it. */
+
+/* Dense layer with 4-bit weights, y[m, j] = act(bias[j] + sum_k x[m, k] w[j, k]),
+ * w[j, k] = q[j, k] * scale[j, k / group], q in [-8, 7], group 32, 64 or 128 (the
+ * last group of a row may be cut off); scales fp16 or bf16.
+ * packed holds the weights in the kernels' own layout (sn_q4_bytes bytes of
+ * device memory aligned to 256, filled by sn_q4_pack).
+ * Numerics: for few rows codes times inputs are summed exactly (fp32 inputs in
+ * three parts) and each group's sum is scaled in fp32; for many rows the scaled
+ * weight is rounded to x's 16-bit type first (fp32 x: two parts, no rounding). */
+typedef struct {
+    int32_t n, k, group;  /* output features, input features, weights per scale */
+    int32_t scale_dtype;  /* SN_F16 or SN_BF16 */
+    int32_t act;          /* sn_act */
+    void *packed;
+    const float *bias;    /* device fp32 [n] or NULL (zeros) */
+} sn_q4_weights;
+SN_API sn_status sn_q4_bytes(int32_t n, int32_t k, int32_t group, int64_t *bytes);
+/* Symmetric codes and scales of float weights w [n][k] (dense), by group:
+ * scale = max |w| / 7 rounded to scale_dtype (1 for an all-zero group), code =
+ * clamp(rint(w / scale), -8, 7), the division in fp32.  codes: [n][(k + 1) / 2]
+ * bytes, two codes a byte in two's complement, the lower k in the low half;
+ * scales [n][ceil(k / group)]. */
+SN_API sn_status sn_q4_quantize(const void *w_dev, int32_t dtype, int32_t n, int32_t k, int32_t group,
+                                int32_t scale_dtype, uint8_t *codes, void *scales, void *stream);
+/* Lay out codes and scales (as sn_q4_quantize leaves them) into w->packed.
+ * Synchronises stream: the layout is for any stream once the call returns. */
+SN_API sn_status sn_q4_pack(const uint8_t *codes, const void *scales, const sn_q4_weights *w, void *stream);
+/* Device scratch that sn_q4_dense wants for `rows` rows of x (0: none). */
+SN_API sn_status sn_q4_workspace(const sn_q4_weights *w, int32_t dtype, int64_t rows, const void *x,
+                                 int64_t x_stride, int64_t *bytes);
+SN_API sn_status sn_q4_dense(const sn_q4_weights *w, int32_t dtype, int64_t rows, const void *x, int64_t x_stride,
+                             void *y, int64_t y_stride, void *work, int64_t work_bytes, void *stream);
+
+/* The norms behind and before a block with the block's gate, residual scale and
+ * sum, row by row:
+ *   t = post_norm(y * g)  (gate_after 0)   or   g * post_norm(y)  (gate_after 1)
+ *   sum = residual + scale * t,   normed = pre_norm(sum)
+ * g = gate, sigmoid(gate) or silu(gate) by `gate`; gate row m / rows_per_gate
+ * serves row m.  Norms: v / sqrt(mean(v^2) + eps) * weight + bias (rms), of
+ * v - mean(v) instead of v (layer).  post, pre, scale NULL: without that norm or
+ * factor.  residual NULL: the sum is scale * t, stored as dtype.  y NULL: the sum
+ * is the residual (a block's first norm).  sum_out NULL: not stored; normed NULL
+ * exactly when pre is.  normed is of the unrounded sum.  sum_out may be residual
+ * or y, and normed may be y, with equal strides. */
+typedef enum { SN_NORM_RMS = 0, SN_NORM_LAYER = 1 } sn_norm_kind;
+typedef enum { SN_GATE_NONE = 0, SN_GATE_LINEAR = 1, SN_GATE_SIGMOID = 2, SN_GATE_SILU = 3 } sn_gate;
+typedef struct {
+    int32_t dim, kind, gate, gate_after;
+    float eps;
+    const float *post, *post_bias, *pre, *pre_bias, *scale;  /* device fp32 [dim] */
+} sn_norm_params;
+SN_API sn_status sn_block_norm(const sn_norm_params *p, int32_t dtype, int64_t rows, const void *y, int64_t y_stride,
+                               const void *gate, int64_t gate_stride, int64_t rows_per_gate, int32_t res_dtype,
+                               const void *residual, int64_t residual_stride, void *sum_out, int64_t sum_stride,
+                               void *normed, int64_t normed_stride, void *stream);
+
+/* Causal convolution of every channel along the tokens of its sequence,
+ *   y[t, c] = act(bias[c] + sum_w weight[c][w] * x[t - width + 1 + w, c]),
+ * weight fp32 [channels][width], width 1 to 8, silu != 0: act(v) = v sigmoid(v).
+ * kept (x's dtype, [n_slots][width][channels], NULL: none) holds the last `width`
+ * inputs of a sequence, the input of position i at i % width.  pos (device int32
+ * [batch], NULL: zeros) is the position of each sequence's first token here: the
+ * inputs before it are read from kept (zeros before position 0), and the last
+ * ones of this call are stored there. */
+SN_API sn_status sn_causal_conv(int32_t dtype, int32_t channels, int32_t width, int32_t silu, const float *weight,
+                                const float *bias, int64_t tokens, int32_t batch, int64_t max_len,
+                                const int32_t *offsets, const void *x, int64_t x_stride, void *y, int64_t y_stride,
+                                void *kept, int32_t n_slots, const int32_t *slots, const int32_t *pos, void *stream);
+
+/* Selective scan.  Head h keeps a state S of head_dim x state fp32 values; with
+ * d = softplus(dt[t, h] + dt_bias[h]), at every token
+ *   S = exp(d a[h]) S + d x_t B_t^T,   y_t = S C_t + D[h] x_t,
+ * where a token's row of xbc is [heads][head_dim] of x, then [groups][state] of B
+ * and of C; head h reads group h / (heads / groups).  head_dim and state up to
+ * 256.  State buffers are fp32 [n_slots][heads][head_dim][state].
+ * sn_ssm_scan: all tokens of every sequence; state_in NULL: from zero; state_out
+ * NULL: the last state is not stored; state_out may be state_in.
+ * sn_ssm_step: one token of every sequence, from the convolution's input: xbc is
+ * convolved (conv_w, conv_b, width as in sn_causal_conv, with silu) from the kept
+ * inputs and pos, which are those of sn_causal_conv, in fp32 without rounding in
+ * between; kept and state_out are brought up to date (pos is not).  A sequence
+ * without a slot gets y = 0. */
+typedef struct {
+    int32_t heads, head_dim, groups, state, width;
+    const float *a, *d, *dt_bias;    /* device fp32 [heads]; d, dt_bias may be NULL (zeros) */
+    const float *conv_w, *conv_b;    /* sn_ssm_step only; conv_b may be NULL */
+} sn_ssm_params;
+SN_API sn_status sn_ssm_workspace(const sn_ssm_params *p, int32_t dtype, int64_t tokens, int32_t batch,
+                                  int64_t max_len, int64_t *bytes);
+SN_API sn_status sn_ssm_scan(const sn_ssm_params *p, int32_t dtype, int64_t tokens, int32_t batch, int64_t max_len,
+                             const int32_t *offsets, const void *xbc, int64_t xbc_stride, const void *dt,
+                             int64_t dt_stride, const float *state_in, float *state_out, int32_t n_slots,
+                             const int32_t *slots, void *y, int64_t y_stride, void *work, int64_t work_bytes,
+                             void *stream);
+SN_API sn_status sn_ssm_step(const sn_ssm_params *p, int32_t dtype, int32_t batch, const void *xbc,
+                             int64_t xbc_stride, const void *dt, int64_t dt_stride, void *kept,
+                             const float *state_in, float *state_out, int32_t n_slots, const int32_t *slots,
+                             const int32_t *pos, void *y, int64_t y_stride, void *stream);
+/* Waits for `stream` and reports whether a bounded wait of one of the library's
+ * kernels gave up since the last report (SN_ETIMEOUT, and the record is cleared). */
+SN_API sn_status sn_check_device(void *stream);
+
 SN_API const char *sn_last_error(void);
 
 #ifdef __cplusplus

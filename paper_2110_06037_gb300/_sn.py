@@ -70,6 +70,23 @@ class sn_profile_opts(C.Structure):
     _fields_ = [("warmup", C.c_int32), ("iters", C.c_int32), ("topk", C.c_int32), ("passes", C.c_int32)]
 
 
+class sn_q4_weights(C.Structure):
+    _fields_ = [("n", C.c_int32), ("k", C.c_int32), ("group", C.c_int32), ("scale_dtype", C.c_int32),
+                ("act", C.c_int32), ("packed", C.c_void_p), ("bias", C.c_void_p)]
+
+
+class sn_norm_params(C.Structure):
+    _fields_ = [("dim", C.c_int32), ("kind", C.c_int32), ("gate", C.c_int32), ("gate_after", C.c_int32),
+                ("eps", C.c_float), ("post", C.c_void_p), ("post_bias", C.c_void_p), ("pre", C.c_void_p),
+                ("pre_bias", C.c_void_p), ("scale", C.c_void_p)]
+
+
+class sn_ssm_params(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("head_dim", C.c_int32), ("groups", C.c_int32), ("state", C.c_int32),
+                ("width", C.c_int32), ("a", C.c_void_p), ("d", C.c_void_p), ("dt_bias", C.c_void_p),
+                ("conv_w", C.c_void_p), ("conv_b", C.c_void_p)]
+
+
 ALLOC_FN = C.CFUNCTYPE(C.c_void_p, C.c_size_t, C.c_void_p)
 FREE_FN = C.CFUNCTYPE(None, C.c_void_p, C.c_void_p)
 
@@ -113,6 +130,26 @@ SIGNATURES = {
                                C.c_void_p]),
     "sn_conv2d_wino_noalloc": (C.c_int, [C.c_void_p, sn_schema, C.POINTER(C.c_int64), C.c_int32, C.c_int32,
                                          C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "sn_q4_bytes": (C.c_int, [C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_int64)]),
+    "sn_q4_quantize": (C.c_int, [C.c_void_p] + [C.c_int32] * 5 + [C.c_void_p] * 3),
+    "sn_q4_pack": (C.c_int, [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "sn_q4_workspace": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int64, C.POINTER(C.c_int64)]),
+    "sn_q4_dense": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                              C.c_void_p, C.c_int64, C.c_void_p]),
+    "sn_block_norm": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                                C.c_int64, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                C.c_int64, C.c_void_p]),
+    "sn_causal_conv": (C.c_int, [C.c_int32] * 4 + [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_int64, C.c_void_p,
+                                                   C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                                   C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]),
+    "sn_ssm_workspace": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.POINTER(C.c_int64)]),
+    "sn_ssm_scan": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
+                              C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
+                              C.c_int64, C.c_void_p, C.c_int64, C.c_void_p]),
+    "sn_ssm_step": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
+                              C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
+                              C.c_int64, C.c_void_p]),
+    "sn_check_device": (C.c_int, [C.c_void_p]),
     "sn_last_error": (C.c_char_p, []),
 }
 NOALLOC_SCRATCH_BYTES = 32 * 1024 * 1024

@@ -1,0 +1,286 @@
+// The norms behind and before a block, fused with the block's gate, its residual
+// scale and the sum into the residual stream (sn_block_norm in include/sn.h):
+//   t = post(y g) or g post(y),  sum = residual + scale t,  normed = pre(sum).
+//
+// Bound by memory: y, gate and residual are read once, sum and normed written
+// once.  A row stays in registers between its statistics, its sum and its second
+// statistics, so nothing is read twice; mean and variance are two reductions over
+// the registers (the variance of v - mean, not a difference of squares).
+#include "kern_common.cuh"
+
+namespace sn {
+namespace k {
+
+namespace {
+
+constexpr int PIECE = 8;  // elements a thread handles together: 16 bytes of a 16-bit type
+
+struct NormP {
+    NormArgs a;
+    const float *post, *post_b, *pre, *pre_b, *scale;
+    int32_t d, kind, gate, after, vec;
+    float eps;
+};
+
+template <typename T>
+__device__ __forceinline__ void load_piece(float (&v)[PIECE], const T *row, int at, int d, bool vec) {
+    if (vec && at + PIECE <= d) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 a = *reinterpret_cast<const float4 *>(row + at), b = *reinterpret_cast<const float4 *>(row + at + 4);
+            v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+        } else {
+            uint4 u = *reinterpret_cast<const uint4 *>(row + at);
+            const T *e = reinterpret_cast<const T *>(&u);
+#pragma unroll
+            for (int i = 0; i < PIECE; ++i) v[i] = ldf(e + i);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PIECE; ++i) v[i] = at + i < d ? ldf(row + at + i) : 0.0f;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_piece(T *row, const float (&v)[PIECE], int at, int d, bool vec) {
+    if (vec && at + PIECE <= d) {
+        if constexpr (sizeof(T) == 4) {
+            *reinterpret_cast<float4 *>(row + at) = make_float4(v[0], v[1], v[2], v[3]);
+            *reinterpret_cast<float4 *>(row + at + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        } else {
+            uint4 u;
+            T *e = reinterpret_cast<T *>(&u);
+#pragma unroll
+            for (int i = 0; i < PIECE; ++i) e[i] = cvt<T>(v[i]);
+            *reinterpret_cast<uint4 *>(row + at) = u;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < PIECE; ++i)
+            if (at + i < d) stf(row + at + i, v[i]);
+    }
+}
+
+__device__ __forceinline__ float gate_value(float g, int kind) {
+    if (kind == SN_GATE_LINEAR) return g;
+    const float s = 1.0f / (1.0f + expf(-g));
+    return kind == SN_GATE_SIGMOID ? s : g * s;
+}
+
+// the sum over the row's TPR threads, the same in each of them
+template <int TPR>
+__device__ __forceinline__ float row_sum(float v, float *sh) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    if constexpr (TPR > 32) {
+        const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+        __syncthreads();  // the previous sum has been read
+        if (lane == 0) sh[warp] = v;
+        __syncthreads();
+        v = lane < TPR / 32 ? sh[lane] : 0.0f;
+#pragma unroll
+        for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    }
+    return v;
+}
+
+// norm of the values in registers, in place; entries behind the row's end are zero before and ignored after
+template <int TPR, int NP>
+__device__ __forceinline__ void norm_row(float (&v)[NP][PIECE], const NormP &p, const float *w, const float *b, int t,
+                                         float *sh) {
+    const float inv_d = 1.0f / (float)p.d;
+    if (p.kind == SN_NORM_LAYER) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) s += v[i][j];
+        const float mean = row_sum<TPR>(s, sh) * inv_d;
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) v[i][j] = (t + i * TPR) * PIECE + j < p.d ? v[i][j] - mean : 0.0f;
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int j = 0; j < PIECE; ++j) s = fmaf(v[i][j], v[i][j], s);
+    const float r = rsqrtf(row_sum<TPR>(s, sh) * inv_d + p.eps);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int at = (t + i * TPR) * PIECE;
+        if (at >= p.d) break;
+        float wv[PIECE], bv[PIECE];
+        load_piece(wv, w, at, p.d, p.vec);
+        if (b) load_piece(bv, b, at, p.d, p.vec);
+#pragma unroll
+        for (int j = 0; j < PIECE; ++j) v[i][j] = b ? fmaf(v[i][j] * r, wv[j], bv[j]) : v[i][j] * r * wv[j];
+    }
+}
+
+template <typename T, typename R, int TPR, int NP>
+__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) block_norm_kernel(const __grid_constant__ NormP p) {
+    constexpr int RPB = TPR < 128 ? 128 / TPR : 1;
+    __shared__ float sh[32];
+    const int t = threadIdx.x % TPR;
+    const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / TPR;
+    griddep_launch();
+    griddep_wait();
+    if (row >= p.a.rows) return;  // whole warps: TPR is 32 where a block has several rows
+    const T *y = static_cast<const T *>(p.a.y), *gate = static_cast<const T *>(p.a.gate);
+    const R *res = static_cast<const R *>(p.a.res);
+    float v[NP][PIECE], g[NP][PIECE], r[NP][PIECE];
+#pragma unroll
+    for (int i = 0; i < NP; ++i) {
+        const int at = (t + i * TPR) * PIECE;
+        if (y) load_piece(v[i], y + row * p.a.ldy, at, p.d, p.vec);
+        if (gate) load_piece(g[i], gate + (row / p.a.per_gate) * p.a.ldg, at, p.d, p.vec);
+        if (res) load_piece(r[i], res + row * p.a.ldr, at, p.d, p.vec);
+    }
+    if (y) {
+        if (gate) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int j = 0; j < PIECE; ++j) {
+                    // (a gate behind the row's end multiplies a zero)
+                    g[i][j] = (t + i * TPR) * PIECE + j < p.d ? gate_value(g[i][j], p.gate) : 1.0f;
+                    if (!p.after) v[i][j] *= g[i][j];
+                }
+        }
+        if (p.post) norm_row<TPR, NP>(v, p, p.post, p.post_b, t, sh);
+        if (gate && p.after) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int j = 0; j < PIECE; ++j) v[i][j] *= g[i][j];
+        }
+        if (p.scale) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i) {
+                const int at = (t + i * TPR) * PIECE;
+                if (at >= p.d) break;
+                float s[PIECE];
+                load_piece(s, p.scale, at, p.d, p.vec);
+#pragma unroll
+                for (int j = 0; j < PIECE; ++j) v[i][j] *= s[j];
+            }
+        }
+        if (res) {
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+#pragma unroll
+                for (int j = 0; j < PIECE; ++j) v[i][j] += r[i][j];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) v[i][j] = r[i][j];
+    }
+    if (p.a.sum) {
+#pragma unroll
+        for (int i = 0; i < NP; ++i) {
+            const int at = (t + i * TPR) * PIECE;
+            if (res) store_piece(static_cast<R *>(p.a.sum) + row * p.a.lds, v[i], at, p.d, p.vec);
+            else store_piece(static_cast<T *>(p.a.sum) + row * p.a.lds, v[i], at, p.d, p.vec);
+        }
+    }
+    if (p.pre) {
+        // what lies behind the row's end is zero again: the post norm's and scale's loops stop there, and sums of zeros are zero
+        norm_row<TPR, NP>(v, p, p.pre, p.pre_b, t, sh);
+#pragma unroll
+        for (int i = 0; i < NP; ++i)
+            store_piece(static_cast<T *>(p.a.normed) + row * p.a.ldn, v[i], (t + i * TPR) * PIECE, p.d, p.vec);
+    }
+}
+
+// Rows too long for registers: a block a row, each statistic a pass over it (the
+// later ones from L2), the values formed again in each pass.
+template <typename T, typename R>
+__global__ void __launch_bounds__(1024) block_norm_long_kernel(const __grid_constant__ NormP p) {
+    __shared__ float sh[32];
+    const int64_t row = blockIdx.x;
+    griddep_launch();
+    griddep_wait();
+    const T *y = p.a.y ? static_cast<const T *>(p.a.y) + row * p.a.ldy : nullptr;
+    const T *gate = p.a.gate ? static_cast<const T *>(p.a.gate) + (row / p.a.per_gate) * p.a.ldg : nullptr;
+    const R *res = p.a.res ? static_cast<const R *>(p.a.res) + row * p.a.ldr : nullptr;
+    const float inv_d = 1.0f / (float)p.d;
+    float m1 = 0.0f, r1 = 1.0f, m2 = 0.0f, r2 = 1.0f;
+    auto inner = [&](int i) {
+        float v = ldf(y + i);
+        return gate && !p.after ? v * gate_value(ldf(gate + i), p.gate) : v;
+    };
+    auto outer = [&](int i) {
+        float v = 0.0f;
+        if (y) {
+            v = inner(i);
+            if (p.post) v = fmaf((v - m1) * r1, p.post[i], p.post_b ? p.post_b[i] : 0.0f);
+            if (gate && p.after) v *= gate_value(ldf(gate + i), p.gate);
+            if (p.scale) v *= p.scale[i];
+        }
+        return res ? v + ldf(res + i) : v;
+    };
+    auto stats = [&](auto value, float &m, float &r) {
+        if (p.kind == SN_NORM_LAYER) {
+            float s = 0.0f;
+            for (int i = threadIdx.x; i < p.d; i += blockDim.x) s += value(i);
+            m = row_sum<1024>(s, sh) * inv_d;
+        }
+        float s = 0.0f;
+        for (int i = threadIdx.x; i < p.d; i += blockDim.x) {
+            const float c = value(i) - m;
+            s = fmaf(c, c, s);
+        }
+        r = rsqrtf(row_sum<1024>(s, sh) * inv_d + p.eps);
+    };
+    if (y && p.post) stats(inner, m1, r1);
+    if (p.pre) stats(outer, m2, r2);
+    for (int i = threadIdx.x; i < p.d; i += blockDim.x) {  // (an output may be an input: each element is read before it is written)
+        const float v = outer(i);
+        if (p.a.sum) {
+            if (res) stf(static_cast<R *>(p.a.sum) + row * p.a.lds + i, v);
+            else stf(static_cast<T *>(p.a.sum) + row * p.a.lds + i, v);
+        }
+        if (p.pre)
+            stf(static_cast<T *>(p.a.normed) + row * p.a.ldn + i, fmaf((v - m2) * r2, p.pre[i], p.pre_b ? p.pre_b[i] : 0.0f));
+    }
+}
+
+template <typename T, typename R, int TPR, int NP>
+cudaError_t launch_rows(const NormP &p, cudaStream_t st) {
+    constexpr int RPB = TPR < 128 ? 128 / TPR : 1;
+    return launch_pdl(block_norm_kernel<T, R, TPR, NP>, dim3((unsigned)((p.a.rows + RPB - 1) / RPB)),
+                      dim3(TPR < 128 ? 128 : TPR), 0, st, p);
+}
+
+template <typename T, typename R>
+cudaError_t launch_norm(const NormP &p, cudaStream_t st) {
+    const int pieces = (p.d + PIECE - 1) / PIECE;
+    if (pieces <= 32) return launch_rows<T, R, 32, 1>(p, st);
+    if (pieces <= 64) return launch_rows<T, R, 32, 2>(p, st);
+    if (pieces <= 128) return launch_rows<T, R, 128, 1>(p, st);
+    if (pieces <= 256) return launch_rows<T, R, 128, 2>(p, st);
+    if (pieces <= 512) return launch_rows<T, R, 256, 2>(p, st);
+    if (pieces <= 1024) return launch_rows<T, R, 512, 2>(p, st);
+    return launch_pdl(block_norm_long_kernel<T, R>, dim3((unsigned)p.a.rows), dim3(1024), 0, st, p);
+}
+
+}  // namespace
+
+cudaError_t block_norm(const sn_norm_params &q, int dt, int res_dt, const NormArgs &a, cudaStream_t st) {
+    NormP p{a, q.post, q.post_bias, q.pre, q.pre_bias, q.scale, q.dim, q.kind, q.gate, q.gate_after, 0, q.eps};
+    const int64_t es = dt == SN_F32 ? 4 : 2, rs = a.res ? (res_dt == SN_F32 ? 4 : 2) : es;
+    auto ok = [](const void *ptr, int64_t stride_bytes) {
+        return !ptr || (reinterpret_cast<uintptr_t>(ptr) % 16 == 0 && stride_bytes % 16 == 0);
+    };
+    p.vec = ok(a.y, a.ldy * es) && ok(a.gate, a.ldg * es) && ok(a.res, a.ldr * rs) && ok(a.sum, a.lds * rs) &&
+            ok(a.normed, a.ldn * es) && ok(q.post, 0) && ok(q.post_bias, 0) && ok(q.pre, 0) && ok(q.pre_bias, 0) &&
+            ok(q.scale, 0);
+    if (dt == SN_F32) return launch_norm<float, float>(p, st);
+    if (dt == SN_F16) return res_dt == SN_F32 ? launch_norm<__half, float>(p, st) : launch_norm<__half, __half>(p, st);
+    return res_dt == SN_F32 ? launch_norm<__nv_bfloat16, float>(p, st) : launch_norm<__nv_bfloat16, __nv_bfloat16>(p, st);
+}
+
+}  // namespace k
+}  // namespace sn

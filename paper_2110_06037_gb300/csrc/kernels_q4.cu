@@ -1,0 +1,394 @@
+// 4-bit weights: quantisation, layout, and the product with few rows of x
+// (sn_q4_quantize, sn_q4_pack, sn_q4_dense in include/sn.h; layout in q4_common.cuh).
+#include <algorithm>
+
+#include "q4_common.cuh"
+
+namespace sn {
+namespace k {
+
+namespace {
+
+// -------------------------------------------------------- codes and scales
+__device__ __forceinline__ float round_scale(float s, int bf16) {
+    return bf16 ? __bfloat162float(__float2bfloat16_rn(s)) : __half2float(__float2half_rn(s));
+}
+
+// a warp a group of a row; group <= 128, so a lane has at most 4 weights, neighbours in pairs
+template <typename T>
+__global__ void __launch_bounds__(128) q4_quantize_kernel(const T *__restrict__ w, int64_t n, int64_t k, int group, int bf16,
+                                                          uint8_t *__restrict__ codes, void *__restrict__ scales) {
+    const int64_t kg = (k + group - 1) / group, id = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
+    if (id >= n * kg) return;
+    const int64_t row = id / kg, k0 = id % kg * group;
+    const int lane = threadIdx.x % 32, len = (int)min((int64_t)group, k - k0);
+    float v[2][2], m = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int e = i * 64 + lane * 2 + j;
+            v[i][j] = e < len ? ldf(w + row * k + k0 + e) : 0.0f;
+            m = fmaxf(m, fabsf(v[i][j]));
+        }
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    float s = round_scale(fminf(__fdiv_rn(m, 7.0f), bf16 ? 3.3895314e38f : 65504.0f), bf16);  // (the types' largest)
+    if (!(s > 0.0f)) s = 1.0f;
+    if (lane == 0) {
+        if (bf16) static_cast<__nv_bfloat16 *>(scales)[id] = __float2bfloat16_rn(s);
+        else static_cast<__half *>(scales)[id] = __float2half_rn(s);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int e = i * 64 + lane * 2;
+        if (e >= len) continue;
+        int b = 0;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const int q = max(-8, min(7, __float2int_rn(__fdiv_rn(v[i][j], s))));
+            b |= (e + j < len ? q & 15 : 0) << (4 * j);
+        }
+        codes[row * ((k + 1) / 2) + (k0 + e) / 2] = (uint8_t)b;
+    }
+}
+
+__device__ __forceinline__ uint32_t code_at(const uint8_t *codes, int64_t row, int64_t c, int64_t n, int64_t k) {
+    if (row >= n || c >= k) return 8;
+    return ((codes[row * ((k + 1) / 2) + c / 2] >> (4 * (c % 2))) & 15) ^ 8;
+}
+
+__global__ void __launch_bounds__(256) q4_pack_kernel(const uint8_t *__restrict__ codes, int64_t n, int64_t k, int64_t kb,
+                                                      int64_t total, uint4 *__restrict__ out) {
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= total) return;
+    const int lane = (int)(id % 32), g = lane / 4, t = lane % 4;
+    const int64_t tile = id / 32, row = tile / kb * 16 + g, c0 = tile % kb * 64 + 8 * t;
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        w[i] = 0;
+        const int64_t c = c0 + 32 * (i / 2) + 4 * (i % 2);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int nib = (e / 2) * 2 + (e % 2) * 4;
+            w[i] |= code_at(codes, row, c + e, n, k) << (4 * nib);
+            w[i] |= code_at(codes, row + 8, c + e, n, k) << (4 * (nib + 1));
+        }
+    }
+    out[id] = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// a warp a row: its scales into place, and its power of two
+__global__ void __launch_bounds__(128) q4_pack_scales_kernel(const uint16_t *__restrict__ scales, int bf16, int64_t n,
+                                                             int64_t groups, int64_t kg, int64_t nt,
+                                                             uint16_t *__restrict__ out, float *__restrict__ row_pow) {
+    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
+    const int lane = threadIdx.x % 32, r = (int)(row % 16);
+    if (row >= nt * 16) return;
+    float m = 0.0f;
+    for (int64_t i = lane; i < kg; i += 32) {
+        const uint16_t s = row < n && i < groups ? scales[row * groups + i] : 0;
+        out[(row / 16 * kg + i) * 16 + (r % 8) * 2 + r / 8] = s;
+        const float v = bf16 ? __uint_as_float((uint32_t)s << 16) : __half2float(*reinterpret_cast<const __half *>(&s));
+        m = fmaxf(m, fabsf(v));
+    }
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) {
+        int e = 0;
+        if (m > 0.0f && m < INFINITY) frexpf(m, &e);
+        row_pow[row] = ldexpf(1.0f, max(-126, min(126, e)));
+    }
+}
+
+// ------------------------------------------------------------ few rows of x
+// Bound by reading the weights (half a byte a product and row): 16 x 8 x 16
+// products on the tensor cores with the codes as the A operand, x as columns of B
+// (rows of fp32 x as three bf16 columns each), one fp32 multiply-add a group to
+// scale its sum.  A warp runs along k over one 16-row tile, its weights straight
+// from global memory to registers in the operand's layout, U tiles in flight; the
+// block's part of x lies in shared memory.  k is split over the WK warps of a
+// block that share a tile and over the S blocks of a cluster, whose sums meet in a
+// fixed order.
+constexpr int WARPS = 8, U = 4;
+
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __nv_bfloat16) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float ld_cluster_f32(uint32_t caddr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(caddr) : "memory");
+    return v;
+}
+__device__ __forceinline__ uint4 ld_stream(const uint4 *p) {
+    uint4 v;
+    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+                 : "l"(p));
+    return v;
+}
+
+struct FewP {
+    Q4P q;
+    int32_t rows, wk, s, phase;  // warps along k, blocks a cluster, tiles along k in shared memory at once
+    int64_t ldx, ldy;
+};
+
+// T: the operands' type, X: x's and y's, NC: groups of 8 columns, G32: two scales a tile
+template <typename T, typename X, int NC, bool G32>
+__global__ void __launch_bounds__(WARPS * 32) q4_few_kernel(const __grid_constant__ FewP p, const X *__restrict__ x,
+                                                            X *__restrict__ y) {
+    constexpr int PL = std::is_same<X, float>::value ? 3 : 1, COLS = NC * 8;
+    extern __shared__ __align__(16) unsigned char smem[];
+    float *red = reinterpret_cast<float *>(smem);                  // [WARPS][16][COLS]
+    T *xs = reinterpret_cast<T *>(smem + WARPS * 16 * COLS * 4);   // [rows * PL][phase * 64 + 32]
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, g = lane / 4, t = lane % 4;
+    const int rank = (int)(blockIdx.x % (unsigned)p.s), wn = WARPS / p.wk;
+    const int nt0 = (int)(blockIdx.x / (unsigned)p.s) * wn, nt = nt0 + warp / p.wk, wki = warp % p.wk;
+    const int b0 = (int)((int64_t)p.q.kb * rank / p.s), b1 = (int)((int64_t)p.q.kb * (rank + 1) / p.s);
+    const bool live = nt < p.q.nt;
+    const int ldxs = p.phase * 64 + 32;  // (columns of x half a bank row apart)
+    float acc[NC][4];
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[c][i] = 0.0f;
+    griddep_launch();
+
+    const uint4 *codes = p.q.codes + (int64_t)(live ? nt : 0) * p.q.kb * 32 + lane;
+    const uint32_t *scales = p.q.scales + (int64_t)(live ? nt : 0) * p.q.kg * 8 + g;
+    uint4 cw[U];
+    uint32_t sw[U][G32 ? 2 : 1];
+    auto fetch = [&](int at, int end) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (at + u < end) {
+                cw[u] = ld_stream(codes + (int64_t)(at + u) * 32);
+                if constexpr (G32) {
+                    sw[u][0] = __ldg(scales + (int64_t)(2 * (at + u)) * 8);
+                    sw[u][1] = __ldg(scales + (int64_t)(2 * (at + u) + 1) * 8);
+                } else {
+                    sw[u][0] = __ldg(scales + (int64_t)((at + u) >> (p.q.glog - 6)) * 8);
+                }
+            }
+        }
+    };
+    bool first = true;
+    for (int ph = b0; ph < b1; ph += p.phase) {
+        const int pe = min(ph + p.phase, b1);
+        const int w0 = ph + (pe - ph) * wki / p.wk, w1 = live ? ph + (pe - ph) * (wki + 1) / p.wk : w0;
+        fetch(w0, w1);  // (the weights do not depend on the kernel before)
+        if (first) griddep_wait();
+        else __syncthreads();
+        first = false;
+        // the phase's columns of x, padded with zeros
+        const int width = (pe - ph) * 64;
+        for (int e = threadIdx.x; e < p.rows * width; e += WARPS * 32) {
+            const int m = e / width, c = e - m * width;
+            const int64_t kk = (int64_t)ph * 64 + c;
+            const float v = kk < p.q.k ? ldf(x + m * p.ldx + kk) : 0.0f;
+            if constexpr (PL == 3) {
+                const Planes pl = planes_of(v);
+#pragma unroll
+                for (int i = 0; i < 3; ++i) xs[(m * 3 + i) * ldxs + c] = pl.v[i];
+            } else {
+                xs[m * ldxs + c] = cvt<T>(v);
+            }
+        }
+        __syncthreads();
+        for (int at = w0; at < w1; at += U) {
+            uint4 cur[U];
+            uint32_t csw[U][G32 ? 2 : 1];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                cur[u] = cw[u];
+                csw[u][0] = sw[u][0];
+                if constexpr (G32) csw[u][1] = sw[u][1];
+            }
+            fetch(at + U, w1);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (at + u >= w1) break;
+                const uint32_t w[4] = {cur[u].x, cur[u].y, cur[u].z, cur[u].w};
+                uint32_t a[4][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) a[i][j] = code_pair<T>(w[i], j);
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const int col = c * 8 + g;
+                    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+                    if (col < p.rows * PL) {
+                        const uint4 *xp = reinterpret_cast<const uint4 *>(xs + col * ldxs + (at + u - ph) * 64 + 8 * t);
+                        lo = xp[0];
+                        hi = xp[4];
+                    }
+                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                    mma16816(d, a[0], lo.x, lo.y, T{});
+                    mma16816(d, a[1], lo.z, lo.w, T{});
+                    if constexpr (G32) {
+                        const float2 s = scale_pair(csw[u][0], p.q.scale_bf16);
+                        acc[c][0] = fmaf(d[0], s.x, acc[c][0]), acc[c][1] = fmaf(d[1], s.x, acc[c][1]);
+                        acc[c][2] = fmaf(d[2], s.y, acc[c][2]), acc[c][3] = fmaf(d[3], s.y, acc[c][3]);
+                        d[0] = d[1] = d[2] = d[3] = 0.0f;
+                    }
+                    mma16816(d, a[2], hi.x, hi.y, T{});
+                    mma16816(d, a[3], hi.z, hi.w, T{});
+                    const float2 s = scale_pair(csw[u][G32 ? 1 : 0], p.q.scale_bf16);
+                    acc[c][0] = fmaf(d[0], s.x, acc[c][0]), acc[c][1] = fmaf(d[1], s.x, acc[c][1]);
+                    acc[c][2] = fmaf(d[2], s.y, acc[c][2]), acc[c][3] = fmaf(d[3], s.y, acc[c][3]);
+                }
+            }
+        }
+    }
+    if (first) griddep_wait();  // a block without columns of its own still may not leave early
+    // the sums of the WK warps of a tile, then of the S blocks, in order
+    float *mine = red + warp * 16 * COLS;
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+        *reinterpret_cast<float2 *>(mine + g * COLS + c * 8 + 2 * t) = make_float2(acc[c][0], acc[c][1]);
+        *reinterpret_cast<float2 *>(mine + (g + 8) * COLS + c * 8 + 2 * t) = make_float2(acc[c][2], acc[c][3]);
+    }
+    __syncthreads();
+    const int outs = wn * 16 * p.rows;  // output o: row o % 16 of tile o / 16 % wn, row of x o / (16 wn)
+    auto block_sum = [&](int o) {
+        const int r = o % 16, tile = o / 16 % wn, m = o / (16 * wn);
+        float v = 0.0f;
+        for (int i = 0; i < p.wk; ++i)
+#pragma unroll
+            for (int pl = PL - 1; pl >= 0; --pl) v += red[((tile * p.wk + i) * 16 + r) * COLS + m * PL + pl];
+        return v;
+    };
+    auto finish = [&](int o, float v) {
+        const int j = (nt0 + o / 16 % wn) * 16 + o % 16, m = o / (16 * wn);
+        if (j < p.q.n) stf(y + m * p.ldy + j, act_apply(v + (p.q.bias ? p.q.bias[j] : 0.0f), p.q.act));
+    };
+    if (p.s == 1) {
+        for (int o = threadIdx.x; o < outs; o += WARPS * 32) finish(o, block_sum(o));
+        return;
+    }
+    float *part = reinterpret_cast<float *>(xs);  // the block's sums; x is done with
+    for (int o = threadIdx.x; o < outs; o += WARPS * 32) part[o] = block_sum(o);
+    tc::cluster_sync_all();
+    for (int o = threadIdx.x * p.s + rank; o < outs; o += WARPS * 32 * p.s) {
+        float v = 0.0f;
+        for (int r = 0; r < p.s; ++r) v += ld_cluster_f32(tc::mapa(tc::su32(part + o), (uint32_t)r));
+        finish(o, v);
+    }
+    tc::cluster_sync_all();  // peers may still be reading this block's sums
+}
+
+constexpr int FEW_COLS = 32;       // columns of B that the kernel has
+constexpr size_t X_SMEM = 64 << 10;  // shared memory for x
+
+template <typename T, typename X, int NC, bool G32>
+cudaError_t launch_few(const Q4P &q, int rows, const X *x, int64_t ldx, X *y, int64_t ldy, cudaStream_t st) {
+    constexpr int PL = std::is_same<X, float>::value ? 3 : 1;
+    // warps along k until there are about 16 a multiprocessor, at least 4 tiles each
+    FewP p{q, rows, 1, 1, 0, ldx, ldy};
+    const int64_t want = 16LL * num_sms();
+    while (p.wk < WARPS && (int64_t)q.nt * p.wk < want && q.kb >= 8 * p.wk) p.wk *= 2;
+    while (p.s < 8 && (int64_t)q.nt * p.wk * p.s < want && q.kb >= 8 * p.wk * p.s) p.s *= 2;
+    const int fit = (int)(X_SMEM / (rows * PL * 128)) - 1;  // tiles along k that fit
+    while (p.s < 8 && (q.kb + p.s - 1) / p.s > fit && q.kb >= 2 * p.s) p.s *= 2;
+    p.phase = std::min((q.kb + p.s - 1) / p.s, fit);
+    size_t smem = (size_t)WARPS * 16 * NC * 8 * 4;
+    smem += std::max((size_t)rows * PL * (p.phase * 64 + 32) * 2, (size_t)WARPS / p.wk * 16 * rows * 4);
+    auto kern = q4_few_kernel<T, X, NC, G32>;
+    static bool set = false;  // (idempotent)
+    if (!set) {
+        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                             (int)(X_SMEM + WARPS * 16 * NC * 8 * 4 + 1024));
+        if (e != cudaSuccess) return e;
+        set = true;
+    }
+    const int wn = WARPS / p.wk;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)((q.nt + wn - 1) / wn * p.s));
+    cfg.blockDim = dim3(WARPS * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = (unsigned)p.s;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.s > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, p, x, y);
+}
+
+template <typename T, typename X, bool G32>
+cudaError_t few_cols(const Q4P &q, int rows, const X *x, int64_t ldx, X *y, int64_t ldy, cudaStream_t st) {
+    constexpr int PL = std::is_same<X, float>::value ? 3 : 1;
+    switch ((rows * PL + 7) / 8) {
+    case 1: return launch_few<T, X, 1, G32>(q, rows, x, ldx, y, ldy, st);
+    case 2: return launch_few<T, X, 2, G32>(q, rows, x, ldx, y, ldy, st);
+    case 3: return launch_few<T, X, 3, G32>(q, rows, x, ldx, y, ldy, st);
+    default: return launch_few<T, X, 4, G32>(q, rows, x, ldx, y, ldy, st);
+    }
+}
+
+template <typename T, typename X>
+cudaError_t q4_few(const Q4P &q, int64_t rows, const X *x, int64_t ldx, X *y, int64_t ldy, cudaStream_t st) {
+    constexpr int PL = std::is_same<X, float>::value ? 3 : 1, cap = FEW_COLS / PL;
+    for (int64_t m = 0; m < rows; m += cap) {
+        const int now = (int)std::min<int64_t>(cap, rows - m);
+        const cudaError_t e = q.glog == 5 ? few_cols<T, X, true>(q, now, x + m * ldx, ldx, y + m * ldy, ldy, st)
+                                          : few_cols<T, X, false>(q, now, x + m * ldx, ldx, y + m * ldy, ldy, st);
+        if (e != cudaSuccess) return e;
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+size_t q4_bytes(int64_t n, int64_t k, int group) { return (size_t)q4_layout(n, k, group).bytes; }
+
+cudaError_t q4_quantize(const void *w, int dt, int64_t n, int64_t k, int group, int scale_dt, uint8_t *codes, void *scales,
+                        cudaStream_t st) {
+    const int64_t groups = n * ((k + group - 1) / group);
+    const dim3 grid((unsigned)((groups + 3) / 4));
+    SN_DT_SWITCH(dt, T, q4_quantize_kernel<T><<<grid, 128, 0, st>>>(static_cast<const T *>(w), n, k, group,
+                                                                    scale_dt == SN_BF16, codes, scales))
+    return cudaGetLastError();
+}
+
+cudaError_t q4_pack(const uint8_t *codes, const void *scales, const sn_q4_weights &w, cudaStream_t st) {
+    const Q4Layout l = q4_layout(w.n, w.k, w.group);
+    char *out = static_cast<char *>(w.packed);
+    const int64_t total = l.nt * l.kb * 32, groups = (w.k + w.group - 1) / w.group;
+    q4_pack_kernel<<<(unsigned)((total + 255) / 256), 256, 0, st>>>(codes, w.n, w.k, l.kb, total, reinterpret_cast<uint4 *>(out));
+    cudaError_t e = cudaGetLastError();
+    if (e != cudaSuccess) return e;
+    q4_pack_scales_kernel<<<(unsigned)(l.nt * 4), 128, 0, st>>>(static_cast<const uint16_t *>(scales), w.scale_dtype == SN_BF16,
+                                                                w.n, groups, l.kg, l.nt,
+                                                                reinterpret_cast<uint16_t *>(out + l.scales_at),
+                                                                reinterpret_cast<float *>(out + l.pow_at));
+    e = cudaGetLastError();
+    return e != cudaSuccess ? e : cudaStreamSynchronize(st);
+}
+
+size_t q4_workspace(const sn_q4_weights &, int, int64_t, const void *, int64_t) { return 0; }
+
+cudaError_t q4_dense(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx, void *y, int64_t ldy,
+                     void *, cudaStream_t st) {
+    const Q4P q = q4_params(w);
+    if (dt == SN_F32)
+        return q4_few<__nv_bfloat16, float>(q, rows, static_cast<const float *>(x), ldx, static_cast<float *>(y), ldy, st);
+    if (dt == SN_F16)
+        return q4_few<__half, __half>(q, rows, static_cast<const __half *>(x), ldx, static_cast<__half *>(y), ldy, st);
+    return q4_few<__nv_bfloat16, __nv_bfloat16>(q, rows, static_cast<const __nv_bfloat16 *>(x), ldx,
+                                                static_cast<__nv_bfloat16 *>(y), ldy, st);
+}
+
+}  // namespace k
+}  // namespace sn

@@ -1,0 +1,387 @@
+// Causal convolution, selective scan and token step of a state-space block
+// (sn_causal_conv, sn_ssm_scan, sn_ssm_step in include/sn.h).
+#include "kern_common.cuh"
+
+namespace sn {
+namespace k {
+
+namespace {
+
+struct Seq {  // one sequence of the batch
+    int64_t first, pos;  // its first token row, that token's position
+    int32_t len, slot;
+};
+__device__ __forceinline__ Seq sequence(const SeqArgs &q, int b) {
+    Seq s;
+    if (q.offsets) {  // (clipped to the rows there are, so that bad offsets read nothing else)
+        const int64_t n = q.tokens;
+        const int64_t i = q.offsets[b], j = q.offsets[b + 1];
+        s.first = i < 0 ? 0 : i > n ? n : i;
+        const int64_t e = j < s.first ? s.first : j > n ? n : j;
+        s.len = (int32_t)(e - s.first);
+    } else {
+        s.first = (int64_t)b * q.max_len;
+        s.len = (int32_t)q.max_len;
+    }
+    const int slot = q.slots ? q.slots[b] : b;
+    s.slot = slot >= 0 && slot < q.n_slots ? slot : -1;
+    s.pos = q.pos ? q.pos[b] : 0;
+    if (s.pos < 0) s.pos = 0;
+    return s;
+}
+
+__device__ __forceinline__ float silu(float v) { return v / (1.0f + expf(-v)); }
+// log(1 + e^v) without overflow, and exact where e^v is small
+__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v))); }
+
+constexpr int MAX_W = 8;
+
+// ------------------------------------------------------------- convolution
+// A thread takes V neighbouring channels (16 bytes where rows and weights allow)
+// over TT tokens, the last W - 1 inputs in registers: each input is read once,
+// and the W - 1 before the run once more (from L2).  Bound by memory.
+template <typename T, int W, int V, int TT>
+__global__ void __launch_bounds__(128) causal_conv_kernel(SeqArgs q, const T *__restrict__ x, int64_t ldx, T *__restrict__ y,
+                                                          int64_t ldy, T *kept, const float *__restrict__ w,
+                                                          const float *__restrict__ bias, int C, int act) {
+    griddep_launch();
+    griddep_wait();
+    const int cb = (C + 128 * V - 1) / (128 * V), run = blockIdx.x / cb;
+    const int c0 = ((blockIdx.x - run * cb) * 128 + threadIdx.x) * V;
+    const Seq s = sequence(q, blockIdx.y);
+    const int64_t t0 = (int64_t)run * TT;
+    if (c0 >= C || t0 >= s.len) return;
+    struct alignas(sizeof(T) * V) Piece {
+        T v[V];
+    };
+    float wt[W][V], b[V], h[W][V];  // h[j]: the input j + 1 - W tokens from the present one
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        b[v] = bias ? bias[c0 + v] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < W; ++j) wt[j][v] = w[(int64_t)(c0 + v) * W + j];
+    }
+    const T *xr = x + (s.first + t0) * ldx + c0;
+    T *yr = y + (s.first + t0) * ldy + c0;
+    T *kp = kept && s.slot >= 0 ? kept + (int64_t)s.slot * W * C + c0 : nullptr;
+#pragma unroll
+    for (int j = 1; j < W; ++j) {  // inputs before the run
+        const int back = W - j;
+        Piece p;
+        bool have = true;
+        if (t0 >= back) p = *reinterpret_cast<const Piece *>(xr - back * ldx);
+        else if (kp && s.pos + t0 >= back) p = *reinterpret_cast<const Piece *>(kp + (int64_t)((s.pos + t0 - back) % W) * C);
+        else have = false;
+#pragma unroll
+        for (int v = 0; v < V; ++v) h[j][v] = have ? ldf(p.v + v) : 0.0f;
+    }
+    const int n = (int)min((int64_t)TT, s.len - t0);
+    constexpr int U = 8;  // loads in flight
+    for (int t = 0; t < n; t += U) {
+        Piece in[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (t + u < n) in[u] = *reinterpret_cast<const Piece *>(xr + (int64_t)(t + u) * ldx);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (t + u < n) {
+                Piece out;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+#pragma unroll
+                    for (int j = 0; j + 1 < W; ++j) h[j][v] = h[j + 1][v];
+                    h[W - 1][v] = ldf(in[u].v + v);
+                    float a = b[v];
+#pragma unroll
+                    for (int j = 0; j < W; ++j) a = fmaf(wt[j][v], h[j][v], a);
+                    out.v[v] = cvt<T>(act ? silu(a) : a);
+                }
+                *reinterpret_cast<Piece *>(yr + (int64_t)(t + u) * ldy) = out;
+            }
+        }
+    }
+    // The thread of the first run also leaves the last W inputs behind: it alone
+    // has read the kept ones of its channels.
+    if (t0 == 0 && kp) {
+        for (int t = max(0, s.len - W); t < s.len; ++t)
+            *reinterpret_cast<Piece *>(kp + (int64_t)((s.pos + t) % W) * C) =
+                *reinterpret_cast<const Piece *>(x + (s.first + t) * ldx + c0);
+    }
+}
+
+template <typename T, int W>
+cudaError_t launch_conv(const SeqArgs &q, const T *x, int64_t ldx, T *y, int64_t ldy, T *kept, const float *w,
+                        const float *bias, int C, int act, cudaStream_t st) {
+    constexpr int V = 16 / sizeof(T), TT = 32;
+    const bool vec = C % V == 0 && ldx % V == 0 && ldy % V == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0 &&
+                     reinterpret_cast<uintptr_t>(y) % 16 == 0 && reinterpret_cast<uintptr_t>(kept) % 16 == 0;
+    const int per = vec ? V : 1;
+    const int64_t blocks = (q.max_len + TT - 1) / TT * ((C + 128 * per - 1) / (128 * per));
+    if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+    const dim3 grid((unsigned)blocks, (unsigned)q.batch);
+    if (vec) return launch_pdl(causal_conv_kernel<T, W, V, TT>, grid, dim3(128), 0, st, q, x, ldx, y, ldy, kept, w, bias, C, act);
+    return launch_pdl(causal_conv_kernel<T, W, 1, TT>, grid, dim3(128), 0, st, q, x, ldx, y, ldy, kept, w, bias, C, act);
+}
+
+template <typename T>
+cudaError_t conv_width(int W, const SeqArgs &q, const T *x, int64_t ldx, T *y, int64_t ldy, T *kept, const float *w,
+                       const float *bias, int C, int act, cudaStream_t st) {
+    switch (W) {
+#define SN_CASE(N) case N: return launch_conv<T, N>(q, x, ldx, y, ldy, kept, w, bias, C, act, st);
+        SN_CASE(1) SN_CASE(2) SN_CASE(3) SN_CASE(4) SN_CASE(5) SN_CASE(6) SN_CASE(7) SN_CASE(8)
+#undef SN_CASE
+    }
+    return cudaErrorInvalidValue;
+}
+
+// --------------------------------------------------------------------- scan
+struct SsmP {
+    SeqArgs q;
+    int32_t H, P, G, N, W;
+    const float *a, *d, *dt_bias, *conv_w, *conv_b;
+    int64_t ldx, lddt, ldy;
+    const float *s_in;
+    float *s_out;
+};
+
+// The recurrence itself in fp32.  A block takes 32 rows of one head's state of one
+// sequence; 8 lanes share a row, each with NL of its values in registers, lane l
+// the float4s l, l + 8, ... of the row.  Inputs come in runs of RT tokens through
+// shared memory.
+constexpr int RT = 16;
+template <typename T, int NL>
+__global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant__ SsmP p, const T *__restrict__ xbc,
+                                                           const T *__restrict__ dtv, T *__restrict__ y) {
+    constexpr int NPAD = NL * 8;
+    __shared__ __align__(16) float sb[RT][NPAD], sc[RT][NPAD];
+    __shared__ float sx[RT][32], sy[RT][32], sd[RT], sda[RT];
+    griddep_launch();
+    griddep_wait();
+    const int head = blockIdx.y, p0 = blockIdx.x * 32, tid = threadIdx.x;
+    const int row = p0 + tid / 8, l = tid % 8;
+    const Seq s = sequence(p.q, blockIdx.z);
+    const int grp = head / (p.H / p.G);
+    const float a = p.a[head], dskip = p.d ? p.d[head] : 0.0f, dtb = p.dt_bias ? p.dt_bias[head] : 0.0f;
+    float st[NL];
+    const int64_t srow = s.slot >= 0 ? (((int64_t)s.slot * p.H + head) * p.P + row) * p.N : -1;
+#pragma unroll
+    for (int i = 0; i < NL; ++i) {
+        const int n = ((i / 4) * 8 + l) * 4 + i % 4;
+        st[i] = p.s_in && srow >= 0 && row < p.P && n < p.N ? p.s_in[srow + n] : 0.0f;
+    }
+    const int np = min(32, p.P - p0);
+    for (int t0 = 0; t0 < s.len; t0 += RT) {
+        const int nt = min(RT, s.len - t0);
+        __syncthreads();
+        const T *r0 = xbc + (s.first + t0) * p.ldx;
+        for (int e = tid; e < RT * NPAD; e += 256) {
+            const int t = e / NPAD, n = e % NPAD;
+            const bool in = t < nt && n < p.N;
+            const T *r = r0 + (int64_t)t * p.ldx + p.H * p.P + grp * p.N + n;
+            sb[t][n] = in ? ldf(r) : 0.0f;
+            sc[t][n] = in ? ldf(r + p.G * p.N) : 0.0f;
+        }
+        for (int e = tid; e < RT * 32; e += 256) {
+            const int t = e / 32, i = e % 32;
+            sx[t][i] = t < nt && i < np ? ldf(r0 + (int64_t)t * p.ldx + head * p.P + p0 + i) : 0.0f;
+        }
+        if (tid < nt) {
+            const float d = softplus(ldf(dtv + (s.first + t0 + tid) * p.lddt + head) + dtb);
+            sd[tid] = d;
+            sda[tid] = expf(d * a);
+        }
+        __syncthreads();
+        for (int t = 0; t < nt; ++t) {
+            const float da = sda[t], x = sx[t][tid / 8], dx = sd[t] * x;
+            float acc = 0.0f;
+#pragma unroll
+            for (int i = 0; i < NL / 4; ++i) {
+                const float4 b = *reinterpret_cast<const float4 *>(&sb[t][(i * 8 + l) * 4]);
+                const float4 c = *reinterpret_cast<const float4 *>(&sc[t][(i * 8 + l) * 4]);
+                st[4 * i] = fmaf(st[4 * i], da, dx * b.x), acc = fmaf(st[4 * i], c.x, acc);
+                st[4 * i + 1] = fmaf(st[4 * i + 1], da, dx * b.y), acc = fmaf(st[4 * i + 1], c.y, acc);
+                st[4 * i + 2] = fmaf(st[4 * i + 2], da, dx * b.z), acc = fmaf(st[4 * i + 2], c.z, acc);
+                st[4 * i + 3] = fmaf(st[4 * i + 3], da, dx * b.w), acc = fmaf(st[4 * i + 3], c.w, acc);
+            }
+            acc += __shfl_xor_sync(0xffffffffu, acc, 4);
+            acc += __shfl_xor_sync(0xffffffffu, acc, 2);
+            acc += __shfl_xor_sync(0xffffffffu, acc, 1);
+            if (l == 0) sy[t][tid / 8] = fmaf(dskip, x, acc);
+        }
+        __syncthreads();
+        for (int e = tid; e < nt * 32; e += 256) {
+            const int t = e / 32, i = e % 32;
+            if (i < np) stf(y + (s.first + t0 + t) * p.ldy + head * p.P + p0 + i, sy[t][i]);
+        }
+    }
+    if (p.s_out && srow >= 0 && row < p.P) {
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+            const int n = ((i / 4) * 8 + l) * 4 + i % 4;
+            if (n < p.N) p.s_out[srow + n] = st[i];
+        }
+    }
+}
+
+template <typename T>
+cudaError_t launch_scan(const SsmP &p, const T *xbc, const T *dtv, T *y, cudaStream_t st) {
+    const dim3 grid((unsigned)((p.P + 31) / 32), (unsigned)p.H, (unsigned)p.q.batch);
+    if (p.N <= 32) return launch_pdl(ssm_scan_rec_kernel<T, 4>, grid, dim3(256), 0, st, p, xbc, dtv, y);
+    if (p.N <= 64) return launch_pdl(ssm_scan_rec_kernel<T, 8>, grid, dim3(256), 0, st, p, xbc, dtv, y);
+    if (p.N <= 128) return launch_pdl(ssm_scan_rec_kernel<T, 16>, grid, dim3(256), 0, st, p, xbc, dtv, y);
+    return launch_pdl(ssm_scan_rec_kernel<T, 32>, grid, dim3(256), 0, st, p, xbc, dtv, y);
+}
+
+// --------------------------------------------------------------------- step
+// One token: the state is read, updated and written once.  A block takes `rows`
+// rows of one head of one sequence; a warp's lanes lie along the state's rows (VEC
+// values a piece, VPL pieces a lane, `lpr` lanes a row), RU rows per lane in
+// flight.  The convolution of the block's own channels and of its group's B and C
+// is done again by every block of the group (its inputs come from L2); each
+// channel's new input is stored by one of them, at a place none of them reads.
+template <typename T, int VEC, int VPL>
+__global__ void __launch_bounds__(256) ssm_step_kernel(const __grid_constant__ SsmP p, const T *__restrict__ xbc,
+                                                       const T *__restrict__ dtv, T *kept, T *__restrict__ y, int rows,
+                                                       int lpr) {
+    __shared__ __align__(16) float sv[256 + 2 * 256];  // x of the block's rows, B, C
+    __shared__ float sd[2];
+    constexpr int RU = VPL * VEC >= 8 ? 2 : 4;
+    griddep_launch();
+    griddep_wait();
+    const int b = blockIdx.z, head = blockIdx.y, p0 = blockIdx.x * rows, tid = threadIdx.x;
+    const int np = min(rows, p.P - p0), grp = head / (p.H / p.G);
+    const int slot0 = p.q.slots ? p.q.slots[b] : b;
+    T *yr = y + (int64_t)b * p.ldy + head * p.P + p0;
+    if (slot0 < 0 || slot0 >= p.q.n_slots) {  // no slot: nothing to continue
+        for (int i = tid; i < np; i += 256) stf(yr + i, 0.0f);
+        return;
+    }
+    const int pos = max(p.q.pos ? p.q.pos[b] : 0, 0);
+    const int sub = tid % lpr, rpb = 256 / lpr;  // rows that the block handles at once
+    const int64_t base = (((int64_t)slot0 * p.H + head) * p.P + p0) * p.N;
+    const int nv = (p.N + VEC - 1) / VEC;  // (VEC divides N)
+    struct alignas(4 * VEC) Piece {
+        float v[VEC];
+    };
+    // the first rows' states, in flight before the convolution
+    Piece h[RU][VPL];
+    auto load = [&](int r0) {
+#pragma unroll
+        for (int u = 0; u < RU; ++u) {
+            const int r = r0 + u * rpb;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) {
+                const int c = sub + i * lpr;
+                if (p.s_in && r < np && c < nv) h[u][i] = *reinterpret_cast<const Piece *>(p.s_in + base + (int64_t)r * p.N + c * VEC);
+                else
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) h[u][i].v[e] = 0.0f;
+            }
+        }
+    };
+    load(tid / lpr);
+    if (tid == 0) {
+        const float d = softplus(ldf(dtv + (int64_t)b * p.lddt + head) + (p.dt_bias ? p.dt_bias[head] : 0.0f));
+        sd[0] = d;
+        sd[1] = expf(d * p.a[head]);
+    }
+    const int C = p.H * p.P + 2 * p.G * p.N;
+    const T *xr = xbc + (int64_t)b * p.ldx;
+    for (int e = tid; e < np + 2 * p.N; e += 256) {
+        const int n = e - np;
+        const int c = n < 0 ? head * p.P + p0 + e
+                            : p.H * p.P + (n < p.N ? grp * p.N + n : p.G * p.N + grp * p.N + n - p.N);
+        T *kp = kept + (int64_t)slot0 * p.W * C + c;
+        const float *w = p.conv_w + (int64_t)c * p.W;
+        float acc = p.conv_b ? p.conv_b[c] : 0.0f;
+        for (int j = 0; j + 1 < p.W; ++j) {
+            const int back = p.W - 1 - j;
+            if (pos >= back) acc = fmaf(w[j], ldf(kp + (int64_t)((pos - back) % p.W) * C), acc);
+        }
+        const T now = xr[c];
+        acc = fmaf(w[p.W - 1], ldf(&now), acc);
+        sv[n < 0 ? e : 256 + n + (n >= p.N ? 256 - p.N : 0)] = silu(acc);
+        if (n < 0 || (p0 == 0 && head % (p.H / p.G) == 0)) kp[(int64_t)(pos % p.W) * C] = now;
+    }
+    __syncthreads();
+    const float d = sd[0], da = sd[1], skip = p.d ? p.d[head] : 0.0f;
+    for (int r0 = tid / lpr; r0 - tid / lpr < np; r0 += RU * rpb) {  // (the same trips for every thread)
+        if (r0 != tid / lpr) load(r0);
+#pragma unroll
+        for (int u = 0; u < RU; ++u) {
+            const int r = r0 + u * rpb;
+            const float x = r < np ? sv[r] : 0.0f, dx = d * x;
+            float acc = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) {
+                const int c = sub + i * lpr;
+                if (c < nv) {
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        h[u][i].v[e] = fmaf(h[u][i].v[e], da, dx * sv[256 + c * VEC + e]);
+                        acc = fmaf(h[u][i].v[e], sv[512 + c * VEC + e], acc);
+                    }
+                    if (p.s_out && r < np) *reinterpret_cast<Piece *>(p.s_out + base + (int64_t)r * p.N + c * VEC) = h[u][i];
+                }
+            }
+            for (int o = lpr / 2; o; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
+            if (sub == 0 && r < np) stf(yr + r, fmaf(skip, x, acc));
+        }
+    }
+}
+
+template <typename T>
+cudaError_t launch_step(const SsmP &p, const T *xbc, const T *dtv, T *kept, T *y, cudaStream_t st) {
+    // enough blocks for two a multiprocessor, at least 8 rows each
+    int split = 1;
+    while ((int64_t)p.q.batch * p.H * split < 2 * num_sms() && p.P / (2 * split) >= 8) split *= 2;
+    const int rows = (p.P + split - 1) / split;
+    const dim3 grid((unsigned)((p.P + rows - 1) / rows), (unsigned)p.H, (unsigned)p.q.batch);
+    const bool vec = p.N % 4 == 0 && reinterpret_cast<uintptr_t>(p.s_in) % 16 == 0 && reinterpret_cast<uintptr_t>(p.s_out) % 16 == 0;
+    const int nv = vec ? p.N / 4 : p.N;
+    int lpr = 1;
+    while (lpr < 32 && lpr < nv) lpr *= 2;
+    const int vpl = (nv + lpr - 1) / lpr;
+#define SN_STEP(VEC, VPL) return launch_pdl(ssm_step_kernel<T, VEC, VPL>, grid, dim3(256), 0, st, p, xbc, dtv, kept, y, rows, lpr)
+    if (vec) {
+        if (vpl == 1) SN_STEP(4, 1);
+        SN_STEP(4, 2);
+    }
+    if (vpl == 1) SN_STEP(1, 1);
+    if (vpl <= 4) SN_STEP(1, 4);
+    SN_STEP(1, 8);
+#undef SN_STEP
+}
+
+SsmP ssm_params(const sn_ssm_params &c, const SeqArgs &q, int64_t ldx, int64_t lddt, const float *s_in, float *s_out,
+                int64_t ldy) {
+    return SsmP{q, c.heads, c.head_dim, c.groups, c.state, c.width, c.a, c.d, c.dt_bias, c.conv_w, c.conv_b,
+                ldx, lddt, ldy, s_in, s_out};
+}
+
+}  // namespace
+
+cudaError_t causal_conv(int dt, int channels, int width, int act, const float *w, const float *bias, const SeqArgs &q,
+                        const void *x, int64_t ldx, void *y, int64_t ldy, void *kept, cudaStream_t st) {
+    SN_DT_SWITCH(dt, T, return conv_width<T>(width, q, static_cast<const T *>(x), ldx, static_cast<T *>(y), ldy,
+                                             static_cast<T *>(kept), w, bias, channels, act, st))
+}
+
+size_t ssm_workspace(const sn_ssm_params &, int, const SeqArgs &) { return 0; }
+
+cudaError_t ssm_scan(const sn_ssm_params &c, int dt, const SeqArgs &q, const void *xbc, int64_t ldx, const void *dtv,
+                     int64_t lddt, const float *s_in, float *s_out, void *y, int64_t ldy, void *, cudaStream_t st) {
+    const SsmP p = ssm_params(c, q, ldx, lddt, s_in, s_out, ldy);
+    SN_DT_SWITCH(dt, T, return launch_scan<T>(p, static_cast<const T *>(xbc), static_cast<const T *>(dtv),
+                                              static_cast<T *>(y), st))
+}
+
+cudaError_t ssm_step(const sn_ssm_params &c, int dt, const SeqArgs &q, const void *xbc, int64_t ldx, const void *dtv,
+                     int64_t lddt, void *kept, const float *s_in, float *s_out, void *y, int64_t ldy, cudaStream_t st) {
+    const SsmP p = ssm_params(c, q, ldx, lddt, s_in, s_out, ldy);
+    SN_DT_SWITCH(dt, T, return launch_step<T>(p, static_cast<const T *>(xbc), static_cast<const T *>(dtv),
+                                              static_cast<T *>(kept), static_cast<T *>(y), st))
+}
+
+}  // namespace k
+}  // namespace sn

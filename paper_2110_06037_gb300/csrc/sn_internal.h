@@ -427,6 +427,32 @@ cudaError_t q8_maxpool(const LaunchArgs &a);
 cudaError_t q8_gap(const LaunchArgs &a);
 cudaError_t q8_add(const LaunchArgs &a);
 cudaError_t q8_mul(const LaunchArgs &a);
+// operators of a state-space block (declared in include/sn.h; arguments checked there)
+size_t q4_bytes(int64_t n, int64_t k, int group);
+cudaError_t q4_quantize(const void *w, int dt, int64_t n, int64_t k, int group, int scale_dt, uint8_t *codes,
+                        void *scales, cudaStream_t st);
+cudaError_t q4_pack(const uint8_t *codes, const void *scales, const sn_q4_weights &w, cudaStream_t st);
+size_t q4_workspace(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx);
+cudaError_t q4_dense(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx, void *y, int64_t ldy,
+                     void *work, cudaStream_t st);
+struct NormArgs {
+    const void *y, *gate, *res;
+    void *sum, *normed;
+    int64_t rows, ldy, ldg, per_gate, ldr, lds, ldn;
+};
+cudaError_t block_norm(const sn_norm_params &p, int dt, int res_dt, const NormArgs &a, cudaStream_t st);
+struct SeqArgs {  // sequences of a batch, and the entries of the kept and state buffers that they use
+    int64_t tokens, max_len;
+    int32_t batch, n_slots;
+    const int32_t *offsets, *slots, *pos;
+};
+cudaError_t causal_conv(int dt, int channels, int width, int silu, const float *w, const float *bias, const SeqArgs &q,
+                        const void *x, int64_t ldx, void *y, int64_t ldy, void *kept, cudaStream_t st);
+size_t ssm_workspace(const sn_ssm_params &p, int dt, const SeqArgs &q);
+cudaError_t ssm_scan(const sn_ssm_params &p, int dt, const SeqArgs &q, const void *xbc, int64_t ldx, const void *dtv,
+                     int64_t lddt, const float *s_in, float *s_out, void *y, int64_t ldy, void *work, cudaStream_t st);
+cudaError_t ssm_step(const sn_ssm_params &p, int dt, const SeqArgs &q, const void *xbc, int64_t ldx, const void *dtv,
+                     int64_t lddt, void *kept, const float *s_in, float *s_out, void *y, int64_t ldy, cudaStream_t st);
 // running max |x| of a float blob into *out (fp32 bits; zero it first)
 cudaError_t absmax(const void *x, int dt, int64_t n, unsigned *out, cudaStream_t st);
 }  // namespace k
