@@ -338,16 +338,12 @@ cudaError_t few_cols(const Q4P &q, int rows, const X *x, int64_t ldx, X *y, int6
 }
 
 template <typename T, typename X>
-cudaError_t q4_few(const Q4P &q, int64_t rows, const X *x, int64_t ldx, X *y, int64_t ldy, cudaStream_t st) {
-    constexpr int PL = std::is_same<X, float>::value ? 3 : 1, cap = FEW_COLS / PL;
-    for (int64_t m = 0; m < rows; m += cap) {
-        const int now = (int)std::min<int64_t>(cap, rows - m);
-        const cudaError_t e = q.glog == 5 ? few_cols<T, X, true>(q, now, x + m * ldx, ldx, y + m * ldy, ldy, st)
-                                          : few_cols<T, X, false>(q, now, x + m * ldx, ldx, y + m * ldy, ldy, st);
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
+cudaError_t q4_few(const Q4P &q, int rows, const X *x, int64_t ldx, X *y, int64_t ldy, cudaStream_t st) {
+    return q.glog == 5 ? few_cols<T, X, true>(q, rows, x, ldx, y, ldy, st) : few_cols<T, X, false>(q, rows, x, ldx, y, ldy, st);
 }
+
+// rows that fill the columns of the few-row kernel; more go to the tensor-core tiles
+int few_rows(int dt) { return dt == SN_F32 ? FEW_COLS / 3 : FEW_COLS; }
 
 }  // namespace
 
@@ -377,16 +373,20 @@ cudaError_t q4_pack(const uint8_t *codes, const void *scales, const sn_q4_weight
     return e != cudaSuccess ? e : cudaStreamSynchronize(st);
 }
 
-size_t q4_workspace(const sn_q4_weights &, int, int64_t, const void *, int64_t) { return 0; }
+size_t q4_workspace(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx) {
+    return rows <= few_rows(dt) ? 0 : q4_prompt_workspace(w, dt, rows, x, ldx);
+}
 
 cudaError_t q4_dense(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx, void *y, int64_t ldy,
-                     void *, cudaStream_t st) {
+                     void *work, cudaStream_t st) {
+    if (rows > few_rows(dt)) return q4_prompt(w, dt, rows, x, ldx, y, ldy, work, st);
     const Q4P q = q4_params(w);
+    const int m = (int)rows;
     if (dt == SN_F32)
-        return q4_few<__nv_bfloat16, float>(q, rows, static_cast<const float *>(x), ldx, static_cast<float *>(y), ldy, st);
+        return q4_few<__nv_bfloat16, float>(q, m, static_cast<const float *>(x), ldx, static_cast<float *>(y), ldy, st);
     if (dt == SN_F16)
-        return q4_few<__half, __half>(q, rows, static_cast<const __half *>(x), ldx, static_cast<__half *>(y), ldy, st);
-    return q4_few<__nv_bfloat16, __nv_bfloat16>(q, rows, static_cast<const __nv_bfloat16 *>(x), ldx,
+        return q4_few<__half, __half>(q, m, static_cast<const __half *>(x), ldx, static_cast<__half *>(y), ldy, st);
+    return q4_few<__nv_bfloat16, __nv_bfloat16>(q, m, static_cast<const __nv_bfloat16 *>(x), ldx,
                                                 static_cast<__nv_bfloat16 *>(y), ldy, st);
 }
 

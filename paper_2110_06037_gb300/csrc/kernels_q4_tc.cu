@@ -1,0 +1,551 @@
+// 4-bit weights with many rows of x, on the 5th-generation tensor cores
+// (sn_q4_dense in include/sn.h; layout in q4_common.cuh).
+//
+//   D[m, j] = sum_k x[m, k] * w[j, k],  w = q * scale rounded to the operand type
+//
+// A tile is 128 G rows of x by BN outputs, accumulated in TMEM over steps of 64
+// columns.  x comes by TMA; the weights are expanded in the kernel: a warp reads a
+// 16 x 64 tile of codes (512 contiguous bytes, four steps ahead, in registers),
+// makes codes exact 16-bit values, multiplies by the group's scale in packed
+// 16-bit arithmetic, one rounding, and writes the operand's 128-byte-swizzled rows
+// into the stage.  Codes are a quarter of the bytes that 16-bit weights would
+// move, and an SM expands only the BN / G rows it stages.
+// G = 2: a CTA pair shares a tile of 256 rows; each stages 128 rows of x and half
+// of the weights, which halves what a tile reads through L2 and expands per MMA.
+//
+// fp16 operands: scales are divided by their row's power of two (and multiplied by
+// 2^12), so that a product neither overflows nor, for groups within 2^-26 of the
+// row's largest scale, loses bits; the epilogue multiplies it back.
+// Scales that are not values of the operand type go in as two parts (a product
+// with the small one, a fused multiply-add with the large one).
+// fp32 x: three bf16 planes of x (written to scratch by a first kernel) times two
+// bf16 parts of w, which hold q * scale exactly; of the six products the smallest
+// (2^-25 and less) is left out.  One k step then is five.  (A fourth plane is the
+// first with zeros for what is not finite: the second part of w is often 0.)
+//
+// Warps: 0 loads x and allocates TMEM, 1 issues the MMAs (of the pair's leader), 4
+// to 7 drain the accumulators (two, so that a tile's epilogue overlaps the next
+// tile's products), 8 to 15 expand weights.  Waits are bounded; one that expires
+// records its cause in the library's error word and stops the pair.
+#include <algorithm>
+
+#include "q4_common.cuh"
+
+namespace sn {
+namespace k {
+
+namespace {
+
+using namespace tc;
+
+constexpr int Q4_STAGES = 6, Q4_THREADS = 512, Q4_EXPAND = 8, Q4_AHEAD = 4;
+constexpr uint32_t Q4_A_BYTES = BM * BK * 2, Q4_B_BYTES = 128 * BK * 2, Q4_STAGE = Q4_A_BYTES + Q4_B_BYTES;
+constexpr uint32_t Q4_OUT_ROW = 128 + 16;  // staged output row: 32 values, and 16 bytes against bank conflicts
+constexpr size_t Q4_SMEM = Q4_STAGES * (size_t)Q4_STAGE + 4 * 32 * Q4_OUT_ROW + 1024;
+
+struct PromptP {
+    Q4P q;
+    int64_t rows, ldy;
+    int32_t bn, mtiles, ntiles, steps;  // outputs a tile, tiles, k steps (five a column block for fp32)
+    int32_t plane_rows;                 // fp32: rows of a plane of x
+    int32_t parts;                      // scales in two parts
+    int32_t vec_out;
+    int *err;
+    long long wait_limit;
+};
+
+template <typename T>
+__device__ __forceinline__ uint32_t mul2(uint32_t a, uint32_t b);
+template <>
+__device__ __forceinline__ uint32_t mul2<__half>(uint32_t a, uint32_t b) {
+    const __half2 r = __hmul2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+template <>
+__device__ __forceinline__ uint32_t mul2<__nv_bfloat16>(uint32_t a, uint32_t b) {
+    const __nv_bfloat162 r = __hmul2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+template <typename T>
+__device__ __forceinline__ uint32_t fma2(uint32_t a, uint32_t b, uint32_t c);
+template <>
+__device__ __forceinline__ uint32_t fma2<__half>(uint32_t a, uint32_t b, uint32_t c) {
+    const __half2 r = __hfma2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b), *reinterpret_cast<__half2 *>(&c));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+template <>
+__device__ __forceinline__ uint32_t fma2<__nv_bfloat16>(uint32_t a, uint32_t b, uint32_t c) {
+    const __nv_bfloat162 r = __hfma2(*reinterpret_cast<__nv_bfloat162 *>(&a), *reinterpret_cast<__nv_bfloat162 *>(&b),
+                                     *reinterpret_cast<__nv_bfloat162 *>(&c));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+
+// a scale as two parts of the operand type, each twice in a register
+struct Scale2 {
+    uint32_t hi, lo;
+};
+template <typename T>
+__device__ __forceinline__ Scale2 scale_parts(float s) {
+    Scale2 r;
+    r.hi = pack2<T>(s, s);
+    const float rest = s - unpack2<T>(r.hi).x;
+    r.lo = pack2<T>(rest, rest);
+    return r;
+}
+// code * scale in one rounding (parts: of a scale in two parts)
+template <typename T>
+__device__ __forceinline__ uint32_t expand(uint32_t c, const Scale2 &s, bool parts) {
+    return parts ? fma2<T>(c, s.hi, mul2<T>(c, s.lo)) : mul2<T>(c, s.hi);
+}
+// what that rounding dropped: exact in bf16 (the scale has at most 11 bits, the code 4)
+__device__ __forceinline__ uint32_t expand_rest(uint32_t c, const Scale2 &s, uint32_t w) {
+    const uint32_t neg = w ^ 0x80008000u;
+    return fma2<__nv_bfloat16>(c, s.lo, fma2<__nv_bfloat16>(c, s.hi, neg));
+}
+
+// T: the operands' type; X: x's and y's
+template <typename T, typename X, int G>
+__global__ void __launch_bounds__(Q4_THREADS, 1)
+    q4_prompt_kernel(const __grid_constant__ CUtensorMap mX, const __grid_constant__ PromptP p, X *__restrict__ y) {
+    constexpr bool F32 = std::is_same<X, float>::value;
+    constexpr int COMBOS = F32 ? 5 : 1;
+    constexpr uint32_t TMEM_COLS = G == 2 ? 512 : 256, ACC = TMEM_COLS / 2;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t full_bar[Q4_STAGES], empty_bar[Q4_STAGES], accf_bar[2], acce_bar[2];
+    __shared__ __align__(16) float bias_sh[4][32], pow_sh[4][32];
+    __shared__ uint32_t tmem_sh;
+    __shared__ volatile int abort_sh;
+    __shared__ int issued_sh, consumed_sh;
+    uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t *stg = smem + Q4_STAGES * Q4_STAGE;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = G == 2 ? cluster_rank() : 0u;
+    const bool leader = rank == 0;
+    const int cid = (int)(blockIdx.x / G), ncl = (int)(gridDim.x / G);
+    const int total = p.mtiles * p.ntiles;
+    auto set_abort = [&]() {
+        abort_sh = 1;
+        if (G == 2) st_cluster_u32(mapa(su32((const void *)&abort_sh), rank ^ 1u), 1u);
+    };
+    if (warp == 0) {
+        tmem_alloc<G>(&tmem_sh, TMEM_COLS);
+    } else if (warp == 1) {
+        if (lane < Q4_STAGES) {
+            mbar_init(&full_bar[lane], 1 + G * Q4_EXPAND);  // the (leader's) loader, every expanding warp
+            mbar_init(&empty_bar[lane], 1);
+        }
+        if (lane >= 8 && lane < 10) {
+            mbar_init(&accf_bar[lane - 8], 1);
+            mbar_init(&acce_bar[lane - 8], G * 4);
+        }
+        if (lane == 10) {
+            abort_sh = 0;
+            issued_sh = consumed_sh = 0;
+        }
+        fence_mbar_init();
+    } else if (warp == 2 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mX)) : "memory");
+    }
+    if (G == 2) cluster_sync_all();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_sh;
+    griddep_launch();  // (behind the allocation: see tmem_alloc)
+
+    if (warp == 0) {
+        if (lane == 0) {  // ---------------- loader of x
+            int s = 0, g = 0;
+            uint32_t par = 0;
+            bool stop = false;
+            griddep_wait();
+            for (int t = cid; t < total && !stop; t += ncl) {
+                const int m0 = (t / p.ntiles * G + (int)rank) * BM;
+                for (int it = 0; it < p.steps; ++it, ++g) {
+                    if (!mbar_wait(&empty_bar[s], par ^ 1u, p.wait_limit)) {
+                        atomicOr(p.err, ERR_TMA_WAIT);
+                        set_abort();
+                    }
+                    if (abort_sh) {
+                        stop = true;
+                        break;
+                    }
+                    if (leader) mbar_expect_tx(&full_bar[s], G * Q4_A_BYTES);
+                    const uint32_t bar = G == 2 ? mapa(su32(&full_bar[s]), 0u) : su32(&full_bar[s]);
+                    const int kb = F32 ? it / COMBOS : it, c = F32 ? it - kb * COMBOS : 0;
+                    const int plane = F32 ? (c == 3 ? 3 : c == 4 ? 1 : c) : 0;
+                    tma_2d<G>(su32(smem + s * Q4_STAGE), &mX, bar, kb * BK, m0 + plane * p.plane_rows);
+                    if (++s == Q4_STAGES) {
+                        s = 0;
+                        par ^= 1u;
+                    }
+                }
+            }
+            issued_sh = g;
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && leader) {  // ---------------- MMA issuer
+            const uint32_t idesc = idesc_f16<T>(BM * G, p.bn);
+            const uint64_t desc0 = sdesc_sw128(su32(smem));
+            int g = 0, lt = 0, s = 0;
+            uint32_t par = 0;
+            bool stop = false;
+            for (int t = cid; t < total && !stop; t += ncl, ++lt) {
+                const int b = lt & 1;
+                const uint32_t aph = (uint32_t)(lt >> 1) & 1u;
+                if (!(G == 2 ? mbar_wait_cluster(&acce_bar[b], aph ^ 1u, p.wait_limit) : mbar_wait(&acce_bar[b], aph ^ 1u, p.wait_limit))) {
+                    atomicOr(p.err, ERR_EPI_WAIT);
+                    set_abort();
+                    break;
+                }
+                tc_fence_after();
+                const uint32_t d = tmem + (uint32_t)b * ACC;
+                for (int it = 0; it < p.steps; ++it, ++g) {
+                    if (!(G == 2 ? mbar_wait_cluster(&full_bar[s], par, p.wait_limit) : mbar_wait(&full_bar[s], par, p.wait_limit))) {
+                        atomicOr(p.err, ERR_MMA_WAIT);
+                        set_abort();
+                        stop = true;
+                        break;
+                    }
+                    tc_fence_after();
+                    const uint64_t da = desc0 + (uint64_t)((s * Q4_STAGE) >> 4), db = da + (Q4_A_BYTES >> 4);
+#pragma unroll
+                    for (int k = 0; k < BK / 16; ++k) umma<G>(d, da + 2 * k, db + 2 * k, idesc, (it > 0 || k > 0) ? 1u : 0u);
+                    umma_commit<G>(&empty_bar[s]);
+                    if (++s == Q4_STAGES) {
+                        s = 0;
+                        par ^= 1u;
+                    }
+                }
+                if (!stop) umma_commit<G>(&accf_bar[b]);
+            }
+            consumed_sh = g;
+        }
+    } else if (warp >= 4 && warp < 8) {  // ---------------- epilogue: 32 rows a warp
+        const int q = warp - 4;
+        uint8_t *out = stg + q * 32 * Q4_OUT_ROW;
+        griddep_wait();
+        int lt = 0;
+        for (int t = cid; t < total; t += ncl, ++lt) {
+            const int b = lt & 1;
+            const int64_t r0 = (int64_t)(t / p.ntiles * G + (int)rank) * BM + q * 32;
+            const int n0 = t % p.ntiles * p.bn;
+            if (!mbar_wait(&accf_bar[b], (uint32_t)(lt >> 1) & 1u, p.wait_limit)) {
+                if (lane == 0) {
+                    atomicOr(p.err, ERR_ACC_WAIT);
+                    set_abort();
+                }
+                break;
+            }
+            tc_fence_after();
+            if (r0 < p.rows) {
+#pragma unroll 1
+                for (int c0 = 0; c0 < p.bn && n0 + c0 < p.q.n; c0 += 32) {
+                    const int j0 = n0 + c0;
+                    uint32_t v[32];
+                    __syncwarp();
+                    tmem_ld32(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)b * ACC + (uint32_t)c0, v);
+                    bias_sh[q][lane] = p.q.bias && j0 + lane < p.q.n ? p.q.bias[j0 + lane] : 0.0f;
+                    if constexpr (std::is_same<X, __half>::value)
+                        pow_sh[q][lane] = j0 + lane < p.q.n ? p.q.row_pow[j0 + lane] * 0x1p-12f : 0.0f;
+                    __syncwarp();
+                    X *mine = reinterpret_cast<X *>(out + lane * Q4_OUT_ROW);
+                    constexpr int V = 16 / sizeof(X);  // values in 16 bytes
+#pragma unroll
+                    for (int i = 0; i < 32; i += V) {
+                        struct alignas(16) {
+                            X v[V];
+                        } piece;
+#pragma unroll
+                        for (int e = 0; e < V; ++e) {
+                            float f = __uint_as_float(v[i + e]);
+                            if constexpr (std::is_same<X, __half>::value) f *= pow_sh[q][i + e];
+                            piece.v[e] = cvt<X>(act_apply(f + bias_sh[q][i + e], p.q.act));
+                        }
+                        *reinterpret_cast<uint4 *>(mine + i) = *reinterpret_cast<const uint4 *>(&piece);
+                    }
+                    __syncwarp();
+                    const int live = (int)min((int64_t)32, p.rows - r0), cols = min(32, p.q.n - j0);
+                    if (p.vec_out && cols == 32) {
+                        constexpr int LPR = 32 / V;  // lanes a row
+#pragma unroll
+                        for (int r = 0; r < 32; r += 32 / LPR) {
+                            const int row = r + lane / LPR;
+                            if (row < live)
+                                *reinterpret_cast<uint4 *>(y + (r0 + row) * p.ldy + j0 + lane % LPR * V) =
+                                    *reinterpret_cast<const uint4 *>(out + row * Q4_OUT_ROW + lane % LPR * 16);
+                        }
+                    } else if (lane < cols) {
+                        for (int r = 0; r < live; ++r)
+                            y[(r0 + r) * p.ldy + j0 + lane] = reinterpret_cast<const X *>(out + r * Q4_OUT_ROW)[lane];
+                    }
+                }
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) {
+                if (G == 2) mbar_arrive_cluster(mapa(su32(&acce_bar[b]), 0u));
+                else mbar_arrive(&acce_bar[b]);
+            }
+        }
+    } else if (warp >= 8) {  // ---------------- weights: one 16-row tile of this CTA's rows a step and warp
+        const int dw = warp - 8, g = lane / 4, t4 = lane % 4;
+        const int own = p.bn / G;  // rows this CTA stages
+        const bool has = dw * 16 < own;
+        const uint32_t row_at = (uint32_t)(dw * 16 + g) * 128;
+        // rows g of even g store their columns' first half first, the others the
+        // second, so that eight lanes' 16-byte pieces cover all banks
+        const int first = g & 1;
+        const uint32_t at0 = row_at + ((uint32_t)((4 * first + t4) ^ g) << 4), at1 = row_at + ((uint32_t)((4 * (first ^ 1) + t4) ^ g) << 4);
+        int s = 0;
+        uint32_t par = 0;
+        bool stop = false;
+        for (int t = cid; t < total && !stop; t += ncl) {
+            const int tile = min((t % p.ntiles * p.bn + (int)rank * own) / 16 + dw, p.q.nt - 1);
+            const uint4 *codes = p.q.codes + (int64_t)tile * p.q.kb * 32 + lane;
+            const uint32_t *scales = p.q.scales + (int64_t)tile * p.q.kg * 8 + g;
+            float rp[2] = {1.0f, 1.0f};
+            if constexpr (std::is_same<T, __half>::value) {
+                rp[0] = 0x1p12f / __ldg(p.q.row_pow + tile * 16 + g);
+                rp[1] = 0x1p12f / __ldg(p.q.row_pow + tile * 16 + g + 8);
+            }
+            uint4 cw[Q4_AHEAD];
+            uint32_t sw[Q4_AHEAD][2];
+            auto fetch = [&](int i, int kb) {
+                if (!has || kb >= p.q.kb) return;
+                cw[i] = __ldg(codes + (int64_t)kb * 32);
+                if (p.q.glog == 5) {
+                    sw[i][0] = __ldg(scales + (int64_t)(2 * kb) * 8);
+                    sw[i][1] = __ldg(scales + (int64_t)(2 * kb + 1) * 8);
+                } else {
+                    sw[i][0] = sw[i][1] = __ldg(scales + (int64_t)(kb >> (p.q.glog - 6)) * 8);
+                }
+            };
+#pragma unroll
+            for (int i = 0; i < Q4_AHEAD; ++i) fetch(i, i);
+            for (int kb0 = 0; kb0 < p.q.kb && !stop; kb0 += Q4_AHEAD) {
+#pragma unroll
+                for (int i = 0; i < Q4_AHEAD; ++i) {
+                    if (kb0 + i >= p.q.kb || stop) break;
+                    const uint32_t w[4] = {cw[i].x, cw[i].y, cw[i].z, cw[i].w};
+                    Scale2 sc[2][2];  // [row g, row g + 8][half of the tile]
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float2 f = scale_pair(sw[i][h], p.q.scale_bf16);
+                        sc[0][h] = scale_parts<T>(f.x * rp[0]);
+                        sc[1][h] = scale_parts<T>(f.y * rp[1]);
+                    }
+                    fetch(i, kb0 + i + Q4_AHEAD);
+#pragma unroll 1
+                    for (int c = 0; c < COMBOS; ++c) {
+                        if (!mbar_wait(&empty_bar[s], par ^ 1u, p.wait_limit)) {
+                            if (lane == 0) {
+                                atomicOr(p.err, ERR_TMA_WAIT);
+                                set_abort();
+                            }
+                        }
+                        if (__any_sync(0xffffffffu, abort_sh)) {
+                            stop = true;
+                            break;
+                        }
+                        if (has) {
+                            uint8_t *b = smem + s * Q4_STAGE + Q4_A_BYTES;
+#pragma unroll
+                            for (int r = 0; r < 2; ++r) {
+                                uint32_t v[2][4];
+#pragma unroll
+                                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e) {
+                                        const uint32_t code = code_pair<T>(w[2 * h + e / 2], r + 2 * (e % 2));
+                                        v[h][e] = expand<T>(code, sc[r][h], p.parts);
+                                        if (F32 && c >= 3) v[h][e] = expand_rest(code, sc[r][h], v[h][e]);
+                                    }
+                                *reinterpret_cast<uint4 *>(b + at0 + r * 1024) =
+                                    first ? make_uint4(v[1][0], v[1][1], v[1][2], v[1][3]) : make_uint4(v[0][0], v[0][1], v[0][2], v[0][3]);
+                                *reinterpret_cast<uint4 *>(b + at1 + r * 1024) =
+                                    first ? make_uint4(v[0][0], v[0][1], v[0][2], v[0][3]) : make_uint4(v[1][0], v[1][1], v[1][2], v[1][3]);
+                            }
+                            fence_proxy_async_smem();
+                        }
+                        __syncwarp();
+                        if (lane == 0) {
+                            if (G == 2) mbar_arrive_cluster(mapa(su32(&full_bar[s]), 0u));
+                            else mbar_arrive(&full_bar[s]);
+                        }
+                        if (++s == Q4_STAGES) {
+                            s = 0;
+                            par ^= 1u;
+                        }
+                    }
+                }
+            }
+        }
+    }
+    tc_fence_before();
+    __syncthreads();
+    if (warp == 0) {
+        if (abort_sh && lane == 0) {
+            // let the copies and MMAs in flight land before the memory goes away
+            // (one deadline; a stage whose weights never came completes no phase)
+            const long long t0 = clock64();
+            if (leader)
+                for (int g = consumed_sh; g < issued_sh; ++g)
+                    while (!mbar_try(&full_bar[g % Q4_STAGES], (uint32_t)(g / Q4_STAGES) & 1u) && clock64() - t0 < WAIT_LIMIT) {
+                    }
+            if (leader && consumed_sh > 0) {
+                const int g = consumed_sh - 1;
+                while (!mbar_try(&empty_bar[g % Q4_STAGES], (uint32_t)(g / Q4_STAGES) & 1u) && clock64() - t0 < WAIT_LIMIT) {
+                }
+            }
+        }
+        __syncwarp();
+    }
+    if (G == 2) cluster_sync_all();
+    else __syncthreads();
+    if (warp == 0) {
+        tc_fence_after();
+        tmem_dealloc<G>(tmem, TMEM_COLS);
+    }
+}
+
+// x where TMA cannot read it in place: 16-bit rows copied to rows of `kp` values, fp32
+// rows cut into bf16 planes of plane_rows rows
+template <typename X>
+__global__ void __launch_bounds__(256) q4_planes_kernel(const X *__restrict__ x, int64_t ldx, int64_t rows, int k, int kp,
+                                                        int64_t plane_rows, void *__restrict__ out) {
+    griddep_launch();
+    griddep_wait();
+    const int64_t row = blockIdx.x;
+    for (int c = threadIdx.x; c < kp; c += 256) {
+        const X v = c < k ? x[row * ldx + c] : cvt<X>(0.0f);
+        if constexpr (std::is_same<X, float>::value) {
+            const Planes pl = planes_of(v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                static_cast<__nv_bfloat16 *>(out)[(plane_rows * i + row) * kp + c] =
+                    i < 3 ? pl.v[i] : fabsf(v) <= 3.4028234664e38f ? pl.v[0] : __float2bfloat16_rn(0.0f);
+        } else {
+            static_cast<X *>(out)[row * kp + c] = v;
+        }
+    }
+}
+
+bool in_place(int dt, const void *x, int64_t ldx) {
+    return dt != SN_F32 && reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx % 8 == 0;
+}
+
+// Rows of x and outputs a tile: the pair of CTAs or the single one, and the width,
+// whose rounds of tiles over the SMs times the time of a tile are least.  A step
+// takes 2 BN cycles of the tensor core and at least about 256 for its weights; a
+// tile some 1500 more to fill and drain.
+struct Shape4 {
+    int g, bn;
+};
+Shape4 choose(int64_t rows, int n, int64_t steps) {
+    Shape4 best{1, 32};
+    double least = 1e300;
+    for (int g = 1; g <= 2; ++g)
+        for (int bn = 32; bn <= (g == 2 ? 256 : 128); bn += 32) {
+            const int64_t tiles = ((rows + 128 * g - 1) / (128 * g)) * ((n + bn - 1) / bn);
+            const int64_t slots = num_sms() / g, rounds = (tiles + slots - 1) / slots;
+            const double cost = (double)rounds * ((double)std::max(2 * bn, 256) * (double)steps + 1500.0);
+            if (cost < least) {
+                least = cost;
+                best = Shape4{g, bn};
+            }
+        }
+    return best;
+}
+
+template <typename T, typename X, int G>
+cudaError_t launch_prompt(const CUtensorMap &mX, PromptP &p, X *y, cudaStream_t st) {
+    auto kern = q4_prompt_kernel<T, X, G>;
+    static bool set = false;  // (idempotent)
+    if (!set) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Q4_SMEM);
+        if (e != cudaSuccess) return e;
+        set = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.blockDim = dim3(Q4_THREADS);
+    cfg.dynamicSmemBytes = Q4_SMEM;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = G;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = G == 2 ? 2 : 1;
+    const int64_t total = (int64_t)p.mtiles * p.ntiles;
+    if (total > INT32_MAX) return cudaErrorInvalidValue;
+    cfg.gridDim = dim3((unsigned)(G * std::min<int64_t>(total, num_sms() / G)));
+    return cudaLaunchKernelEx(&cfg, kern, mX, p, y);
+}
+
+template <typename T, typename X>
+cudaError_t prompt(const sn_q4_weights &w, int dt, int64_t rows, const X *x, int64_t ldx, X *y, int64_t ldy, void *work,
+                   cudaStream_t st) {
+    constexpr bool F32 = std::is_same<X, float>::value;
+    PromptP p{};
+    p.q = q4_params(w);
+    p.rows = rows;
+    p.ldy = ldy;
+    p.steps = p.q.kb * (F32 ? 5 : 1);
+    const Shape4 sh = choose(rows, w.n, p.steps);
+    p.bn = sh.bn;
+    const int64_t mtiles = (rows + 128 * sh.g - 1) / (128 * sh.g);
+    p.mtiles = (int32_t)mtiles;
+    p.ntiles = (w.n + sh.bn - 1) / sh.bn;
+    p.parts = F32 || !(std::is_same<T, __nv_bfloat16>::value && w.scale_dtype == SN_BF16);
+    p.vec_out = reinterpret_cast<uintptr_t>(y) % 16 == 0 && (ldy * (int64_t)sizeof(X)) % 16 == 0;
+    p.err = device_error_word();
+    p.wait_limit = WAIT_LIMIT;
+    const void *base = x;
+    int64_t ld = ldx;
+    uint64_t dims[2] = {(uint64_t)w.k, (uint64_t)rows};
+    if (!in_place(dt, x, ldx)) {
+        const int kp = p.q.kb * 64;
+        const int64_t plane_rows = (rows + 255) / 256 * 256;
+        const cudaError_t e = launch_pdl(q4_planes_kernel<X>, dim3((unsigned)rows), dim3(256), 0, st, x, ldx, rows, (int)w.k, kp,
+                                         plane_rows, work);
+        if (e != cudaSuccess) return e;
+        base = work;
+        ld = kp;
+        dims[0] = (uint64_t)kp;
+        if (F32) {
+            p.plane_rows = (int32_t)plane_rows;
+            dims[1] = (uint64_t)(4 * plane_rows);
+        }
+    }
+    if (dims[1] > INT32_MAX) return cudaErrorInvalidValue;
+    const uint64_t strides[1] = {(uint64_t)ld * 2};
+    const uint32_t box[2] = {BK, BM};
+    CUtensorMap mX;
+    if (!tma_encode(&mX, std::is_same<T, __half>::value ? SN_F16 : SN_BF16, 2, base, dims, strides, box, CU_TENSOR_MAP_SWIZZLE_128B))
+        return cudaErrorInvalidValue;
+    return sh.g == 2 ? launch_prompt<T, X, 2>(mX, p, y, st) : launch_prompt<T, X, 1>(mX, p, y, st);
+}
+
+}  // namespace
+
+size_t q4_prompt_workspace(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx) {
+    if (in_place(dt, x, ldx)) return 0;
+    const int64_t kp = ((int64_t)w.k + 63) / 64 * 64;
+    return (size_t)((rows + 255) / 256 * 256 * kp * 2 * (dt == SN_F32 ? 4 : 1));
+}
+
+cudaError_t q4_prompt(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx, void *y, int64_t ldy, void *work,
+                      cudaStream_t st) {
+    if (dt == SN_F32)
+        return prompt<__nv_bfloat16, float>(w, dt, rows, static_cast<const float *>(x), ldx, static_cast<float *>(y), ldy, work, st);
+    if (dt == SN_F16)
+        return prompt<__half, __half>(w, dt, rows, static_cast<const __half *>(x), ldx, static_cast<__half *>(y), ldy, work, st);
+    return prompt<__nv_bfloat16, __nv_bfloat16>(w, dt, rows, static_cast<const __nv_bfloat16 *>(x), ldx,
+                                                static_cast<__nv_bfloat16 *>(y), ldy, work, st);
+}
+
+}  // namespace k
+}  // namespace sn

@@ -90,5 +90,10 @@ __device__ __forceinline__ Planes planes_of(float x) {
     return p;
 }
 
+// many rows, on the tensor cores
+size_t q4_prompt_workspace(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx);
+cudaError_t q4_prompt(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx, void *y, int64_t ldy,
+                      void *work, cudaStream_t st);
+
 }  // namespace k
 }  // namespace sn
