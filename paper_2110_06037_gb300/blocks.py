@@ -29,13 +29,31 @@ from .api import _stream_ptr, _torch
 NORM_KINDS = {"rms": 0, "layer": 1}
 GATES = {"none": 0, None: 0, "linear": 1, "sigmoid": 2, "silu": 3}
 _dtypes = {}  # torch dtype -> sn_dtype, filled on first use (the import of torch is not this module's)
+_torch_mod = None
+
+# A call's own work on the GPU can be a few microseconds, as much as marshalling it on
+# the host: the usual case (rows in two axes, the current stream) goes straight through.
+
+
+def _setup():
+    global _torch_mod
+    _torch_mod = _torch()
+    _dtypes.update({_torch_mod.float32: _sn.SN_F32, _torch_mod.float16: _sn.SN_F16, _torch_mod.bfloat16: _sn.SN_BF16})
+    return _torch_mod
 
 
 def _dtype_map():
     if not _dtypes:
-        torch = _torch()
-        _dtypes.update({torch.float32: _sn.SN_F32, torch.float16: _sn.SN_F16, torch.bfloat16: _sn.SN_BF16})
+        _setup()
     return _dtypes
+
+
+def _stream(stream, device):
+    """Handle of the stream, or of the device's current one."""
+    if stream is not None:
+        return stream.cuda_stream
+    raw = getattr(_torch_mod._C, "_cuda_getCurrentRawStream", None)
+    return raw(device) if raw is not None else _stream_ptr(None)
 
 
 def _refuse(msg):
@@ -51,6 +69,16 @@ def _dt(t, what):
 
 def _rows(t, width, what, like=None):
     """(data pointer, row stride, rows) of a tensor [..., width] whose leading axes collapse to rows."""
+    shape = t.shape
+    if len(shape) == 2 and shape[1] == width and t.is_cuda and (like is None or t.dtype is like):
+        s0, s1 = t.stride()
+        if s1 == 1:
+            rows = shape[0]
+            return t.data_ptr(), (s0 if rows > 1 or s0 > width else width), rows
+    return _any_rows(t, width, what, like)
+
+
+def _any_rows(t, width, what, like):
     if not t.is_cuda:
         _refuse(f"{what} must be a CUDA tensor")
     if like is not None and t.dtype != like:
@@ -80,37 +108,38 @@ def _whole(t, shape, dtype, what):
     """Data pointer of a contiguous CUDA tensor of exactly this shape and type; 0 for None."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype != dtype or (shape is not None and tuple(t.shape) != tuple(shape)) or not t.is_contiguous():
-        _refuse(f"{what} must be a contiguous CUDA {dtype} tensor" + ("" if shape is None else f" of shape {tuple(shape)}")
-                + f", not {t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
+    if t.dtype is dtype and t.shape == shape and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(f"{what} must be a contiguous CUDA {dtype} tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)} "
+            f"on {t.device}")
 
 
 def _index(t, n, what):
-    return _whole(t, (n,), _torch().int32, what)
+    return None if t is None else _whole(t, (n,), _torch_mod.int32, what)
 
 
 def _new(shape, dtype, device, stream):
-    torch = _torch()
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return _torch_mod.empty(shape, dtype=dtype, device=device)
+    with _torch_mod.cuda.stream(stream):
+        return _torch_mod.empty(shape, dtype=dtype, device=device)
 
 
-def _out(out, shape, dtype, device, stream, what):
+def _out(out, shape, width, dtype, like, stream, what):
+    """(tensor, data pointer, row stride) of an output, allocated where none is given."""
     if out is None:
-        return _new(shape, dtype, device, stream)
+        out = _new(shape, dtype, like.device, stream)
+        return out, out.data_ptr(), width
     if tuple(out.shape) != tuple(shape) or out.dtype != dtype:
         _refuse(f"{what} must be {dtype} of shape {tuple(shape)}")
-    return out
+    return out, *_rows(out, width, what)[:2]
 
 
 def _scratch(call, device, stream):
     """A buffer of the bytes that `call` names (through its last argument), or None."""
     n = C.c_int64()
-    check(call(C.byref(n)))
-    return _new((n.value,), _torch().uint8, device, stream) if n.value else None
+    check(call(n))
+    return _new((n.value,), _torch_mod.uint8, device, stream) if n.value else None
 
 
 def check_device(stream=None):
@@ -125,7 +154,7 @@ def quantize_q4(w, group=64, scale_dtype=None, stream=None):
 
     scale = max |w| / 7 in scale_dtype (torch.bfloat16 by default, or torch.float16), code = w / scale
     rounded, in -8..7; two codes a byte in two's complement, the lower k in the low half."""
-    torch = _torch()
+    torch = _setup()
     scale_dtype = scale_dtype or torch.bfloat16
     if w.dim() != 2:
         _refuse("w must be a matrix")
@@ -138,7 +167,7 @@ def quantize_q4(w, group=64, scale_dtype=None, stream=None):
     codes = _new((n, (k + 1) // 2), torch.uint8, w.device, stream)
     scales = _new((n, -(-k // group)), scale_dtype, w.device, stream)
     check(lib().sn_q4_quantize(ptr, dt, n, k, group, _dtype_map()[scale_dtype], codes.data_ptr(), scales.data_ptr(),
-                               _stream_ptr(stream)))
+                               _stream(stream, w.get_device())))
     return codes, scales
 
 
@@ -148,7 +177,7 @@ class Q4Weights:
     "hsigmoid").  Building it waits for `stream`; after that it serves any stream."""
 
     def __init__(self, codes, scales, k, group, bias=None, act="none", stream=None):
-        torch = _torch()
+        torch = _setup()
         n, k, group = int(codes.shape[0]), int(k), int(group)
         if act not in _sn.SN_ACT:
             _refuse(f"unknown act {act!r}")
@@ -163,21 +192,23 @@ class Q4Weights:
         self.bias, self.n, self.k, self.group, self.act = bias, n, k, group, act
         self._c = _sn.sn_q4_weights(n, k, group, _dtype_map()[scales.dtype], _sn.SN_ACT[act], self.packed.data_ptr(), bp)
         self._ref = C.byref(self._c)
-        check(lib().sn_q4_pack(cp, sp, self._ref, _stream_ptr(stream)))
+        check(lib().sn_q4_pack(cp, sp, self._ref, _stream(stream, codes.get_device())))
+        self._call, self._want = lib().sn_q4_dense, lib().sn_q4_workspace
 
 
 def dense_q4(x, w, out=None, stream=None):
     """y = act(x W^T + bias) with 4-bit weights: x [..., k] -> [..., n] of x's type, for any number of rows."""
     dt = _dt(x, "x")
     ptr, ld, rows = _rows(x, w.k, "x")
-    out = _out(out, (*x.shape[:-1], w.n), x.dtype, x.device, stream, "out")
-    optr, old, _ = _rows(out, w.n, "out")
-    work, nbytes = None, 0
+    shape = x.shape
+    out, optr, old = _out(out, (rows, w.n) if len(shape) == 2 else (*shape[:-1], w.n), w.n, x.dtype, x, stream, "out")
+    work = None
     if rows > 8:  # (fewer never need scratch)
-        work = _scratch(lambda n: lib().sn_q4_workspace(w._ref, dt, rows, ptr, ld, n), x.device, stream)
-        nbytes = work.numel() if work is not None else 0
-    check(lib().sn_q4_dense(w._ref, dt, rows, ptr, ld, optr, old, work.data_ptr() if nbytes else None, nbytes,
-                            _stream_ptr(stream)))
+        work = _scratch(lambda n: w._want(w._ref, dt, rows, ptr, ld, C.byref(n)), x.device, stream)
+    rc = w._call(w._ref, dt, rows, ptr, ld, optr, old, None if work is None else work.data_ptr(),
+                 0 if work is None else work.numel(), _stream(stream, x.get_device()))
+    if rc:
+        check(rc)
     return out
 
 
@@ -197,11 +228,11 @@ class BlockNorm:
             _refuse(f"unknown kind {kind!r}, gate {gate!r} or gate_at {gate_at!r}")
         self.dim, self.has_pre = int(dim), pre is not None
         self.weights = (post, post_bias, pre, pre_bias, scale)
-        f32 = _torch().float32
+        f32 = _setup().float32
         ptrs = [_whole(t, (self.dim,), f32, what)
                 for t, what in zip(self.weights, ("post", "post_bias", "pre", "pre_bias", "scale"))]
         self._c = _sn.sn_norm_params(self.dim, NORM_KINDS[kind], GATES[gate], int(gate_at == "after"), eps, *ptrs)
-        self._ref = C.byref(self._c)
+        self._ref, self._call = C.byref(self._c), lib().sn_block_norm
 
     def __call__(self, y=None, residual=None, gate=None, rows_per_gate=1, out=None, out_normed=None, dtype=None, stream=None):
         """(total, normed): total in the residual's type (y's without one), normed in y's type, or None
@@ -214,31 +245,31 @@ class BlockNorm:
         dt, d = (_dtypes or _dtype_map()).get(dtype), self.dim
         if dt is None:
             _refuse(f"rows must be fp32, fp16 or bf16, not {dtype}")
-        yp, ldy, rows = _rows(y, d, "y") if y is not None else (None, 0, 0)
-        rp = ldr = gp = ldg = 0
-        rdt = dt
+        yp = rp = gp = total = sp = normed = np_ = None
+        ldy = ldr = ldg = lds = ldn = 0
+        sdt, rdt = dtype, dt
+        if y is not None:
+            yp, ldy, rows = _rows(y, d, "y")
         if residual is not None:
+            sdt = residual.dtype
             rdt = _dt(residual, "residual")
             rp, ldr, n = _rows(residual, d, "residual")
             if y is not None and n != rows:
                 _refuse("residual and y have different rows")
             rows = n
         if gate is not None:
-            gp, ldg, n = _rows(gate, d, "gate", like=first.dtype)
+            gp, ldg, n = _rows(gate, d, "gate", dtype)
             if rows_per_gate < 1 or n * rows_per_gate < rows:
                 _refuse("too few gate rows")
-        total = sp = lds = None
         if y is not None or out is not None:
-            total = _out(out, first.shape, residual.dtype if residual is not None else first.dtype, first.device, stream,
-                         "out")
-            sp, lds, _ = _rows(total, d, "out")
-        normed = np_ = ldn = None
+            total, sp, lds = _out(out, first.shape, d, sdt, first, stream, "out")
         if self.has_pre:
-            normed = _out(out_normed, first.shape, dtype, first.device, stream, "out_normed")
-            np_, ldn, _ = _rows(normed, d, "out_normed")
-        check(lib().sn_block_norm(self._ref, dt, rows, yp, ldy, gp or None, ldg, rows_per_gate, rdt, rp or None, ldr,
-                                  sp, lds or 0, np_, ldn or 0, _stream_ptr(stream)))
-        return (total if total is not None else residual), normed
+            normed, np_, ldn = _out(out_normed, first.shape, d, dtype, first, stream, "out_normed")
+        rc = self._call(self._ref, dt, rows, yp, ldy, gp, ldg, rows_per_gate, rdt, rp, ldr, sp, lds, np_, ldn,
+                        _stream(stream, first.get_device()))
+        if rc:
+            check(rc)
+        return (residual if total is None else total), normed
 
 
 # --------------------------------------------------- convolution and scan
@@ -268,24 +299,25 @@ def causal_conv(x, weight, bias=None, act="silu", offsets=None, max_len=None, ke
     index; -1: none)."""
     if act not in ("silu", "none", None):
         _refuse(f"unknown act {act!r}")
-    f32 = _torch().float32
+    f32 = (_torch_mod or _setup()).float32
     if weight.dim() != 2:
         _refuse("weight must be [channels, width]")
     c, width = weight.shape
     dt = _dt(x, "x")
     tokens, batch, max_len, op = _sequences(x, offsets, max_len)
     xp, ldx, _ = _rows(x, c, "x")
-    out = _out(out, x.shape, x.dtype, x.device, stream, "out")
-    yp, ldy, _ = _rows(out, c, "out")
+    out, yp, ldy = _out(out, x.shape, c, x.dtype, x, stream, "out")
     kp, n = None, batch
     if kept is not None:
         n = kept.shape[0]
         kp = _whole(kept, (n, width, c), x.dtype, "kept")
     if kept is not None and slots is None and n < batch:
         _refuse("kept has fewer entries than there are sequences")
-    check(lib().sn_causal_conv(dt, c, width, int(act == "silu"), _whole(weight, (c, width), f32, "weight"),
-                               _whole(bias, (c,), f32, "bias"), tokens, batch, max_len, op, xp, ldx, yp, ldy, kp, n,
-                               _index(slots, batch, "slots"), _index(pos, batch, "pos"), _stream_ptr(stream)))
+    rc = lib().sn_causal_conv(dt, c, width, int(act == "silu"), _whole(weight, (c, width), f32, "weight"),
+                              _whole(bias, (c,), f32, "bias"), tokens, batch, max_len, op, xp, ldx, yp, ldy, kp, n,
+                              _index(slots, batch, "slots"), _index(pos, batch, "pos"), _stream(stream, x.get_device()))
+    if rc:
+        check(rc)
     return out
 
 
@@ -297,7 +329,7 @@ class StateSpace:
     def __init__(self, heads, head_dim, groups, state, a, d=None, dt_bias=None, conv_weight=None, conv_bias=None):
         self.heads, self.head_dim, self.groups, self.state = int(heads), int(head_dim), int(groups), int(state)
         self.inner, self.channels = self.heads * self.head_dim, self.heads * self.head_dim + 2 * self.groups * self.state
-        f32 = _torch().float32
+        f32 = _setup().float32
         self.width = int(conv_weight.shape[1]) if conv_weight is not None else 0
         self.weights = (a, d, dt_bias, conv_weight, conv_bias)
         if a is None:
@@ -307,14 +339,14 @@ class StateSpace:
             _whole(d, (self.heads,), f32, "d"), _whole(dt_bias, (self.heads,), f32, "dt_bias"),
             _whole(conv_weight, (self.channels, self.width), f32, "conv_weight"),
             _whole(conv_bias, (self.channels,), f32, "conv_bias"))
-        self._ref = C.byref(self._c)
+        self._ref, self._scan, self._step = C.byref(self._c), lib().sn_ssm_scan, lib().sn_ssm_step
 
     def _states(self, state_in, state_out, batch, slots):
         n, ptrs = batch, []
         for t, what in ((state_in, "state_in"), (state_out, "state_out")):
             if t is not None:
                 n = t.shape[0]
-            ptrs.append(_whole(t, (n, self.heads, self.head_dim, self.state), _torch().float32, what))
+            ptrs.append(_whole(t, (n, self.heads, self.head_dim, self.state), _torch_mod.float32, what))
         if state_in is not None and state_out is not None and state_in.shape[0] != state_out.shape[0]:
             _refuse("state_in and state_out have different entries")
         if slots is None and n < batch:
@@ -334,12 +366,14 @@ class StateSpace:
         if n != tokens:
             _refuse("dt and xbc have different tokens")
         n, si, so = self._states(state_in, state_out, batch, slots)
-        out = _out(out, (*xbc.shape[:-1], self.inner), xbc.dtype, xbc.device, stream, "out")
-        yp, ldy, _ = _rows(out, self.inner, "out")
-        work = _scratch(lambda b: lib().sn_ssm_workspace(self._ref, code, tokens, batch, max_len, b), xbc.device, stream)
-        check(lib().sn_ssm_scan(self._ref, code, tokens, batch, max_len, op, xp, ldx, dp, ldd, si, so, n,
-                                _index(slots, batch, "slots"), yp, ldy, work.data_ptr() if work is not None else None,
-                                work.numel() if work is not None else 0, _stream_ptr(stream)))
+        out, yp, ldy = _out(out, (*xbc.shape[:-1], self.inner), self.inner, xbc.dtype, xbc, stream, "out")
+        work = _scratch(lambda b: lib().sn_ssm_workspace(self._ref, code, tokens, batch, max_len, C.byref(b)), xbc.device,
+                        stream)
+        rc = self._scan(self._ref, code, tokens, batch, max_len, op, xp, ldx, dp, ldd, si, so, n,
+                        _index(slots, batch, "slots"), yp, ldy, None if work is None else work.data_ptr(),
+                        0 if work is None else work.numel(), _stream(stream, xbc.get_device()))
+        if rc:
+            check(rc)
         return out
 
     def step(self, xbc, dt, kept, state, pos, state_out=None, slots=None, out=None, stream=None):
@@ -357,8 +391,11 @@ class StateSpace:
         if kept.shape[0] != n:
             _refuse("kept and the states have different entries")
         kp = _whole(kept, (n, self.width, self.channels), xbc.dtype, "kept")
-        out = _out(out, (*xbc.shape[:-1], self.inner), xbc.dtype, xbc.device, stream, "out")
-        yp, ldy, _ = _rows(out, self.inner, "out")
-        check(lib().sn_ssm_step(self._ref, code, batch, xp, ldx, dp, ldd, kp, si, so, n, _index(slots, batch, "slots"),
-                                _index(pos, batch, "pos"), yp, ldy, _stream_ptr(stream)))
+        shape = xbc.shape
+        out, yp, ldy = _out(out, (batch, self.inner) if len(shape) == 2 else (*shape[:-1], self.inner), self.inner,
+                            xbc.dtype, xbc, stream, "out")
+        rc = self._step(self._ref, code, batch, xp, ldx, dp, ldd, kp, si, so, n, _index(slots, batch, "slots"),
+                        _index(pos, batch, "pos"), yp, ldy, _stream(stream, xbc.get_device()))
+        if rc:
+            check(rc)
         return out

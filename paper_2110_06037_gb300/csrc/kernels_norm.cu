@@ -6,7 +6,17 @@
 // once.  A row stays in registers between its statistics, its sum and its second
 // statistics, so nothing is read twice; mean and variance are two reductions over
 // the registers (the variance of v - mean, not a difference of squares).
-#include "kern_common.cuh"
+//
+// Three kernels.  Many rows of up to 4096 aligned values: persistent blocks, a thread
+// to eight neighbours of a row, whose weights stay in its registers; the next rows
+// come by bulk copies into a ring of shared memory while one is worked on.  Few or
+// unaligned rows, or up to 8192 values: a block (or a warp) a row, straight from
+// global memory.  Longer rows: a block a row, the row read again for each statistic.
+// 8190 x 4096, bf16 with an fp32 residual: the block a row took 208 us (the loads of
+// a block wait while it reduces, and the weights go through L1 for every row).
+#include <algorithm>
+
+#include "tc_common.cuh"
 
 namespace sn {
 namespace k {
@@ -61,8 +71,8 @@ __device__ __forceinline__ void store_piece(T *row, const float (&v)[PIECE], int
 
 __device__ __forceinline__ float gate_value(float g, int kind) {
     if (kind == SN_GATE_LINEAR) return g;
-    const float s = 1.0f / (1.0f + expf(-g));
-    return kind == SN_GATE_SIGMOID ? s : g * s;
+    // by the approximate exponential and division, 2 ulp each (a denominator beyond 2^126 gives 0)
+    return __fdividef(kind == SN_GATE_SIGMOID ? 1.0f : g, 1.0f + __expf(-g));
 }
 
 // the sum over the row's TPR threads, the same in each of them
@@ -247,6 +257,204 @@ __global__ void __launch_bounds__(1024) block_norm_long_kernel(const __grid_cons
     }
 }
 
+// Many rows: block b takes the rows b, b + gridDim, ...; row i of the block lies in
+// stage i % stages, filled by one thread's bulk copies of y, gate and residual.
+constexpr int RING_MAX = 8;
+struct RingP {
+    NormP n;
+    int32_t stages, stage_bytes, gate_at, res_at;  // offsets of the parts of a stage
+    int *err;
+};
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void *src, uint32_t bytes, uint64_t *bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(tc::su32(bar))
+                 : "memory");
+}
+// the sum over the block; sums take turns with the two halves of sh, so that one barrier each is enough
+__device__ __forceinline__ float block_sum(float v, float *sh, int &turn) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    const int lane = threadIdx.x % 32;
+    float *half = sh + 32 * (turn ^= 1);
+    if (lane == 0) half[threadIdx.x / 32] = v;
+    __syncthreads();
+    v = lane < (int)blockDim.x / 32 ? half[lane] : 0.0f;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+template <typename T>
+__device__ __forceinline__ void load4(float *v, const T *src) {
+    if constexpr (sizeof(T) == 4) {
+        const float4 a = *reinterpret_cast<const float4 *>(src);
+        v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w;
+    } else {
+        const uint2 a = *reinterpret_cast<const uint2 *>(src);
+        const float2 x = tc::unpack2<T>(a.x), y = tc::unpack2<T>(a.y);
+        v[0] = x.x, v[1] = x.y, v[2] = y.x, v[3] = y.y;
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store4(T *dst, const float *v) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(dst) = make_float4(v[0], v[1], v[2], v[3]);
+    else *reinterpret_cast<uint2 *>(dst) = make_uint2(tc::pack2<T>(v[0], v[1]), tc::pack2<T>(v[2], v[3]));
+}
+
+template <typename T, typename R>
+__global__ void __launch_bounds__(512) block_norm_ring_kernel(const __grid_constant__ RingP q) {
+    extern __shared__ __align__(128) uint8_t ring[];
+    __shared__ __align__(8) uint64_t full[RING_MAX];
+    __shared__ float sh[64];
+    __shared__ int stop_sh;
+    const NormP &p = q.n;
+    // a thread's values: four at 4 t and four half a row of threads further on, so that
+    // a warp's accesses to fp32 rows are as contiguous as those to 16-bit ones
+    const int at[2] = {(int)threadIdx.x * 4, (int)(threadIdx.x + blockDim.x) * 4};
+    const bool live[2] = {at[0] < p.d, at[1] < p.d};  // (d is a multiple of 4)
+    const int64_t step = gridDim.x;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < q.stages; ++i) tc::mbar_init(&full[i], 1);
+        stop_sh = 0;
+        tc::fence_mbar_init();
+    }
+    __syncthreads();
+    griddep_launch();
+    griddep_wait();
+    const uint32_t tb = (uint32_t)p.d * sizeof(T), rb = (uint32_t)p.d * sizeof(R);
+    int64_t ahead = blockIdx.x;  // the next row to load, and its stage
+    int s_ahead = 0;
+    auto issue = [&]() {
+        const int64_t row = ahead;
+        const int s = s_ahead;
+        ahead += step;
+        s_ahead = s + 1 == q.stages ? 0 : s + 1;
+        const uint32_t dst = tc::su32(ring) + (uint32_t)(s * q.stage_bytes);
+        tc::mbar_expect_tx(&full[s], (p.a.y ? tb : 0u) + (p.a.gate ? tb : 0u) + (p.a.res ? rb : 0u));
+        if (p.a.y) bulk_load(dst, static_cast<const T *>(p.a.y) + row * p.a.ldy, tb, &full[s]);
+        if (p.a.gate) bulk_load(dst + q.gate_at, static_cast<const T *>(p.a.gate) + (p.a.per_gate == 1 ? row : row / p.a.per_gate) * p.a.ldg, tb, &full[s]);
+        if (p.a.res) bulk_load(dst + q.res_at, static_cast<const R *>(p.a.res) + row * p.a.ldr, rb, &full[s]);
+    };
+    if (threadIdx.x == 0)
+        for (int i = 0; i < q.stages && ahead < p.a.rows; ++i) issue();
+    // the weights of this thread's eight values; scale and post norm in one where nothing is added between
+    float w[PIECE], wb[PIECE], sc[PIECE], u[PIECE], ub[PIECE];
+#pragma unroll
+    for (int j = 0; j < PIECE; ++j) w[j] = sc[j] = u[j] = 1.0f, wb[j] = ub[j] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (!live[i]) continue;
+        if (p.post) load4(w + 4 * i, p.post + at[i]);
+        if (p.post_b) load4(wb + 4 * i, p.post_b + at[i]);
+        if (p.scale) load4(sc + 4 * i, p.scale + at[i]);
+        if (p.pre) load4(u + 4 * i, p.pre + at[i]);
+        if (p.pre_b) load4(ub + 4 * i, p.pre_b + at[i]);
+    }
+    const float inv_d = 1.0f / (float)p.d;
+    int turn = 0;
+    auto norm = [&](float (&v)[PIECE], const float (&wt)[PIECE], const float (&b)[PIECE], bool biased) {
+        if (p.kind == SN_NORM_LAYER) {
+            float s = 0.0f;
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) s += v[j];
+            const float mean = block_sum(s, sh, turn) * inv_d;
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) v[j] = live[j / 4] ? v[j] - mean : 0.0f;
+        }
+        float s = 0.0f;
+#pragma unroll
+        for (int j = 0; j < PIECE; ++j) s = fmaf(v[j], v[j], s);
+        const float r = rsqrtf(block_sum(s, sh, turn) * inv_d + p.eps);
+#pragma unroll
+        for (int j = 0; j < PIECE; ++j) v[j] = biased ? fmaf(v[j] * r, wt[j], b[j]) : v[j] * r * wt[j];
+    };
+    int s = 0;
+    uint32_t par = 0;
+    for (int64_t row = blockIdx.x; row < p.a.rows; row += step) {
+        if (!tc::mbar_wait(&full[s], par)) stop_sh = 1;
+        const uint8_t *st = ring + s * q.stage_bytes;
+        float v[PIECE], g[PIECE], r[PIECE];
+#pragma unroll
+        for (int j = 0; j < PIECE; ++j) v[j] = r[j] = 0.0f, g[j] = 1.0f;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            if (!live[i]) continue;
+            if (p.a.y) load4(v + 4 * i, reinterpret_cast<const T *>(st) + at[i]);
+            if (p.a.gate) load4(g + 4 * i, reinterpret_cast<const T *>(st + q.gate_at) + at[i]);
+            if (p.a.res) load4(r + 4 * i, reinterpret_cast<const R *>(st + q.res_at) + at[i]);
+        }
+        __syncthreads();  // the stage has been read
+        if (stop_sh) break;
+        if (threadIdx.x == 0 && ahead < p.a.rows) issue();
+        if (p.a.y) {
+            if (p.a.gate) {
+#pragma unroll
+                for (int j = 0; j < PIECE; ++j) {
+                    g[j] = gate_value(g[j], p.gate);
+                    if (!p.after) v[j] *= g[j];
+                }
+            }
+            if (p.post) norm(v, w, wb, p.post_b != nullptr);
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) {
+                if (p.a.gate && p.after) v[j] *= g[j];
+                v[j] = p.scale ? fmaf(v[j], sc[j], r[j]) : v[j] + r[j];
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < PIECE; ++j) v[j] = r[j];
+        }
+        if (p.a.sum) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (!live[i]) continue;
+                if (p.a.res) store4(static_cast<R *>(p.a.sum) + row * p.a.lds + at[i], v + 4 * i);
+                else store4(static_cast<T *>(p.a.sum) + row * p.a.lds + at[i], v + 4 * i);
+            }
+        }
+        if (p.pre) {
+            norm(v, u, ub, p.pre_b != nullptr);
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (live[i]) store4(static_cast<T *>(p.a.normed) + row * p.a.ldn + at[i], v + 4 * i);
+        }
+        if (++s == q.stages) {
+            s = 0;
+            par ^= 1u;
+        }
+    }
+    if (threadIdx.x == 0 && stop_sh) {  // a wait gave up: record it, and let the copies in flight land (bounded)
+        atomicOr(q.err, tc::ERR_TMA_WAIT);
+        const long long t0 = clock64();
+        for (int i = 0; i < q.stages; ++i)
+            while (!tc::mbar_try(&full[(s + i) % q.stages], (s + i < q.stages) ? par : par ^ 1u) &&
+                   clock64() - t0 < tc::WAIT_LIMIT) {
+            }
+    }
+}
+
+template <typename T, typename R>
+cudaError_t launch_ring(const NormP &p, cudaStream_t st) {
+    RingP q{p, 0, 0, 0, 0, device_error_word()};
+    auto up = [](int64_t b) { return (int32_t)((b + 127) / 128 * 128); };
+    const int32_t tb = up((int64_t)p.d * sizeof(T)), rb = up((int64_t)p.d * sizeof(R));
+    q.gate_at = p.a.y ? tb : 0;
+    q.res_at = q.gate_at + (p.a.gate ? tb : 0);
+    q.stage_bytes = q.res_at + (p.a.res ? rb : 0);
+    const int threads = (p.d / PIECE + 31) / 32 * 32, blocks = threads <= 128 ? 4 : threads <= 256 ? 2 : 1;  // of 128 registers, a multiprocessor
+    const int room = 220 * 1024 / blocks - 1024;
+    q.stages = std::min(RING_MAX, room / q.stage_bytes);
+    static int set = 0;  // (idempotent)
+    const int smem = q.stages * q.stage_bytes;
+    if (smem > set) {
+        const cudaError_t e = cudaFuncSetAttribute(block_norm_ring_kernel<T, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, room);
+        if (e != cudaSuccess) return e;
+        set = room;
+    }
+    return launch_pdl(block_norm_ring_kernel<T, R>, dim3((unsigned)std::min<int64_t>(p.a.rows, (int64_t)blocks * num_sms())),
+                      dim3((unsigned)threads), (size_t)smem, st, q);
+}
+
 template <typename T, typename R, int TPR, int NP>
 cudaError_t launch_rows(const NormP &p, cudaStream_t st) {
     constexpr int RPB = TPR < 128 ? 128 / TPR : 1;
@@ -257,6 +465,8 @@ cudaError_t launch_rows(const NormP &p, cudaStream_t st) {
 template <typename T, typename R>
 cudaError_t launch_norm(const NormP &p, cudaStream_t st) {
     const int pieces = (p.d + PIECE - 1) / PIECE;
+    // the ring pays from the second row of a block on, and for rows that fill a block's warps
+    if (p.vec && p.d % PIECE == 0 && p.d >= 512 && p.d <= 4096 && p.a.rows >= 4 * num_sms()) return launch_ring<T, R>(p, st);
     if (pieces <= 32) return launch_rows<T, R, 32, 1>(p, st);
     if (pieces <= 64) return launch_rows<T, R, 32, 2>(p, st);
     if (pieces <= 128) return launch_rows<T, R, 128, 1>(p, st);

@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(128) q4_pack_scales_kernel(const uint16_t *__r
 // block's part of x lies in shared memory.  k is split over the WK warps of a
 // block that share a tile and over the S blocks of a cluster, whose sums meet in a
 // fixed order.
-constexpr int WARPS = 8, U = 4;
+constexpr int WARPS = 8;
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, __half) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -137,6 +137,7 @@ __device__ __forceinline__ uint4 ld_stream(const uint4 *p) {
 struct FewP {
     Q4P q;
     int32_t rows, wk, s, phase;  // warps along k, blocks a cluster, tiles along k in shared memory at once
+    int32_t vec;                 // x's rows begin at 16 bytes
     int64_t ldx, ldy;
 };
 
@@ -144,7 +145,7 @@ struct FewP {
 template <typename T, typename X, int NC, bool G32>
 __global__ void __launch_bounds__(WARPS * 32) q4_few_kernel(const __grid_constant__ FewP p, const X *__restrict__ x,
                                                             X *__restrict__ y) {
-    constexpr int PL = std::is_same<X, float>::value ? 3 : 1, COLS = NC * 8;
+    constexpr int PL = std::is_same<X, float>::value ? 3 : 1, COLS = NC * 8, U = NC == 1 ? 8 : 4;  // U: tiles in flight
     extern __shared__ __align__(16) unsigned char smem[];
     float *red = reinterpret_cast<float *>(smem);                  // [WARPS][16][COLS]
     T *xs = reinterpret_cast<T *>(smem + WARPS * 16 * COLS * 4);   // [rows * PL][phase * 64 + 32]
@@ -187,18 +188,39 @@ __global__ void __launch_bounds__(WARPS * 32) q4_few_kernel(const __grid_constan
         if (first) griddep_wait();
         else __syncthreads();
         first = false;
-        // the phase's columns of x, padded with zeros
-        const int width = (pe - ph) * 64;
-        for (int e = threadIdx.x; e < p.rows * width; e += WARPS * 32) {
-            const int m = e / width, c = e - m * width;
-            const int64_t kk = (int64_t)ph * 64 + c;
-            const float v = kk < p.q.k ? ldf(x + m * p.ldx + kk) : 0.0f;
-            if constexpr (PL == 3) {
-                const Planes pl = planes_of(v);
+        // the phase's columns of x, padded with zeros, eight at a time
+        const int chunks = (pe - ph) * 8;
+        for (int m = 0; m < p.rows; ++m) {
+            const X *xr = x + m * p.ldx + (int64_t)ph * 64;
+            for (int c = threadIdx.x * 8; c < chunks * 8; c += WARPS * 32 * 8) {
+                const int left = p.q.k - ph * 64 - c;  // columns there are
+                struct alignas(16) {
+                    X v[8];
+                } in;
+                if (p.vec && left >= 8) {
+                    const uint4 *src = reinterpret_cast<const uint4 *>(xr + c);
+                    uint4 *dst = reinterpret_cast<uint4 *>(&in);
 #pragma unroll
-                for (int i = 0; i < 3; ++i) xs[(m * 3 + i) * ldxs + c] = pl.v[i];
-            } else {
-                xs[m * ldxs + c] = cvt<T>(v);
+                    for (int i = 0; i < (int)sizeof(in) / 16; ++i) dst[i] = __ldg(src + i);
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) in.v[i] = i < left ? xr[c + i] : cvt<X>(0.0f);
+                }
+                if constexpr (PL == 3) {
+                    struct alignas(16) {
+                        T v[3][8];
+                    } out;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const Planes pl = planes_of(in.v[i]);
+                        out.v[0][i] = pl.v[0], out.v[1][i] = pl.v[1], out.v[2][i] = pl.v[2];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 3; ++i)
+                        *reinterpret_cast<uint4 *>(xs + (m * 3 + i) * ldxs + c) = reinterpret_cast<const uint4 *>(&out)[i];
+                } else {
+                    *reinterpret_cast<uint4 *>(xs + m * ldxs + c) = *reinterpret_cast<const uint4 *>(&in);
+                }
             }
         }
         __syncthreads();
@@ -292,7 +314,8 @@ template <typename T, typename X, int NC, bool G32>
 cudaError_t launch_few(const Q4P &q, int rows, const X *x, int64_t ldx, X *y, int64_t ldy, cudaStream_t st) {
     constexpr int PL = std::is_same<X, float>::value ? 3 : 1;
     // warps along k until there are about 16 a multiprocessor, at least 4 tiles each
-    FewP p{q, rows, 1, 1, 0, ldx, ldy};
+    FewP p{q, rows, 1, 1, 0, 0, ldx, ldy};
+    p.vec = reinterpret_cast<uintptr_t>(x) % 16 == 0 && ldx * (int64_t)sizeof(X) % 16 == 0;
     const int64_t want = 16LL * num_sms();
     while (p.wk < WARPS && (int64_t)q.nt * p.wk < want && q.kb >= 8 * p.wk) p.wk *= 2;
     while (p.s < 8 && (int64_t)q.nt * p.wk * p.s < want && q.kb >= 8 * p.wk * p.s) p.s *= 2;

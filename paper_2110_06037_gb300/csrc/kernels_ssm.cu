@@ -30,7 +30,8 @@ __device__ __forceinline__ Seq sequence(const SeqArgs &q, int b) {
     return s;
 }
 
-__device__ __forceinline__ float silu(float v) { return v / (1.0f + expf(-v)); }
+// by the approximate exponential and division (2 ulp each; a denominator beyond 2^126 gives 0)
+__device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
 // log(1 + e^v) without overflow, and exact where e^v is small
 __device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v))); }
 
@@ -41,7 +42,7 @@ constexpr int MAX_W = 8;
 // over TT tokens, the last W - 1 inputs in registers: each input is read once,
 // and the W - 1 before the run once more (from L2).  Bound by memory.
 template <typename T, int W, int V, int TT>
-__global__ void __launch_bounds__(128) causal_conv_kernel(SeqArgs q, const T *__restrict__ x, int64_t ldx, T *__restrict__ y,
+__global__ void __launch_bounds__(128, 4) causal_conv_kernel(SeqArgs q, const T *__restrict__ x, int64_t ldx, T *__restrict__ y,
                                                           int64_t ldy, T *kept, const float *__restrict__ w,
                                                           const float *__restrict__ bias, int C, int act) {
     griddep_launch();
@@ -76,29 +77,42 @@ __global__ void __launch_bounds__(128) causal_conv_kernel(SeqArgs q, const T *__
         for (int v = 0; v < V; ++v) h[j][v] = have ? ldf(p.v + v) : 0.0f;
     }
     const int n = (int)min((int64_t)TT, s.len - t0);
-    constexpr int U = 8;  // loads in flight
+    constexpr int U = 4;  // tokens at once; the next ones' loads are in flight meanwhile
+    Piece next[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+        if (u < n) next[u] = *reinterpret_cast<const Piece *>(xr + (int64_t)u * ldx);
     for (int t = 0; t < n; t += U) {
-        Piece in[U];
+        float win[W - 1 + U][V];  // inputs t + 1 - W to t + U - 1
+#pragma unroll
+        for (int j = 0; j + 1 < W; ++j)
+#pragma unroll
+            for (int v = 0; v < V; ++v) win[j][v] = h[j + 1][v];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (t + u < n) in[u] = *reinterpret_cast<const Piece *>(xr + (int64_t)(t + u) * ldx);
+#pragma unroll
+            for (int v = 0; v < V; ++v) win[W - 1 + u][v] = ldf(next[u].v + v);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (t + U + u < n) next[u] = *reinterpret_cast<const Piece *>(xr + (int64_t)(t + U + u) * ldx);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (t + u < n) {
                 Piece out;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-#pragma unroll
-                    for (int j = 0; j + 1 < W; ++j) h[j][v] = h[j + 1][v];
-                    h[W - 1][v] = ldf(in[u].v + v);
                     float a = b[v];
 #pragma unroll
-                    for (int j = 0; j < W; ++j) a = fmaf(wt[j][v], h[j][v], a);
+                    for (int j = 0; j < W; ++j) a = fmaf(wt[j][v], win[u + j][v], a);
                     out.v[v] = cvt<T>(act ? silu(a) : a);
                 }
                 *reinterpret_cast<Piece *>(yr + (int64_t)(t + u) * ldy) = out;
             }
         }
+#pragma unroll
+        for (int j = 1; j < W; ++j)
+#pragma unroll
+            for (int v = 0; v < V; ++v) h[j][v] = win[U - 1 + j][v];
     }
     // The thread of the first run also leaves the last W inputs behind: it alone
     // has read the kept ones of its channels.

@@ -214,6 +214,43 @@ def test_norm(dt, rdt, rows, d, kind):
         close(normed, refn, 64 * E32 * size * 32 * 32, dt)
 
 
+@pytest.mark.parametrize("dt, rdt", [("f32", "f32"), ("f16", "f16"), ("bf16", "f32")])
+@pytest.mark.parametrize("d", [512, 1000, 2056, 4096])
+@pytest.mark.parametrize("kind, gate, at, per, parts", [
+    ("rms", "silu", "after", 1, "all"), ("layer", "sigmoid", "before", 3, "all"), ("rms", "none", "after", 1, "pre"),
+    ("rms", "silu", "before", 1, "post"), ("layer", "linear", "after", 1000, "plain")])
+def test_norm_of_many_rows(dt, rdt, d, kind, gate, at, per, parts):
+    """More rows than a wave of blocks; every row against the rows one by one, in place too."""
+    import torch
+    import paper_2110_06037_gb300 as sn
+    rng = np.random.default_rng(d)
+    rows = 1301
+    w = {k: (1 + 0.2 * rng.normal(size=d)).astype(np.float32) for k in ("post", "post_bias", "pre", "pre_bias", "scale")}
+    names = {"all": w, "pre": ("pre",), "post": ("post",), "plain": ("scale",)}[parts]
+    use = {k: w[k] for k in names}
+    wide = dev(rng.normal(size=(rows, 2 * d + 16)) + 0.5, dt)
+    y, g = (None if parts == "pre" else wide[:, 8:d + 8]), wide[:: per if per > 1 else 1, d + 8:2 * d + 8]
+    g = None if gate == "none" else g[: -(-rows // per)]
+    if g is not None and g.shape[0] * per < rows:
+        g = wide[: -(-rows // per), d + 8:2 * d + 8]
+    r = None if parts == "post" else dev(2 * rng.normal(size=(rows, d)), rdt)
+    norm = sn.BlockNorm(d, kind, 1e-3, gate=gate, gate_at=at, **{k: dev(v) for k, v in use.items()})
+    total, normed = norm(y, residual=r, gate=g, rows_per_gate=per, dtype=tdt(dt))
+    ref, refn = ob.block_norm(None if y is None else host(y), None if r is None else host(r), None if g is None else host(g),
+                              per, kind, 1e-3, gate_act=gate, at=at, **use)
+    size = 1 + np.abs(ref).max(1, keepdims=True) + np.abs(host(wide)).max()
+    if g is not None:
+        size = size * (1 + np.abs(host(g)).max())
+    if total is not r:
+        close(total, ref, 64 * E32 * size * 32, rdt if r is not None else dt)
+    if normed is not None:
+        close(normed, refn, 64 * E32 * size * 32 * 32, dt)
+    if y is not None and r is not None and normed is not None:
+        r2, y2 = r.clone(), y.clone()
+        a, b = norm(y2, residual=r2, gate=g, rows_per_gate=per, out=r2, out_normed=y2)
+        assert torch.equal(a, total) and torch.equal(b, normed)
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("d", [40, 1000, 9000])
 def test_norm_parts_alone_strides_and_in_place(dt, d):
