@@ -7,9 +7,9 @@
 // statistics, so nothing is read twice; mean and variance are two reductions over
 // the registers (the variance of v - mean, not a difference of squares).
 //
-// Three kernels.  Many rows of up to 4096 aligned values: persistent blocks, a thread
-// to eight neighbours of a row, whose weights stay in its registers; the next rows
-// come by bulk copies into a ring of shared memory while one is worked on.  Few or
+// Three kernels.  Many rows of up to 4096 aligned values: persistent blocks, a
+// thread's weights in its registers; the next rows come by bulk copies into a ring
+// of shared memory while one is worked on.  Few or
 // unaligned rows, or up to 8192 values: a block (or a warp) a row, straight from
 // global memory.  Longer rows: a block a row, the row read again for each statistic.
 // 8190 x 4096, bf16 with an fp32 residual: the block a row took 208 us (the loads of
@@ -301,17 +301,17 @@ __device__ __forceinline__ void store4(T *dst, const float *v) {
     else *reinterpret_cast<uint2 *>(dst) = make_uint2(tc::pack2<T>(v[0], v[1]), tc::pack2<T>(v[2], v[3]));
 }
 
-template <typename T, typename R>
-__global__ void __launch_bounds__(512) block_norm_ring_kernel(const __grid_constant__ RingP q) {
+template <typename T, typename R, int NP>
+__global__ void __launch_bounds__(256, 2) block_norm_ring_kernel(const __grid_constant__ RingP q) {
+    constexpr int V = 4 * NP;
     extern __shared__ __align__(128) uint8_t ring[];
     __shared__ __align__(8) uint64_t full[RING_MAX];
     __shared__ float sh[64];
     __shared__ int stop_sh;
     const NormP &p = q.n;
-    // a thread's values: four at 4 t and four half a row of threads further on, so that
-    // a warp's accesses to fp32 rows are as contiguous as those to 16-bit ones
-    const int at[2] = {(int)threadIdx.x * 4, (int)(threadIdx.x + blockDim.x) * 4};
-    const bool live[2] = {at[0] < p.d, at[1] < p.d};  // (d is a multiple of 4)
+    // a thread's values: four neighbours every blockDim fours, so that a warp's
+    // accesses to fp32 rows are as contiguous as those to 16-bit ones
+    const int at = threadIdx.x * 4, hop = blockDim.x * 4;
     const int64_t step = gridDim.x;
     if (threadIdx.x == 0) {
         for (int i = 0; i < q.stages; ++i) tc::mbar_init(&full[i], 1);
@@ -332,91 +332,135 @@ __global__ void __launch_bounds__(512) block_norm_ring_kernel(const __grid_const
         const uint32_t dst = tc::su32(ring) + (uint32_t)(s * q.stage_bytes);
         tc::mbar_expect_tx(&full[s], (p.a.y ? tb : 0u) + (p.a.gate ? tb : 0u) + (p.a.res ? rb : 0u));
         if (p.a.y) bulk_load(dst, static_cast<const T *>(p.a.y) + row * p.a.ldy, tb, &full[s]);
-        if (p.a.gate) bulk_load(dst + q.gate_at, static_cast<const T *>(p.a.gate) + (p.a.per_gate == 1 ? row : row / p.a.per_gate) * p.a.ldg, tb, &full[s]);
+        if (p.a.gate)
+            bulk_load(dst + q.gate_at, static_cast<const T *>(p.a.gate) + (p.a.per_gate == 1 ? row : row / p.a.per_gate) * p.a.ldg, tb,
+                      &full[s]);
         if (p.a.res) bulk_load(dst + q.res_at, static_cast<const R *>(p.a.res) + row * p.a.ldr, rb, &full[s]);
     };
     if (threadIdx.x == 0)
         for (int i = 0; i < q.stages && ahead < p.a.rows; ++i) issue();
-    // the weights of this thread's eight values; scale and post norm in one where nothing is added between
-    float w[PIECE], wb[PIECE], sc[PIECE], u[PIECE], ub[PIECE];
+    // this thread's weights: the post norm's times the scale, and the pre norm's (zero
+    // behind the row's end, so that nothing there counts; biases are read in place)
+    float w[V], u[V];
 #pragma unroll
-    for (int j = 0; j < PIECE; ++j) w[j] = sc[j] = u[j] = 1.0f, wb[j] = ub[j] = 0.0f;
+    for (int i = 0; i < NP; ++i) {
+        const int c = at + i * hop;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (!live[i]) continue;
-        if (p.post) load4(w + 4 * i, p.post + at[i]);
-        if (p.post_b) load4(wb + 4 * i, p.post_b + at[i]);
-        if (p.scale) load4(sc + 4 * i, p.scale + at[i]);
-        if (p.pre) load4(u + 4 * i, p.pre + at[i]);
-        if (p.pre_b) load4(ub + 4 * i, p.pre_b + at[i]);
+        for (int j = 0; j < 4; ++j) w[4 * i + j] = u[4 * i + j] = c < p.d ? 1.0f : 0.0f;
+        if (c >= p.d) continue;
+        if (p.post) load4(w + 4 * i, p.post + c);
+        if (p.scale) {
+            float f[4];
+            load4(f, p.scale + c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[4 * i + j] *= f[j];
+        }
+        if (p.pre) load4(u + 4 * i, p.pre + c);
     }
     const float inv_d = 1.0f / (float)p.d;
     int turn = 0;
-    auto norm = [&](float (&v)[PIECE], const float (&wt)[PIECE], const float (&b)[PIECE], bool biased) {
+    // v centred (layer), and its factor 1 / sqrt(mean square + eps)
+    auto stats = [&](float (&v)[V]) {
         if (p.kind == SN_NORM_LAYER) {
             float s = 0.0f;
 #pragma unroll
-            for (int j = 0; j < PIECE; ++j) s += v[j];
+            for (int j = 0; j < V; ++j) s += v[j];
             const float mean = block_sum(s, sh, turn) * inv_d;
 #pragma unroll
-            for (int j = 0; j < PIECE; ++j) v[j] = live[j / 4] ? v[j] - mean : 0.0f;
+            for (int i = 0; i < NP; ++i)
+                if (at + i * hop < p.d) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[4 * i + j] -= mean;
+                }
         }
-        float s = 0.0f;
+        float s[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-        for (int j = 0; j < PIECE; ++j) s = fmaf(v[j], v[j], s);
-        const float r = rsqrtf(block_sum(s, sh, turn) * inv_d + p.eps);
+        for (int j = 0; j < V; ++j) s[j % 4] = fmaf(v[j], v[j], s[j % 4]);
+        return rsqrtf(block_sum((s[0] + s[1]) + (s[2] + s[3]), sh, turn) * inv_d + p.eps);
+    };
+    // += bias (times scale), of the row's values there are
+    auto add_bias = [&](float (&v)[V], const float *b, const float *scale) {
 #pragma unroll
-        for (int j = 0; j < PIECE; ++j) v[j] = biased ? fmaf(v[j] * r, wt[j], b[j]) : v[j] * r * wt[j];
+        for (int i = 0; i < NP; ++i) {
+            const int c = at + i * hop;
+            if (c >= p.d) break;
+            float f[4], g[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+            load4(f, b + c);
+            if (scale) load4(g, scale + c);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[4 * i + j] = fmaf(f[j], g[j], v[4 * i + j]);
+        }
     };
     int s = 0;
     uint32_t par = 0;
     for (int64_t row = blockIdx.x; row < p.a.rows; row += step) {
         if (!tc::mbar_wait(&full[s], par)) stop_sh = 1;
         const uint8_t *st = ring + s * q.stage_bytes;
-        float v[PIECE], g[PIECE], r[PIECE];
+        float v[V], g[V], r[V];
 #pragma unroll
-        for (int j = 0; j < PIECE; ++j) v[j] = r[j] = 0.0f, g[j] = 1.0f;
+        for (int i = 0; i < NP; ++i) {
+            const int c = at + i * hop;
+            const bool in = c < p.d;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            if (!live[i]) continue;
-            if (p.a.y) load4(v + 4 * i, reinterpret_cast<const T *>(st) + at[i]);
-            if (p.a.gate) load4(g + 4 * i, reinterpret_cast<const T *>(st + q.gate_at) + at[i]);
-            if (p.a.res) load4(r + 4 * i, reinterpret_cast<const R *>(st + q.res_at) + at[i]);
+            for (int j = 0; j < 4; ++j) v[4 * i + j] = g[4 * i + j] = r[4 * i + j] = 0.0f;
+            if (in && p.a.y) load4(v + 4 * i, reinterpret_cast<const T *>(st) + c);
+            if (in && p.a.gate) load4(g + 4 * i, reinterpret_cast<const T *>(st + q.gate_at) + c);
+            if (in && p.a.res) load4(r + 4 * i, reinterpret_cast<const R *>(st + q.res_at) + c);
         }
         __syncthreads();  // the stage has been read
         if (stop_sh) break;
         if (threadIdx.x == 0 && ahead < p.a.rows) issue();
         if (p.a.y) {
             if (p.a.gate) {
+                if (p.gate != SN_GATE_LINEAR) {
+                    const bool sig = p.gate == SN_GATE_SIGMOID;
 #pragma unroll
-                for (int j = 0; j < PIECE; ++j) {
-                    g[j] = gate_value(g[j], p.gate);
-                    if (!p.after) v[j] *= g[j];
+                    for (int j = 0; j < V; ++j) g[j] = __fdividef(sig ? 1.0f : g[j], 1.0f + __expf(-g[j]));
+                }
+                if (!p.after) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) v[j] *= g[j];
                 }
             }
-            if (p.post) norm(v, w, wb, p.post_b != nullptr);
+            if (p.post) {
+                const float f = stats(v);
 #pragma unroll
-            for (int j = 0; j < PIECE; ++j) {
-                if (p.a.gate && p.after) v[j] *= g[j];
-                v[j] = p.scale ? fmaf(v[j], sc[j], r[j]) : v[j] + r[j];
+                for (int j = 0; j < V; ++j) v[j] *= f * w[j];
+                if (p.post_b) add_bias(v, p.post_b, p.scale);
+            } else if (p.scale) {
+#pragma unroll
+                for (int j = 0; j < V; ++j) v[j] *= w[j];
             }
-        } else {
+            if (p.a.gate && p.after) {
 #pragma unroll
-            for (int j = 0; j < PIECE; ++j) v[j] = r[j];
+                for (int j = 0; j < V; ++j) r[j] = fmaf(v[j], g[j], r[j]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j) r[j] += v[j];
+            }
         }
         if (p.a.sum) {
+            if (p.a.res) {
+                R *o = static_cast<R *>(p.a.sum) + row * p.a.lds;
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                if (!live[i]) continue;
-                if (p.a.res) store4(static_cast<R *>(p.a.sum) + row * p.a.lds + at[i], v + 4 * i);
-                else store4(static_cast<T *>(p.a.sum) + row * p.a.lds + at[i], v + 4 * i);
+                for (int i = 0; i < NP; ++i)
+                    if (at + i * hop < p.d) store4(o + at + i * hop, r + 4 * i);
+            } else {
+                T *o = static_cast<T *>(p.a.sum) + row * p.a.lds;
+#pragma unroll
+                for (int i = 0; i < NP; ++i)
+                    if (at + i * hop < p.d) store4(o + at + i * hop, r + 4 * i);
             }
         }
         if (p.pre) {
-            norm(v, u, ub, p.pre_b != nullptr);
+            const float f = stats(r);
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-                if (live[i]) store4(static_cast<T *>(p.a.normed) + row * p.a.ldn + at[i], v + 4 * i);
+            for (int j = 0; j < V; ++j) r[j] *= f * u[j];
+            if (p.pre_b) add_bias(r, p.pre_b, nullptr);
+            T *o = static_cast<T *>(p.a.normed) + row * p.a.ldn;
+#pragma unroll
+            for (int i = 0; i < NP; ++i)
+                if (at + i * hop < p.d) store4(o + at + i * hop, r + 4 * i);
         }
         if (++s == q.stages) {
             s = 0;
@@ -433,6 +477,22 @@ __global__ void __launch_bounds__(512) block_norm_ring_kernel(const __grid_const
     }
 }
 
+template <typename T, typename R, int NP>
+cudaError_t launch_ring_np(const RingP &q, int threads, cudaStream_t st) {
+    const int per_sm = 512 / threads, room = 220 * 1024 / per_sm;  // blocks a multiprocessor, shared memory of each
+    static bool set = false;          // (idempotent)
+    if (!set) {
+        const cudaError_t e = cudaFuncSetAttribute(block_norm_ring_kernel<T, R, NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, 110 * 1024);
+        if (e != cudaSuccess) return e;
+        set = true;
+    }
+    RingP p = q;
+    p.stages = std::min(RING_MAX, room / q.stage_bytes);
+    const int64_t blocks = std::min<int64_t>(q.n.a.rows, (int64_t)per_sm * num_sms());
+    return launch_pdl(block_norm_ring_kernel<T, R, NP>, dim3((unsigned)blocks), dim3((unsigned)threads),
+                      (size_t)(p.stages * p.stage_bytes), st, p);
+}
+
 template <typename T, typename R>
 cudaError_t launch_ring(const NormP &p, cudaStream_t st) {
     RingP q{p, 0, 0, 0, 0, device_error_word()};
@@ -441,18 +501,9 @@ cudaError_t launch_ring(const NormP &p, cudaStream_t st) {
     q.gate_at = p.a.y ? tb : 0;
     q.res_at = q.gate_at + (p.a.gate ? tb : 0);
     q.stage_bytes = q.res_at + (p.a.res ? rb : 0);
-    const int threads = (p.d / PIECE + 31) / 32 * 32, blocks = threads <= 128 ? 4 : threads <= 256 ? 2 : 1;  // of 128 registers, a multiprocessor
-    const int room = 220 * 1024 / blocks - 1024;
-    q.stages = std::min(RING_MAX, room / q.stage_bytes);
-    static int set = 0;  // (idempotent)
-    const int smem = q.stages * q.stage_bytes;
-    if (smem > set) {
-        const cudaError_t e = cudaFuncSetAttribute(block_norm_ring_kernel<T, R>, cudaFuncAttributeMaxDynamicSharedMemorySize, room);
-        if (e != cudaSuccess) return e;
-        set = room;
-    }
-    return launch_pdl(block_norm_ring_kernel<T, R>, dim3((unsigned)std::min<int64_t>(p.a.rows, (int64_t)blocks * num_sms())),
-                      dim3((unsigned)threads), (size_t)smem, st, q);
+    if (p.d > 2048) return launch_ring_np<T, R, 4>(q, 256, st);
+    if (p.d > 1024) return launch_ring_np<T, R, 2>(q, 256, st);
+    return launch_ring_np<T, R, 2>(q, 128, st);
 }
 
 template <typename T, typename R, int TPR, int NP>

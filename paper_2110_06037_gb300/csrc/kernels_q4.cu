@@ -1,6 +1,7 @@
 // 4-bit weights: quantisation, layout, and the product with few rows of x
 // (sn_q4_quantize, sn_q4_pack, sn_q4_dense in include/sn.h; layout in q4_common.cuh).
 #include <algorithm>
+#include <climits>
 
 #include "q4_common.cuh"
 
@@ -105,7 +106,7 @@ __global__ void __launch_bounds__(128) q4_pack_scales_kernel(const uint16_t *__r
 // products on the tensor cores with the codes as the A operand, x as columns of B
 // (rows of fp32 x as three bf16 columns each), one fp32 multiply-add a group to
 // scale its sum.  A warp runs along k over one 16-row tile, its weights straight
-// from global memory to registers in the operand's layout, U tiles in flight; the
+// from global memory to registers in the operand's layout, eight tiles in flight; the
 // block's part of x lies in shared memory.  k is split over the WK warps of a
 // block that share a tile and over the S blocks of a cluster, whose sums meet in a
 // fixed order.
@@ -145,7 +146,7 @@ struct FewP {
 template <typename T, typename X, int NC, bool G32>
 __global__ void __launch_bounds__(WARPS * 32) q4_few_kernel(const __grid_constant__ FewP p, const X *__restrict__ x,
                                                             X *__restrict__ y) {
-    constexpr int PL = std::is_same<X, float>::value ? 3 : 1, COLS = NC * 8, U = NC == 1 ? 8 : 4;  // U: tiles in flight
+    constexpr int PL = std::is_same<X, float>::value ? 3 : 1, COLS = NC * 8, U = 4;
     extern __shared__ __align__(16) unsigned char smem[];
     float *red = reinterpret_cast<float *>(smem);                  // [WARPS][16][COLS]
     T *xs = reinterpret_cast<T *>(smem + WARPS * 16 * COLS * 4);   // [rows * PL][phase * 64 + 32]
@@ -162,29 +163,66 @@ __global__ void __launch_bounds__(WARPS * 32) q4_few_kernel(const __grid_constan
         for (int i = 0; i < 4; ++i) acc[c][i] = 0.0f;
     griddep_launch();
 
+    // the warp's tiles along k, U to a batch, two batches in flight
+    struct Batch {
+        uint4 codes[U];
+        uint32_t scales[U][G32 ? 2 : 1];
+    };
     const uint4 *codes = p.q.codes + (int64_t)(live ? nt : 0) * p.q.kb * 32 + lane;
     const uint32_t *scales = p.q.scales + (int64_t)(live ? nt : 0) * p.q.kg * 8 + g;
-    uint4 cw[U];
-    uint32_t sw[U][G32 ? 2 : 1];
-    auto fetch = [&](int at, int end) {
+    auto fetch = [&](Batch &f, int at, int end) {
+        const uint4 *cp = codes + (int64_t)at * 32;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (at + u < end) {
-                cw[u] = ld_stream(codes + (int64_t)(at + u) * 32);
+                f.codes[u] = ld_stream(cp + u * 32);
                 if constexpr (G32) {
-                    sw[u][0] = __ldg(scales + (int64_t)(2 * (at + u)) * 8);
-                    sw[u][1] = __ldg(scales + (int64_t)(2 * (at + u) + 1) * 8);
+                    f.scales[u][0] = __ldg(scales + (2 * (at + u)) * 8);
+                    f.scales[u][1] = __ldg(scales + (2 * (at + u) + 1) * 8);
                 } else {
-                    sw[u][0] = __ldg(scales + (int64_t)((at + u) >> (p.q.glog - 6)) * 8);
+                    f.scales[u][0] = __ldg(scales + ((at + u) >> (p.q.glog - 6)) * 8);
                 }
             }
+        }
+    };
+    // lane (g, t) reads columns g, g + 8, ... of B; behind the last column there is the
+    // last one again (its products land in columns that nobody reads)
+    const T *xcol[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) xcol[c] = xs + min(c * 8 + g, p.rows * PL - 1) * ldxs + 8 * t;
+    auto products = [&](const Batch &f, int u, int off) {  // off: the tile's columns in the phase
+        const uint32_t w[4] = {f.codes[u].x, f.codes[u].y, f.codes[u].z, f.codes[u].w};
+        uint32_t a[4][4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) a[i][j] = code_pair<T>(w[i], j);
+        const float2 s0 = scale_pair(f.scales[u][0], p.q.scale_bf16);
+        const float2 s1 = G32 ? scale_pair(f.scales[u][G32 ? 1 : 0], p.q.scale_bf16) : s0;
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            const uint4 lo = *reinterpret_cast<const uint4 *>(xcol[c] + off), hi = *reinterpret_cast<const uint4 *>(xcol[c] + off + 32);
+            float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            mma16816(d, a[0], lo.x, lo.y, T{});
+            mma16816(d, a[1], lo.z, lo.w, T{});
+            if constexpr (G32) {
+                acc[c][0] = fmaf(d[0], s0.x, acc[c][0]), acc[c][1] = fmaf(d[1], s0.x, acc[c][1]);
+                acc[c][2] = fmaf(d[2], s0.y, acc[c][2]), acc[c][3] = fmaf(d[3], s0.y, acc[c][3]);
+                d[0] = d[1] = d[2] = d[3] = 0.0f;
+            }
+            mma16816(d, a[2], hi.x, hi.y, T{});
+            mma16816(d, a[3], hi.z, hi.w, T{});
+            acc[c][0] = fmaf(d[0], s1.x, acc[c][0]), acc[c][1] = fmaf(d[1], s1.x, acc[c][1]);
+            acc[c][2] = fmaf(d[2], s1.y, acc[c][2]), acc[c][3] = fmaf(d[3], s1.y, acc[c][3]);
         }
     };
     bool first = true;
     for (int ph = b0; ph < b1; ph += p.phase) {
         const int pe = min(ph + p.phase, b1);
         const int w0 = ph + (pe - ph) * wki / p.wk, w1 = live ? ph + (pe - ph) * (wki + 1) / p.wk : w0;
-        fetch(w0, w1);  // (the weights do not depend on the kernel before)
+        Batch f0, f1;  // (the weights do not depend on the kernel before)
+        fetch(f0, w0, w1);
+        fetch(f1, w0 + U, w1);
         if (first) griddep_wait();
         else __syncthreads();
         first = false;
@@ -224,50 +262,24 @@ __global__ void __launch_bounds__(WARPS * 32) q4_few_kernel(const __grid_constan
             }
         }
         __syncthreads();
-        for (int at = w0; at < w1; at += U) {
-            uint4 cur[U];
-            uint32_t csw[U][G32 ? 2 : 1];
+        int at = w0, off = (w0 - ph) * 64;
+        for (; at + 4 * U <= w1; at += 2 * U, off += 2 * U * 64) {  // whole batches, whole batches ahead
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                cur[u] = cw[u];
-                csw[u][0] = sw[u][0];
-                if constexpr (G32) csw[u][1] = sw[u][1];
-            }
-            fetch(at + U, w1);
+            for (int u = 0; u < U; ++u) products(f0, u, off + u * 64);
+            fetch(f0, at + 2 * U, INT_MAX);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (at + u >= w1) break;
-                const uint32_t w[4] = {cur[u].x, cur[u].y, cur[u].z, cur[u].w};
-                uint32_t a[4][4];
+            for (int u = 0; u < U; ++u) products(f1, u, off + (U + u) * 64);
+            fetch(f1, at + 3 * U, INT_MAX);
+        }
+        for (; at < w1; at += 2 * U, off += 2 * U * 64) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
+            for (int u = 0; u < U; ++u)
+                if (at + u < w1) products(f0, u, off + u * 64);
+            fetch(f0, at + 2 * U, w1);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) a[i][j] = code_pair<T>(w[i], j);
-#pragma unroll
-                for (int c = 0; c < NC; ++c) {
-                    const int col = c * 8 + g;
-                    uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-                    if (col < p.rows * PL) {
-                        const uint4 *xp = reinterpret_cast<const uint4 *>(xs + col * ldxs + (at + u - ph) * 64 + 8 * t);
-                        lo = xp[0];
-                        hi = xp[4];
-                    }
-                    float d[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                    mma16816(d, a[0], lo.x, lo.y, T{});
-                    mma16816(d, a[1], lo.z, lo.w, T{});
-                    if constexpr (G32) {
-                        const float2 s = scale_pair(csw[u][0], p.q.scale_bf16);
-                        acc[c][0] = fmaf(d[0], s.x, acc[c][0]), acc[c][1] = fmaf(d[1], s.x, acc[c][1]);
-                        acc[c][2] = fmaf(d[2], s.y, acc[c][2]), acc[c][3] = fmaf(d[3], s.y, acc[c][3]);
-                        d[0] = d[1] = d[2] = d[3] = 0.0f;
-                    }
-                    mma16816(d, a[2], hi.x, hi.y, T{});
-                    mma16816(d, a[3], hi.z, hi.w, T{});
-                    const float2 s = scale_pair(csw[u][G32 ? 1 : 0], p.q.scale_bf16);
-                    acc[c][0] = fmaf(d[0], s.x, acc[c][0]), acc[c][1] = fmaf(d[1], s.x, acc[c][1]);
-                    acc[c][2] = fmaf(d[2], s.y, acc[c][2]), acc[c][3] = fmaf(d[3], s.y, acc[c][3]);
-                }
-            }
+            for (int u = 0; u < U; ++u)
+                if (at + U + u < w1) products(f1, u, off + (U + u) * 64);
+            fetch(f1, at + 3 * U, w1);
         }
     }
     if (first) griddep_wait();  // a block without columns of its own still may not leave early

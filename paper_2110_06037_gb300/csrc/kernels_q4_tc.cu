@@ -4,12 +4,13 @@
 //   D[m, j] = sum_k x[m, k] * w[j, k],  w = q * scale rounded to the operand type
 //
 // A tile is 128 G rows of x by BN outputs, accumulated in TMEM over steps of 64
-// columns.  x comes by TMA; the weights are expanded in the kernel: a warp reads a
-// 16 x 64 tile of codes (512 contiguous bytes, four steps ahead, in registers),
-// makes codes exact 16-bit values, multiplies by the group's scale in packed
-// 16-bit arithmetic, one rounding, and writes the operand's 128-byte-swizzled rows
-// into the stage.  Codes are a quarter of the bytes that 16-bit weights would
-// move, and an SM expands only the BN / G rows it stages.
+// columns.  x, codes and scales come by TMA; the weights are expanded in the kernel:
+// a warp reads 16 x 64 tiles of codes from shared memory, makes codes exact 16-bit
+// values, multiplies by the group's scale in packed 16-bit arithmetic, one rounding,
+// and writes the operand's 128-byte-swizzled rows into the stage.  Codes are a
+// quarter of the bytes that 16-bit weights would move, and an SM expands only the
+// BN / G rows it stages.  (Codes loaded straight into registers, some steps ahead,
+// were waited for by every step's proxy fence: 338 us for 2048 rows, 4096 -> 8448.)
 // G = 2: a CTA pair shares a tile of 256 rows; each stages 128 rows of x and half
 // of the weights, which halves what a tile reads through L2 and expands per MMA.
 //
@@ -23,9 +24,10 @@
 // (2^-25 and less) is left out.  One k step then is five.  (A fourth plane is the
 // first with zeros for what is not finite: the second part of w is often 0.)
 //
-// Warps: 0 loads x and allocates TMEM, 1 issues the MMAs (of the pair's leader), 4
-// to 7 drain the accumulators (two, so that a tile's epilogue overlaps the next
-// tile's products), 8 to 15 expand weights.  Waits are bounded; one that expires
+// Warps: 0 loads x and allocates TMEM, 1 issues the MMAs (of the pair's leader), 2
+// loads codes and scales, 4 to 7 drain the accumulators (two, so that a tile's
+// epilogue overlaps the next tile's products), 8 to 15 expand weights, four the even
+// column blocks and four the odd ones.  Waits are bounded; one that expires
 // records its cause in the library's error word and stops the pair.
 #include <algorithm>
 
@@ -38,10 +40,13 @@ namespace {
 
 using namespace tc;
 
-constexpr int Q4_STAGES = 6, Q4_THREADS = 512, Q4_EXPAND = 8, Q4_AHEAD = 4;
+constexpr int Q4_STAGES = 5, Q4_THREADS = 512;
+constexpr int Q4_EXPAND = 4;                          // warps that expand a column block
+constexpr int Q4_CSTAGES = 6;                         // column blocks of codes and scales in flight
+constexpr uint32_t Q4_CBYTES = 8 * 512, Q4_CSTAGE = Q4_CBYTES + 8 * 64;  // eight tiles: codes; up to two groups' scales
 constexpr uint32_t Q4_A_BYTES = BM * BK * 2, Q4_B_BYTES = 128 * BK * 2, Q4_STAGE = Q4_A_BYTES + Q4_B_BYTES;
 constexpr uint32_t Q4_OUT_ROW = 128 + 16;  // staged output row: 32 values, and 16 bytes against bank conflicts
-constexpr size_t Q4_SMEM = Q4_STAGES * (size_t)Q4_STAGE + 4 * 32 * Q4_OUT_ROW + 1024;
+constexpr size_t Q4_SMEM = Q4_STAGES * (size_t)Q4_STAGE + Q4_CSTAGES * (size_t)Q4_CSTAGE + 4 * 32 * Q4_OUT_ROW + 1024;
 
 struct PromptP {
     Q4P q;
@@ -106,18 +111,20 @@ __device__ __forceinline__ uint32_t expand_rest(uint32_t c, const Scale2 &s, uin
 // T: the operands' type; X: x's and y's
 template <typename T, typename X, int G>
 __global__ void __launch_bounds__(Q4_THREADS, 1)
-    q4_prompt_kernel(const __grid_constant__ CUtensorMap mX, const __grid_constant__ PromptP p, X *__restrict__ y) {
+    q4_prompt_kernel(const __grid_constant__ CUtensorMap mX, const __grid_constant__ CUtensorMap mC,
+                     const __grid_constant__ CUtensorMap mS, const __grid_constant__ PromptP p, X *__restrict__ y) {
     constexpr bool F32 = std::is_same<X, float>::value;
     constexpr int COMBOS = F32 ? 5 : 1;
     constexpr uint32_t TMEM_COLS = G == 2 ? 512 : 256, ACC = TMEM_COLS / 2;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t full_bar[Q4_STAGES], empty_bar[Q4_STAGES], accf_bar[2], acce_bar[2];
+    __shared__ __align__(8) uint64_t cfull_bar[Q4_CSTAGES], cempty_bar[Q4_CSTAGES];
     __shared__ __align__(16) float bias_sh[4][32], pow_sh[4][32];
     __shared__ uint32_t tmem_sh;
     __shared__ volatile int abort_sh;
-    __shared__ int issued_sh, consumed_sh;
+    __shared__ int issued_sh, cissued_sh, consumed_sh;
     uint8_t *smem = reinterpret_cast<uint8_t *>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t *stg = smem + Q4_STAGES * Q4_STAGE;
+    uint8_t *cst = smem + Q4_STAGES * Q4_STAGE, *stg = cst + Q4_CSTAGES * Q4_CSTAGE;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = G == 2 ? cluster_rank() : 0u;
     const bool leader = rank == 0;
@@ -140,11 +147,16 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
         }
         if (lane == 10) {
             abort_sh = 0;
-            issued_sh = consumed_sh = 0;
+            issued_sh = cissued_sh = consumed_sh = 0;
+        }
+        if (lane >= 16 && lane < 16 + Q4_CSTAGES) {
+            mbar_init(&cfull_bar[lane - 16], 1);
+            mbar_init(&cempty_bar[lane - 16], Q4_EXPAND);
         }
         fence_mbar_init();
-    } else if (warp == 2 && lane == 0) {
-        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&mX)) : "memory");
+    } else if (warp == 2 && lane < 3) {
+        const CUtensorMap *m = lane == 0 ? &mX : lane == 1 ? &mC : &mS;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");
     }
     if (G == 2) cluster_sync_all();
     tc_fence_before();
@@ -288,54 +300,95 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                 else mbar_arrive(&acce_bar[b]);
             }
         }
-    } else if (warp >= 8) {  // ---------------- weights: one 16-row tile of this CTA's rows a step and warp
-        const int dw = warp - 8, g = lane / 4, t4 = lane % 4;
-        const int own = p.bn / G;  // rows this CTA stages
-        const bool has = dw * 16 < own;
-        const uint32_t row_at = (uint32_t)(dw * 16 + g) * 128;
+    } else if (warp == 2) {
+        if (lane == 0) {  // ---------------- loader of codes and scales (not written by the kernel before)
+            const int own = p.bn / G, halves = p.q.glog == 5 ? 2 : 1;
+            const uint32_t bytes = (uint32_t)(own / 16) * (512 + 32 * halves);
+            int s = 0, g = 0;
+            uint32_t par = 0;
+            bool stop = false;
+            for (int t = cid; t < total && !stop; t += ncl) {
+                const int tile = (t % p.ntiles * p.bn + (int)rank * own) / 16;
+                for (int kb = 0; kb < p.q.kb; ++kb, ++g) {
+                    if (!mbar_wait(&cempty_bar[s], par ^ 1u, p.wait_limit)) {
+                        atomicOr(p.err, ERR_TMA_WAIT);
+                        set_abort();
+                    }
+                    if (abort_sh) {
+                        stop = true;
+                        break;
+                    }
+                    const uint32_t dst = su32(cst + s * Q4_CSTAGE), bar = su32(&cfull_bar[s]);
+                    mbar_expect_tx(&cfull_bar[s], bytes);
+                    tma_3d<1>(dst, &mC, bar, 0, kb, tile);
+                    tma_3d<1>(dst + Q4_CBYTES, &mS, bar, 0, halves == 2 ? 2 * kb : kb >> (p.q.glog - 6), tile);
+                    if (++s == Q4_CSTAGES) {
+                        s = 0;
+                        par ^= 1u;
+                    }
+                }
+            }
+            cissued_sh = g;
+        }
+    } else if (warp >= 8) {  // ---------------- weights: this CTA's rows, two 16-row tiles a warp
+        const int grp = (warp - 8) / Q4_EXPAND, dw = (warp - 8) % Q4_EXPAND, g = lane / 4, t4 = lane % 4;
+        const int tiles = p.bn / G / 16, halves = p.q.glog == 5 ? 2 : 1;
         // rows g of even g store their columns' first half first, the others the
         // second, so that eight lanes' 16-byte pieces cover all banks
-        const int first = g & 1;
-        const uint32_t at0 = row_at + ((uint32_t)((4 * first + t4) ^ g) << 4), at1 = row_at + ((uint32_t)((4 * (first ^ 1) + t4) ^ g) << 4);
-        int s = 0;
-        uint32_t par = 0;
+        const bool odd = g & 1;
+        const uint32_t at0 = (uint32_t)g * 128 + ((uint32_t)((4 * (odd ? 1 : 0) + t4) ^ g) << 4);
+        const uint32_t at1 = (uint32_t)g * 128 + ((uint32_t)((4 * (odd ? 0 : 1) + t4) ^ g) << 4);
+        int s = 0, cs = 0, gk = 0;  // stage of the operands, stage of the codes, column blocks so far
+        uint32_t par = 0, cpar = 0;
         bool stop = false;
         for (int t = cid; t < total && !stop; t += ncl) {
-            const int tile = min((t % p.ntiles * p.bn + (int)rank * own) / 16 + dw, p.q.nt - 1);
-            const uint4 *codes = p.q.codes + (int64_t)tile * p.q.kb * 32 + lane;
-            const uint32_t *scales = p.q.scales + (int64_t)tile * p.q.kg * 8 + g;
-            float rp[2] = {1.0f, 1.0f};
+            float rp[2][2];
             if constexpr (std::is_same<T, __half>::value) {
-                rp[0] = 0x1p12f / __ldg(p.q.row_pow + tile * 16 + g);
-                rp[1] = 0x1p12f / __ldg(p.q.row_pow + tile * 16 + g + 8);
+                const int tile = (t % p.ntiles * p.bn + (int)rank * (p.bn / G)) / 16 + dw;
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        rp[i][r] = 0x1p12f / __ldg(p.q.row_pow + min(tile + i * Q4_EXPAND, p.q.nt - 1) * 16 + g + 8 * r);
             }
-            uint4 cw[Q4_AHEAD];
-            uint32_t sw[Q4_AHEAD][2];
-            auto fetch = [&](int i, int kb) {
-                if (!has || kb >= p.q.kb) return;
-                cw[i] = __ldg(codes + (int64_t)kb * 32);
-                if (p.q.glog == 5) {
-                    sw[i][0] = __ldg(scales + (int64_t)(2 * kb) * 8);
-                    sw[i][1] = __ldg(scales + (int64_t)(2 * kb + 1) * 8);
-                } else {
-                    sw[i][0] = sw[i][1] = __ldg(scales + (int64_t)(kb >> (p.q.glog - 6)) * 8);
-                }
-            };
-#pragma unroll
-            for (int i = 0; i < Q4_AHEAD; ++i) fetch(i, i);
-            for (int kb0 = 0; kb0 < p.q.kb && !stop; kb0 += Q4_AHEAD) {
-#pragma unroll
-                for (int i = 0; i < Q4_AHEAD; ++i) {
-                    if (kb0 + i >= p.q.kb || stop) break;
-                    const uint32_t w[4] = {cw[i].x, cw[i].y, cw[i].z, cw[i].w};
-                    Scale2 sc[2][2];  // [row g, row g + 8][half of the tile]
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float2 f = scale_pair(sw[i][h], p.q.scale_bf16);
-                        sc[0][h] = scale_parts<T>(f.x * rp[0]);
-                        sc[1][h] = scale_parts<T>(f.y * rp[1]);
+            for (int kb = 0; kb < p.q.kb && !stop; ++kb, ++gk) {
+                if ((gk & 1) == grp) {
+                    if (!mbar_wait(&cfull_bar[cs], cpar, p.wait_limit)) {
+                        if (lane == 0) {
+                            atomicOr(p.err, ERR_TMA_WAIT);
+                            set_abort();
+                        }
                     }
-                    fetch(i, kb0 + i + Q4_AHEAD);
+                    if (__any_sync(0xffffffffu, abort_sh)) {
+                        stop = true;
+                        break;
+                    }
+                    uint4 cw[2];
+                    uint32_t sw[2][2];
+                    const uint8_t *cb = cst + cs * Q4_CSTAGE;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int tile = dw + i * Q4_EXPAND;  // (behind the last: whatever lies there)
+                        cw[i] = *reinterpret_cast<const uint4 *>(cb + tile * 512 + lane * 16);
+                        sw[i][0] = *reinterpret_cast<const uint32_t *>(cb + Q4_CBYTES + (tile * halves) * 32 + g * 4);
+                        sw[i][1] = *reinterpret_cast<const uint32_t *>(cb + Q4_CBYTES + (tile * halves + halves - 1) * 32 + g * 4);
+                    }
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(&cempty_bar[cs]);
+                    Scale2 sc[2][2][2];  // [tile][row g, row g + 8][half]
+#pragma unroll
+                    for (int i = 0; i < 2; ++i)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float2 f = scale_pair(sw[i][h], p.q.scale_bf16);
+                            if constexpr (std::is_same<T, __half>::value) {
+                                sc[i][0][h] = scale_parts<T>(f.x * rp[i][0]);
+                                sc[i][1][h] = scale_parts<T>(f.y * rp[i][1]);
+                            } else {
+                                sc[i][0][h] = scale_parts<T>(f.x);
+                                sc[i][1][h] = scale_parts<T>(f.y);
+                            }
+                        }
 #pragma unroll 1
                     for (int c = 0; c < COMBOS; ++c) {
                         if (!mbar_wait(&empty_bar[s], par ^ 1u, p.wait_limit)) {
@@ -348,8 +401,12 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                             stop = true;
                             break;
                         }
-                        if (has) {
-                            uint8_t *b = smem + s * Q4_STAGE + Q4_A_BYTES;
+                        uint8_t *b = smem + s * Q4_STAGE + Q4_A_BYTES;
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            const int tile = dw + i * Q4_EXPAND;
+                            if (tile >= tiles) break;
+                            const uint32_t w[4] = {cw[i].x, cw[i].y, cw[i].z, cw[i].w};
 #pragma unroll
                             for (int r = 0; r < 2; ++r) {
                                 uint32_t v[2][4];
@@ -358,16 +415,17 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
 #pragma unroll
                                     for (int e = 0; e < 4; ++e) {
                                         const uint32_t code = code_pair<T>(w[2 * h + e / 2], r + 2 * (e % 2));
-                                        v[h][e] = expand<T>(code, sc[r][h], p.parts);
-                                        if (F32 && c >= 3) v[h][e] = expand_rest(code, sc[r][h], v[h][e]);
+                                        v[h][e] = expand<T>(code, sc[i][r][h], p.parts);
+                                        if (F32 && c >= 3) v[h][e] = expand_rest(code, sc[i][r][h], v[h][e]);
                                     }
-                                *reinterpret_cast<uint4 *>(b + at0 + r * 1024) =
-                                    first ? make_uint4(v[1][0], v[1][1], v[1][2], v[1][3]) : make_uint4(v[0][0], v[0][1], v[0][2], v[0][3]);
-                                *reinterpret_cast<uint4 *>(b + at1 + r * 1024) =
-                                    first ? make_uint4(v[0][0], v[0][1], v[0][2], v[0][3]) : make_uint4(v[1][0], v[1][1], v[1][2], v[1][3]);
+                                const uint4 lo = make_uint4(v[0][0], v[0][1], v[0][2], v[0][3]);
+                                const uint4 hi = make_uint4(v[1][0], v[1][1], v[1][2], v[1][3]);
+                                uint8_t *o = b + tile * 2048 + r * 1024;
+                                *reinterpret_cast<uint4 *>(o + at0) = odd ? hi : lo;
+                                *reinterpret_cast<uint4 *>(o + at1) = odd ? lo : hi;
                             }
-                            fence_proxy_async_smem();
                         }
+                        fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
                             if (G == 2) mbar_arrive_cluster(mapa(su32(&full_bar[s]), 0u));
@@ -378,6 +436,16 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                             par ^= 1u;
                         }
                     }
+                } else {  // the other warps' block
+                    s += COMBOS;
+                    if (s >= Q4_STAGES) {
+                        s -= Q4_STAGES;
+                        par ^= 1u;
+                    }
+                }
+                if (++cs == Q4_CSTAGES) {
+                    cs = 0;
+                    cpar ^= 1u;
                 }
             }
         }
@@ -393,6 +461,9 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                 for (int g = consumed_sh; g < issued_sh; ++g)
                     while (!mbar_try(&full_bar[g % Q4_STAGES], (uint32_t)(g / Q4_STAGES) & 1u) && clock64() - t0 < WAIT_LIMIT) {
                     }
+            for (int g = cissued_sh > Q4_CSTAGES ? cissued_sh - Q4_CSTAGES : 0; g < cissued_sh; ++g)
+                while (!mbar_try(&cfull_bar[g % Q4_CSTAGES], (uint32_t)(g / Q4_CSTAGES) & 1u) && clock64() - t0 < WAIT_LIMIT) {
+                }
             if (leader && consumed_sh > 0) {
                 const int g = consumed_sh - 1;
                 while (!mbar_try(&empty_bar[g % Q4_STAGES], (uint32_t)(g / Q4_STAGES) & 1u) && clock64() - t0 < WAIT_LIMIT) {
@@ -460,6 +531,7 @@ Shape4 choose(int64_t rows, int n, int64_t steps) {
 
 template <typename T, typename X, int G>
 cudaError_t launch_prompt(const CUtensorMap &mX, PromptP &p, X *y, cudaStream_t st) {
+    static_assert(!std::is_same<X, float>::value || Q4_STAGES == 5, "a column block of fp32 rows is one round of the stages");
     auto kern = q4_prompt_kernel<T, X, G>;
     static bool set = false;  // (idempotent)
     if (!set) {
@@ -482,7 +554,15 @@ cudaError_t launch_prompt(const CUtensorMap &mX, PromptP &p, X *y, cudaStream_t 
     const int64_t total = (int64_t)p.mtiles * p.ntiles;
     if (total > INT32_MAX) return cudaErrorInvalidValue;
     cfg.gridDim = dim3((unsigned)(G * std::min<int64_t>(total, num_sms() / G)));
-    return cudaLaunchKernelEx(&cfg, kern, mX, p, y);
+    // codes as [nt][kb][256 halfwords], scales as [nt][kg][16]: a box is this CTA's tiles of one column block
+    CUtensorMap mC, mS;
+    const uint64_t cdims[3] = {256, (uint64_t)p.q.kb, (uint64_t)p.q.nt}, cstr[2] = {512, (uint64_t)p.q.kb * 512};
+    const uint64_t sdims[3] = {16, (uint64_t)p.q.kg, (uint64_t)p.q.nt}, sstr[2] = {32, (uint64_t)p.q.kg * 32};
+    const uint32_t tiles = (uint32_t)(p.bn / G / 16), cbox[3] = {256, 1, tiles}, sbox[3] = {16, p.q.glog == 5 ? 2u : 1u, tiles};
+    if (!tma_encode(&mC, SN_F16, 3, p.q.codes, cdims, cstr, cbox, CU_TENSOR_MAP_SWIZZLE_NONE) ||
+        !tma_encode(&mS, SN_F16, 3, p.q.scales, sdims, sstr, sbox, CU_TENSOR_MAP_SWIZZLE_NONE))
+        return cudaErrorInvalidValue;
+    return cudaLaunchKernelEx(&cfg, kern, mX, mC, mS, p, y);
 }
 
 template <typename T, typename X>

@@ -38,29 +38,41 @@ __device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.0f) + log
 constexpr int MAX_W = 8;
 
 // ------------------------------------------------------------- convolution
-// A thread takes V neighbouring channels (16 bytes where rows and weights allow)
-// over TT tokens, the last W - 1 inputs in registers: each input is read once,
-// and the W - 1 before the run once more (from L2).  Bound by memory.
-template <typename T, int W, int V, int TT>
-__global__ void __launch_bounds__(128, 4) causal_conv_kernel(SeqArgs q, const T *__restrict__ x, int64_t ldx, T *__restrict__ y,
-                                                          int64_t ldy, T *kept, const float *__restrict__ w,
-                                                          const float *__restrict__ bias, int C, int act) {
+// A thread takes V neighbouring channels (four where rows and weights allow)
+// over a run of tokens, its weights and the last W - 1 inputs in registers: each
+// input is read once, and the W - 1 before the run once more (from L2).  The run is
+// as long as one wave of blocks needs it to be, so that weights are loaded once for
+// as many tokens as can be.  Bound by memory.
+constexpr int CONV_THREADS = 128, CONV_BLOCKS = 4;  // blocks of 128 registers a thread on a multiprocessor
+template <typename T, int W, int V>
+__global__ void __launch_bounds__(CONV_THREADS, CONV_BLOCKS)
+    causal_conv_kernel(SeqArgs q, const T *__restrict__ x, int64_t ldx, T *__restrict__ y, int64_t ldy, T *kept,
+                       const float *__restrict__ w, const float *__restrict__ bias, int C, int act, int len) {
     griddep_launch();
     griddep_wait();
-    const int cb = (C + 128 * V - 1) / (128 * V), run = blockIdx.x / cb;
-    const int c0 = ((blockIdx.x - run * cb) * 128 + threadIdx.x) * V;
+    const uint32_t cg = (uint32_t)(C / V), id = blockIdx.x * CONV_THREADS + threadIdx.x;  // (V divides C)
+    const uint32_t run = id / cg;
+    const int c0 = (int)(id - run * cg) * V;
     const Seq s = sequence(q, blockIdx.y);
-    const int64_t t0 = (int64_t)run * TT;
-    if (c0 >= C || t0 >= s.len) return;
+    const int64_t t0 = (int64_t)run * len;
+    if (t0 >= s.len) return;
     struct alignas(sizeof(T) * V) Piece {
         T v[V];
     };
-    float wt[W][V], b[V], h[W][V];  // h[j]: the input j + 1 - W tokens from the present one
+    float wt[V * W], b[V], h[W][V];  // h[j]: the input j + 1 - W tokens from the present one
+    if constexpr (V % 4 == 0) {
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        b[v] = bias ? bias[c0 + v] : 0.0f;
+        for (int i = 0; i < V * W / 4; ++i)
+            *reinterpret_cast<float4 *>(wt + 4 * i) = __ldg(reinterpret_cast<const float4 *>(w + (int64_t)c0 * W) + i);
 #pragma unroll
-        for (int j = 0; j < W; ++j) wt[j][v] = w[(int64_t)(c0 + v) * W + j];
+        for (int i = 0; i < V / 4; ++i)
+            *reinterpret_cast<float4 *>(b + 4 * i) =
+                bias ? __ldg(reinterpret_cast<const float4 *>(bias + c0) + i) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < V * W; ++i) wt[i] = w[(int64_t)c0 * W + i];
+#pragma unroll
+        for (int v = 0; v < V; ++v) b[v] = bias ? bias[c0 + v] : 0.0f;
     }
     const T *xr = x + (s.first + t0) * ldx + c0;
     T *yr = y + (s.first + t0) * ldy + c0;
@@ -76,13 +88,14 @@ __global__ void __launch_bounds__(128, 4) causal_conv_kernel(SeqArgs q, const T 
 #pragma unroll
         for (int v = 0; v < V; ++v) h[j][v] = have ? ldf(p.v + v) : 0.0f;
     }
-    const int n = (int)min((int64_t)TT, s.len - t0);
-    constexpr int U = 4;  // tokens at once; the next ones' loads are in flight meanwhile
-    Piece next[U];
+    const int n = (int)min((int64_t)len, s.len - t0);
+    constexpr int U = 4;  // tokens at once; the next eight's loads are in flight meanwhile
+    Piece raw[2][U];
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (u < n) next[u] = *reinterpret_cast<const Piece *>(xr + (int64_t)u * ldx);
-    for (int t = 0; t < n; t += U) {
+    for (int u = 0; u < 2 * U; ++u)
+        if (u < n) raw[u / U][u % U] = *reinterpret_cast<const Piece *>(xr + u * ldx);
+    xr += 2 * U * ldx;
+    auto tokens = [&](Piece(&in)[U], int t) {
         float win[W - 1 + U][V];  // inputs t + 1 - W to t + U - 1
 #pragma unroll
         for (int j = 0; j + 1 < W; ++j)
@@ -91,28 +104,40 @@ __global__ void __launch_bounds__(128, 4) causal_conv_kernel(SeqArgs q, const T 
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int v = 0; v < V; ++v) win[W - 1 + u][v] = ldf(next[u].v + v);
+            for (int v = 0; v < V; ++v) win[W - 1 + u][v] = ldf(in[u].v + v);
 #pragma unroll
         for (int u = 0; u < U; ++u)
-            if (t + U + u < n) next[u] = *reinterpret_cast<const Piece *>(xr + (int64_t)(t + U + u) * ldx);
+            if (t + 2 * U + u < n) in[u] = *reinterpret_cast<const Piece *>(xr + u * ldx);
+        xr += U * ldx;
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (t + u < n) {
-                Piece out;
+                float a[V];
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    float a = b[v];
+                    a[v] = b[v];
 #pragma unroll
-                    for (int j = 0; j < W; ++j) a = fmaf(wt[j][v], win[u + j][v], a);
-                    out.v[v] = cvt<T>(act ? silu(a) : a);
+                    for (int j = 0; j < W; ++j) a[v] = fmaf(wt[v * W + j], win[u + j][v], a[v]);
                 }
-                *reinterpret_cast<Piece *>(yr + (int64_t)(t + u) * ldy) = out;
+                if (act) {
+#pragma unroll
+                    for (int v = 0; v < V; ++v) a[v] = silu(a[v]);
+                }
+                Piece out;
+#pragma unroll
+                for (int v = 0; v < V; ++v) out.v[v] = cvt<T>(a[v]);
+                *reinterpret_cast<Piece *>(yr) = out;
             }
+            yr += ldy;
         }
 #pragma unroll
         for (int j = 1; j < W; ++j)
 #pragma unroll
             for (int v = 0; v < V; ++v) h[j][v] = win[U - 1 + j][v];
+    };
+    for (int t = 0; t < n; t += 2 * U) {
+        tokens(raw[0], t);
+        tokens(raw[1], t + U);
     }
     // The thread of the first run also leaves the last W inputs behind: it alone
     // has read the kept ones of its channels.
@@ -126,15 +151,21 @@ __global__ void __launch_bounds__(128, 4) causal_conv_kernel(SeqArgs q, const T 
 template <typename T, int W>
 cudaError_t launch_conv(const SeqArgs &q, const T *x, int64_t ldx, T *y, int64_t ldy, T *kept, const float *w,
                         const float *bias, int C, int act, cudaStream_t st) {
-    constexpr int V = 16 / sizeof(T), TT = 32;
-    const bool vec = C % V == 0 && ldx % V == 0 && ldy % V == 0 && reinterpret_cast<uintptr_t>(x) % 16 == 0 &&
-                     reinterpret_cast<uintptr_t>(y) % 16 == 0 && reinterpret_cast<uintptr_t>(kept) % 16 == 0;
-    const int per = vec ? V : 1;
-    const int64_t blocks = (q.max_len + TT - 1) / TT * ((C + 128 * per - 1) / (128 * per));
-    if (blocks > INT32_MAX) return cudaErrorInvalidValue;
+    constexpr int V = 4;  // (eight 16-bit channels would need twice the registers)
+    auto at = [](const void *p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; };
+    constexpr size_t n = V * sizeof(T);
+    const bool vec = C % V == 0 && ldx % V == 0 && ldy % V == 0 && at(x, n) && at(y, n) && at(kept, n) && at(w, 16) && at(bias, 16);
+    // Runs of 8 to 256 tokens (a run's start has up to W - 1 = 7 tokens before it in
+    // its sequence), as long as the blocks fill one wave.
+    const int64_t groups = vec ? C / V : C, threads = (int64_t)num_sms() * CONV_BLOCKS * CONV_THREADS;
+    int64_t len = (q.tokens * groups + threads - 1) / threads;
+    len = len < 8 ? 8 : len > 256 ? 256 : (len + 3) / 4 * 4;
+    const int64_t blocks = ((q.max_len + len - 1) / len * groups + CONV_THREADS - 1) / CONV_THREADS;
+    if (blocks > (int64_t)UINT32_MAX / CONV_THREADS) return cudaErrorInvalidValue;
     const dim3 grid((unsigned)blocks, (unsigned)q.batch);
-    if (vec) return launch_pdl(causal_conv_kernel<T, W, V, TT>, grid, dim3(128), 0, st, q, x, ldx, y, ldy, kept, w, bias, C, act);
-    return launch_pdl(causal_conv_kernel<T, W, 1, TT>, grid, dim3(128), 0, st, q, x, ldx, y, ldy, kept, w, bias, C, act);
+    if (vec)
+        return launch_pdl(causal_conv_kernel<T, W, V>, grid, dim3(CONV_THREADS), 0, st, q, x, ldx, y, ldy, kept, w, bias, C, act, (int)len);
+    return launch_pdl(causal_conv_kernel<T, W, 1>, grid, dim3(CONV_THREADS), 0, st, q, x, ldx, y, ldy, kept, w, bias, C, act, (int)len);
 }
 
 template <typename T>
@@ -247,116 +278,162 @@ cudaError_t launch_scan(const SsmP &p, const T *xbc, const T *dtv, T *y, cudaStr
 }
 
 // --------------------------------------------------------------------- step
-// One token: the state is read, updated and written once.  A block takes `rows`
-// rows of one head of one sequence; a warp's lanes lie along the state's rows (VEC
-// values a piece, VPL pieces a lane, `lpr` lanes a row), RU rows per lane in
-// flight.  The convolution of the block's own channels and of its group's B and C
-// is done again by every block of the group (its inputs come from L2); each
-// channel's new input is stored by one of them, at a place none of them reads.
-template <typename T, int VEC, int VPL>
+// One token: the state is read, updated and written once.  The state's rows of the
+// heads of a group lie one behind the other and share B and C: a block takes `rows`
+// of them.  A warp's lanes lie along a row (VEC values a piece, VPL pieces a lane,
+// `lpr` lanes a row), RU rows per lane at once and the next RU in flight.  The
+// convolution of the block's own channels and of the group's B and C is done again
+// by every block of the group (its inputs come from L2); each channel's new input is
+// stored by one of them, at a place none of them reads.
+constexpr int STEP_ROWS = 256;  // most rows of a block
+// W: the convolution's width, or 0: p.W
+template <typename T, int VEC, int VPL, int W>
 __global__ void __launch_bounds__(256) ssm_step_kernel(const __grid_constant__ SsmP p, const T *__restrict__ xbc,
                                                        const T *__restrict__ dtv, T *kept, T *__restrict__ y, int rows,
                                                        int lpr) {
-    __shared__ __align__(16) float sv[256 + 2 * 256];  // x of the block's rows, B, C
-    __shared__ float sd[2];
+    __shared__ __align__(16) float sx[STEP_ROWS], sbc[2][256];  // x of the block's rows; B, C
+    __shared__ float2 sd[STEP_ROWS];                            // of the block's rows: time step, decay
     constexpr int RU = VPL * VEC >= 8 ? 2 : 4;
     griddep_launch();
     griddep_wait();
-    const int b = blockIdx.z, head = blockIdx.y, p0 = blockIdx.x * rows, tid = threadIdx.x;
-    const int np = min(rows, p.P - p0), grp = head / (p.H / p.G);
-    const int slot0 = p.q.slots ? p.q.slots[b] : b;
-    T *yr = y + (int64_t)b * p.ldy + head * p.P + p0;
-    if (slot0 < 0 || slot0 >= p.q.n_slots) {  // no slot: nothing to continue
-        for (int i = tid; i < np; i += 256) stf(yr + i, 0.0f);
+    const int b = blockIdx.z, grp = blockIdx.y, tid = threadIdx.x, hpg = p.H / p.G;
+    const int r0 = grp * hpg * p.P + blockIdx.x * rows, nr = min(rows, hpg * p.P - (int)blockIdx.x * rows);
+    const int slot = p.q.slots ? p.q.slots[b] : b;
+    T *yr = y + (int64_t)b * p.ldy + r0;
+    if (slot < 0 || slot >= p.q.n_slots) {  // no slot: nothing to continue
+        for (int i = tid; i < nr; i += 256) stf(yr + i, 0.0f);
         return;
     }
     const int pos = max(p.q.pos ? p.q.pos[b] : 0, 0);
-    const int sub = tid % lpr, rpb = 256 / lpr;  // rows that the block handles at once
-    const int64_t base = (((int64_t)slot0 * p.H + head) * p.P + p0) * p.N;
-    const int nv = (p.N + VEC - 1) / VEC;  // (VEC divides N)
+    const int sub = tid % lpr, first = tid / lpr, rpb = 256 / lpr;  // rows that the block handles at once
+    const int64_t base = ((int64_t)slot * p.H * p.P + r0) * p.N + sub * VEC;
+    const int nv = p.N / VEC;  // (VEC divides N)
     struct alignas(4 * VEC) Piece {
         float v[VEC];
     };
-    // the first rows' states, in flight before the convolution
     Piece h[RU][VPL];
-    auto load = [&](int r0) {
+    auto load = [&](Piece(&d)[RU][VPL], int r) {
 #pragma unroll
-        for (int u = 0; u < RU; ++u) {
-            const int r = r0 + u * rpb;
+        for (int u = 0; u < RU; ++u)
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
-                const int c = sub + i * lpr;
-                if (p.s_in && r < np && c < nv) h[u][i] = *reinterpret_cast<const Piece *>(p.s_in + base + (int64_t)r * p.N + c * VEC);
+                if (p.s_in && r + u * rpb < nr && sub + i * lpr < nv)
+                    d[u][i] = *reinterpret_cast<const Piece *>(p.s_in + base + (int64_t)(r + u * rpb) * p.N + i * lpr * VEC);
                 else
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) h[u][i].v[e] = 0.0f;
+                    for (int e = 0; e < VEC; ++e) d[u][i].v[e] = 0.0f;
             }
-        }
     };
-    load(tid / lpr);
-    if (tid == 0) {
+    load(h, first);  // in flight before the convolution
+    for (int i = tid; i < nr; i += 256) {
+        const int head = (r0 + i) / p.P;
         const float d = softplus(ldf(dtv + (int64_t)b * p.lddt + head) + (p.dt_bias ? p.dt_bias[head] : 0.0f));
-        sd[0] = d;
-        sd[1] = expf(d * p.a[head]);
+        sd[i] = make_float2(d, expf(d * p.a[head]));
     }
-    const int C = p.H * p.P + 2 * p.G * p.N;
+    const int C = p.H * p.P + 2 * p.G * p.N, width = W ? W : p.W;
     const T *xr = xbc + (int64_t)b * p.ldx;
-    for (int e = tid; e < np + 2 * p.N; e += 256) {
-        const int n = e - np;
-        const int c = n < 0 ? head * p.P + p0 + e
-                            : p.H * p.P + (n < p.N ? grp * p.N + n : p.G * p.N + grp * p.N + n - p.N);
-        T *kp = kept + (int64_t)slot0 * p.W * C + c;
-        const float *w = p.conv_w + (int64_t)c * p.W;
-        float acc = p.conv_b ? p.conv_b[c] : 0.0f;
-        for (int j = 0; j + 1 < p.W; ++j) {
-            const int back = p.W - 1 - j;
-            if (pos >= back) acc = fmaf(w[j], ldf(kp + (int64_t)((pos - back) % p.W) * C), acc);
-        }
+    T *kb = kept + (int64_t)slot * width * C;
+    int64_t at[W ? W : MAX_W];  // of tap j's kept input; -1: before the sequence's first
+#pragma unroll
+    for (int j = 0; j < (W ? W : MAX_W); ++j) {
+        const int back = width - 1 - j;
+        at[j] = back >= 0 && pos >= back ? (int64_t)((pos - back) % width) * C : -1;
+    }
+    const int64_t at_new = (int64_t)(pos % width) * C;
+    for (int e = tid; e < nr + 2 * p.N; e += 256) {
+        const int n = e - nr;
+        const int c = n < 0 ? r0 + e : p.H * p.P + (n < p.N ? grp * p.N + n : (p.G + grp - 1) * p.N + n);
+        const float *w = p.conv_w + (int64_t)c * width;
         const T now = xr[c];
-        acc = fmaf(w[p.W - 1], ldf(&now), acc);
-        sv[n < 0 ? e : 256 + n + (n >= p.N ? 256 - p.N : 0)] = silu(acc);
-        if (n < 0 || (p0 == 0 && head % (p.H / p.G) == 0)) kp[(int64_t)(pos % p.W) * C] = now;
+        T old[W ? W : MAX_W];
+#pragma unroll
+        for (int j = 0; j < (W ? W : MAX_W) - 1; ++j)
+            if (at[j] >= 0 && j + 1 < width) old[j] = kb[at[j] + c];
+        float acc = p.conv_b ? p.conv_b[c] : 0.0f;
+#pragma unroll
+        for (int j = 0; j < (W ? W : MAX_W) - 1; ++j)
+            if (at[j] >= 0 && j + 1 < width) acc = fmaf(w[j], ldf(old + j), acc);
+        acc = silu(fmaf(w[width - 1], ldf(&now), acc));
+        if (n < 0) sx[e] = acc;
+        else sbc[n >= p.N][n >= p.N ? n - p.N : n] = acc;
+        if (n < 0 || blockIdx.x == 0) kb[at_new + c] = now;
     }
     __syncthreads();
-    const float d = sd[0], da = sd[1], skip = p.d ? p.d[head] : 0.0f;
-    for (int r0 = tid / lpr; r0 - tid / lpr < np; r0 += RU * rpb) {  // (the same trips for every thread)
-        if (r0 != tid / lpr) load(r0);
+    Piece bv[VPL], cv[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i)
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+            const int n = (sub + i * lpr) * VEC + e;
+            bv[i].v[e] = n < p.N ? sbc[0][n] : 0.0f;
+            cv[i].v[e] = n < p.N ? sbc[1][n] : 0.0f;
+        }
+    for (int at_row = first; at_row - first < nr; at_row += RU * rpb) {  // (the same trips for every thread)
+        Piece nx[RU][VPL];
+        load(nx, at_row + RU * rpb);
+        float acc[RU];
 #pragma unroll
         for (int u = 0; u < RU; ++u) {
-            const int r = r0 + u * rpb;
-            const float x = r < np ? sv[r] : 0.0f, dx = d * x;
-            float acc = 0.0f;
+            const int r = at_row + u * rpb;
+            const bool in = r < nr;
+            const float2 dd = in ? sd[r] : make_float2(0.0f, 0.0f);
+            const float dx = in ? dd.x * sx[r] : 0.0f;
+            acc[u] = 0.0f;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
-                const int c = sub + i * lpr;
-                if (c < nv) {
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) {
-                        h[u][i].v[e] = fmaf(h[u][i].v[e], da, dx * sv[256 + c * VEC + e]);
-                        acc = fmaf(h[u][i].v[e], sv[512 + c * VEC + e], acc);
-                    }
-                    if (p.s_out && r < np) *reinterpret_cast<Piece *>(p.s_out + base + (int64_t)r * p.N + c * VEC) = h[u][i];
+                for (int e = 0; e < VEC; ++e) {
+                    h[u][i].v[e] = fmaf(h[u][i].v[e], dd.y, dx * bv[i].v[e]);
+                    acc[u] = fmaf(h[u][i].v[e], cv[i].v[e], acc[u]);
                 }
+                if (p.s_out && in && sub + i * lpr < nv)
+                    *reinterpret_cast<Piece *>(p.s_out + base + (int64_t)r * p.N + i * lpr * VEC) = h[u][i];
             }
-            for (int o = lpr / 2; o; o >>= 1) acc += __shfl_xor_sync(0xffffffffu, acc, o);
-            if (sub == 0 && r < np) stf(yr + r, fmaf(skip, x, acc));
         }
+        auto skip = [&](int r) { return p.d ? p.d[(r0 + r) / p.P] * sx[r] : 0.0f; };
+        if (RU == 4 && lpr == 32) {
+            // four rows' sums in six exchanges: lanes of each quarter end with one row's
+            const bool up = sub & 16, up2 = sub & 8;
+            float a0 = up ? acc[2 % RU] : acc[0], a1 = up ? acc[3 % RU] : acc[1 % RU];
+            a0 += __shfl_xor_sync(0xffffffffu, up ? acc[0] : acc[2 % RU], 16);
+            a1 += __shfl_xor_sync(0xffffffffu, up ? acc[1 % RU] : acc[3 % RU], 16);
+            float v = up2 ? a1 : a0;
+            v += __shfl_xor_sync(0xffffffffu, up2 ? a0 : a1, 8);
+            v += __shfl_xor_sync(0xffffffffu, v, 4);
+            v += __shfl_xor_sync(0xffffffffu, v, 2);
+            v += __shfl_xor_sync(0xffffffffu, v, 1);
+            const int r = at_row + (sub / 8) * rpb;
+            if (sub % 8 == 0 && r < nr) stf(yr + r, v + skip(r));
+        } else {
+#pragma unroll
+            for (int u = 0; u < RU; ++u) {
+                for (int o = lpr / 2; o; o >>= 1) acc[u] += __shfl_xor_sync(0xffffffffu, acc[u], o);
+                const int r = at_row + u * rpb;
+                if (sub == 0 && r < nr) stf(yr + r, acc[u] + skip(r));
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < RU; ++u)
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) h[u][i] = nx[u][i];
     }
 }
 
 template <typename T>
 cudaError_t launch_step(const SsmP &p, const T *xbc, const T *dtv, T *kept, T *y, cudaStream_t st) {
-    // enough blocks for two a multiprocessor, at least 8 rows each
-    int split = 1;
-    while ((int64_t)p.q.batch * p.H * split < 2 * num_sms() && p.P / (2 * split) >= 8) split *= 2;
-    const int rows = (p.P + split - 1) / split;
-    const dim3 grid((unsigned)((p.P + rows - 1) / rows), (unsigned)p.H, (unsigned)p.q.batch);
+    // up to 256 rows a block, fewer (8 at least) until there are two blocks a multiprocessor
+    const int grp_rows = p.H / p.G * p.P;
+    int rows = STEP_ROWS;
+    while (rows > 8 && (int64_t)p.q.batch * p.G * ((grp_rows + rows - 1) / rows) < 2 * num_sms()) rows /= 2;
+    const dim3 grid((unsigned)((grp_rows + rows - 1) / rows), (unsigned)p.G, (unsigned)p.q.batch);
     const bool vec = p.N % 4 == 0 && reinterpret_cast<uintptr_t>(p.s_in) % 16 == 0 && reinterpret_cast<uintptr_t>(p.s_out) % 16 == 0;
     const int nv = vec ? p.N / 4 : p.N;
     int lpr = 1;
     while (lpr < 32 && lpr < nv) lpr *= 2;
     const int vpl = (nv + lpr - 1) / lpr;
-#define SN_STEP(VEC, VPL) return launch_pdl(ssm_step_kernel<T, VEC, VPL>, grid, dim3(256), 0, st, p, xbc, dtv, kept, y, rows, lpr)
+#define SN_STEP(VEC, VPL)                                                                                              \
+    return p.W == 4 ? launch_pdl(ssm_step_kernel<T, VEC, VPL, 4>, grid, dim3(256), 0, st, p, xbc, dtv, kept, y, rows, lpr) \
+                    : launch_pdl(ssm_step_kernel<T, VEC, VPL, 0>, grid, dim3(256), 0, st, p, xbc, dtv, kept, y, rows, lpr)
     if (vec) {
         if (vpl == 1) SN_STEP(4, 1);
         SN_STEP(4, 2);
