@@ -230,6 +230,15 @@ __global__ void __launch_bounds__(WARPS * 32) q4_few_kernel(const __grid_constan
         const int chunks = (pe - ph) * 8;
         for (int m = 0; m < p.rows; ++m) {
             const X *xr = x + m * p.ldx + (int64_t)ph * 64;
+            if (PL == 1 && p.vec) {  // asynchronous copies, all in flight at once; zeros behind the row's end
+                for (int c = threadIdx.x * 8; c < chunks * 8; c += WARPS * 32 * 8) {
+                    const int left = max(0, min(8, p.q.k - ph * 64 - c));
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(tc::su32(xs + m * ldxs + c)),
+                                 "l"(left ? xr + c : x), "r"(left * 2)
+                                 : "memory");
+                }
+                continue;
+            }
             for (int c = threadIdx.x * 8; c < chunks * 8; c += WARPS * 32 * 8) {
                 const int left = p.q.k - ph * 64 - c;  // columns there are
                 struct alignas(16) {
@@ -261,6 +270,7 @@ __global__ void __launch_bounds__(WARPS * 32) q4_few_kernel(const __grid_constan
                 }
             }
         }
+        asm volatile("cp.async.wait_all;" ::: "memory");
         __syncthreads();
         int at = w0, off = (w0 - ph) * 64;
         for (; at + 4 * U <= w1; at += 2 * U, off += 2 * U * 64) {  // whole batches, whole batches ahead

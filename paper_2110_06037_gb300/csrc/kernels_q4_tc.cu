@@ -26,8 +26,9 @@
 //
 // Warps: 0 loads x and allocates TMEM, 1 issues the MMAs (of the pair's leader), 2
 // loads codes and scales, 4 to 7 drain the accumulators (two, so that a tile's
-// epilogue overlaps the next tile's products), 8 to 15 expand weights, four the even
-// column blocks and four the odd ones.  Waits are bounded; one that expires
+// epilogue overlaps the next tile's products), 8 to 19 expand weights, three groups
+// of four that fill stages in turn (a fill takes a group about 1100 cycles, mostly
+// latencies, the MMAs of a stage 450).  Waits are bounded; one that expires
 // records its cause in the library's error word and stops the pair.
 #include <algorithm>
 
@@ -40,8 +41,8 @@ namespace {
 
 using namespace tc;
 
-constexpr int Q4_STAGES = 5, Q4_THREADS = 512;
-constexpr int Q4_EXPAND = 4;                          // warps that expand a column block
+constexpr int Q4_STAGES = 5, Q4_THREADS = 640;
+constexpr int Q4_EXPAND = 4, Q4_TURNS = 3;            // warps that expand a column block; groups of them taking turns
 constexpr int Q4_CSTAGES = 6;                         // column blocks of codes and scales in flight
 constexpr uint32_t Q4_CBYTES = 8 * 512, Q4_CSTAGE = Q4_CBYTES + 8 * 64;  // eight tiles: codes; up to two groups' scales
 constexpr uint32_t Q4_A_BYTES = BM * BK * 2, Q4_B_BYTES = 128 * BK * 2, Q4_STAGE = Q4_A_BYTES + Q4_B_BYTES;
@@ -108,6 +109,16 @@ __device__ __forceinline__ uint32_t expand_rest(uint32_t c, const Scale2 &s, uin
     return fma2<__nv_bfloat16>(c, s.lo, fma2<__nv_bfloat16>(c, s.hi, neg));
 }
 
+// Expanded weights are for the MMAs that the pair's leader issues: what this warp has
+// written to shared memory, made visible to the async proxy, before the arrival at the
+// leader's barrier.  The release is restricted to shared memory: the usual one at
+// cluster scope took about 1000 cycles (223 us in all, against 167).
+__device__ __forceinline__ void arrive_expanded(uint32_t caddr) {
+    asm volatile("fence.release.sync_restrict::shared::cta.cluster;\n\t"
+                 "mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(caddr)
+                 : "memory");
+}
+
 // T: the operands' type; X: x's and y's
 template <typename T, typename X, int G>
 __global__ void __launch_bounds__(Q4_THREADS, 1)
@@ -151,7 +162,7 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
         }
         if (lane >= 16 && lane < 16 + Q4_CSTAGES) {
             mbar_init(&cfull_bar[lane - 16], 1);
-            mbar_init(&cempty_bar[lane - 16], Q4_EXPAND);
+            mbar_init(&cempty_bar[lane - 16], F32 ? Q4_TURNS * Q4_EXPAND : Q4_EXPAND);  // (fp32: every group reads a block)
         }
         fence_mbar_init();
     } else if (warp == 2 && lane < 3) {
@@ -331,16 +342,27 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
             cissued_sh = g;
         }
     } else if (warp >= 8) {  // ---------------- weights: this CTA's rows, two 16-row tiles a warp
-        const int grp = (warp - 8) / Q4_EXPAND, dw = (warp - 8) % Q4_EXPAND, g = lane / 4, t4 = lane % 4;
+        const int grp = (warp - 8) / Q4_EXPAND, dw = (warp - 8) % Q4_EXPAND;
+        // a lane takes the tile's row pair g and columns t4 of each half such that eight
+        // lanes' 16-byte pieces, four of row g and four of row g + 4, cover all banks
+        const int g = lane / 8 + 4 * (lane % 8 / 4), t4 = lane % 4;
         const int tiles = p.bn / G / 16, halves = p.q.glog == 5 ? 2 : 1;
-        // rows g of even g store their columns' first half first, the others the
-        // second, so that eight lanes' 16-byte pieces cover all banks
-        const bool odd = g & 1;
-        const uint32_t at0 = (uint32_t)g * 128 + ((uint32_t)((4 * (odd ? 1 : 0) + t4) ^ g) << 4);
-        const uint32_t at1 = (uint32_t)g * 128 + ((uint32_t)((4 * (odd ? 0 : 1) + t4) ^ g) << 4);
-        int s = 0, cs = 0, gk = 0;  // stage of the operands, stage of the codes, column blocks so far
+        const uint32_t at[2] = {(uint32_t)g * 128 + ((uint32_t)(t4 ^ g) << 4), (uint32_t)g * 128 + ((uint32_t)((4 + t4) ^ g) << 4)};
+        const uint32_t full0 = G == 2 ? mapa(su32(full_bar), 0u) : su32(full_bar);
+        // Stages are filled by the groups in turn.  A group's fill f waits until fill f - 5
+        // has been read; it last waited for fill f - 8, so the barrier it looks at is never
+        // two phases behind what it waits for, which parities could not tell apart.
+        static_assert(Q4_TURNS < Q4_STAGES, "a group waits in every round of the stages");
+        int s = 0, cs = 0, turn = 0;  // stage of the operands, stage of the codes, whose fill it is
         uint32_t par = 0, cpar = 0;
-        bool stop = false;
+        bool stop = false;  // (an aborting pair's barriers stand still, so the waits here end by themselves)
+        auto give_up = [&]() {
+            if (lane == 0) {
+                atomicOr(p.err, ERR_TMA_WAIT);
+                set_abort();
+            }
+            stop = true;
+        };
         for (int t = cid; t < total && !stop; t += ncl) {
             float rp[2][2];
             if constexpr (std::is_same<T, __half>::value) {
@@ -351,95 +373,83 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                     for (int r = 0; r < 2; ++r)
                         rp[i][r] = 0x1p12f / __ldg(p.q.row_pow + min(tile + i * Q4_EXPAND, p.q.nt - 1) * 16 + g + 8 * r);
             }
-            for (int kb = 0; kb < p.q.kb && !stop; ++kb, ++gk) {
-                if ((gk & 1) == grp) {
-                    if (!mbar_wait(&cfull_bar[cs], cpar, p.wait_limit)) {
-                        if (lane == 0) {
-                            atomicOr(p.err, ERR_TMA_WAIT);
-                            set_abort();
-                        }
-                    }
-                    if (__any_sync(0xffffffffu, abort_sh)) {
-                        stop = true;
+            for (int kb = 0; kb < p.q.kb && !stop; ++kb) {
+                uint4 cw[2];
+                Scale2 sc[2][2][2];  // [tile][row g, row g + 8][half]
+                if (F32 || turn == grp) {
+                    if (!__all_sync(0xffffffffu, mbar_wait(&cfull_bar[cs], cpar, p.wait_limit))) {
+                        give_up();
                         break;
                     }
-                    uint4 cw[2];
-                    uint32_t sw[2][2];
                     const uint8_t *cb = cst + cs * Q4_CSTAGE;
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
                         const int tile = dw + i * Q4_EXPAND;  // (behind the last: whatever lies there)
-                        cw[i] = *reinterpret_cast<const uint4 *>(cb + tile * 512 + lane * 16);
-                        sw[i][0] = *reinterpret_cast<const uint32_t *>(cb + Q4_CBYTES + (tile * halves) * 32 + g * 4);
-                        sw[i][1] = *reinterpret_cast<const uint32_t *>(cb + Q4_CBYTES + (tile * halves + halves - 1) * 32 + g * 4);
+                        cw[i] = *reinterpret_cast<const uint4 *>(cb + tile * 512 + (4 * g + t4) * 16);
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            if (h < halves) {
+                                const uint32_t sw =
+                                    *reinterpret_cast<const uint32_t *>(cb + Q4_CBYTES + (tile * halves + h) * 32 + g * 4);
+                                if (std::is_same<T, __nv_bfloat16>::value && p.q.scale_bf16) {
+                                    sc[i][0][h] = Scale2{__byte_perm(sw, sw, 0x1010), 0u};  // the scale is its own large part
+                                    sc[i][1][h] = Scale2{__byte_perm(sw, sw, 0x3232), 0u};
+                                } else {
+                                    float2 f = scale_pair(sw, p.q.scale_bf16);
+                                    if constexpr (std::is_same<T, __half>::value) f = make_float2(f.x * rp[i][0], f.y * rp[i][1]);
+                                    sc[i][0][h] = scale_parts<T>(f.x);
+                                    sc[i][1][h] = scale_parts<T>(f.y);
+                                }
+                            } else {
+                                sc[i][0][h] = sc[i][0][0];
+                                sc[i][1][h] = sc[i][1][0];
+                            }
+                        }
                     }
                     __syncwarp();
                     if (lane == 0) mbar_arrive(&cempty_bar[cs]);
-                    Scale2 sc[2][2][2];  // [tile][row g, row g + 8][half]
-#pragma unroll
-                    for (int i = 0; i < 2; ++i)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const float2 f = scale_pair(sw[i][h], p.q.scale_bf16);
-                            if constexpr (std::is_same<T, __half>::value) {
-                                sc[i][0][h] = scale_parts<T>(f.x * rp[i][0]);
-                                sc[i][1][h] = scale_parts<T>(f.y * rp[i][1]);
-                            } else {
-                                sc[i][0][h] = scale_parts<T>(f.x);
-                                sc[i][1][h] = scale_parts<T>(f.y);
-                            }
-                        }
+                }
 #pragma unroll 1
-                    for (int c = 0; c < COMBOS; ++c) {
-                        if (!mbar_wait(&empty_bar[s], par ^ 1u, p.wait_limit)) {
-                            if (lane == 0) {
-                                atomicOr(p.err, ERR_TMA_WAIT);
-                                set_abort();
-                            }
-                        }
-                        if (__any_sync(0xffffffffu, abort_sh)) {
-                            stop = true;
+                for (int c = 0; c < COMBOS; ++c) {
+                    if (turn == grp) {
+                        if (!__all_sync(0xffffffffu, mbar_wait(&empty_bar[s], par ^ 1u, p.wait_limit))) {
+                            give_up();
                             break;
                         }
                         uint8_t *b = smem + s * Q4_STAGE + Q4_A_BYTES;
+                        auto tile_rows = [&](auto parts) {
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const int tile = dw + i * Q4_EXPAND;
-                            if (tile >= tiles) break;
-                            const uint32_t w[4] = {cw[i].x, cw[i].y, cw[i].z, cw[i].w};
+                            for (int i = 0; i < 2; ++i) {
+                                const int tile = dw + i * Q4_EXPAND;
+                                if (tile >= tiles) break;
+                                const uint32_t w[4] = {cw[i].x, cw[i].y, cw[i].z, cw[i].w};
 #pragma unroll
-                            for (int r = 0; r < 2; ++r) {
-                                uint32_t v[2][4];
+                                for (int r = 0; r < 2; ++r)
 #pragma unroll
-                                for (int h = 0; h < 2; ++h)
+                                    for (int h = 0; h < 2; ++h) {
+                                        uint32_t v[4];
 #pragma unroll
-                                    for (int e = 0; e < 4; ++e) {
-                                        const uint32_t code = code_pair<T>(w[2 * h + e / 2], r + 2 * (e % 2));
-                                        v[h][e] = expand<T>(code, sc[i][r][h], p.parts);
-                                        if (F32 && c >= 3) v[h][e] = expand_rest(code, sc[i][r][h], v[h][e]);
+                                        for (int e = 0; e < 4; ++e) {
+                                            const uint32_t code = code_pair<T>(w[2 * h + e / 2], r + 2 * (e % 2));
+                                            v[e] = expand<T>(code, sc[i][r][h], parts.value);
+                                            if (F32 && c >= 3) v[e] = expand_rest(code, sc[i][r][h], v[e]);
+                                        }
+                                        *reinterpret_cast<uint4 *>(b + tile * 2048 + r * 1024 + at[h]) = make_uint4(v[0], v[1], v[2], v[3]);
                                     }
-                                const uint4 lo = make_uint4(v[0][0], v[0][1], v[0][2], v[0][3]);
-                                const uint4 hi = make_uint4(v[1][0], v[1][1], v[1][2], v[1][3]);
-                                uint8_t *o = b + tile * 2048 + r * 1024;
-                                *reinterpret_cast<uint4 *>(o + at0) = odd ? hi : lo;
-                                *reinterpret_cast<uint4 *>(o + at1) = odd ? lo : hi;
                             }
-                        }
+                        };
+                        if (F32 || p.parts) tile_rows(std::true_type{});
+                        else tile_rows(std::false_type{});
                         fence_proxy_async_smem();
                         __syncwarp();
                         if (lane == 0) {
-                            if (G == 2) mbar_arrive_cluster(mapa(su32(&full_bar[s]), 0u));
+                            if (G == 2 && rank) arrive_expanded(full0 + 8 * s);
                             else mbar_arrive(&full_bar[s]);
                         }
-                        if (++s == Q4_STAGES) {
-                            s = 0;
-                            par ^= 1u;
-                        }
                     }
-                } else {  // the other warps' block
-                    s += COMBOS;
-                    if (s >= Q4_STAGES) {
-                        s -= Q4_STAGES;
+                    if (++turn == Q4_TURNS) turn = 0;
+                    if (++s == Q4_STAGES) {
+                        s = 0;
                         par ^= 1u;
                     }
                 }
@@ -531,7 +541,6 @@ Shape4 choose(int64_t rows, int n, int64_t steps) {
 
 template <typename T, typename X, int G>
 cudaError_t launch_prompt(const CUtensorMap &mX, PromptP &p, X *y, cudaStream_t st) {
-    static_assert(!std::is_same<X, float>::value || Q4_STAGES == 5, "a column block of fp32 rows is one round of the stages");
     auto kern = q4_prompt_kernel<T, X, G>;
     static bool set = false;  // (idempotent)
     if (!set) {
