@@ -1,39 +1,11 @@
 // Causal convolution, selective scan and token step of a state-space block
 // (sn_causal_conv, sn_ssm_scan, sn_ssm_step in include/sn.h).
-#include "kern_common.cuh"
+#include "ssm_common.cuh"
 
 namespace sn {
 namespace k {
 
 namespace {
-
-struct Seq {  // one sequence of the batch
-    int64_t first, pos;  // its first token row, that token's position
-    int32_t len, slot;
-};
-__device__ __forceinline__ Seq sequence(const SeqArgs &q, int b) {
-    Seq s;
-    if (q.offsets) {  // (clipped to the rows there are, so that bad offsets read nothing else)
-        const int64_t n = q.tokens;
-        const int64_t i = q.offsets[b], j = q.offsets[b + 1];
-        s.first = i < 0 ? 0 : i > n ? n : i;
-        const int64_t e = j < s.first ? s.first : j > n ? n : j;
-        s.len = (int32_t)(e - s.first);
-    } else {
-        s.first = (int64_t)b * q.max_len;
-        s.len = (int32_t)q.max_len;
-    }
-    const int slot = q.slots ? q.slots[b] : b;
-    s.slot = slot >= 0 && slot < q.n_slots ? slot : -1;
-    s.pos = q.pos ? q.pos[b] : 0;
-    if (s.pos < 0) s.pos = 0;
-    return s;
-}
-
-// by the approximate exponential and division (2 ulp each; a denominator beyond 2^126 gives 0)
-__device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
-// log(1 + e^v) without overflow, and exact where e^v is small
-__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v))); }
 
 constexpr int MAX_W = 8;
 
@@ -180,15 +152,6 @@ cudaError_t conv_width(int W, const SeqArgs &q, const T *x, int64_t ldx, T *y, i
 }
 
 // --------------------------------------------------------------------- scan
-struct SsmP {
-    SeqArgs q;
-    int32_t H, P, G, N, W;
-    const float *a, *d, *dt_bias, *conv_w, *conv_b;
-    int64_t ldx, lddt, ldy;
-    const float *s_in;
-    float *s_out;
-};
-
 // The recurrence itself in fp32.  A block takes 32 rows of one head's state of one
 // sequence; 8 lanes share a row, each with NL of its values in registers, lane l
 // the float4s l, l + 8, ... of the row.  Inputs come in runs of RT tokens through
@@ -458,11 +421,16 @@ cudaError_t causal_conv(int dt, int channels, int width, int act, const float *w
                                              static_cast<T *>(kept), w, bias, channels, act, st))
 }
 
-size_t ssm_workspace(const sn_ssm_params &, int, const SeqArgs &) { return 0; }
+size_t ssm_workspace(const sn_ssm_params &c, int dt, const SeqArgs &q) {
+    return dt == SN_BF16 && c.state <= 128 ? ssm_tc_workspace(ssm_params(c, q, 0, 0, nullptr, nullptr, 0)) : 0;
+}
 
 cudaError_t ssm_scan(const sn_ssm_params &c, int dt, const SeqArgs &q, const void *xbc, int64_t ldx, const void *dtv,
-                     int64_t lddt, const float *s_in, float *s_out, void *y, int64_t ldy, void *, cudaStream_t st) {
+                     int64_t lddt, const float *s_in, float *s_out, void *y, int64_t ldy, void *work, cudaStream_t st) {
     const SsmP p = ssm_params(c, q, ldx, lddt, s_in, s_out, ldy);
+    if (dt == SN_BF16 && q.tokens && ssm_tc_applies(p, xbc, y))
+        return ssm_tc_scan(p, static_cast<const __nv_bfloat16 *>(xbc), static_cast<const __nv_bfloat16 *>(dtv),
+                           static_cast<__nv_bfloat16 *>(y), work, st);
     SN_DT_SWITCH(dt, T, return launch_scan<T>(p, static_cast<const T *>(xbc), static_cast<const T *>(dtv),
                                               static_cast<T *>(y), st))
 }

@@ -1,0 +1,53 @@
+// Pieces that the scan's kernels share.
+#pragma once
+
+#include "kern_common.cuh"
+
+namespace sn {
+namespace k {
+
+struct Seq {  // one sequence of the batch
+    int64_t first, pos;  // its first token row, that token's position
+    int32_t len, slot;
+};
+__device__ __forceinline__ Seq sequence(const SeqArgs &q, int b) {
+    Seq s;
+    if (q.offsets) {  // (clipped to the rows there are, so that bad offsets read nothing else)
+        const int64_t n = q.tokens;
+        const int64_t i = q.offsets[b], j = q.offsets[b + 1];
+        s.first = i < 0 ? 0 : i > n ? n : i;
+        const int64_t e = j < s.first ? s.first : j > n ? n : j;
+        s.len = (int32_t)(e - s.first);
+    } else {
+        s.first = (int64_t)b * q.max_len;
+        s.len = (int32_t)q.max_len;
+    }
+    const int slot = q.slots ? q.slots[b] : b;
+    s.slot = slot >= 0 && slot < q.n_slots ? slot : -1;
+    s.pos = q.pos ? q.pos[b] : 0;
+    if (s.pos < 0) s.pos = 0;
+    return s;
+}
+
+// by the approximate exponential and division (2 ulp each; a denominator beyond 2^126 gives 0)
+__device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
+// log(1 + e^v) without overflow, and exact where e^v is small
+__device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v))); }
+
+struct SsmP {
+    SeqArgs q;
+    int32_t H, P, G, N, W;
+    const float *a, *d, *dt_bias, *conv_w, *conv_b;
+    int64_t ldx, lddt, ldy;
+    const float *s_in;
+    float *s_out;
+};
+
+// the scan of bf16 tokens by matrix products (kernels_ssm_tc.cu)
+bool ssm_tc_applies(const SsmP &p, const void *xbc, const void *y);
+size_t ssm_tc_workspace(const SsmP &p);
+cudaError_t ssm_tc_scan(const SsmP &p, const __nv_bfloat16 *xbc, const __nv_bfloat16 *dtv, __nv_bfloat16 *y, void *work,
+                        cudaStream_t st);
+
+}  // namespace k
+}  // namespace sn

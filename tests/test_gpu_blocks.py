@@ -405,6 +405,51 @@ def test_scan(dt, lens, sizes):
     assert torch.equal(again, y) and torch.equal(state[used], out[used])  # in place, and the same to the bit
 
 
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("lens, sizes", [([1500, 3, 1100], (3, 64, 1, 128)), ([2300], (2, 40, 2, 24)), ([1025], (1, 80, 1, 72))])
+def test_scan_of_long_prompts_with_few_heads(dt, lens, sizes):
+    """Sequences that are cut into segments, short ones beside them; states from and to the same buffer."""
+    import torch
+    import paper_2110_06037_gb300 as sn
+    h, p, g, n = sizes
+    rng = np.random.default_rng(sum(lens))
+    a, d, b = ssm_weights(rng, h)
+    rows, c = sum(lens), h * p + 2 * g * n
+    xbc, step = dev(rng.normal(size=(rows, c)), dt), dev(rng.normal(size=(rows, h)) - 2, dt)
+    state = dev(rng.normal(size=(len(lens), h, p, n)))
+    slots = list(range(len(lens)))[::-1]
+    off = ints(np.concatenate(([0], np.cumsum(lens))).tolist())
+    ref, my, sref, ms = run_scan(host(xbc), host(step), lens, sizes, a, d, b, host(state), slots)
+    ssm = sn.StateSpace(h, p, g, n, dev(a), dev(d), dev(b))
+    out = torch.empty_like(state)
+    y = ssm.scan(xbc, step, offsets=off, max_len=max(lens), state_in=state, state_out=out, slots=ints(slots))
+    close(y, ref, scan_bound(my, max(lens)) + (2.0 ** -14 * my if dt != "f32" else 0), dt)
+    close(out, sref, scan_bound(ms, max(lens)), "f32")
+    again = ssm.scan(xbc, step, offsets=off, max_len=max(lens), state_in=state, state_out=state, slots=ints(slots))
+    assert torch.equal(again, y) and torch.equal(state, out)
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+def test_scan_of_infinite_and_nan_channels(dt):
+    """One channel's x is not finite at one token: every other channel, and that one before it, as without."""
+    import torch
+    import paper_2110_06037_gb300 as sn
+    torch.manual_seed(4)
+    h, p, g, n = 3, 64, 1, 128
+    xbc = torch.randn(1, 400, h * p + 2 * g * n, device="cuda").to(tdt(dt))
+    step = torch.randn(1, 400, h, device="cuda").to(tdt(dt))
+    ssm = sn.StateSpace(h, p, g, n, -torch.rand(h, device="cuda"))
+    ref = ssm.scan(xbc, step)
+    for value in (float("nan"), float("inf"), -float("inf")):
+        x = xbc.clone()
+        x[0, 200, 70], x[0, 37, 191] = value, value
+        y = ssm.scan(x, step)
+        keep = torch.ones_like(y, dtype=torch.bool)
+        keep[0, 200:, 70], keep[0, 37:, 191] = False, False
+        assert torch.equal(y[keep], ref[keep])
+        assert not bool(y[0, 200:, 70].isfinite().any()) and not bool(y[0, 37:, 191].isfinite().any())
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 def test_scan_equal_lengths_from_zero_without_skip_or_bias(dt):
     import paper_2110_06037_gb300 as sn
