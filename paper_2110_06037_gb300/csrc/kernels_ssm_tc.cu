@@ -67,20 +67,33 @@ __device__ __forceinline__ int2 segment(int len, int segs, int g) {
 }
 
 // ------------------------------------------------------------ time steps
-__global__ void __launch_bounds__(256) ssm_steps_kernel(const __grid_constant__ TcP p, const __nv_bfloat16 *__restrict__ dtv) {
-    __shared__ float sh[32][Q + 1];
+// a block takes eight heads of a chunk, a warp one of them
+__global__ void __launch_bounds__(256) ssm_steps_kernel(const __grid_constant__ TcP p, const __nv_bfloat16 *__restrict__ dtv, int vec) {
+    __shared__ float sh[8][Q + 1];
     griddep_launch();
     griddep_wait();
-    const int b = blockIdx.z, c = blockIdx.x, h0 = blockIdx.y * 32, nh = min(32, p.s.H - h0);
+    const int b = blockIdx.z, c = blockIdx.x, h0 = blockIdx.y * 8, nh = min(8, p.s.H - h0);
     const Seq s = sequence(p.s.q, b);
     if ((int64_t)c * Q >= s.len) return;
     const int n = min(Q, s.len - c * Q), warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    for (int e = threadIdx.x; e < Q * 32; e += 256) {
-        const int t = e / 32, h = e % 32;
-        sh[h][t] = t < n && h < nh ? ldf(dtv + (s.first + c * Q + t) * p.s.lddt + h0 + h) : -INFINITY;
+    if (vec) {
+        const int t = threadIdx.x;
+        if (t < n) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(dtv + (s.first + c * Q + t) * p.s.lddt + h0);
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = unpack2<__nv_bfloat16>(w[i]);
+                sh[2 * i][t] = f.x, sh[2 * i + 1][t] = f.y;
+            }
+        }
+    } else {
+        for (int e = threadIdx.x; e < Q * 8; e += 256)
+            if (e / 8 < n && e % 8 < nh) sh[e % 8][e / 8] = ldf(dtv + (s.first + c * Q + e / 8) * p.s.lddt + h0 + e % 8);
     }
     __syncthreads();
-    for (int hh = warp; hh < nh; hh += 8) {
+    const int hh = warp;
+    if (hh < nh) {
         const int head = h0 + hh;
         const float a = p.s.a[head] * LOG2E, bias = p.s.dt_bias ? p.s.dt_bias[head] : 0.0f;
         // a lane's four tokens; sums up to them and from behind them
@@ -169,8 +182,7 @@ __device__ __forceinline__ float ex2(float v) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-__device__ __forceinline__ bool finite(float v) { return fabsf(v) <= 3.4028234664e38f; }
-// two values as the large and small bf16 parts of each (the small part of what is not finite is 0)
+// two values as the large and small bf16 parts of each
 struct Parts2 {
     uint32_t hi, lo;
 };
@@ -181,18 +193,10 @@ __device__ __forceinline__ Parts2 parts2(float a, float b) {
     r.lo = pack2<__nv_bfloat16>(a - h.x, b - h.y);
     return r;
 }
-__device__ __forceinline__ Parts2 parts2_any(float a, float b) {
-    Parts2 r;
-    r.hi = pack2<__nv_bfloat16>(a, b);
-    const float2 h = unpack2<__nv_bfloat16>(r.hi);
-    r.lo = pack2<__nv_bfloat16>(finite(h.x) ? a - h.x : 0.0f, finite(h.y) ? b - h.y : 0.0f);
-    return r;
-}
-
 // ------------------------------------------------------------------- scan
 constexpr uint32_t TILE64 = Q * 128;  // 128 rows of 64 bf16 values
 constexpr uint32_t OFF_B = 0, OFF_C = 2 * TILE64, OFF_X = 4 * TILE64, OFF_H = 5 * TILE64, OFF_BARS = 7 * TILE64;
-constexpr size_t SCAN_SMEM = OFF_BARS + 512;
+constexpr size_t SCAN_SMEM = OFF_BARS + 1024;  // twice this and 1 KB each is all that an SM has
 // barriers (F_*: copies landed, M_*: MMAs done), one phase a chunk (F_B, F_B1: every other one without outputs)
 enum Bar { F_B, F_B1, F_C, F_X, M_PAIRS, M_CARRIED, M_MADE, M_INSIDE, BARS };
 struct Shared {
@@ -200,8 +204,9 @@ struct Shared {
     uint32_t tmem;
     int abort, any_bad;
     int bad[PB];  // first token of the chunk whose x is not finite, by channel
+    alignas(16) float as[Q];  // the chunk's A_s - log2 d_s
 };
-static_assert(sizeof(Shared) <= 512, "behind the tiles");
+static_assert(sizeof(Shared) <= 1024, "behind the tiles");
 
 // FULL: the outputs; otherwise a segment's state from nothing (segment 0: from s_in).
 // A wait that gives up leaves the warp's later ones and all further issues out; the
@@ -356,7 +361,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
             uint32_t hi[4], lo[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const Parts2 v = parts2_any(h[8 * i + 2 * e], h[8 * i + 2 * e + 1]);
+                const Parts2 v = parts2(h[8 * i + 2 * e], h[8 * i + 2 * e + 1]);  // (an infinite state's small part is NaN, as its sums over B's signs are)
                 hi[e] = v.hi, lo[e] = v.lo;
             }
             const uint32_t at = (uint32_t)((4 * half + i) ^ (row & 7)) << 4;
@@ -366,18 +371,35 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
         fence_proxy_async_smem();
     };
     if (FULL) put_state();
+    // what this thread needs of a chunk's table, loaded a chunk ahead
+    struct {
+        float at, as, w, total;  // A of its row, A_s - log2 d_s (threads 0 to 127: of token s), the weight of its token, A_127
+    } now, next{};
+    const int64_t tab0 = chunk_at(s, b, chunks.x) * q.H + head;
+    auto fetch = [&](int c) {
+        if (c >= nc) return;
+        const float *table = p.table + (tab0 + (int64_t)c * q.H) * TABLE;
+        if (FULL) {
+            next.at = __ldg(table + row);
+            next.as = __ldg(table + Q + (threadIdx.x & (Q - 1)));
+        }
+        next.w = __ldg(table + 2 * Q + threadIdx.x / 2);
+        next.total = __ldg(p.total + tab0 + (int64_t)c * q.H);
+    };
+    fetch(0);
+    const float skip = FULL && q.d ? q.d[head] : 0.0f;
     for (int c = 0; c < nc; ++c) {
         const uint32_t par = c & 1;
         const int valid = min(Q, s.len - (chunks.x + c) * Q);  // tokens there are
-        const int64_t tab = chunk_at(s, b, chunks.x + c) * q.H + head;
-        const float *table = p.table + tab * TABLE;
+        now = next;
+        fetch(c + 1);
         if constexpr (FULL) {
+            if (threadIdx.x < Q) sh.as[threadIdx.x] = now.as;  // (last read before the barrier ahead of the products inside)
             // ---- the state's parts are written, the chunk before has been read everywhere
             tc_fence_before();
             __syncthreads();
             if (warp == 1) issue_carried(c);
             if (warp == 0) issue_pairs(c);
-            if (warp == 4 && c > 0) load_x(c);
             __syncwarp();
             must(M_CARRIED, par);  // X' takes the place of the state's parts
         }
@@ -389,7 +411,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
         }
         {
             const int t = threadIdx.x / 2, j0 = 4 * (threadIdx.x & 1);
-            const float w = __ldg(table + 2 * Q + t);
+            const float w = now.w;
             uint8_t *xr = smem + OFF_X + t * 128, *hr = smem + OFF_H + t * 128;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -402,26 +424,27 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
                     *reinterpret_cast<uint4 *>(br) = xv;
                     *reinterpret_cast<uint4 *>(br + TILE64) = xv;
                 }
-                uint32_t u[4] = {xv.x, xv.y, xv.z, xv.w}, hi[4], lo[4];
-                bool all = true;
+                uint32_t u[4] = {xv.x, xv.y, xv.z, xv.w}, hi[4], lo[4], odd = 0u;  // odd: a value's exponent is all ones
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float2 f = unpack2<__nv_bfloat16>(u[e]);
-                    all = all && finite(f.x) && finite(f.y);
-                    const Parts2 v = parts2_any(f.x * w, f.y * w);
+                    odd |= ((u[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                    const Parts2 v = parts2(f.x * w, f.y * w);
                     hi[e] = v.hi, lo[e] = v.lo;
                 }
-                if (FULL && !all) {  // out of the product inside the chunk; its channel is NaN from here on
+                if (odd) {
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const uint32_t shift = 16 * (e % 2);
-                        if ((u[e / 2] >> shift & 0x7f80u) == 0x7f80u) {
+                        if ((u[e / 2] >> shift & 0x7f80u) != 0x7f80u) continue;
+                        lo[e / 2] &= ~(0xffffu << shift);  // into the state as it is
+                        if (FULL) {  // out of the product inside the chunk; its channel is NaN from here on
                             u[e / 2] &= ~(0xffffu << shift);
                             atomicMin(&sh.bad[8 * (j0 + i) + e], t);
                             sh.any_bad = 1;
                         }
                     }
-                    *reinterpret_cast<uint4 *>(xr + at) = make_uint4(u[0], u[1], u[2], u[3]);
+                    if (FULL) *reinterpret_cast<uint4 *>(xr + at) = make_uint4(u[0], u[1], u[2], u[3]);
                 }
                 *reinterpret_cast<uint4 *>(hr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                 *reinterpret_cast<uint4 *>(hr + TILE64 + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -432,10 +455,10 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
         if (warp == 2) issue_made(c);
         if (!FULL && warp == 4) load_x(c + 1);
         __syncwarp();
-        float At = 0.0f;
         if constexpr (FULL) {
-            // ---- P from the pairs: 32 x 32 blocks, this warp's two of its rows' four
-            At = __ldg(table + row);
+            // ---- P from the pairs: 32 x 32 blocks, this warp's two of its rows' four; D, the
+            // factor of x itself, joins the diagonal
+            const float At = now.at;
             must(M_PAIRS, par);
             tc_fence_after();
             if (warp == 4) load_c(c + 1);  // (both of its products are done)
@@ -448,20 +471,23 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
                 if (blk <= quarter) {
                     uint32_t v[32];
                     tmem_ld32(tmem + lanes + T_S + 32 * blk, v);
-                    const float4 *col = reinterpret_cast<const float4 *>(table + Q + 32 * blk);
+                    auto weigh = [&](auto diagonal) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const float4 As = __ldg(col + j);
-                        const float as[4] = {As.x, As.y, As.z, As.w};
-                        float f[4];
+                        for (int j = 0; j < 8; ++j) {
+                            const float4 As = *reinterpret_cast<const float4 *>(&sh.as[32 * blk + 4 * j]);
+                            const float as[4] = {As.x, As.y, As.z, As.w};
+                            float f[4];
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            f[e] = __uint_as_float(v[4 * j + e]) * ex2(At - as[e]);
-                            if (blk == quarter && 4 * j + e > lane) f[e] = 0.0f;
+                            for (int e = 0; e < 4; ++e) {
+                                f[e] = __uint_as_float(v[4 * j + e]) * ex2(At - as[e]);
+                                if (diagonal.value) f[e] = 4 * j + e < lane ? f[e] : 4 * j + e == lane ? f[e] + skip : 0.0f;
+                            }
+                            const Parts2 a = parts2(f[0], f[1]), bb = parts2(f[2], f[3]);
+                            hi[2 * j] = a.hi, hi[2 * j + 1] = bb.hi, lo[2 * j] = a.lo, lo[2 * j + 1] = bb.lo;
                         }
-                        const Parts2 a = parts2(f[0], f[1]), bb = parts2(f[2], f[3]);
-                        hi[2 * j] = a.hi, hi[2 * j + 1] = bb.hi, lo[2 * j] = a.lo, lo[2 * j + 1] = bb.lo;
-                    }
+                    };
+                    if (blk == quarter) weigh(std::true_type{});
+                    else weigh(std::false_type{});
                 } else {
 #pragma unroll
                     for (int j = 0; j < 16; ++j) hi[j] = lo[j] = 0u;
@@ -476,7 +502,7 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
         must(M_MADE, par);
         tc_fence_after();
         {
-            const float e = exp2f(__ldg(p.total + tab));
+            const float e = exp2f(now.total);
             uint32_t v[32];
             __syncwarp();
             tmem_ld32(tmem + lanes + T_D + 32 * half, v);
@@ -491,8 +517,10 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
             __syncwarp();
             put_state();
             // ---- the chunk's outputs
-            const float et = ex2(At), skip = q.d ? __ldg(q.d + head) : 0.0f;
+            const float et = ex2(now.at);
             must(M_INSIDE, par);
+            if (warp == 4) load_x(c + 1);
+            __syncwarp();
             tc_fence_after();
             const bool bad = *reinterpret_cast<volatile int *>(&sh.any_bad);
             __nv_bfloat16 *yr = y + (s.first + (int64_t)(chunks.x + c) * Q + row) * q.ldy + (int64_t)head * q.P + p0 + 32 * half;
@@ -504,16 +532,11 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int i = 2 * i2 + j;
-                    const uint4 xv = *reinterpret_cast<const uint4 *>(smem + OFF_X + row * 128 + (((4 * half + i) ^ (row & 7)) << 4));
-                    const uint32_t u[4] = {xv.x, xv.y, xv.z, xv.w};
                     uint32_t o[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        const float2 x = unpack2<__nv_bfloat16>(u[e]);
                         float f0 = fmaf(__uint_as_float(y0[8 * j + 2 * e]), et, __uint_as_float(y1[8 * j + 2 * e]));
                         float f1 = fmaf(__uint_as_float(y0[8 * j + 2 * e + 1]), et, __uint_as_float(y1[8 * j + 2 * e + 1]));
-                        f0 = fmaf(skip, x.x, f0);
-                        f1 = fmaf(skip, x.y, f1);
                         if (bad) {
                             if (row >= sh.bad[32 * half + 8 * i + 2 * e]) f0 = NAN;
                             if (row >= sh.bad[32 * half + 8 * i + 2 * e + 1]) f1 = NAN;
@@ -616,7 +639,8 @@ cudaError_t ssm_tc_scan(const SsmP &s, const __nv_bfloat16 *xbc, const __nv_bflo
         set = true;
     }
     const unsigned chunks = (unsigned)((s.q.max_len + Q - 1) / Q), heads = (unsigned)(s.H * p.pblocks);
-    cudaError_t e = launch_pdl(ssm_steps_kernel, dim3(chunks, (unsigned)((s.H + 31) / 32), (unsigned)s.q.batch), dim3(256), 0, st, p, dtv);
+    const int vec = s.H % 8 == 0 && s.lddt % 8 == 0 && reinterpret_cast<uintptr_t>(dtv) % 16 == 0;
+    cudaError_t e = launch_pdl(ssm_steps_kernel, dim3(chunks, (unsigned)((s.H + 7) / 8), (unsigned)s.q.batch), dim3(256), 0, st, p, dtv, vec);
     if (e != cudaSuccess) return e;
     if (p.segs > 1) {
         e = launch_pdl(ssm_scan_tc_kernel<false>, dim3(heads, (unsigned)(p.segs - 1), (unsigned)s.q.batch), dim3(SCAN_THREADS), SCAN_SMEM, st,
