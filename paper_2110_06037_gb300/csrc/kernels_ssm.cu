@@ -1,5 +1,7 @@
 // Causal convolution, selective scan and token step of a state-space block
 // (sn_causal_conv, sn_ssm_scan, sn_ssm_step in include/sn.h).
+#include <algorithm>
+
 #include "ssm_common.cuh"
 
 namespace sn {
@@ -152,92 +154,200 @@ cudaError_t conv_width(int W, const SeqArgs &q, const T *x, int64_t ldx, T *y, i
 }
 
 // --------------------------------------------------------------------- scan
-// The recurrence itself in fp32.  A block takes 32 rows of one head's state of one
-// sequence; 8 lanes share a row, each with NL of its values in registers, lane l
-// the float4s l, l + 8, ... of the row.  Inputs come in runs of RT tokens through
-// shared memory.
-constexpr int RT = 16;
-template <typename T, int NL>
-__global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant__ SsmP p, const T *__restrict__ xbc,
+// The recurrence itself in fp32.  A block takes 32 rows of one head's state and a
+// segment of one sequence; 8 lanes share a row, each with NL of its values in
+// registers, lane l the float4s l, l + 8, ... of the row.  Inputs come in runs of RT
+// tokens through shared memory, the next run's loads in flight meanwhile; four
+// tokens' sums are exchanged together.  What bounds it is the chain of a row's
+// tokens, so few rows are spread over segments of the sequence: a first pass makes
+// every segment's state from nothing, the second starts from the joined ones.
+// (Six sequences, 1030 tokens the longest, 6 heads of 48 x 40: in one piece 256 us.)
+constexpr int RT = 16, SEG_MIN = 64;  // tokens of a run, and of a segment at least
+
+struct RecP {
+    SsmP s;
+    int32_t segs;
+    float *part, *total;  // [batch][H][segs][P][N] states: before segment 0, then after segment j; [batch][H][segs]: sums of d a
+};
+__device__ __forceinline__ int2 rec_segment(int len, int segs, int g) {  // tokens [first, last), whole runs
+    const int runs = (len + RT - 1) / RT;
+    return make_int2(min(len, (int)((int64_t)runs * g / segs) * RT), min(len, (int)((int64_t)runs * (g + 1) / segs) * RT));
+}
+
+// FULL: the outputs; otherwise a segment's state from nothing (segment 0: from s_in)
+template <typename T, int NL, bool FULL>
+__global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant__ RecP p, const T *__restrict__ xbc,
                                                            const T *__restrict__ dtv, T *__restrict__ y) {
-    constexpr int NPAD = NL * 8;
-    __shared__ __align__(16) float sb[RT][NPAD], sc[RT][NPAD];
-    __shared__ float sx[RT][32], sy[RT][32], sd[RT], sda[RT];
+    constexpr int NPAD = NL * 8, E = RT * NPAD / 256, EX = RT * 32 / 256;  // values of B (and C), and of x, a thread loads
+    __shared__ __align__(16) float sb[RT][NPAD], sc[FULL ? RT : 1][NPAD];
+    __shared__ float sx[RT][32], sy[FULL ? RT : 1][32], sd[RT], sda[RT];
     griddep_launch();
     griddep_wait();
-    const int head = blockIdx.y, p0 = blockIdx.x * 32, tid = threadIdx.x;
-    const int row = p0 + tid / 8, l = tid % 8;
-    const Seq s = sequence(p.q, blockIdx.z);
-    const int grp = head / (p.H / p.G);
-    const float a = p.a[head], dskip = p.d ? p.d[head] : 0.0f, dtb = p.dt_bias ? p.dt_bias[head] : 0.0f;
+    const SsmP &q = p.s;
+    const int pblocks = (q.P + 31) / 32, head = blockIdx.x / pblocks, p0 = blockIdx.x % pblocks * 32, seg = blockIdx.y;
+    const int tid = threadIdx.x, row = p0 + tid / 8, l = tid % 8, b = blockIdx.z;
+    const Seq s = sequence(q.q, b);
+    const int2 tok = rec_segment(s.len, p.segs, seg);
+    const int grp = head / (q.H / q.G), np = min(32, q.P - p0);
+    const float a = q.a[head], dskip = q.d ? q.d[head] : 0.0f, dtb = q.dt_bias ? q.dt_bias[head] : 0.0f;
+    const int64_t part0 = ((int64_t)b * q.H + head) * p.segs, srow = s.slot >= 0 ? (((int64_t)s.slot * q.H + head) * q.P + row) * q.N : -1;
+    auto state_at = [&](int j) { return p.part + ((part0 + j) * q.P + row) * q.N; };
     float st[NL];
-    const int64_t srow = s.slot >= 0 ? (((int64_t)s.slot * p.H + head) * p.P + row) * p.N : -1;
+    auto value = [&](int i) { return ((i / 4) * 8 + l) * 4 + i % 4; };
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
-        const int n = ((i / 4) * 8 + l) * 4 + i % 4;
-        st[i] = p.s_in && srow >= 0 && row < p.P && n < p.N ? p.s_in[srow + n] : 0.0f;
+        const int n = value(i);
+        st[i] = 0.0f;
+        if (row >= q.P || n >= q.N) continue;
+        if (FULL && p.segs > 1) st[i] = state_at(seg > 0 ? 1 : 0)[n];
+        else if (seg == 0 && q.s_in && srow >= 0) st[i] = q.s_in[srow + n];
     }
-    const int np = min(32, p.P - p0);
-    for (int t0 = 0; t0 < s.len; t0 += RT) {
-        const int nt = min(RT, s.len - t0);
-        __syncthreads();
-        const T *r0 = xbc + (s.first + t0) * p.ldx;
-        for (int e = tid; e < RT * NPAD; e += 256) {
-            const int t = e / NPAD, n = e % NPAD;
-            const bool in = t < nt && n < p.N;
-            const T *r = r0 + (int64_t)t * p.ldx + p.H * p.P + grp * p.N + n;
-            sb[t][n] = in ? ldf(r) : 0.0f;
-            sc[t][n] = in ? ldf(r + p.G * p.N) : 0.0f;
-        }
-        for (int e = tid; e < RT * 32; e += 256) {
-            const int t = e / 32, i = e % 32;
-            sx[t][i] = t < nt && i < np ? ldf(r0 + (int64_t)t * p.ldx + head * p.P + p0 + i) : 0.0f;
-        }
-        if (tid < nt) {
-            const float d = softplus(ldf(dtv + (s.first + t0 + tid) * p.lddt + head) + dtb);
-            sd[tid] = d;
-            sda[tid] = expf(d * a);
-        }
-        __syncthreads();
-        for (int t = 0; t < nt; ++t) {
-            const float da = sda[t], x = sx[t][tid / 8], dx = sd[t] * x;
-            float acc = 0.0f;
+    if (FULL) {
+#pragma unroll 4
+        for (int j = 1; j < seg; ++j) {
+            const float e = expf(p.total[part0 + j]);
 #pragma unroll
-            for (int i = 0; i < NL / 4; ++i) {
-                const float4 b = *reinterpret_cast<const float4 *>(&sb[t][(i * 8 + l) * 4]);
-                const float4 c = *reinterpret_cast<const float4 *>(&sc[t][(i * 8 + l) * 4]);
-                st[4 * i] = fmaf(st[4 * i], da, dx * b.x), acc = fmaf(st[4 * i], c.x, acc);
-                st[4 * i + 1] = fmaf(st[4 * i + 1], da, dx * b.y), acc = fmaf(st[4 * i + 1], c.y, acc);
-                st[4 * i + 2] = fmaf(st[4 * i + 2], da, dx * b.z), acc = fmaf(st[4 * i + 2], c.z, acc);
-                st[4 * i + 3] = fmaf(st[4 * i + 3], da, dx * b.w), acc = fmaf(st[4 * i + 3], c.w, acc);
+            for (int i = 0; i < NL; ++i)
+                if (row < q.P && value(i) < q.N) st[i] = fmaf(st[i], e, state_at(j + 1)[value(i)]);
+        }
+    } else if (seg == 0) {  // the second pass may store over s_in: it reads this copy
+#pragma unroll
+        for (int i = 0; i < NL; ++i)
+            if (row < q.P && value(i) < q.N) state_at(0)[value(i)] = st[i];
+    }
+    // a run's inputs, in registers until the run before has been worked on
+    T nb[E], ncv[FULL ? E : 1], nx[EX];
+    float nd = 0.0f, sum = 0.0f;  // (threads 0 to RT - 1: a token's step; sum of steps)
+    auto fetch = [&](int t0) {
+        const int nt = min(RT, tok.y - t0);
+        if (nt <= 0) return;
+        const T *r0 = xbc + (s.first + t0) * q.ldx;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const int e = tid + i * 256, t = e / NPAD, n = e % NPAD;
+            if (t < nt && n < q.N) {
+                const T *r = r0 + (int64_t)t * q.ldx + q.H * q.P + grp * q.N + n;
+                nb[i] = *r;
+                if (FULL) ncv[i] = r[q.G * q.N];
             }
-            acc += __shfl_xor_sync(0xffffffffu, acc, 4);
-            acc += __shfl_xor_sync(0xffffffffu, acc, 2);
-            acc += __shfl_xor_sync(0xffffffffu, acc, 1);
-            if (l == 0) sy[t][tid / 8] = fmaf(dskip, x, acc);
+        }
+#pragma unroll
+        for (int i = 0; i < EX; ++i) {
+            const int e = tid + i * 256, t = e / 32, c = e % 32;
+            if (t < nt && c < np) nx[i] = r0[(int64_t)t * q.ldx + head * q.P + p0 + c];
+        }
+        if (tid < nt) nd = softplus(ldf(dtv + (s.first + t0 + tid) * q.lddt + head) + dtb);
+    };
+    fetch(tok.x);
+    for (int t0 = tok.x; t0 < tok.y; t0 += RT) {
+        const int nt = min(RT, tok.y - t0);
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const int e = tid + i * 256, t = e / NPAD, n = e % NPAD;
+            const bool in = t < nt && n < q.N;
+            sb[t][n] = in ? ldf(nb + i) : 0.0f;
+            if (FULL) sc[t][n] = in ? ldf(ncv + i) : 0.0f;
+        }
+#pragma unroll
+        for (int i = 0; i < EX; ++i) {
+            const int e = tid + i * 256, t = e / 32, c = e % 32;
+            sx[t][c] = t < nt && c < np ? ldf(nx + i) : 0.0f;
+        }
+        if (tid < RT) {  // (behind the segment's end: a step of 0)
+            sd[tid] = tid < nt ? nd : 0.0f;
+            sda[tid] = tid < nt ? expf(nd * a) : 1.0f;
+            sum += tid < nt ? nd * a : 0.0f;
         }
         __syncthreads();
-        for (int e = tid; e < nt * 32; e += 256) {
-            const int t = e / 32, i = e % 32;
-            if (i < np) stf(y + (s.first + t0 + t) * p.ldy + head * p.P + p0 + i, sy[t][i]);
+        fetch(t0 + RT);
+        for (int t = 0; t < nt; t += 4) {  // (RT is a multiple of 4: what lies behind the end changes nothing)
+            float acc[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float da = sda[t + u], dx = sd[t + u] * sx[t + u][tid / 8];
+                float4 c4 = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                for (int i = 0; i < NL / 4; ++i) {
+                    const float4 bv = *reinterpret_cast<const float4 *>(&sb[t + u][(i * 8 + l) * 4]);
+                    st[4 * i] = fmaf(st[4 * i], da, dx * bv.x);
+                    st[4 * i + 1] = fmaf(st[4 * i + 1], da, dx * bv.y);
+                    st[4 * i + 2] = fmaf(st[4 * i + 2], da, dx * bv.z);
+                    st[4 * i + 3] = fmaf(st[4 * i + 3], da, dx * bv.w);
+                    if (FULL) {
+                        const float4 cv = *reinterpret_cast<const float4 *>(&sc[t + u][(i * 8 + l) * 4]);
+                        c4.x = fmaf(st[4 * i], cv.x, c4.x), c4.y = fmaf(st[4 * i + 1], cv.y, c4.y);
+                        c4.z = fmaf(st[4 * i + 2], cv.z, c4.z), c4.w = fmaf(st[4 * i + 3], cv.w, c4.w);
+                    }
+                }
+                acc[u] = (c4.x + c4.y) + (c4.z + c4.w);
+            }
+            if (FULL) {
+                // four tokens' sums over eight lanes in four exchanges: lanes 0 and 1 of each pair end with one token's
+                const bool up = l & 4, up2 = l & 2;
+                float a0 = up ? acc[2] : acc[0], a1 = up ? acc[3] : acc[1];
+                a0 += __shfl_xor_sync(0xffffffffu, up ? acc[0] : acc[2], 4);
+                a1 += __shfl_xor_sync(0xffffffffu, up ? acc[1] : acc[3], 4);
+                float v = up2 ? a1 : a0;
+                v += __shfl_xor_sync(0xffffffffu, up2 ? a0 : a1, 2);
+                v += __shfl_xor_sync(0xffffffffu, v, 1);
+                const int tt = t + l / 2;
+                if (l % 2 == 0) sy[tt][tid / 8] = fmaf(dskip, sx[tt][tid / 8], v);
+            }
+        }
+        if (FULL) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < EX; ++i) {
+                const int e = tid + i * 256, t = e / 32, c = e % 32;
+                if (t < nt && c < np) stf(y + (s.first + t0 + t) * q.ldy + head * q.P + p0 + c, sy[t][c]);
+            }
         }
     }
-    if (p.s_out && srow >= 0 && row < p.P) {
+    float *out = FULL ? (seg == p.segs - 1 && q.s_out && srow >= 0 ? q.s_out + srow : nullptr) : state_at(seg + 1);
+    if (out && row < q.P) {
 #pragma unroll
-        for (int i = 0; i < NL; ++i) {
-            const int n = ((i / 4) * 8 + l) * 4 + i % 4;
-            if (n < p.N) p.s_out[srow + n] = st[i];
-        }
+        for (int i = 0; i < NL; ++i)
+            if (value(i) < q.N) out[value(i)] = st[i];
+    }
+    if (!FULL && p0 == 0 && tid < 32) {  // threads 0 to RT - 1 hold the parts of the sum
+        if (tid >= RT) sum = 0.0f;
+#pragma unroll
+        for (int o = RT / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (tid == 0) p.total[part0 + seg] = sum;
     }
 }
 
+// Segments: as many as give three blocks an SM for the tokens there are, of SEG_MIN tokens at least
+int rec_segments(const SsmP &p) {
+    const int64_t full = (p.q.tokens + p.q.max_len - 1) / std::max<int64_t>(p.q.max_len, 1);  // sequences, counted by length
+    const int64_t blocks = std::max<int64_t>(full * p.H * ((p.P + 31) / 32), 1);
+    return (int)std::max<int64_t>(1, std::min<int64_t>({3LL * num_sms() / blocks, 64, p.q.max_len / SEG_MIN}));
+}
+int64_t rec_workspace(const SsmP &p) {
+    const int64_t segs = rec_segments(p);
+    return segs > 1 ? ((int64_t)p.q.batch * p.H * segs * ((int64_t)p.P * p.N + 1) * 4 + 255) / 256 * 256 : 0;
+}
+
+template <typename T, int NL>
+cudaError_t launch_rec(const RecP &p, const T *xbc, const T *dtv, T *y, cudaStream_t st) {
+    const unsigned heads = (unsigned)(p.s.H * ((p.s.P + 31) / 32)), batch = (unsigned)p.s.q.batch;
+    if (p.segs > 1) {
+        const cudaError_t e = launch_pdl(ssm_scan_rec_kernel<T, NL, false>, dim3(heads, (unsigned)(p.segs - 1), batch), dim3(256), 0, st, p, xbc,
+                                         dtv, y);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_pdl(ssm_scan_rec_kernel<T, NL, true>, dim3(heads, (unsigned)p.segs, batch), dim3(256), 0, st, p, xbc, dtv, y);
+}
+
 template <typename T>
-cudaError_t launch_scan(const SsmP &p, const T *xbc, const T *dtv, T *y, cudaStream_t st) {
-    const dim3 grid((unsigned)((p.P + 31) / 32), (unsigned)p.H, (unsigned)p.q.batch);
-    if (p.N <= 32) return launch_pdl(ssm_scan_rec_kernel<T, 4>, grid, dim3(256), 0, st, p, xbc, dtv, y);
-    if (p.N <= 64) return launch_pdl(ssm_scan_rec_kernel<T, 8>, grid, dim3(256), 0, st, p, xbc, dtv, y);
-    if (p.N <= 128) return launch_pdl(ssm_scan_rec_kernel<T, 16>, grid, dim3(256), 0, st, p, xbc, dtv, y);
-    return launch_pdl(ssm_scan_rec_kernel<T, 32>, grid, dim3(256), 0, st, p, xbc, dtv, y);
+cudaError_t launch_scan(const SsmP &s, const T *xbc, const T *dtv, T *y, void *work, cudaStream_t st) {
+    RecP p{s, s.q.tokens ? rec_segments(s) : 1, static_cast<float *>(work), nullptr};
+    p.total = p.part + (int64_t)s.q.batch * s.H * p.segs * s.P * s.N;
+    if (s.N <= 32) return launch_rec<T, 4>(p, xbc, dtv, y, st);
+    if (s.N <= 64) return launch_rec<T, 8>(p, xbc, dtv, y, st);
+    if (s.N <= 128) return launch_rec<T, 16>(p, xbc, dtv, y, st);
+    return launch_rec<T, 32>(p, xbc, dtv, y, st);
 }
 
 // --------------------------------------------------------------------- step
@@ -422,7 +532,9 @@ cudaError_t causal_conv(int dt, int channels, int width, int act, const float *w
 }
 
 size_t ssm_workspace(const sn_ssm_params &c, int dt, const SeqArgs &q) {
-    return dt == SN_BF16 && c.state <= 128 ? ssm_tc_workspace(ssm_params(c, q, 0, 0, nullptr, nullptr, 0)) : 0;
+    const SsmP p = ssm_params(c, q, 0, 0, nullptr, nullptr, 0);  // (which of the two it is depends on alignments too)
+    const size_t rec = (size_t)rec_workspace(p);
+    return dt == SN_BF16 && c.state <= 128 ? std::max(rec, ssm_tc_workspace(p)) : rec;
 }
 
 cudaError_t ssm_scan(const sn_ssm_params &c, int dt, const SeqArgs &q, const void *xbc, int64_t ldx, const void *dtv,
@@ -432,7 +544,7 @@ cudaError_t ssm_scan(const sn_ssm_params &c, int dt, const SeqArgs &q, const voi
         return ssm_tc_scan(p, static_cast<const __nv_bfloat16 *>(xbc), static_cast<const __nv_bfloat16 *>(dtv),
                            static_cast<__nv_bfloat16 *>(y), work, st);
     SN_DT_SWITCH(dt, T, return launch_scan<T>(p, static_cast<const T *>(xbc), static_cast<const T *>(dtv),
-                                              static_cast<T *>(y), st))
+                                              static_cast<T *>(y), work, st))
 }
 
 cudaError_t ssm_step(const sn_ssm_params &c, int dt, const SeqArgs &q, const void *xbc, int64_t ldx, const void *dtv,

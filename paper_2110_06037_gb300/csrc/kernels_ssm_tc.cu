@@ -585,7 +585,8 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
 
 // Segments that a sequence is cut into: as many as fill two blocks an SM, of four chunks at least
 int segments_of(const SsmP &p) {
-    const int64_t blocks = (int64_t)p.q.batch * p.H * ((p.P + PB - 1) / PB), chunks = (p.q.max_len + Q - 1) / Q;
+    const int64_t full = (p.q.tokens + p.q.max_len - 1) / std::max<int64_t>(p.q.max_len, 1);  // sequences, counted by length
+    const int64_t blocks = full * p.H * ((p.P + PB - 1) / PB), chunks = (p.q.max_len + Q - 1) / Q;
     const int64_t want = 2LL * num_sms() / std::max<int64_t>(blocks, 1);
     return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, 64), chunks / 4));
 }
