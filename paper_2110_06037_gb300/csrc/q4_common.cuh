@@ -90,6 +90,11 @@ __device__ __forceinline__ Planes planes_of(float x) {
     return p;
 }
 
+// few rows, at most FEW_COLS columns of B (fp32 x takes three a row)
+constexpr int FEW_COLS = 32;
+cudaError_t q4_few_f32(const Q4P &q, int rows, const float *x, int64_t ldx, float *y, int64_t ldy, cudaStream_t st);
+cudaError_t q4_few_f16(const Q4P &q, int rows, const __half *x, int64_t ldx, __half *y, int64_t ldy, cudaStream_t st);
+cudaError_t q4_few_bf16(const Q4P &q, int rows, const __nv_bfloat16 *x, int64_t ldx, __nv_bfloat16 *y, int64_t ldy, cudaStream_t st);
 // many rows, on the tensor cores
 size_t q4_prompt_workspace(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx);
 cudaError_t q4_prompt(const sn_q4_weights &w, int dt, int64_t rows, const void *x, int64_t ldx, void *y, int64_t ldy,
