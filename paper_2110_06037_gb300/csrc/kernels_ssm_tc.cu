@@ -15,16 +15,16 @@
 // registers in fp32: each chunk's product is added by an fp32 multiply-add, since the
 // tensor core's own sums do not round to nearest.
 //
-// Work: a block takes one head, 64 of its channels and a segment of a sequence's
-// chunks, two blocks an SM.  With few heads the sequence is cut into segments: a first
-// pass makes each segment's state from nothing (the last product alone), and the
+// Work: a block of one SM takes one head, 64 of its channels and a segment of a
+// sequence's chunks.  With few heads the sequence is cut into segments: a first pass
+// makes the states of (finer) segments from nothing, the last product alone, and the
 // second starts each segment from the joined ones.  A small kernel before both turns
 // time steps into sums of a and weights, once per token and head.
 //
-// Eight warps: warp w has TMEM lanes 32 (w % 4) + 0..31 (tokens t, or the state's n)
-// and half w / 4 of the columns; one lane of warps 0 to 4 each also issues one of the
-// products, or the copies, behind a barrier of the block (a ninth warp for that would
-// take a quarter of the registers).
+// Each product has warps of its own for what goes into and comes out of it, so that
+// only the state's one multiply-add a chunk runs from chunk to chunk: in one order, two
+// blocks an SM, a chunk took a block 17.9 thousand cycles of waiting for one step after
+// the other (198 us for 8192 tokens of 64 heads, the MMAs 32 of them).
 // Non-finite x: 0 * NaN would reach tokens before it, so such an x goes into the
 // product as 0 and makes its channel NaN from its token on; into the state it goes as
 // it is.  Waits are bounded.
@@ -42,7 +42,6 @@ using namespace tc;
 
 constexpr int Q = 128;          // tokens a chunk
 constexpr int PB = 64;          // channels a block
-constexpr int SCAN_THREADS = 256;
 constexpr float LOG2E = 1.4426950408889634f;
 
 // per chunk and head: A_t (inclusive, in units of log 2), A_s - log2 d_s, weights d_s e^{A_127 - A_s}
@@ -50,9 +49,9 @@ constexpr int TABLE = 3 * Q;
 
 struct TcP {
     SsmP s;
-    int32_t segs;            // segments a sequence
+    int32_t segs, fine;      // segments a sequence; finer ones of the first pass in each
     float *table, *total;    // [chunks][H][TABLE], [chunks][H]: A_127
-    float *part;             // [batch][H][p blocks][segs][64][N]: state before segment 0, then after segment j
+    float *part;             // [batch][H][p blocks][segs * fine][64][N]: state before the first, then after fine segment j
     int32_t pblocks;
     int *err;
 };
@@ -155,15 +154,21 @@ __device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint
         "r"(a), "l"(b), "r"(idesc), "r"(acc)
         : "memory");
 }
-__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&v)[16]) {
+__device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(v[0]), "r"(v[1]),
+                 "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+// 16 columns, at one, two or three addresses (the wait in the same statement: nothing of them is used before it)
+__device__ __forceinline__ void tmem_ld16(uint32_t ta, float (&a)[16]) {
     asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(
-            taddr),
-        "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]),
-        "r"(v[11]), "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15])
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=f"(a[0]), "=f"(a[1]), "=f"(a[2]), "=f"(a[3]), "=f"(a[4]), "=f"(a[5]), "=f"(a[6]), "=f"(a[7]), "=f"(a[8]), "=f"(a[9]),
+          "=f"(a[10]), "=f"(a[11]), "=f"(a[12]), "=f"(a[13]), "=f"(a[14]), "=f"(a[15])
+        : "r"(ta)
         : "memory");
 }
-// 16 columns at each of two addresses (the wait in the same statement: nothing of them is used before it)
 __device__ __forceinline__ void tmem_ld16x2(uint32_t ta, uint32_t (&a)[16], uint32_t tb, uint32_t (&b)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
@@ -174,6 +179,18 @@ __device__ __forceinline__ void tmem_ld16x2(uint32_t ta, uint32_t (&a)[16], uint
           "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]), "=r"(b[4]), "=r"(b[5]), "=r"(b[6]), "=r"(b[7]),
           "=r"(b[8]), "=r"(b[9]), "=r"(b[10]), "=r"(b[11]), "=r"(b[12]), "=r"(b[13]), "=r"(b[14]), "=r"(b[15])
         : "r"(ta), "r"(tb)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_ld16x3(uint32_t ta, uint32_t (&a)[16], uint32_t tb, uint32_t (&b)[16], uint32_t tc_, uint32_t (&c)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%48];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%49];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47}, [%50];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(a[4]), "=r"(a[5]), "=r"(a[6]), "=r"(a[7]), "=r"(a[8]), "=r"(a[9]), "=r"(a[10]), "=r"(a[11]), "=r"(a[12]), "=r"(a[13]), "=r"(a[14]), "=r"(a[15]),
+          "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]), "=r"(b[4]), "=r"(b[5]), "=r"(b[6]), "=r"(b[7]), "=r"(b[8]), "=r"(b[9]), "=r"(b[10]), "=r"(b[11]), "=r"(b[12]), "=r"(b[13]), "=r"(b[14]), "=r"(b[15]),
+          "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3]), "=r"(c[4]), "=r"(c[5]), "=r"(c[6]), "=r"(c[7]), "=r"(c[8]), "=r"(c[9]), "=r"(c[10]), "=r"(c[11]), "=r"(c[12]), "=r"(c[13]), "=r"(c[14]), "=r"(c[15])
+        : "r"(ta), "r"(tb), "r"(tc_)
         : "memory");
 }
 __device__ __forceinline__ void tmem_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
@@ -195,30 +212,44 @@ __device__ __forceinline__ Parts2 parts2(float a, float b) {
 }
 // ------------------------------------------------------------------- scan
 constexpr uint32_t TILE64 = Q * 128;  // 128 rows of 64 bf16 values
-constexpr uint32_t OFF_B = 0, OFF_C = 2 * TILE64, OFF_X = 4 * TILE64, OFF_H = 5 * TILE64, OFF_BARS = 7 * TILE64;
-constexpr size_t SCAN_SMEM = OFF_BARS + 1024;  // twice this and 1 KB each is all that an SM has
-// barriers (F_*: copies landed, M_*: MMAs done), one phase a chunk (F_B, F_B1: every other one without outputs)
-enum Bar { F_B, F_B1, F_C, F_X, M_PAIRS, M_CARRIED, M_MADE, M_INSIDE, BARS };
+// B, C (two tiles each) and x twice; X' and the state's parts (two tiles each) once
+constexpr uint32_t OFF_B = 0, OFF_C = 4 * TILE64, OFF_X = 8 * TILE64, OFF_XW = 10 * TILE64, OFF_H = 12 * TILE64, OFF_SHARED = 14 * TILE64;
+constexpr size_t SCAN_SMEM = OFF_SHARED + 2048;
+static_assert(SCAN_SMEM <= 227 * 1024, "shared memory of a block");
+// Barriers, one phase a chunk, or (two of a kind) a phase every other chunk.  F_*:
+// copies landed; E_*: MMAs have read the tile; M_*: MMAs done; A_*: arrivals of the
+// warps that have written or read what the name says.
+enum Bar {
+    F_B, F_C = F_B + 2, F_X = F_C + 2, E_B = F_X + 2, E_C = E_B + 2, E_X = E_C + 2,
+    M_PAIRS = E_X + 2, M_CARRIED, M_MADE, M_INSIDE, A_XW, A_MADE, A_STATE, A_P, A_OUT, BARS
+};
 struct Shared {
+    alignas(16) float as[2][Q];  // A_s - log2 d_s of a chunk
     uint64_t bar[BARS];
     uint32_t tmem;
-    int abort, any_bad;
-    int bad[PB];  // first token of the chunk whose x is not finite, by channel
-    alignas(16) float as[Q];  // the chunk's A_s - log2 d_s
+    int abort, any_bad[2];
+    int bad[2][PB];              // first token of a chunk whose x is not finite, by channel
 };
-static_assert(sizeof(Shared) <= 1024, "behind the tiles");
+static_assert(sizeof(Shared) <= 2048, "behind the tiles");
+// TMEM columns: pairs, and P's large parts in their place; carried and made with their
+// large and small parts' products apart; inside; P's small parts
+constexpr uint32_t T_S = 0, T_Y0 = 128, T_D = 256, T_Y1 = 384, T_LO = 448;
+
+// Warps: 0 copies, 1 issues the MMAs, 2 to 9 make P (FULL) or X' (two threads a row),
+// 10 to 13 carry the state, 14 to 17 (FULL) make X' (a thread a row) and the outputs.
+constexpr int FULL_THREADS = 18 * 32, STATE_THREADS = 14 * 32;
 
 // FULL: the outputs; otherwise a segment's state from nothing (segment 0: from s_in).
-// A wait that gives up leaves the warp's later ones and all further issues out; the
-// barriers of the block are passed by every warp in any case.
+// The MMAs' order, chunk i: carried(i), inside(i), pairs(i + 1), made(i + 1).  Every
+// role then has most of a chunk's time for its part: P(i + 1) between pairs(i + 1) and
+// inside(i + 1), the state between made(i) and carried(i + 1), copies more than that.
 template <bool FULL>
-__global__ void __launch_bounds__(SCAN_THREADS, 2)
+__global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
     ssm_scan_tc_kernel(const __grid_constant__ CUtensorMap mX, const __grid_constant__ CUtensorMap mB,
                        const __grid_constant__ CUtensorMap mC, const __grid_constant__ TcP p, __nv_bfloat16 *__restrict__ y) {
     extern __shared__ __align__(1024) uint8_t smem[];
-    Shared &sh = *reinterpret_cast<Shared *>(smem + OFF_BARS);
-    constexpr uint32_t COLS = FULL ? 256 : 64;
-    constexpr uint32_t T_S = 0, T_Y0 = 128, T_D = FULL ? 192 : 0;  // pairs and P; carried; made and inside
+    Shared &sh = *reinterpret_cast<Shared *>(smem + OFF_SHARED);
+    constexpr int XWARPS = FULL ? 4 : 8;  // warps that make X'
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int pb = blockIdx.x % p.pblocks, head = blockIdx.x / p.pblocks, seg = blockIdx.y, b = blockIdx.z;
     if (su32(smem) & 1023) {  // (the swizzled tiles need it; uniform over the block)
@@ -226,14 +257,15 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
         return;
     }
     if (warp == 0) {
-        tmem_alloc<1>(&sh.tmem, COLS);
-    } else if (warp == 1 && lane == 0) {
-        for (int i = 0; i < BARS; ++i) mbar_init(&sh.bar[i], 1);
-        sh.abort = sh.any_bad = 0;
+        tmem_alloc<1>(&sh.tmem, 512);
+    } else if (warp == 1) {
+        if (lane < BARS) mbar_init(&sh.bar[lane], lane < A_XW ? 1 : lane == A_XW ? XWARPS : lane == A_P ? 8 : 4);
+        if (lane == 31) sh.abort = sh.any_bad[0] = sh.any_bad[1] = 0;
         fence_mbar_init();
-    } else if (warp >= 6) {
-        sh.bad[threadIdx.x - 192] = Q;
+    } else if (warp >= 2 && warp < 6) {
+        (&sh.bad[0][0])[threadIdx.x - 64] = Q;
     }
+    static_assert(BARS < 31, "one lane a barrier");
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -242,189 +274,296 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
     griddep_wait();
     const SsmP &q = p.s;
     const Seq s = sequence(q.q, b);
-    const int2 chunks = segment(s.len, p.segs, seg);
+    const int2 chunks = FULL ? segment(s.len, p.segs, seg) : segment(s.len, p.segs * p.fine, seg);
     const int nc = chunks.y - chunks.x, grp = head / (q.H / q.G);
     const int p0 = pb * PB, np = min(PB, q.P - p0);
-    const int64_t part0 = (((int64_t)b * q.H + head) * p.pblocks + pb) * p.segs * PB * q.N;
+    const int64_t part0 = (((int64_t)b * q.H + head) * p.pblocks + pb) * (p.segs * p.fine) * PB * q.N;
     const uint32_t base = su32(smem);
-    const int quarter = warp % 4, half = warp / 4, row = quarter * 32 + lane;  // token, or n of the state
-    const uint32_t lanes = (uint32_t)(quarter * 32) << 16;
+    const int row = (warp % 4) * 32 + lane;  // token t, or n of the state, by the warp's TMEM lanes
+    const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
+    const int64_t tab0 = chunk_at(s, b, chunks.x) * q.H + head;
+    auto table = [&](int c) { return p.table + (tab0 + (int64_t)c * q.H) * TABLE; };
     bool ok = true;
-    auto must = [&](int i, uint32_t par) {  // the whole warp
+    auto gave_up = [&](int code) {
+        atomicOr(p.err, code);
+        *reinterpret_cast<volatile int *>(&sh.abort) = 1;
+    };
+    auto must = [&](int i, uint32_t par) {  // a whole warp's wait; after one that gave up, no further ones
         if (ok && !__all_sync(0xffffffffu, mbar_wait(&sh.bar[i], par))) {
-            if (lane == 0) {
-                atomicOr(p.err, ERR_EPI_WAIT);
-                *reinterpret_cast<volatile int *>(&sh.abort) = 1;
-            }
+            if (lane == 0) gave_up(ERR_EPI_WAIT);
             ok = false;
         }
+        return ok;
     };
-    auto may = [&]() { return ok && !*reinterpret_cast<volatile int *>(&sh.abort); };
-    // ---- what single lanes issue
-    auto load = [&](const CUtensorMap *m, int bar, uint32_t off, int c, int boxes, int x0, int g) {
-        if (lane != 0 || c >= nc || !may()) return;
-        mbar_expect_tx(&sh.bar[bar], boxes * TILE64);
-        for (int i = 0; i < boxes; ++i)
-            tma_3d<1>(base + off + i * TILE64, m, su32(&sh.bar[bar]), x0 + 64 * i, g, (int)(s.first + (int64_t)(chunks.x + c) * Q));
-    };
-    // (without outputs the C tile's place takes every other B)
-    auto b_bar = [&](int c) { return FULL || !(c & 1) ? F_B : F_B1; };
-    auto b_par = [&](int c) { return FULL ? (uint32_t)c & 1u : (uint32_t)(c >> 1) & 1u; };
-    auto b_off = [&](int c) { return FULL || !(c & 1) ? OFF_B : OFF_C; };
-    auto load_b = [&](int c) { load(&mB, b_bar(c), b_off(c), c, 2, 0, grp); };
-    auto load_c = [&](int c) { load(&mC, F_C, OFF_C, c, 2, 0, grp); };
-    auto load_x = [&](int c) { load(&mX, F_X, OFF_X, c, 1, p0, head); };
-    constexpr uint32_t FMT = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);  // fp32 sums of bf16, M = 128
-    constexpr uint32_t N128 = (128u >> 3) << 17, N64 = ((uint32_t)PB >> 3) << 17;
-    const int nk = (q.N + 15) / 16;
-    auto issue_carried = [&](int c) {  // warp 1
-        must(F_C, c & 1);
-        if (lane != 0 || !may()) return;
-        tc_fence_after();
-        for (int part = 0; part < 2; ++part)
-            for (int k = 0; k < nk; ++k)
-                umma<1>(tmem + T_Y0, sdesc_sw128(base + OFF_C + (uint32_t)(k / 4) * TILE64 + (uint32_t)(k % 4) * 32),
-                        sdesc_mn(base + OFF_H + part * TILE64 + k * 2048, TILE64), FMT | N64 | B_MN, part > 0 || k > 0);
-        umma_commit<1>(&sh.bar[M_CARRIED]);
-    };
-    auto issue_pairs = [&](int c) {  // warp 0
-        must(F_B, c & 1);
-        must(F_C, c & 1);
-        if (lane != 0 || !may()) return;
-        tc_fence_after();
-        for (int k = 0; k < nk; ++k) {
-            const uint32_t o = (uint32_t)(k / 4) * TILE64 + (uint32_t)(k % 4) * 32;
-            umma<1>(tmem + T_S, sdesc_sw128(base + OFF_C + o), sdesc_sw128(base + OFF_B + o), FMT | N128, k > 0);
-        }
-        umma_commit<1>(&sh.bar[M_PAIRS]);
-    };
-    auto issue_made = [&](int c) {  // warp 2
-        must(b_bar(c), b_par(c));
-        if (lane != 0 || !may()) return;
-        tc_fence_after();
-        for (int k = 0; k < Q / 16; ++k)
-            for (int part = 0; part < 2; ++part)
-                umma<1>(tmem + T_D, sdesc_mn(base + b_off(c) + k * 2048, TILE64), sdesc_mn(base + OFF_H + part * TILE64 + k * 2048, TILE64),
-                        FMT | N64 | A_MN | B_MN, part > 0 || k > 0);
-        umma_commit<1>(&sh.bar[M_MADE]);
-    };
-    auto issue_inside = [&]() {  // warp 3
-        if (lane != 0 || !may()) return;
-        tc_fence_after();
-        for (int part = 0; part < 2; ++part)
-            for (int k = 0; k < Q / 16; ++k)
-                umma_ts(tmem + T_D, tmem + T_S + (k / 2) * 32 + (k % 2) * 8 + part * 16, sdesc_mn(base + OFF_X + k * 2048, TILE64), FMT | N64 | B_MN,
-                        part > 0 || k > 0);
-        umma_commit<1>(&sh.bar[M_INSIDE]);
-    };
-    if (warp == 4) {
-        load_b(0);
-        if (FULL) load_c(0);
-        load_x(0);
-        if (!FULL) load_b(1);
+    auto arrive = [&](int i) {
         __syncwarp();
-    }
-    // the state before the segment, [p][n] with lane n: from s_in, or from the segments' parts joined
-    float h[32];
-    const int64_t srow = s.slot >= 0 ? (((int64_t)s.slot * q.H + head) * q.P + p0) * q.N : -1;
-#pragma unroll
-    for (int i = 0; i < 32; ++i) {
-        const int pc = half * 32 + i;
-        h[i] = 0.0f;
-        if (pc >= np || row >= q.N) continue;
-        if (p.segs > 1 && FULL) h[i] = p.part[part0 + ((int64_t)(seg > 0 ? 1 : 0) * PB + pc) * q.N + row];
-        else if (seg == 0 && q.s_in && srow >= 0) h[i] = q.s_in[srow + (int64_t)pc * q.N + row];
-    }
-    if (FULL) {
-        for (int j = 1; j < seg; ++j) {
-            const int2 ch = segment(s.len, p.segs, j);
-            float sum = 0.0f;
-            for (int c = ch.x; c < ch.y; ++c) sum += p.total[chunk_at(s, b, c) * q.H + head];
-            const float e = exp2f(sum);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const int pc = half * 32 + i;
-                if (pc < np && row < q.N) h[i] = fmaf(h[i], e, p.part[part0 + ((int64_t)(j + 1) * PB + pc) * q.N + row]);
+        if (lane == 0) mbar_arrive(&sh.bar[i]);
+    };
+
+    if (warp == 0) {
+        if (lane == 0) {  // ---------------- copies
+            auto load = [&](const CUtensorMap *m, int bar, uint32_t off, int c, int boxes, int x0, int g) {
+                mbar_expect_tx(&sh.bar[bar], boxes * TILE64);
+                for (int i = 0; i < boxes; ++i)
+                    tma_3d<1>(base + off + i * TILE64, m, su32(&sh.bar[bar]), x0 + 64 * i, g, (int)(s.first + (int64_t)(chunks.x + c) * Q));
+            };
+            auto freed = [&](int i, int c) {  // the chunk before in this stage has been read
+                if (ok && c >= 2 && !mbar_wait(&sh.bar[i], (uint32_t)((c >> 1) - 1) & 1u)) {
+                    gave_up(ERR_TMA_WAIT);
+                    ok = false;
+                }
+                return ok;
+            };
+            for (int c = 0; c < nc && ok; ++c) {
+                const int st = c & 1;
+                if (!freed(E_B + st, c)) break;
+                load(&mB, F_B + st, OFF_B + st * 2 * TILE64, c, 2, 0, grp);
+                if (FULL) {
+                    if (!freed(E_C + st, c)) break;
+                    load(&mC, F_C + st, OFF_C + st * 2 * TILE64, c, 2, 0, grp);
+                }
+                if (!freed(E_X + st, c)) break;
+                load(&mX, F_X + st, OFF_X + st * TILE64, c, 1, p0, head);
             }
         }
-    } else if (seg == 0) {  // the second pass may store over s_in: it reads this copy
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {  // ---------------- MMAs
+            constexpr uint32_t FMT = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);  // fp32 sums of bf16, M = 128
+            constexpr uint32_t N128 = (128u >> 3) << 17, N64 = ((uint32_t)PB >> 3) << 17;
+            const int nblk = q.N > 64 ? 2 : 1;  // blocks of 64 of the state's axis (zeros behind N)
+            auto need = [&](int i, uint32_t par) {
+                if (ok && !mbar_wait(&sh.bar[i], par)) {
+                    gave_up(ERR_MMA_WAIT);
+                    ok = false;
+                }
+                return ok;
+            };
+            // operands' descriptors at step 0; a step of 16 adds 32 bytes of a tile's 64 columns
+            // (K-major) or 16 rows (MN-major).  The steps are unrolled: one thread issues all MMAs,
+            // and forming a descriptor for each took it 150 cycles, an MMA takes the tensor core 64.
+            const uint64_t b_k = sdesc_sw128(base + OFF_B), c_k = sdesc_sw128(base + OFF_C);
+            const uint64_t b_mn = sdesc_mn(base + OFF_B, TILE64), x_mn = sdesc_mn(base + OFF_X, TILE64);
+            const uint64_t xw_mn = sdesc_mn(base + OFF_XW, TILE64), h_mn = sdesc_mn(base + OFF_H, TILE64);
+            constexpr uint64_t STAGE2 = 2 * TILE64 >> 4, STAGE1 = TILE64 >> 4;
+            auto mn_major = [](int k) { return (uint64_t)(k * (2048 >> 4)); };
+            auto pairs_and_made = [&](int c) {
+                const uint32_t st = c & 1, half = (uint32_t)(c >> 1) & 1u;
+                if (!need(F_B + st, half)) return;
+                if (FULL) {
+                    // (the pairs take the place of the chunk before's P: only MMAs on one accumulator keep their order by themselves)
+                    if (!need(F_C + st, half) || (c > 0 && !need(M_INSIDE, (c - 1) & 1))) return;
+                    tc_fence_after();
+                    const uint64_t dc = c_k + st * STAGE2, db = b_k + st * STAGE2;
+#pragma unroll 1
+                    for (int blk = 0; blk < nblk; ++blk) {
+                        const uint64_t o = blk * STAGE1;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            const int pc = half * 32 + i;
-            if (pc < np && row < q.N) p.part[part0 + (int64_t)pc * q.N + row] = h[i];
-        }
-    }
-    auto put_state = [&]() {  // its two bf16 parts as an operand: rows n, 64 p
-        uint8_t *hr = smem + OFF_H + row * 128;
+                        for (int k = 0; k < 4; ++k) umma<1>(tmem + T_S, dc + o + 2 * k, db + o + 2 * k, FMT | N128, blk > 0 || k > 0);
+                    }
+                    umma_commit<1>(&sh.bar[M_PAIRS]);
+                }
+                if (!need(A_XW, c & 1) || (c > 0 && !need(A_MADE, (c - 1) & 1))) return;
+                tc_fence_after();
+                const uint64_t db = b_mn + st * STAGE2;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t hi[4], lo[4];
+                for (int k = 0; k < Q / 16; ++k)  // (N = 128: the products with X's two parts side by side)
+                    umma<1>(tmem + T_D, db + mn_major(k), xw_mn + mn_major(k), FMT | N128 | A_MN | B_MN, k > 0);
+                umma_commit<1>(&sh.bar[M_MADE]);
+                umma_commit<1>(&sh.bar[E_B + st]);
+                if (!FULL) umma_commit<1>(&sh.bar[E_X + st]);
+            };
+#pragma unroll 1
+            for (int c = -1; c < nc && ok; ++c) {
+                if (FULL && c >= 0) {
+                    const uint32_t st = c & 1, par = c & 1;
+                    if (!need(A_STATE, par) || (c > 0 && !need(A_OUT, par ^ 1u))) break;
+                    tc_fence_after();
+                    const uint64_t dc = c_k + st * STAGE2, dx = x_mn + st * STAGE1;
+#pragma unroll 1
+                    for (int blk = 0; blk < nblk; ++blk)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const Parts2 v = parts2(h[8 * i + 2 * e], h[8 * i + 2 * e + 1]);  // (an infinite state's small part is NaN, as its sums over B's signs are)
-                hi[e] = v.hi, lo[e] = v.lo;
+                        for (int k = 0; k < 4; ++k)
+                            umma<1>(tmem + T_Y0, dc + blk * STAGE1 + 2 * k, h_mn + mn_major(4 * blk + k), FMT | N128 | B_MN, blk > 0 || k > 0);
+                    umma_commit<1>(&sh.bar[M_CARRIED]);
+                    umma_commit<1>(&sh.bar[E_C + st]);
+                    if (!need(A_P, par)) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int part = 0; part < 2; ++part)
+#pragma unroll
+                        for (int k = 0; k < Q / 16; ++k)
+                            umma_ts(tmem + T_Y1, tmem + (part ? T_LO + k * 8 : T_S + (k / 2) * 32 + (k % 2) * 8), dx + mn_major(k),
+                                    FMT | N64 | B_MN, part > 0 || k > 0);
+                    umma_commit<1>(&sh.bar[M_INSIDE]);
+                    umma_commit<1>(&sh.bar[E_X + st]);
+                }
+                if (c + 1 < nc) pairs_and_made(c + 1);
             }
-            const uint32_t at = (uint32_t)((4 * half + i) ^ (row & 7)) << 4;
-            *reinterpret_cast<uint4 *>(hr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-            *reinterpret_cast<uint4 *>(hr + TILE64 + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
         }
-        fence_proxy_async_smem();
-    };
-    if (FULL) put_state();
-    // what this thread needs of a chunk's table, loaded a chunk ahead
-    struct {
-        float at, as, w, total;  // A of its row, A_s - log2 d_s (threads 0 to 127: of token s), the weight of its token, A_127
-    } now, next{};
-    const int64_t tab0 = chunk_at(s, b, chunks.x) * q.H + head;
-    auto fetch = [&](int c) {
-        if (c >= nc) return;
-        const float *table = p.table + (tab0 + (int64_t)c * q.H) * TABLE;
-        if (FULL) {
-            next.at = __ldg(table + row);
-            next.as = __ldg(table + Q + (threadIdx.x & (Q - 1)));
-        }
-        next.w = __ldg(table + 2 * Q + threadIdx.x / 2);
-        next.total = __ldg(p.total + tab0 + (int64_t)c * q.H);
-    };
-    fetch(0);
-    const float skip = FULL && q.d ? q.d[head] : 0.0f;
-    for (int c = 0; c < nc; ++c) {
-        const uint32_t par = c & 1;
-        const int valid = min(Q, s.len - (chunks.x + c) * Q);  // tokens there are
-        now = next;
-        fetch(c + 1);
-        if constexpr (FULL) {
-            if (threadIdx.x < Q) sh.as[threadIdx.x] = now.as;  // (last read before the barrier ahead of the products inside)
-            // ---- the state's parts are written, the chunk before has been read everywhere
-            tc_fence_before();
-            __syncthreads();
-            if (warp == 1) issue_carried(c);
-            if (warp == 0) issue_pairs(c);
-            __syncwarp();
-            must(M_CARRIED, par);  // X' takes the place of the state's parts
-        }
-        // ---- X': half a row a thread
-        must(F_X, par);
-        if (valid < Q) {
-            must(b_bar(c), b_par(c));
-            if (FULL) must(M_PAIRS, par);
-        }
-        {
-            const int t = threadIdx.x / 2, j0 = 4 * (threadIdx.x & 1);
-            const float w = now.w;
-            uint8_t *xr = smem + OFF_X + t * 128, *hr = smem + OFF_H + t * 128;
-#pragma unroll
+        __syncwarp();
+    } else if (FULL && warp < 10) {
+        // ---------------- P from the pairs: 32 x 32 blocks, this warp's two of its rows' four; D,
+        // the factor of x itself, joins the diagonal
+        const int quarter = warp % 4, half = (warp - 2) / 4, t = threadIdx.x - 64;  // t: 0 to 255
+        const float skip = q.d ? q.d[head] : 0.0f;
+        float at_next = 0.0f, as_next = 0.0f;  // of the next chunk: A of this row, A_s - log2 d_s of token t (t < 128)
+        auto fetch = [&](int c) {
+            if (c >= nc) return;
+            at_next = __ldg(table(c) + row);
+            if (t < Q) as_next = __ldg(table(c) + Q + t);
+        };
+        fetch(0);
+        for (int c = 0; c < nc; ++c) {
+            const uint32_t par = c & 1;
+            const float At = at_next;
+            if (t < Q) sh.as[par][t] = as_next;  // (its last readers, two chunks ago, have passed the barrier since)
+            fetch(c + 1);
+            if (bar_red_or(1, 256, !ok)) break;  // (the group leaves together)
+            if (!must(M_PAIRS, par)) continue;
+            tc_fence_after();
+            // 16 columns at a time in a rolled loop (all 64 unrolled, as every role's loop was,
+            // the warps waited for instructions: some 14 cycles for each)
+#pragma unroll 1
             for (int i = 0; i < 4; ++i) {
+                const int blk = 2 * (i / 2) + half, c0 = 32 * blk + 16 * (i % 2);
+                uint32_t hi[8], lo[8];
+                __syncwarp();
+                if (blk <= quarter) {
+                    float f[16];
+                    tmem_ld16(tmem + lanes + T_S + c0, f);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float4 As = *reinterpret_cast<const float4 *>(&sh.as[par][c0 + 4 * j]);
+                        f[4 * j] *= ex2(At - As.x), f[4 * j + 1] *= ex2(At - As.y);
+                        f[4 * j + 2] *= ex2(At - As.z), f[4 * j + 3] *= ex2(At - As.w);
+                    }
+                    if (blk == quarter) {
+                        const int own = row - c0;  // the diagonal's place among these columns
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) f[j] = j < own ? f[j] : j == own ? f[j] + skip : 0.0f;
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        const Parts2 v = parts2(f[2 * j], f[2 * j + 1]);
+                        hi[j] = v.hi, lo[j] = v.lo;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) hi[j] = lo[j] = 0u;
+                }
+                __syncwarp();
+                tmem_st8(tmem + lanes + T_S + 32 * blk + 8 * (i % 2), hi);  // (these columns' pairs have been read)
+                tmem_st8(tmem + lanes + T_LO + c0 / 2, lo);
+            }
+            tmem_wait_st();
+            tc_fence_before();
+            arrive(A_P);
+        }
+    } else if (warp >= 10 && warp < 14) {
+        // ---------------- the state, [p][n] with lane n, in fp32
+        float h[PB];
+        const int64_t srow = s.slot >= 0 ? (((int64_t)s.slot * q.H + head) * q.P + p0) * q.N + row : -1;
+        auto live = [&](int i) { return i < np && row < q.N; };
+        auto part = [&](int j) { return p.part + part0 + (int64_t)j * PB * q.N + row; };  // before segment 0, after fine segment j - 1
+#pragma unroll
+        for (int i = 0; i < PB; ++i) {
+            h[i] = 0.0f;
+            if (!live(i)) continue;
+            if (FULL && p.segs > 1) h[i] = part(seg > 0 ? 1 : 0)[(int64_t)i * q.N];
+            else if (seg == 0 && q.s_in && srow >= 0) h[i] = q.s_in[srow + (int64_t)i * q.N];
+        }
+        if (FULL) {
+            for (int j = 1; j < seg * p.fine; ++j) {
+                const int2 ch = segment(s.len, p.segs * p.fine, j);
+                float sum = 0.0f;
+                for (int c = ch.x; c < ch.y; ++c) sum += p.total[chunk_at(s, b, c) * q.H + head];
+                const float e = exp2f(sum);
+#pragma unroll
+                for (int i = 0; i < PB; ++i)
+                    if (live(i)) h[i] = fmaf(h[i], e, part(j + 1)[(int64_t)i * q.N]);
+            }
+        } else if (seg == 0) {  // the second pass may store over s_in: it reads this copy
+#pragma unroll
+            for (int i = 0; i < PB; ++i)
+                if (live(i)) part(0)[(int64_t)i * q.N] = h[i];
+        }
+        auto put_state = [&]() {  // its two bf16 parts as an operand: rows n, 64 p
+            uint8_t *hr = smem + OFF_H + row * 128;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t hi[4], lo[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    // (an infinite state's small part is NaN, as its sums over B's signs are)
+                    const Parts2 v = parts2(h[8 * i + 2 * e], h[8 * i + 2 * e + 1]);
+                    hi[e] = v.hi, lo[e] = v.lo;
+                }
+                const uint32_t at = (uint32_t)(i ^ (row & 7)) << 4;
+                *reinterpret_cast<uint4 *>(hr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4 *>(hr + TILE64 + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+            }
+            fence_proxy_async_smem();
+            arrive(A_STATE);
+        };
+        float total_next = nc > 0 ? __ldg(p.total + tab0) : 0.0f;
+#pragma unroll 1
+        for (int c = 0; c < nc; ++c) {
+            if (FULL) {
+                if (c > 0 && !must(M_CARRIED, (c - 1) & 1)) break;  // the operand before has been read
+                put_state();
+            }
+            const float e = exp2f(total_next);
+            if (c + 1 < nc) total_next = __ldg(p.total + tab0 + (int64_t)(c + 1) * q.H);
+            if (!must(M_MADE, c & 1)) break;
+            tc_fence_after();
+#pragma unroll
+            for (int i = 0; i < PB; i += 16) {
+                uint32_t u[16], v[16];
+                __syncwarp();
+                tmem_ld16x2(tmem + lanes + T_D + i, u, tmem + lanes + T_D + PB + i, v);
+#pragma unroll
+                for (int j = 0; j < 16; ++j) h[i + j] = fmaf(h[i + j], e, __uint_as_float(u[j]) + __uint_as_float(v[j]));
+            }
+            tc_fence_before();
+            arrive(A_MADE);
+        }
+        float *out = FULL ? (seg == p.segs - 1 && q.s_out && srow >= 0 ? q.s_out + srow : nullptr) : part(seg + 1);
+        if (ok && out) {
+#pragma unroll
+            for (int i = 0; i < PB; ++i)
+                if (live(i)) out[(int64_t)i * q.N] = h[i];
+        }
+    } else {
+        // ---------------- X' (and, FULL, the outputs)
+        constexpr int PIECES = FULL ? 8 : 4;  // 16-byte pieces of a row a thread takes
+        const int t0 = threadIdx.x - (FULL ? 14 * 32 : 64), t = FULL ? t0 : t0 / 2, j0 = FULL ? 0 : 4 * (t0 & 1);
+        float w_next = nc > 0 ? __ldg(table(0) + 2 * Q + t) : 0.0f, at_next = 0.0f;
+        auto weigh = [&](int c) {
+            const int st = c & 1, valid = min(Q, s.len - (chunks.x + c) * Q);  // tokens there are
+            const float w = w_next;
+            if (c + 1 < nc) w_next = __ldg(table(c + 1) + 2 * Q + t);
+            must(F_X + st, (uint32_t)(c >> 1) & 1u);
+            if (c > 0) must(M_MADE, (c - 1) & 1);  // the X' before has been read
+            if (valid < Q) {
+                must(F_B + st, (uint32_t)(c >> 1) & 1u);
+                if (FULL) must(M_PAIRS, c & 1);
+            }
+            if (!ok) return;
+            uint8_t *xr = smem + OFF_X + st * TILE64 + t * 128, *wr = smem + OFF_XW + t * 128;
+#pragma unroll 2
+            for (int i = 0; i < PIECES; ++i) {
                 const uint32_t at = (uint32_t)((j0 + i) ^ (t & 7)) << 4;
                 uint4 xv = *reinterpret_cast<const uint4 *>(xr + at);
                 if (t >= valid) {  // rows of another sequence: nothing of them may count
                     xv = make_uint4(0u, 0u, 0u, 0u);
                     *reinterpret_cast<uint4 *>(xr + at) = xv;
-                    uint8_t *br = smem + b_off(c) + t * 128 + at;
+                    uint8_t *br = smem + OFF_B + st * 2 * TILE64 + t * 128 + at;
                     *reinterpret_cast<uint4 *>(br) = xv;
                     *reinterpret_cast<uint4 *>(br + TILE64) = xv;
                 }
-                uint32_t u[4] = {xv.x, xv.y, xv.z, xv.w}, hi[4], lo[4], odd = 0u;  // odd: a value's exponent is all ones
+                const uint32_t u[4] = {xv.x, xv.y, xv.z, xv.w};
+                uint32_t hi[4], lo[4], odd = 0u;  // odd: a value's exponent is all ones
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const float2 f = unpack2<__nv_bfloat16>(u[e]);
@@ -432,146 +571,78 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
                     const Parts2 v = parts2(f.x * w, f.y * w);
                     hi[e] = v.hi, lo[e] = v.lo;
                 }
+                *reinterpret_cast<uint4 *>(wr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4 *>(wr + TILE64 + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
                 if (odd) {
-#pragma unroll
+#pragma unroll 1
                     for (int e = 0; e < 8; ++e) {
-                        const uint32_t shift = 16 * (e % 2);
-                        if ((u[e / 2] >> shift & 0x7f80u) != 0x7f80u) continue;
-                        lo[e / 2] &= ~(0xffffu << shift);  // into the state as it is
+                        uint16_t *xe = reinterpret_cast<uint16_t *>(xr + at) + e;
+                        if ((*xe & 0x7f80u) != 0x7f80u) continue;
+                        reinterpret_cast<uint16_t *>(wr + TILE64 + at)[e] = 0;  // into the state as it is
                         if (FULL) {  // out of the product inside the chunk; its channel is NaN from here on
-                            u[e / 2] &= ~(0xffffu << shift);
-                            atomicMin(&sh.bad[8 * (j0 + i) + e], t);
-                            sh.any_bad = 1;
+                            *xe = 0;
+                            atomicMin(&sh.bad[st][8 * (j0 + i) + e], t);
+                            sh.any_bad[st] = 1;
                         }
                     }
-                    if (FULL) *reinterpret_cast<uint4 *>(xr + at) = make_uint4(u[0], u[1], u[2], u[3]);
-                }
-                *reinterpret_cast<uint4 *>(hr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                *reinterpret_cast<uint4 *>(hr + TILE64 + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-            }
-        }
-        fence_proxy_async_smem();
-        __syncthreads();
-        if (warp == 2) issue_made(c);
-        if (!FULL && warp == 4) load_x(c + 1);
-        __syncwarp();
-        if constexpr (FULL) {
-            // ---- P from the pairs: 32 x 32 blocks, this warp's two of its rows' four; D, the
-            // factor of x itself, joins the diagonal
-            const float At = now.at;
-            must(M_PAIRS, par);
-            tc_fence_after();
-            if (warp == 4) load_c(c + 1);  // (both of its products are done)
-#pragma unroll
-            for (int step = 0; step < 2; ++step) {
-                // a block's two parts, 16 columns each, take the place of its pairs
-                const int blk = 2 * step + half;
-                uint32_t hi[16], lo[16];
-                __syncwarp();
-                if (blk <= quarter) {
-                    uint32_t v[32];
-                    tmem_ld32(tmem + lanes + T_S + 32 * blk, v);
-                    auto weigh = [&](auto diagonal) {
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const float4 As = *reinterpret_cast<const float4 *>(&sh.as[32 * blk + 4 * j]);
-                            const float as[4] = {As.x, As.y, As.z, As.w};
-                            float f[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) {
-                                f[e] = __uint_as_float(v[4 * j + e]) * ex2(At - as[e]);
-                                if (diagonal.value) f[e] = 4 * j + e < lane ? f[e] : 4 * j + e == lane ? f[e] + skip : 0.0f;
-                            }
-                            const Parts2 a = parts2(f[0], f[1]), bb = parts2(f[2], f[3]);
-                            hi[2 * j] = a.hi, hi[2 * j + 1] = bb.hi, lo[2 * j] = a.lo, lo[2 * j + 1] = bb.lo;
-                        }
-                    };
-                    if (blk == quarter) weigh(std::true_type{});
-                    else weigh(std::false_type{});
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 16; ++j) hi[j] = lo[j] = 0u;
-                }
-                __syncwarp();
-                tmem_st16(tmem + lanes + T_S + 32 * blk, hi);
-                tmem_st16(tmem + lanes + T_S + 32 * blk + 16, lo);
-            }
-            tmem_wait_st();
-        }
-        // ---- the state behind the chunk
-        must(M_MADE, par);
-        tc_fence_after();
-        {
-            const float e = exp2f(now.total);
-            uint32_t v[32];
-            __syncwarp();
-            tmem_ld32(tmem + lanes + T_D + 32 * half, v);
-#pragma unroll
-            for (int i = 0; i < 32; ++i) h[i] = fmaf(h[i], e, __uint_as_float(v[i]));
-        }
-        tc_fence_before();
-        if constexpr (FULL) {
-            __syncthreads();  // P is written, the made state has been read
-            if (warp == 3) issue_inside();
-            if (warp == 4) load_b(c + 1);
-            __syncwarp();
-            put_state();
-            // ---- the chunk's outputs
-            const float et = ex2(now.at);
-            must(M_INSIDE, par);
-            if (warp == 4) load_x(c + 1);
-            __syncwarp();
-            tc_fence_after();
-            const bool bad = *reinterpret_cast<volatile int *>(&sh.any_bad);
-            __nv_bfloat16 *yr = y + (s.first + (int64_t)(chunks.x + c) * Q + row) * q.ldy + (int64_t)head * q.P + p0 + 32 * half;
-#pragma unroll
-            for (int i2 = 0; i2 < 2; ++i2) {
-                uint32_t y0[16], y1[16];
-                __syncwarp();
-                tmem_ld16x2(tmem + lanes + T_Y0 + 32 * half + 16 * i2, y0, tmem + lanes + T_D + 32 * half + 16 * i2, y1);
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const int i = 2 * i2 + j;
-                    uint32_t o[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float f0 = fmaf(__uint_as_float(y0[8 * j + 2 * e]), et, __uint_as_float(y1[8 * j + 2 * e]));
-                        float f1 = fmaf(__uint_as_float(y0[8 * j + 2 * e + 1]), et, __uint_as_float(y1[8 * j + 2 * e + 1]));
-                        if (bad) {
-                            if (row >= sh.bad[32 * half + 8 * i + 2 * e]) f0 = NAN;
-                            if (row >= sh.bad[32 * half + 8 * i + 2 * e + 1]) f1 = NAN;
-                        }
-                        o[e] = pack2<__nv_bfloat16>(f0, f1);
-                    }
-                    if (row < valid && 32 * half + 8 * i < np) *reinterpret_cast<uint4 *>(yr + 8 * i) = make_uint4(o[0], o[1], o[2], o[3]);
                 }
             }
-            if (bad) {  // (the same in every warp: it was set before the barrier behind X')
-                __syncthreads();
-                if (threadIdx.x < PB) sh.bad[threadIdx.x] = Q;
-                if (threadIdx.x == 0) sh.any_bad = 0;
-            }
+            fence_proxy_async_smem();
+            arrive(A_XW);
+        };
+        if constexpr (!FULL) {
+            for (int c = 0; c < nc && ok; ++c) weigh(c);
         } else {
-            // (the next chunk's X' is written behind this wait: its place has been read)
-            if (warp == 4) load_b(c + 2);
-            __syncwarp();
-        }
-    }
-    // the state behind the segment
-    if (may()) {
-        float *out = FULL ? (seg == p.segs - 1 && q.s_out && srow >= 0 ? q.s_out + srow : nullptr)
-                          : p.part + part0 + (int64_t)(seg + 1) * PB * q.N;
-        if (out) {
+#pragma unroll 1
+            for (int c = -1; c < nc; ++c) {
+                const float et = ex2(at_next);  // (of chunk c)
+                if (c + 1 < nc) {
+                    at_next = __ldg(table(c + 1) + row);
+                    weigh(c + 1);
+                }
+                if (c < 0) continue;
+                const int st = c & 1, valid = min(Q, s.len - (chunks.x + c) * Q);
+                if (bar_red_or(2, 128, !ok)) break;  // (the group leaves together; and bad[st] is complete)
+                if (!must(M_INSIDE, c & 1)) continue;
+                tc_fence_after();
+                const bool bad = *reinterpret_cast<volatile int *>(&sh.any_bad[st]);
+                __nv_bfloat16 *yr = y + (s.first + (int64_t)(chunks.x + c) * Q + row) * q.ldy + (int64_t)head * q.P + p0;
+#pragma unroll 1
+                for (int i = 0; i < PB; i += 16) {
+                    uint32_t u[16], v[16], in[16];
+                    __syncwarp();
+                    tmem_ld16x3(tmem + lanes + T_Y0 + i, u, tmem + lanes + T_Y0 + PB + i, v, tmem + lanes + T_Y1 + i, in);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) {
-                const int pc = half * 32 + i;
-                if (pc < np && row < q.N) out[(int64_t)pc * q.N + row] = h[i];
+                    for (int j = 0; j < 16; j += 8) {
+                        uint32_t o[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float f[2];
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) {
+                                const int n = j + 2 * e + k;
+                                f[k] = fmaf(__uint_as_float(u[n]) + __uint_as_float(v[n]), et, __uint_as_float(in[n]));
+                                if (bad && row >= sh.bad[st][i + n]) f[k] = NAN;
+                            }
+                            o[e] = pack2<__nv_bfloat16>(f[0], f[1]);
+                        }
+                        if (row < valid && i + j < np) *reinterpret_cast<uint4 *>(yr + i + j) = make_uint4(o[0], o[1], o[2], o[3]);
+                    }
+                }
+                tc_fence_before();
+                arrive(A_OUT);
+                if (bad) {  // (the same in the group's every warp: set before the barrier above)
+                    asm volatile("bar.sync 3, 128;" ::: "memory");
+                    if (t < PB) sh.bad[st][t] = Q;
+                    if (t == 0) sh.any_bad[st] = 0;
+                    asm volatile("bar.sync 3, 128;" ::: "memory");
+                }
             }
         }
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 4 && lane == 0 && sh.abort) {  // copies in flight land before the block's memory goes away (bounded)
+    if (threadIdx.x == 0 && sh.abort) {  // copies in flight land before the block's memory goes away (bounded)
         const long long t0 = clock64();
         while (clock64() - t0 < WAIT_LIMIT / 1000) {
         }
@@ -579,16 +650,22 @@ __global__ void __launch_bounds__(SCAN_THREADS, 2)
     __syncthreads();
     if (warp == 0) {
         tc_fence_after();
-        tmem_dealloc<1>(tmem, COLS);
+        tmem_dealloc<1>(tmem, 512);
     }
 }
 
-// Segments that a sequence is cut into: as many as fill two blocks an SM, of four chunks at least
-int segments_of(const SsmP &p) {
+// Segments that a sequence is cut into: as many as fill the SMs, of four chunks at
+// least; and the first pass's, which leaves the last segment out
+struct Cut {
+    int segs, fine;
+};
+Cut cut_of(const SsmP &p) {
     const int64_t full = (p.q.tokens + p.q.max_len - 1) / std::max<int64_t>(p.q.max_len, 1);  // sequences, counted by length
-    const int64_t blocks = full * p.H * ((p.P + PB - 1) / PB), chunks = (p.q.max_len + Q - 1) / Q;
-    const int64_t want = 2LL * num_sms() / std::max<int64_t>(blocks, 1);
-    return (int)std::max<int64_t>(1, std::min<int64_t>(std::min<int64_t>(want, 64), chunks / 4));
+    const int64_t blocks = std::max<int64_t>(full * p.H * ((p.P + PB - 1) / PB), 1), chunks = (p.q.max_len + Q - 1) / Q;
+    Cut c;
+    c.segs = (int)std::max<int64_t>(1, std::min<int64_t>({num_sms() / blocks, 64, chunks / 4}));
+    c.fine = c.segs == 1 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(num_sms() / (blocks * (c.segs - 1)), chunks / c.segs / 2));
+    return c;
 }
 struct TcWork {
     int64_t chunks, table, total, part, bytes;  // offsets
@@ -600,8 +677,8 @@ TcWork work_of(const SsmP &p) {
     w.table = 0;
     w.total = w.table + up(w.chunks * p.H * TABLE * 4);
     w.part = w.total + up(w.chunks * p.H * 4);
-    const int segs = segments_of(p);
-    w.bytes = w.part + (segs > 1 ? up((int64_t)p.q.batch * p.H * ((p.P + PB - 1) / PB) * segs * PB * p.N * 4) : 0);
+    const Cut c = cut_of(p);
+    w.bytes = w.part + (c.segs > 1 ? up((int64_t)p.q.batch * p.H * ((p.P + PB - 1) / PB) * c.segs * c.fine * PB * p.N * 4) : 0);
     return w;
 }
 
@@ -619,7 +696,8 @@ cudaError_t ssm_tc_scan(const SsmP &s, const __nv_bfloat16 *xbc, const __nv_bflo
                         cudaStream_t st) {
     const TcWork w = work_of(s);
     char *base = static_cast<char *>(work);
-    TcP p{s, segments_of(s), reinterpret_cast<float *>(base + w.table), reinterpret_cast<float *>(base + w.total),
+    const Cut cut = cut_of(s);
+    TcP p{s, cut.segs, cut.fine, reinterpret_cast<float *>(base + w.table), reinterpret_cast<float *>(base + w.total),
           reinterpret_cast<float *>(base + w.part), (s.P + PB - 1) / PB, device_error_word()};
     // xbc's rows as [heads][P] of x and [groups][N] of B and C: what lies behind a head's or group's end reads as 0
     CUtensorMap mX, mB, mC;
@@ -644,11 +722,11 @@ cudaError_t ssm_tc_scan(const SsmP &s, const __nv_bfloat16 *xbc, const __nv_bflo
     cudaError_t e = launch_pdl(ssm_steps_kernel, dim3(chunks, (unsigned)((s.H + 7) / 8), (unsigned)s.q.batch), dim3(256), 0, st, p, dtv, vec);
     if (e != cudaSuccess) return e;
     if (p.segs > 1) {
-        e = launch_pdl(ssm_scan_tc_kernel<false>, dim3(heads, (unsigned)(p.segs - 1), (unsigned)s.q.batch), dim3(SCAN_THREADS), SCAN_SMEM, st,
+        e = launch_pdl(ssm_scan_tc_kernel<false>, dim3(heads, (unsigned)((p.segs - 1) * p.fine), (unsigned)s.q.batch), dim3(STATE_THREADS), SCAN_SMEM, st,
                        mX, mB, mC, p, y);
         if (e != cudaSuccess) return e;
     }
-    return launch_pdl(ssm_scan_tc_kernel<true>, dim3(heads, (unsigned)p.segs, (unsigned)s.q.batch), dim3(SCAN_THREADS), SCAN_SMEM, st, mX, mB,
+    return launch_pdl(ssm_scan_tc_kernel<true>, dim3(heads, (unsigned)p.segs, (unsigned)s.q.batch), dim3(FULL_THREADS), SCAN_SMEM, st, mX, mB,
                       mC, p, y);
 }
 

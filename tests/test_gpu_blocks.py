@@ -429,6 +429,32 @@ def test_scan_of_long_prompts_with_few_heads(dt, lens, sizes):
     assert torch.equal(again, y) and torch.equal(state, out)
 
 
+@pytest.mark.parametrize("lens, sizes", [
+    ([16], (1, 64, 1, 128)), ([127, 0, 1, 130, 64], (3, 64, 3, 64)), ([129], (8, 64, 2, 128)), ([385, 5], (2, 32, 1, 96)),
+    ([256, 256], (2, 40, 2, 24)), ([300], (2, 8, 1, 8)), ([40, 500], (2, 136, 1, 104)), ([128] * 9, (4, 64, 1, 16)),
+    ([700], (40, 64, 1, 128)), ([513, 2], (4, 72, 2, 120))])
+def test_scan_of_bf16_rows_that_lie_aligned(lens, sizes):
+    """Rows that the copies of the tensor-core form take: head and state sizes that fill its tiles or not."""
+    import torch
+    import paper_2110_06037_gb300 as sn
+    h, p, g, n = sizes
+    rng = np.random.default_rng(sum(lens) + n)
+    a, d, b = ssm_weights(rng, h, fast=n == 64)
+    rows, c = sum(lens), h * p + 2 * g * n
+    xbc, step = dev(rng.normal(size=(rows, c)), "bf16"), dev(rng.normal(size=(rows, h)) - 1, "bf16")
+    state = dev(rng.normal(size=(len(lens), h, p, n)))
+    off = ints(np.concatenate(([0], np.cumsum(lens))).tolist())
+    ref, my, sref, ms = run_scan(host(xbc), host(step), lens, sizes, a, d, b, host(state), list(range(len(lens))))
+    ssm = sn.StateSpace(h, p, g, n, dev(a), dev(d), dev(b))
+    out = torch.empty_like(state)
+    y = ssm.scan(xbc, step, offsets=off, max_len=max(lens), state_in=state, state_out=out)
+    close(y, ref, scan_bound(my, max(lens)) + 2.0 ** -14 * my, "bf16")
+    close(out, sref, scan_bound(ms, max(lens)), "f32")
+    for _ in range(3):
+        assert torch.equal(ssm.scan(xbc, step, offsets=off, max_len=max(lens), state_in=state, state_out=out), y)
+    sn.check_device()
+
+
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 def test_scan_of_infinite_and_nan_channels(dt):
     """One channel's x is not finite at one token: every other channel, and that one before it, as without."""
