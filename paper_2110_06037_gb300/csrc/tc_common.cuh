@@ -255,6 +255,52 @@ __device__ __forceinline__ void umma_commit(uint64_t *bar) {
                      : "memory");
 }
 
+// The same, issued by one lane (`one` from elect_one) in code that the whole warp
+// runs: descriptors then stay in uniform registers.  In code of one lane alone they are
+// moved there for every MMA, about 130 cycles each, where an MMA of N = 128 takes 64.
+__device__ __forceinline__ uint32_t elect_one() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r;
+}
+template <int G>
+__device__ __forceinline__ void umma_one(uint32_t one, uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    if constexpr (G == 2)
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "setp.ne.b32 q, %5, 0;\n\t"
+            "@q tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred p, q;\n\t"
+            "setp.ne.b32 p, %4, 0;\n\t"
+            "setp.ne.b32 q, %5, 0;\n\t"
+            "@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+            ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
+            : "memory");
+}
+template <int G>
+__device__ __forceinline__ void commit_one(uint32_t one, uint64_t *bar) {
+    if constexpr (G == 2)
+        asm volatile(
+            "{\n\t.reg .pred q;\n\t"
+            "setp.ne.b32 q, %2, 0;\n\t"
+            "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;\n\t}" ::"r"(
+                su32(bar)),
+            "h"((uint16_t)3), "r"(one)
+            : "memory");
+    else
+        asm volatile(
+            "{\n\t.reg .pred q;\n\t"
+            "setp.ne.b32 q, %1, 0;\n\t"
+            "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(su32(bar)),
+            "r"(one)
+            : "memory");
+}
+
 // ----------------------------------------------------------- cluster helpers
 __device__ __forceinline__ uint32_t cluster_rank() {
     uint32_t r;
