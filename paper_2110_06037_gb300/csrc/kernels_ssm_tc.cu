@@ -24,7 +24,8 @@
 // Each product has warps of its own for what goes into and comes out of it, so that
 // only the state's one multiply-add a chunk runs from chunk to chunk: in one order, two
 // blocks an SM, a chunk took a block 17.9 thousand cycles of waiting for one step after
-// the other (198 us for 8192 tokens of 64 heads, the MMAs 32 of them).
+// the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128), the MMAs 32 of
+// them.  So: 152 us.
 // Non-finite x: 0 * NaN would reach tokens before it, so such an x goes into the
 // product as 0 and makes its channel NaN from its token on; into the state it goes as
 // it is.  Waits are bounded.
@@ -145,13 +146,14 @@ __device__ __forceinline__ uint64_t sdesc_mn(uint32_t saddr, uint32_t block) {
     return d;
 }
 constexpr uint32_t A_MN = 1u << 15, B_MN = 1u << 16;  // instruction descriptor: operand is MN-major
-// A from TMEM: a lane's row, two bf16 values a column
-__device__ __forceinline__ void umma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+// umma_one with A from TMEM: a lane's row, two bf16 values a column
+__device__ __forceinline__ void umma_ts_one(uint32_t one, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
     asm volatile(
-        "{\n\t.reg .pred p;\n\t"
+        "{\n\t.reg .pred p, q;\n\t"
         "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"(acc)
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
         : "memory");
 }
 __device__ __forceinline__ void tmem_st8(uint32_t taddr, const uint32_t (&v)[8]) {
@@ -269,7 +271,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = sh.tmem;
+    const uint32_t tmem = __shfl_sync(0xffffffffu, sh.tmem, 0);
     griddep_launch();  // (behind the allocation: see tmem_alloc)
     griddep_wait();
     const SsmP &q = p.s;
@@ -328,13 +330,14 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
         }
         __syncwarp();
     } else if (warp == 1) {
-        if (lane == 0) {  // ---------------- MMAs
+        {  // ---------------- MMAs: the whole warp, so that descriptors stay in uniform registers; one lane issues
+            const uint32_t one = elect_one();
             constexpr uint32_t FMT = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);  // fp32 sums of bf16, M = 128
             constexpr uint32_t N128 = (128u >> 3) << 17, N64 = ((uint32_t)PB >> 3) << 17;
             const int nblk = q.N > 64 ? 2 : 1;  // blocks of 64 of the state's axis (zeros behind N)
             auto need = [&](int i, uint32_t par) {
-                if (ok && !mbar_wait(&sh.bar[i], par)) {
-                    gave_up(ERR_MMA_WAIT);
+                if (ok && !__all_sync(0xffffffffu, mbar_wait(&sh.bar[i], par))) {
+                    if (lane == 0) gave_up(ERR_MMA_WAIT);
                     ok = false;
                 }
                 return ok;
@@ -359,19 +362,19 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                     for (int blk = 0; blk < nblk; ++blk) {
                         const uint64_t o = blk * STAGE1;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) umma<1>(tmem + T_S, dc + o + 2 * k, db + o + 2 * k, FMT | N128, blk > 0 || k > 0);
+                        for (int k = 0; k < 4; ++k) umma_one<1>(one, tmem + T_S, dc + o + 2 * k, db + o + 2 * k, FMT | N128, blk > 0 || k > 0);
                     }
-                    umma_commit<1>(&sh.bar[M_PAIRS]);
+                    commit_one<1>(one, &sh.bar[M_PAIRS]);
                 }
                 if (!need(A_XW, c & 1) || (c > 0 && !need(A_MADE, (c - 1) & 1))) return;
                 tc_fence_after();
                 const uint64_t db = b_mn + st * STAGE2;
 #pragma unroll
                 for (int k = 0; k < Q / 16; ++k)  // (N = 128: the products with X's two parts side by side)
-                    umma<1>(tmem + T_D, db + mn_major(k), xw_mn + mn_major(k), FMT | N128 | A_MN | B_MN, k > 0);
-                umma_commit<1>(&sh.bar[M_MADE]);
-                umma_commit<1>(&sh.bar[E_B + st]);
-                if (!FULL) umma_commit<1>(&sh.bar[E_X + st]);
+                    umma_one<1>(one, tmem + T_D, db + mn_major(k), xw_mn + mn_major(k), FMT | N128 | A_MN | B_MN, k > 0);
+                commit_one<1>(one, &sh.bar[M_MADE]);
+                commit_one<1>(one, &sh.bar[E_B + st]);
+                if (!FULL) commit_one<1>(one, &sh.bar[E_X + st]);
             };
 #pragma unroll 1
             for (int c = -1; c < nc && ok; ++c) {
@@ -384,19 +387,19 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                     for (int blk = 0; blk < nblk; ++blk)
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            umma<1>(tmem + T_Y0, dc + blk * STAGE1 + 2 * k, h_mn + mn_major(4 * blk + k), FMT | N128 | B_MN, blk > 0 || k > 0);
-                    umma_commit<1>(&sh.bar[M_CARRIED]);
-                    umma_commit<1>(&sh.bar[E_C + st]);
+                            umma_one<1>(one, tmem + T_Y0, dc + blk * STAGE1 + 2 * k, h_mn + mn_major(4 * blk + k), FMT | N128 | B_MN, blk > 0 || k > 0);
+                    commit_one<1>(one, &sh.bar[M_CARRIED]);
+                    commit_one<1>(one, &sh.bar[E_C + st]);
                     if (!need(A_P, par)) break;
                     tc_fence_after();
 #pragma unroll
                     for (int part = 0; part < 2; ++part)
 #pragma unroll
                         for (int k = 0; k < Q / 16; ++k)
-                            umma_ts(tmem + T_Y1, tmem + (part ? T_LO + k * 8 : T_S + (k / 2) * 32 + (k % 2) * 8), dx + mn_major(k),
+                            umma_ts_one(one, tmem + T_Y1, tmem + (part ? T_LO + k * 8 : T_S + (k / 2) * 32 + (k % 2) * 8), dx + mn_major(k),
                                     FMT | N64 | B_MN, part > 0 || k > 0);
-                    umma_commit<1>(&sh.bar[M_INSIDE]);
-                    umma_commit<1>(&sh.bar[E_X + st]);
+                    commit_one<1>(one, &sh.bar[M_INSIDE]);
+                    commit_one<1>(one, &sh.bar[E_X + st]);
                 }
                 if (c + 1 < nc) pairs_and_made(c + 1);
             }
