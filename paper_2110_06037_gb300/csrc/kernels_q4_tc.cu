@@ -23,6 +23,10 @@
 // bf16 parts of w, which hold q * scale exactly; of the six products the smallest
 // (2^-25 and less) is left out.  One k step then is five.  (A fourth plane is the
 // first with zeros for what is not finite: the second part of w is often 0.)
+// The tensor cores' sums are truncated, by some 1.4e-8 of them an MMA (4.6e-5 in all for
+// 8192 columns), so they run over one column block, 20 MMAs with the four of the large
+// product last; the epilogue's warps add those sums in fp32 to one that they keep in TMEM.
+// (2.2e-7 then; over two blocks 4.8e-7, and 855 us for 2048 rows, 4096 -> 8448, against 897.)
 //
 // Warps: 0 loads x and allocates TMEM, 1 issues the MMAs (of the pair's leader), 2
 // loads codes and scales, 4 to 7 drain the accumulators (two, so that a tile's
@@ -52,10 +56,13 @@ constexpr uint32_t Q4_A_BYTES = BM * BK * 2, Q4_B_BYTES = 128 * BK * 2, Q4_STAGE
 constexpr uint32_t Q4_OUT_ROW = 128 + 16;  // staged output row: 32 values, and 16 bytes against bank conflicts
 constexpr size_t Q4_SMEM = Q4_STAGES * (size_t)Q4_STAGE + Q4_CSTAGES * (size_t)Q4_CSTAGE + 4 * 32 * Q4_OUT_ROW + 1024;
 
+constexpr int Q4_F32_BN = 160;  // fp32: the widest tile (two accumulators and the sum fit TMEM)
+
 struct PromptP {
     Q4P q;
     int64_t rows, ldy;
     int32_t bn, mtiles, ntiles, steps;  // outputs a tile, tiles, k steps (five a column block for fp32)
+    int32_t run;                        // k steps summed by the tensor cores
     int32_t plane_rows;                 // fp32: rows of a plane of x
     int32_t parts;                      // scales in two parts
     int32_t vec_out;
@@ -129,7 +136,7 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                      const __grid_constant__ CUtensorMap mS, const __grid_constant__ PromptP p, X *__restrict__ y) {
     constexpr bool F32 = std::is_same<X, float>::value;
     constexpr int COMBOS = F32 ? 5 : 1;
-    constexpr uint32_t TMEM_COLS = G == 2 ? 512 : 256, ACC = TMEM_COLS / 2;
+    constexpr uint32_t TMEM_COLS = G == 2 || F32 ? 512 : 256, ACC = F32 ? Q4_F32_BN : TMEM_COLS / 2;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t full_bar[Q4_STAGES], empty_bar[Q4_STAGES], accf_bar[2], acce_bar[2];
     __shared__ __align__(8) uint64_t cfull_bar[Q4_CSTAGES], cempty_bar[Q4_CSTAGES];
@@ -199,7 +206,7 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                     if (leader) mbar_expect_tx(&full_bar[s], G * Q4_A_BYTES);
                     const uint32_t bar = G == 2 ? mapa(su32(&full_bar[s]), 0u) : su32(&full_bar[s]);
                     const int kb = F32 ? it / COMBOS : it, c = F32 ? it - kb * COMBOS : 0;
-                    const int plane = F32 ? (c == 3 ? 3 : c == 4 ? 1 : c) : 0;
+                    const int plane = F32 ? (c < 3 ? c + 1 : c == 3 ? 1 : 0) : 0;
                     tma_2d<G>(su32(smem + s * Q4_STAGE), &mX, bar, kb * BK, m0 + plane * p.plane_rows);
                     if (++s == Q4_STAGES) {
                         s = 0;
@@ -214,11 +221,11 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
             const uint32_t one = elect_one();
             const uint32_t idesc = idesc_f16<T>(BM * G, p.bn);
             const uint64_t desc0 = sdesc_sw128(su32(smem));
-            int g = 0, lt = 0, s = 0;
+            int g = 0, lt = 0, s = 0, i0 = 0;
             uint32_t par = 0;
             bool stop = false;
-            for (int t = cid; t < total && !stop; t += ncl, ++lt) {
-                const int b = lt & 1;
+            for (int t = cid; t < total && !stop; ++lt) {  // run lt: steps i0 to i1 of tile t
+                const int b = lt & 1, i1 = min(i0 + p.run, p.steps);
                 const uint32_t aph = (uint32_t)(lt >> 1) & 1u;
                 if (!__all_sync(0xffffffffu, G == 2 ? mbar_wait_cluster(&acce_bar[b], aph ^ 1u, p.wait_limit)
                                                     : mbar_wait(&acce_bar[b], aph ^ 1u, p.wait_limit))) {
@@ -230,7 +237,7 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                 }
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)b * ACC;
-                for (int it = 0; it < p.steps; ++it, ++g) {
+                for (int it = i0; it < i1; ++it, ++g) {
                     if (!__all_sync(0xffffffffu, G == 2 ? mbar_wait_cluster(&full_bar[s], par, p.wait_limit)
                                                         : mbar_wait(&full_bar[s], par, p.wait_limit))) {
                         if (lane == 0) {
@@ -243,7 +250,7 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                     tc_fence_after();
                     const uint64_t da = desc0 + (uint64_t)((s * Q4_STAGE) >> 4), db = da + (Q4_A_BYTES >> 4);
 #pragma unroll
-                    for (int k = 0; k < BK / 16; ++k) umma_one<G>(one, d, da + 2 * k, db + 2 * k, idesc, (it > 0 || k > 0) ? 1u : 0u);
+                    for (int k = 0; k < BK / 16; ++k) umma_one<G>(one, d, da + 2 * k, db + 2 * k, idesc, (it > i0 || k > 0) ? 1u : 0u);
                     commit_one<G>(one, &empty_bar[s]);
                     if (++s == Q4_STAGES) {
                         s = 0;
@@ -251,6 +258,8 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                     }
                 }
                 if (!stop) commit_one<G>(one, &accf_bar[b]);
+                i0 = i1;
+                if (i0 == p.steps) i0 = 0, t += ncl;
             }
             if (lane == 0) consumed_sh = g;
         }
@@ -258,9 +267,12 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
         const int q = warp - 4;
         uint8_t *out = stg + q * 32 * Q4_OUT_ROW;
         griddep_wait();
-        int lt = 0;
-        for (int t = cid; t < total; t += ncl, ++lt) {
+        int lt = 0, i0 = 0;
+        for (int t = cid; t < total; ++lt) {
             const int b = lt & 1;
+            const bool first = i0 == 0;
+            i0 += p.run;
+            const bool last = i0 >= p.steps;
             const int64_t r0 = (int64_t)(t / p.ntiles * G + (int)rank) * BM + q * 32;
             const int n0 = t % p.ntiles * p.bn;
             if (!mbar_wait(&accf_bar[b], (uint32_t)(lt >> 1) & 1u, p.wait_limit)) {
@@ -276,8 +288,21 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                 for (int c0 = 0; c0 < p.bn && n0 + c0 < p.q.n; c0 += 32) {
                     const int j0 = n0 + c0;
                     uint32_t v[32];
+                    const uint32_t acc = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)c0;
                     __syncwarp();
-                    tmem_ld32(tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)b * ACC + (uint32_t)c0, v);
+                    tmem_ld32(acc + (uint32_t)b * ACC, v);
+                    if constexpr (F32) {
+                        if (!first) {
+                            uint32_t sum[32];
+                            tmem_ld32(acc + 2 * ACC, sum);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) v[i] = __float_as_uint(__uint_as_float(v[i]) + __uint_as_float(sum[i]));
+                        }
+                        if (!last) {
+                            tmem_st32(acc + 2 * ACC, v);
+                            continue;
+                        }
+                    }
                     bias_sh[q][lane] = p.q.bias && j0 + lane < p.q.n ? p.q.bias[j0 + lane] : 0.0f;
                     if constexpr (std::is_same<X, __half>::value)
                         pow_sh[q][lane] = j0 + lane < p.q.n ? p.q.row_pow[j0 + lane] * 0x1p-12f : 0.0f;
@@ -320,6 +345,7 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                 if (G == 2) mbar_arrive_cluster(mapa(su32(&acce_bar[b]), 0u));
                 else mbar_arrive(&acce_bar[b]);
             }
+            if (last) i0 = 0, t += ncl;
         }
     } else if (warp == 2) {
         if (lane == 0) {  // ---------------- loader of codes and scales (not written by the kernel before)
@@ -442,7 +468,7 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                                         for (int e = 0; e < 4; ++e) {
                                             const uint32_t code = code_pair<T>(w[2 * h + e / 2], r + 2 * (e % 2));
                                             v[e] = expand<T>(code, sc[i][r][h], parts.value);
-                                            if (F32 && c >= 3) v[e] = expand_rest(code, sc[i][r][h], v[e]);
+                                            if (F32 && (c == 2 || c == 3)) v[e] = expand_rest(code, sc[i][r][h], v[e]);
                                         }
                                         *reinterpret_cast<uint4 *>(b + tile * 2048 + r * 1024 + at[h]) = make_uint4(v[0], v[1], v[2], v[3]);
                                     }
@@ -533,11 +559,11 @@ bool in_place(int dt, const void *x, int64_t ldx) {
 struct Shape4 {
     int g, bn;
 };
-Shape4 choose(int64_t rows, int n, int64_t steps) {
+Shape4 choose(int64_t rows, int n, int64_t steps, int widest) {
     Shape4 best{1, 32};
     double least = 1e300;
     for (int g = 1; g <= 2; ++g)
-        for (int bn = 32; bn <= (g == 2 ? 256 : 128); bn += 32) {
+        for (int bn = 32; bn <= std::min(widest, 128 * g); bn += 32) {
             const int64_t tiles = ((rows + 128 * g - 1) / (128 * g)) * ((n + bn - 1) / bn);
             const int64_t slots = num_sms() / g, rounds = (tiles + slots - 1) / slots;
             const double cost = (double)rounds * ((double)std::max(2 * bn, 256) * (double)steps + 1500.0);
@@ -593,7 +619,8 @@ cudaError_t prompt(const sn_q4_weights &w, int dt, int64_t rows, const X *x, int
     p.rows = rows;
     p.ldy = ldy;
     p.steps = p.q.kb * (F32 ? 5 : 1);
-    const Shape4 sh = choose(rows, w.n, p.steps);
+    const Shape4 sh = choose(rows, w.n, p.steps, F32 ? Q4_F32_BN : 256);
+    p.run = F32 ? 5 : p.steps;
     p.bn = sh.bn;
     const int64_t mtiles = (rows + 128 * sh.g - 1) / (128 * sh.g);
     p.mtiles = (int32_t)mtiles;

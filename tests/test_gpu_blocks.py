@@ -85,6 +85,20 @@ def test_dense(dt, rows, k, n, group, sdt, act):
     assert sn.dense_q4(x, w).equal(y)  # the same again, to the bit
 
 
+@pytest.mark.parametrize("rows, k, n", [(5, 8192, 96), (40, 2050, 512), (300, 8192, 96), (200, 513, 1700), (600, 3001, 2600)])
+def test_dense_fp32_does_not_lose_precision_with_length(rows, k, n):
+    """The tensor cores' own sums are truncated to some 24 bits at each of at most 40 products, half a unit
+    each on average (40 * 2^-25), and fp32 additions of those sums round at random; the sum of all of them
+    would be off by 5 k / 16 of such steps, all one way."""
+    import paper_2110_06037_gb300 as sn
+    rng = np.random.default_rng(k)
+    w, codes, scales, b = q4(rng, n, k, 64, "f16")
+    x = dev(rng.normal(size=(rows, k)))
+    pre, _ = ob.dense(host(x), codes, scales, k, 64, b)
+    d = host(sn.dense_q4(x, w)) - pre
+    assert np.sqrt((d * d).sum() / (pre * pre).sum()) < 40 * 2.0 ** -25
+
+
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("rows", [1, 7, 40, 200])
 @pytest.mark.parametrize("off", [0, 1, 8])
