@@ -9,11 +9,12 @@
 //   pairs   C B^T       128 x 128, K = N       both as they lie in xbc
 //   carried C S^T       128 x P,   K = N       S in two bf16 parts
 //   inside  P X         128 x P,   K = 128     P (the pairs, weighted) in two parts, from TMEM
-//   made    B^T X'      N x P,     K = 128     X' = weighted X in two parts
-// x, B and C are bf16, exact operands; what is computed goes in as two bf16 parts
-// (2^-18 of it is lost, as much as a few fp32 roundings).  The state stays in
-// registers in fp32: each chunk's product is added by an fp32 multiply-add, since the
-// tensor core's own sums do not round to nearest.
+//   made    B^T X'      N x P,     K = 128     X' = weighted X in three parts
+// x, B and C are bf16, exact operands; what is computed goes in as bf16 parts: two for
+// the outputs, which are bf16 (2^-18 is lost), three for the state, which goes on in
+// fp32 (off by 9e-8 of itself; with two parts 2.4e-6, and 9 us less for 8192 tokens).
+// It stays in registers: each chunk's product is added by an fp32 multiply-add, since
+// the tensor core's own sums do not round to nearest.
 //
 // Work: a block of one SM takes one head, 64 of its channels and a segment of a
 // sequence's chunks.  With few heads the sequence is cut into segments: a first pass
@@ -25,7 +26,7 @@
 // only the state's one multiply-add a chunk runs from chunk to chunk: in one order, two
 // blocks an SM, a chunk took a block 17.9 thousand cycles of waiting for one step after
 // the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128), the MMAs 32 of
-// them.  So: 152 us.
+// them.  So: 161 us.
 // Non-finite x: 0 * NaN would reach tokens before it, so such an x goes into the
 // product as 0 and makes its channel NaN from its token on; into the state it goes as
 // it is.  Waits are bounded.
@@ -214,7 +215,8 @@ __device__ __forceinline__ Parts2 parts2(float a, float b) {
 }
 // ------------------------------------------------------------------- scan
 constexpr uint32_t TILE64 = Q * 128;  // 128 rows of 64 bf16 values
-// B, C (two tiles each) and x twice; X' and the state's parts (two tiles each) once
+// C (two tiles) and x twice, X's and the state's first two parts once; B's two tiles, the
+// third part of X' and a tile of zeros: B once beside C, twice in the place of C
 constexpr uint32_t OFF_B = 0, OFF_C = 4 * TILE64, OFF_X = 8 * TILE64, OFF_XW = 10 * TILE64, OFF_H = 12 * TILE64, OFF_SHARED = 14 * TILE64;
 constexpr size_t SCAN_SMEM = OFF_SHARED + 2048;
 static_assert(SCAN_SMEM <= 227 * 1024, "shared memory of a block");
@@ -237,21 +239,23 @@ static_assert(sizeof(Shared) <= 2048, "behind the tiles");
 // large and small parts' products apart; inside; P's small parts
 constexpr uint32_t T_S = 0, T_Y0 = 128, T_D = 256, T_Y1 = 384, T_LO = 448;
 
-// Warps: 0 copies, 1 issues the MMAs, 2 to 9 make P (FULL) or X' (two threads a row),
-// 10 to 13 carry the state, 14 to 17 (FULL) make X' (a thread a row) and the outputs.
-constexpr int FULL_THREADS = 18 * 32, STATE_THREADS = 14 * 32;
+// Warps: 0 copies, 1 issues the MMAs, 2 to 9 make P (FULL) and the next chunk's X' (two
+// threads a row), 10 to 17 carry the state (half of the columns each four), 18 to 21
+// (FULL) take the outputs.
+constexpr int FULL_THREADS = 22 * 32, STATE_THREADS = 18 * 32;
 
 // FULL: the outputs; otherwise a segment's state from nothing (segment 0: from s_in).
-// The MMAs' order, chunk i: carried(i), inside(i), pairs(i + 1), made(i + 1).  Every
-// role then has most of a chunk's time for its part: P(i + 1) between pairs(i + 1) and
-// inside(i + 1), the state between made(i) and carried(i + 1), copies more than that.
+// The MMAs' order, chunk i: inside(i), pairs(i + 1), carried(i), made(i + 1).  The two
+// that the next P waits for come first; X'(i + 1) is made meanwhile, and the state goes
+// from made(i) to carried(i + 1) beside all of them.
 template <bool FULL>
 __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
     ssm_scan_tc_kernel(const __grid_constant__ CUtensorMap mX, const __grid_constant__ CUtensorMap mB,
                        const __grid_constant__ CUtensorMap mC, const __grid_constant__ TcP p, __nv_bfloat16 *__restrict__ y) {
     extern __shared__ __align__(1024) uint8_t smem[];
     Shared &sh = *reinterpret_cast<Shared *>(smem + OFF_SHARED);
-    constexpr int XWARPS = FULL ? 4 : 8;  // warps that make X'
+    constexpr int B_STAGES = FULL ? 1 : 2;
+    constexpr uint32_t OFF_XW3 = FULL ? 2 * TILE64 : OFF_C;  // the third part of X', and zeros
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int pb = blockIdx.x % p.pblocks, head = blockIdx.x / p.pblocks, seg = blockIdx.y, b = blockIdx.z;
     if (su32(smem) & 1023) {  // (the swizzled tiles need it; uniform over the block)
@@ -261,13 +265,16 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
     if (warp == 0) {
         tmem_alloc<1>(&sh.tmem, 512);
     } else if (warp == 1) {
-        if (lane < BARS) mbar_init(&sh.bar[lane], lane < A_XW ? 1 : lane == A_XW ? XWARPS : lane == A_P ? 8 : 4);
+        if (lane < BARS) mbar_init(&sh.bar[lane], lane < A_XW ? 1 : lane == A_OUT ? 4 : 8);
         if (lane == 31) sh.abort = sh.any_bad[0] = sh.any_bad[1] = 0;
         fence_mbar_init();
     } else if (warp >= 2 && warp < 6) {
         (&sh.bad[0][0])[threadIdx.x - 64] = Q;
     }
     static_assert(BARS < 31, "one lane a barrier");
+    for (uint32_t e = threadIdx.x; e < TILE64 / 16; e += blockDim.x)
+        reinterpret_cast<uint4 *>(smem + OFF_XW3 + TILE64)[e] = make_uint4(0u, 0u, 0u, 0u);
+    fence_proxy_async_smem();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
@@ -309,23 +316,23 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                 for (int i = 0; i < boxes; ++i)
                     tma_3d<1>(base + off + i * TILE64, m, su32(&sh.bar[bar]), x0 + 64 * i, g, (int)(s.first + (int64_t)(chunks.x + c) * Q));
             };
-            auto freed = [&](int i, int c) {  // the chunk before in this stage has been read
-                if (ok && c >= 2 && !mbar_wait(&sh.bar[i], (uint32_t)((c >> 1) - 1) & 1u)) {
+            auto freed = [&](int i, int n) {  // the n-th chunk in a stage waits until the one before has been read
+                if (ok && n > 0 && !mbar_wait(&sh.bar[i], (uint32_t)(n - 1) & 1u)) {
                     gave_up(ERR_TMA_WAIT);
                     ok = false;
                 }
                 return ok;
             };
             for (int c = 0; c < nc && ok; ++c) {
-                const int st = c & 1;
-                if (!freed(E_B + st, c)) break;
-                load(&mB, F_B + st, OFF_B + st * 2 * TILE64, c, 2, 0, grp);
+                const int st = c & 1, bs = c % B_STAGES;
                 if (FULL) {
-                    if (!freed(E_C + st, c)) break;
+                    if (!freed(E_C + st, c >> 1)) break;
                     load(&mC, F_C + st, OFF_C + st * 2 * TILE64, c, 2, 0, grp);
                 }
-                if (!freed(E_X + st, c)) break;
+                if (!freed(E_X + st, c >> 1)) break;
                 load(&mX, F_X + st, OFF_X + st * TILE64, c, 1, p0, head);
+                if (!freed(E_B + bs, c / B_STAGES)) break;
+                load(&mB, F_B + bs, OFF_B + bs * 2 * TILE64, c, 2, 0, grp);
             }
         }
         __syncwarp();
@@ -347,130 +354,210 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             // and forming a descriptor for each took it 150 cycles, an MMA takes the tensor core 64.
             const uint64_t b_k = sdesc_sw128(base + OFF_B), c_k = sdesc_sw128(base + OFF_C);
             const uint64_t b_mn = sdesc_mn(base + OFF_B, TILE64), x_mn = sdesc_mn(base + OFF_X, TILE64);
-            const uint64_t xw_mn = sdesc_mn(base + OFF_XW, TILE64), h_mn = sdesc_mn(base + OFF_H, TILE64);
+            const uint64_t xw_mn = sdesc_mn(base + OFF_XW, TILE64), xw3_mn = sdesc_mn(base + OFF_XW3, TILE64), h_mn = sdesc_mn(base + OFF_H, TILE64);
             constexpr uint64_t STAGE2 = 2 * TILE64 >> 4, STAGE1 = TILE64 >> 4;
             auto mn_major = [](int k) { return (uint64_t)(k * (2048 >> 4)); };
-            auto pairs_and_made = [&](int c) {
+            auto pairs = [&](int c) {
                 const uint32_t st = c & 1, half = (uint32_t)(c >> 1) & 1u;
-                if (!need(F_B + st, half)) return;
-                if (FULL) {
-                    // (the pairs take the place of the chunk before's P: only MMAs on one accumulator keep their order by themselves)
-                    if (!need(F_C + st, half) || (c > 0 && !need(M_INSIDE, (c - 1) & 1))) return;
-                    tc_fence_after();
-                    const uint64_t dc = c_k + st * STAGE2, db = b_k + st * STAGE2;
-#pragma unroll 1
-                    for (int blk = 0; blk < nblk; ++blk) {
-                        const uint64_t o = blk * STAGE1;
-#pragma unroll
-                        for (int k = 0; k < 4; ++k) umma_one<1>(one, tmem + T_S, dc + o + 2 * k, db + o + 2 * k, FMT | N128, blk > 0 || k > 0);
-                    }
-                    commit_one<1>(one, &sh.bar[M_PAIRS]);
-                }
-                if (!need(A_XW, c & 1) || (c > 0 && !need(A_MADE, (c - 1) & 1))) return;
+                // (they take the place of the chunk before's P: only MMAs on one accumulator keep their order by themselves)
+                if (!need(F_B, c & 1) || !need(F_C + st, half) || (c > 0 && !need(M_INSIDE, (c - 1) & 1))) return;
                 tc_fence_after();
-                const uint64_t db = b_mn + st * STAGE2;
+                const uint64_t dc = c_k + st * STAGE2;
+#pragma unroll 1
+                for (int blk = 0; blk < nblk; ++blk) {
+                    const uint64_t o = blk * STAGE1;
 #pragma unroll
-                for (int k = 0; k < Q / 16; ++k)  // (N = 128: the products with X's two parts side by side)
-                    umma_one<1>(one, tmem + T_D, db + mn_major(k), xw_mn + mn_major(k), FMT | N128 | A_MN | B_MN, k > 0);
+                    for (int k = 0; k < 4; ++k) umma_one<1>(one, tmem + T_S, dc + o + 2 * k, b_k + o + 2 * k, FMT | N128, blk > 0 || k > 0);
+                }
+                commit_one<1>(one, &sh.bar[M_PAIRS]);
+            };
+            auto inside = [&](int c) {
+                const uint32_t st = c & 1, par = c & 1;
+                if (!need(A_P, par) || (c > 0 && !need(A_OUT, par ^ 1u))) return;
+                tc_fence_after();
+                const uint64_t dx = x_mn + st * STAGE1;
+#pragma unroll
+                for (int part = 0; part < 2; ++part)
+#pragma unroll
+                    for (int k = 0; k < Q / 16; ++k)
+                        umma_ts_one(one, tmem + T_Y1, tmem + (part ? T_LO + k * 8 : T_S + (k / 2) * 32 + (k % 2) * 8), dx + mn_major(k),
+                                    FMT | N64 | B_MN, part > 0 || k > 0);
+                commit_one<1>(one, &sh.bar[M_INSIDE]);
+                commit_one<1>(one, &sh.bar[E_X + st]);
+            };
+            auto carried = [&](int c) {
+                const uint32_t st = c & 1;
+                if (!need(A_STATE, c & 1)) return;
+                tc_fence_after();
+                const uint64_t dc = c_k + st * STAGE2;
+#pragma unroll 1
+                for (int blk = 0; blk < nblk; ++blk)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        umma_one<1>(one, tmem + T_Y0, dc + blk * STAGE1 + 2 * k, h_mn + mn_major(4 * blk + k), FMT | N128 | B_MN, blk > 0 || k > 0);
+                commit_one<1>(one, &sh.bar[M_CARRIED]);
+                commit_one<1>(one, &sh.bar[E_C + st]);
+            };
+            auto made = [&](int c) {
+                const uint32_t bs = c % B_STAGES;
+                if (!need(F_B + bs, (uint32_t)(c / B_STAGES) & 1u) || !need(A_XW, c & 1) || (c > 0 && !need(A_MADE, (c - 1) & 1))) return;
+                tc_fence_after();
+                const uint64_t db = b_mn + bs * STAGE2;
+                // (N = 128: the products with two parts of X' side by side.  The third part, beside
+                // zeros, comes first, while the sums are small: they are truncated at every MMA)
+#pragma unroll
+                for (int k = 0; k < Q / 16; ++k)
+                    umma_one<1>(one, tmem + T_D, db + mn_major(k), xw3_mn + mn_major(k), FMT | N128 | A_MN | B_MN, k > 0);
+#pragma unroll
+                for (int k = 0; k < Q / 16; ++k)
+                    umma_one<1>(one, tmem + T_D, db + mn_major(k), xw_mn + mn_major(k), FMT | N128 | A_MN | B_MN, 1);
                 commit_one<1>(one, &sh.bar[M_MADE]);
-                commit_one<1>(one, &sh.bar[E_B + st]);
-                if (!FULL) commit_one<1>(one, &sh.bar[E_X + st]);
+                commit_one<1>(one, &sh.bar[E_B + bs]);
+                if (!FULL) commit_one<1>(one, &sh.bar[E_X + (c & 1)]);
             };
 #pragma unroll 1
             for (int c = -1; c < nc && ok; ++c) {
-                if (FULL && c >= 0) {
-                    const uint32_t st = c & 1, par = c & 1;
-                    if (!need(A_STATE, par) || (c > 0 && !need(A_OUT, par ^ 1u))) break;
-                    tc_fence_after();
-                    const uint64_t dc = c_k + st * STAGE2, dx = x_mn + st * STAGE1;
-#pragma unroll 1
-                    for (int blk = 0; blk < nblk; ++blk)
-#pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            umma_one<1>(one, tmem + T_Y0, dc + blk * STAGE1 + 2 * k, h_mn + mn_major(4 * blk + k), FMT | N128 | B_MN, blk > 0 || k > 0);
-                    commit_one<1>(one, &sh.bar[M_CARRIED]);
-                    commit_one<1>(one, &sh.bar[E_C + st]);
-                    if (!need(A_P, par)) break;
-                    tc_fence_after();
-#pragma unroll
-                    for (int part = 0; part < 2; ++part)
-#pragma unroll
-                        for (int k = 0; k < Q / 16; ++k)
-                            umma_ts_one(one, tmem + T_Y1, tmem + (part ? T_LO + k * 8 : T_S + (k / 2) * 32 + (k % 2) * 8), dx + mn_major(k),
-                                    FMT | N64 | B_MN, part > 0 || k > 0);
-                    commit_one<1>(one, &sh.bar[M_INSIDE]);
-                    commit_one<1>(one, &sh.bar[E_X + st]);
-                }
-                if (c + 1 < nc) pairs_and_made(c + 1);
+                if (FULL && c >= 0) inside(c);
+                if (FULL && c + 1 < nc && ok) pairs(c + 1);
+                if (FULL && c >= 0 && ok) carried(c);
+                if (c + 1 < nc && ok) made(c + 1);
             }
         }
         __syncwarp();
-    } else if (FULL && warp < 10) {
-        // ---------------- P from the pairs: 32 x 32 blocks, this warp's two of its rows' four; D,
-        // the factor of x itself, joins the diagonal
-        const int quarter = warp % 4, half = (warp - 2) / 4, t = threadIdx.x - 64;  // t: 0 to 255
-        const float skip = q.d ? q.d[head] : 0.0f;
-        float at_next = 0.0f, as_next = 0.0f;  // of the next chunk: A of this row, A_s - log2 d_s of token t (t < 128)
-        auto fetch = [&](int c) {
-            if (c >= nc) return;
-            at_next = __ldg(table(c) + row);
-            if (t < Q) as_next = __ldg(table(c) + Q + t);
-        };
-        fetch(0);
-        for (int c = 0; c < nc; ++c) {
-            const uint32_t par = c & 1;
-            const float At = at_next;
-            if (t < Q) sh.as[par][t] = as_next;  // (its last readers, two chunks ago, have passed the barrier since)
-            fetch(c + 1);
-            if (bar_red_or(1, 256, !ok)) break;  // (the group leaves together)
-            if (!must(M_PAIRS, par)) continue;
-            tc_fence_after();
-            // 16 columns at a time in a rolled loop (all 64 unrolled, as every role's loop was,
-            // the warps waited for instructions: some 14 cycles for each)
-#pragma unroll 1
-            for (int i = 0; i < 4; ++i) {
-                const int blk = 2 * (i / 2) + half, c0 = 32 * blk + 16 * (i % 2);
-                uint32_t hi[8], lo[8];
-                __syncwarp();
-                if (blk <= quarter) {
-                    float f[16];
-                    tmem_ld16(tmem + lanes + T_S + c0, f);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float4 As = *reinterpret_cast<const float4 *>(&sh.as[par][c0 + 4 * j]);
-                        f[4 * j] *= ex2(At - As.x), f[4 * j + 1] *= ex2(At - As.y);
-                        f[4 * j + 2] *= ex2(At - As.z), f[4 * j + 3] *= ex2(At - As.w);
-                    }
-                    if (blk == quarter) {
-                        const int own = row - c0;  // the diagonal's place among these columns
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) f[j] = j < own ? f[j] : j == own ? f[j] + skip : 0.0f;
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const Parts2 v = parts2(f[2 * j], f[2 * j + 1]);
-                        hi[j] = v.hi, lo[j] = v.lo;
-                    }
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) hi[j] = lo[j] = 0u;
-                }
-                __syncwarp();
-                tmem_st8(tmem + lanes + T_S + 32 * blk + 8 * (i % 2), hi);  // (these columns' pairs have been read)
-                tmem_st8(tmem + lanes + T_LO + c0 / 2, lo);
+    } else if (warp < 10) {
+        // ---------------- X', two threads a row
+        const int tid = threadIdx.x - 64, t = tid / 2, j0 = 4 * (tid & 1);
+        float w_next = nc > 0 ? __ldg(table(0) + 2 * Q + t) : 0.0f;
+        auto weigh = [&](int c) {
+            const int st = c & 1, bs = c % B_STAGES, valid = min(Q, s.len - (chunks.x + c) * Q);  // tokens there are
+            const float w = w_next;
+            if (c + 1 < nc) w_next = __ldg(table(c + 1) + 2 * Q + t);
+            must(F_X + st, (uint32_t)(c >> 1) & 1u);
+            if (c > 0) must(M_MADE, (c - 1) & 1);  // the X' before has been read
+            if (valid < Q) {
+                must(F_B + bs, (uint32_t)(c / B_STAGES) & 1u);
+                if (FULL) must(M_PAIRS, c & 1);
             }
-            tmem_wait_st();
-            tc_fence_before();
-            arrive(A_P);
-        }
-    } else if (warp >= 10 && warp < 14) {
-        // ---------------- the state, [p][n] with lane n, in fp32
-        float h[PB];
-        const int64_t srow = s.slot >= 0 ? (((int64_t)s.slot * q.H + head) * q.P + p0) * q.N + row : -1;
-        auto live = [&](int i) { return i < np && row < q.N; };
-        auto part = [&](int j) { return p.part + part0 + (int64_t)j * PB * q.N + row; };  // before segment 0, after fine segment j - 1
+            if (!ok) return;
+            uint8_t *xr = smem + OFF_X + st * TILE64 + t * 128, *wr = smem + OFF_XW + t * 128, *w3 = smem + OFF_XW3 + t * 128;
+#pragma unroll 2
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t at = (uint32_t)((j0 + i) ^ (t & 7)) << 4;
+                uint4 xv = *reinterpret_cast<const uint4 *>(xr + at);
+                if (t >= valid) {  // rows of another sequence: nothing of them may count
+                    xv = make_uint4(0u, 0u, 0u, 0u);
+                    *reinterpret_cast<uint4 *>(xr + at) = xv;
+                    uint8_t *br = smem + OFF_B + bs * 2 * TILE64 + t * 128 + at;
+                    *reinterpret_cast<uint4 *>(br) = xv;
+                    *reinterpret_cast<uint4 *>(br + TILE64) = xv;
+                }
+                const uint32_t u[4] = {xv.x, xv.y, xv.z, xv.w};
+                uint32_t hi[4], lo[4], lo2[4], odd = 0u;  // odd: a value's exponent is all ones
 #pragma unroll
-        for (int i = 0; i < PB; ++i) {
+                for (int e = 0; e < 4; ++e) {
+                    const float2 f = unpack2<__nv_bfloat16>(u[e]);
+                    odd |= ((u[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                    const float2 m = make_float2(f.x * w, f.y * w);
+                    const Parts2 v = parts2(m.x, m.y);
+                    const float2 h = unpack2<__nv_bfloat16>(v.hi), l = unpack2<__nv_bfloat16>(v.lo);
+                    hi[e] = v.hi, lo[e] = v.lo, lo2[e] = pack2<__nv_bfloat16>(m.x - h.x - l.x, m.y - h.y - l.y);
+                }
+                *reinterpret_cast<uint4 *>(wr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                *reinterpret_cast<uint4 *>(wr + TILE64 + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                *reinterpret_cast<uint4 *>(w3 + at) = make_uint4(lo2[0], lo2[1], lo2[2], lo2[3]);
+                if (odd) {
+#pragma unroll 1
+                    for (int e = 0; e < 8; ++e) {
+                        uint16_t *xe = reinterpret_cast<uint16_t *>(xr + at) + e;
+                        if ((*xe & 0x7f80u) != 0x7f80u) continue;
+                        reinterpret_cast<uint16_t *>(wr + TILE64 + at)[e] = reinterpret_cast<uint16_t *>(w3 + at)[e] = 0;  // into the state as it is
+                        if (FULL) {  // out of the product inside the chunk; its channel is NaN from here on
+                            *xe = 0;
+                            atomicMin(&sh.bad[st][8 * (j0 + i) + e], t);
+                            sh.any_bad[st] = 1;
+                        }
+                    }
+                }
+            }
+            fence_proxy_async_smem();
+            arrive(A_XW);
+        };
+        if constexpr (!FULL) {
+            for (int c = 0; c < nc && ok; ++c) weigh(c);
+        } else {
+            // ---------------- P from the pairs: 32 x 32 blocks, this warp's two of its rows' four; D,
+            // the factor of x itself, joins the diagonal.  After it the next chunk's X'
+            const int quarter = warp % 4, half = (warp - 2) / 4;
+            const float skip = q.d ? q.d[head] : 0.0f;
+            float at_next = 0.0f, as_next = 0.0f;  // of the next chunk: A of this row, A_s - log2 d_s of token tid (tid < 128)
+            auto fetch = [&](int c) {
+                if (c >= nc) return;
+                at_next = __ldg(table(c) + row);
+                if (tid < Q) as_next = __ldg(table(c) + Q + tid);
+            };
+            fetch(0);
+#pragma unroll 1
+            for (int c = -1; c < nc; ++c) {
+                if (c >= 0) {
+                    const uint32_t par = c & 1;
+                    const float At = at_next;
+                    if (tid < Q) sh.as[par][tid] = as_next;  // (its last readers, two chunks ago, have passed the barrier since)
+                    fetch(c + 1);
+                    if (bar_red_or(1, 256, !ok)) break;  // (the group leaves together)
+                    if (!must(M_PAIRS, par)) continue;
+                    tc_fence_after();
+                    // 16 columns at a time in a rolled loop (all 64 unrolled, as every role's loop was,
+                    // the warps waited for instructions: some 14 cycles for each)
+#pragma unroll 1
+                    for (int i = 0; i < 4; ++i) {
+                        const int blk = 2 * (i / 2) + half, c0 = 32 * blk + 16 * (i % 2);
+                        uint32_t hi[8], lo[8];
+                        __syncwarp();
+                        if (blk <= quarter) {
+                            float f[16];
+                            tmem_ld16(tmem + lanes + T_S + c0, f);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float4 As = *reinterpret_cast<const float4 *>(&sh.as[par][c0 + 4 * j]);
+                                f[4 * j] *= ex2(At - As.x), f[4 * j + 1] *= ex2(At - As.y);
+                                f[4 * j + 2] *= ex2(At - As.z), f[4 * j + 3] *= ex2(At - As.w);
+                            }
+                            if (blk == quarter) {
+                                const int own = row - c0;  // the diagonal's place among these columns
+#pragma unroll
+                                for (int j = 0; j < 16; ++j) f[j] = j < own ? f[j] : j == own ? f[j] + skip : 0.0f;
+                            }
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const Parts2 v = parts2(f[2 * j], f[2 * j + 1]);
+                                hi[j] = v.hi, lo[j] = v.lo;
+                            }
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) hi[j] = lo[j] = 0u;
+                        }
+                        __syncwarp();
+                        tmem_st8(tmem + lanes + T_S + 32 * blk + 8 * (i % 2), hi);  // (these columns' pairs have been read)
+                        tmem_st8(tmem + lanes + T_LO + c0 / 2, lo);
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    if (c > 0) must(A_OUT, par ^ 1u);  // (what the next X' says of values that are not finite takes the place of what the outputs have read)
+                    arrive(A_P);
+                }
+                if (c + 1 < nc && ok) weigh(c + 1);
+            }
+        }
+    } else if (warp < 18) {
+        // ---------------- the state, [p][n] with lane n, in fp32: columns c0 to c0 + 31
+        constexpr int HC = PB / 2;
+        float h[HC];
+        const int c0 = (warp - 10) / 4 * HC;
+        const int64_t srow = s.slot >= 0 ? (((int64_t)s.slot * q.H + head) * q.P + p0 + c0) * q.N + row : -1;
+        auto live = [&](int i) { return c0 + i < np && row < q.N; };
+        auto part = [&](int j) { return p.part + part0 + ((int64_t)j * PB + c0) * q.N + row; };  // before segment 0, after fine segment j - 1
+#pragma unroll
+        for (int i = 0; i < HC; ++i) {
             h[i] = 0.0f;
             if (!live(i)) continue;
             if (FULL && p.segs > 1) h[i] = part(seg > 0 ? 1 : 0)[(int64_t)i * q.N];
@@ -483,18 +570,18 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                 for (int c = ch.x; c < ch.y; ++c) sum += p.total[chunk_at(s, b, c) * q.H + head];
                 const float e = exp2f(sum);
 #pragma unroll
-                for (int i = 0; i < PB; ++i)
+                for (int i = 0; i < HC; ++i)
                     if (live(i)) h[i] = fmaf(h[i], e, part(j + 1)[(int64_t)i * q.N]);
             }
         } else if (seg == 0) {  // the second pass may store over s_in: it reads this copy
 #pragma unroll
-            for (int i = 0; i < PB; ++i)
+            for (int i = 0; i < HC; ++i)
                 if (live(i)) part(0)[(int64_t)i * q.N] = h[i];
         }
         auto put_state = [&]() {  // its two bf16 parts as an operand: rows n, 64 p
             uint8_t *hr = smem + OFF_H + row * 128;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < HC / 8; ++i) {
                 uint32_t hi[4], lo[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -502,7 +589,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                     const Parts2 v = parts2(h[8 * i + 2 * e], h[8 * i + 2 * e + 1]);
                     hi[e] = v.hi, lo[e] = v.lo;
                 }
-                const uint32_t at = (uint32_t)(i ^ (row & 7)) << 4;
+                const uint32_t at = (uint32_t)((c0 / 8 + i) ^ (row & 7)) << 4;
                 *reinterpret_cast<uint4 *>(hr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                 *reinterpret_cast<uint4 *>(hr + TILE64 + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
             }
@@ -521,10 +608,10 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             if (!must(M_MADE, c & 1)) break;
             tc_fence_after();
 #pragma unroll
-            for (int i = 0; i < PB; i += 16) {
+            for (int i = 0; i < HC; i += 16) {
                 uint32_t u[16], v[16];
                 __syncwarp();
-                tmem_ld16x2(tmem + lanes + T_D + i, u, tmem + lanes + T_D + PB + i, v);
+                tmem_ld16x2(tmem + lanes + T_D + c0 + i, u, tmem + lanes + T_D + PB + c0 + i, v);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) h[i + j] = fmaf(h[i + j], e, __uint_as_float(u[j]) + __uint_as_float(v[j]));
             }
@@ -534,113 +621,54 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
         float *out = FULL ? (seg == p.segs - 1 && q.s_out && srow >= 0 ? q.s_out + srow : nullptr) : part(seg + 1);
         if (ok && out) {
 #pragma unroll
-            for (int i = 0; i < PB; ++i)
+            for (int i = 0; i < HC; ++i)
                 if (live(i)) out[(int64_t)i * q.N] = h[i];
         }
     } else {
-        // ---------------- X' (and, FULL, the outputs)
-        constexpr int PIECES = FULL ? 8 : 4;  // 16-byte pieces of a row a thread takes
-        const int t0 = threadIdx.x - (FULL ? 14 * 32 : 64), t = FULL ? t0 : t0 / 2, j0 = FULL ? 0 : 4 * (t0 & 1);
-        float w_next = nc > 0 ? __ldg(table(0) + 2 * Q + t) : 0.0f, at_next = 0.0f;
-        auto weigh = [&](int c) {
-            const int st = c & 1, valid = min(Q, s.len - (chunks.x + c) * Q);  // tokens there are
-            const float w = w_next;
-            if (c + 1 < nc) w_next = __ldg(table(c + 1) + 2 * Q + t);
-            must(F_X + st, (uint32_t)(c >> 1) & 1u);
-            if (c > 0) must(M_MADE, (c - 1) & 1);  // the X' before has been read
-            if (valid < Q) {
-                must(F_B + st, (uint32_t)(c >> 1) & 1u);
-                if (FULL) must(M_PAIRS, c & 1);
-            }
-            if (!ok) return;
-            uint8_t *xr = smem + OFF_X + st * TILE64 + t * 128, *wr = smem + OFF_XW + t * 128;
-#pragma unroll 2
-            for (int i = 0; i < PIECES; ++i) {
-                const uint32_t at = (uint32_t)((j0 + i) ^ (t & 7)) << 4;
-                uint4 xv = *reinterpret_cast<const uint4 *>(xr + at);
-                if (t >= valid) {  // rows of another sequence: nothing of them may count
-                    xv = make_uint4(0u, 0u, 0u, 0u);
-                    *reinterpret_cast<uint4 *>(xr + at) = xv;
-                    uint8_t *br = smem + OFF_B + st * 2 * TILE64 + t * 128 + at;
-                    *reinterpret_cast<uint4 *>(br) = xv;
-                    *reinterpret_cast<uint4 *>(br + TILE64) = xv;
-                }
-                const uint32_t u[4] = {xv.x, xv.y, xv.z, xv.w};
-                uint32_t hi[4], lo[4], odd = 0u;  // odd: a value's exponent is all ones
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const float2 f = unpack2<__nv_bfloat16>(u[e]);
-                    odd |= ((u[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-                    const Parts2 v = parts2(f.x * w, f.y * w);
-                    hi[e] = v.hi, lo[e] = v.lo;
-                }
-                *reinterpret_cast<uint4 *>(wr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                *reinterpret_cast<uint4 *>(wr + TILE64 + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
-                if (odd) {
+        // ---------------- the outputs
+        const int t = threadIdx.x - 18 * 32;
+        float at_next = nc > 0 ? __ldg(table(0) + row) : 0.0f;
 #pragma unroll 1
-                    for (int e = 0; e < 8; ++e) {
-                        uint16_t *xe = reinterpret_cast<uint16_t *>(xr + at) + e;
-                        if ((*xe & 0x7f80u) != 0x7f80u) continue;
-                        reinterpret_cast<uint16_t *>(wr + TILE64 + at)[e] = 0;  // into the state as it is
-                        if (FULL) {  // out of the product inside the chunk; its channel is NaN from here on
-                            *xe = 0;
-                            atomicMin(&sh.bad[st][8 * (j0 + i) + e], t);
-                            sh.any_bad[st] = 1;
+        for (int c = 0; c < nc; ++c) {
+            const float et = ex2(at_next);
+            if (c + 1 < nc) at_next = __ldg(table(c + 1) + row);
+            const int st = c & 1, valid = min(Q, s.len - (chunks.x + c) * Q);
+            must(M_INSIDE, c & 1);
+            must(M_CARRIED, c & 1);
+            if (bar_red_or(2, 128, !ok)) break;  // (the group leaves together)
+            tc_fence_after();
+            const bool bad = *reinterpret_cast<volatile int *>(&sh.any_bad[st]);
+            __nv_bfloat16 *yr = y + (s.first + (int64_t)(chunks.x + c) * Q + row) * q.ldy + (int64_t)head * q.P + p0;
+#pragma unroll 1
+            for (int i = 0; i < PB; i += 16) {
+                uint32_t u[16], v[16], in[16];
+                __syncwarp();
+                tmem_ld16x3(tmem + lanes + T_Y0 + i, u, tmem + lanes + T_Y0 + PB + i, v, tmem + lanes + T_Y1 + i, in);
+#pragma unroll
+                for (int j = 0; j < 16; j += 8) {
+                    uint32_t o[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        float f[2];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            const int n = j + 2 * e + k;
+                            f[k] = fmaf(__uint_as_float(u[n]) + __uint_as_float(v[n]), et, __uint_as_float(in[n]));
+                            if (bad && row >= sh.bad[st][i + n]) f[k] = NAN;
                         }
+                        o[e] = pack2<__nv_bfloat16>(f[0], f[1]);
                     }
+                    if (row < valid && i + j < np) *reinterpret_cast<uint4 *>(yr + i + j) = make_uint4(o[0], o[1], o[2], o[3]);
                 }
             }
-            fence_proxy_async_smem();
-            arrive(A_XW);
-        };
-        if constexpr (!FULL) {
-            for (int c = 0; c < nc && ok; ++c) weigh(c);
-        } else {
-#pragma unroll 1
-            for (int c = -1; c < nc; ++c) {
-                const float et = ex2(at_next);  // (of chunk c)
-                if (c + 1 < nc) {
-                    at_next = __ldg(table(c + 1) + row);
-                    weigh(c + 1);
-                }
-                if (c < 0) continue;
-                const int st = c & 1, valid = min(Q, s.len - (chunks.x + c) * Q);
-                if (bar_red_or(2, 128, !ok)) break;  // (the group leaves together; and bad[st] is complete)
-                if (!must(M_INSIDE, c & 1)) continue;
-                tc_fence_after();
-                const bool bad = *reinterpret_cast<volatile int *>(&sh.any_bad[st]);
-                __nv_bfloat16 *yr = y + (s.first + (int64_t)(chunks.x + c) * Q + row) * q.ldy + (int64_t)head * q.P + p0;
-#pragma unroll 1
-                for (int i = 0; i < PB; i += 16) {
-                    uint32_t u[16], v[16], in[16];
-                    __syncwarp();
-                    tmem_ld16x3(tmem + lanes + T_Y0 + i, u, tmem + lanes + T_Y0 + PB + i, v, tmem + lanes + T_Y1 + i, in);
-#pragma unroll
-                    for (int j = 0; j < 16; j += 8) {
-                        uint32_t o[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            float f[2];
-#pragma unroll
-                            for (int k = 0; k < 2; ++k) {
-                                const int n = j + 2 * e + k;
-                                f[k] = fmaf(__uint_as_float(u[n]) + __uint_as_float(v[n]), et, __uint_as_float(in[n]));
-                                if (bad && row >= sh.bad[st][i + n]) f[k] = NAN;
-                            }
-                            o[e] = pack2<__nv_bfloat16>(f[0], f[1]);
-                        }
-                        if (row < valid && i + j < np) *reinterpret_cast<uint4 *>(yr + i + j) = make_uint4(o[0], o[1], o[2], o[3]);
-                    }
-                }
-                tc_fence_before();
-                arrive(A_OUT);
-                if (bad) {  // (the same in the group's every warp: set before the barrier above)
-                    asm volatile("bar.sync 3, 128;" ::: "memory");
-                    if (t < PB) sh.bad[st][t] = Q;
-                    if (t == 0) sh.any_bad[st] = 0;
-                    asm volatile("bar.sync 3, 128;" ::: "memory");
-                }
+            if (bad) {  // (the same in the group's every warp)
+                asm volatile("bar.sync 3, 128;" ::: "memory");
+                if (t < PB) sh.bad[st][t] = Q;
+                if (t == 0) sh.any_bad[st] = 0;
+                asm volatile("bar.sync 3, 128;" ::: "memory");
             }
+            tc_fence_before();
+            arrive(A_OUT);
         }
     }
     tc_fence_before();

@@ -385,6 +385,26 @@ def scan_bound(mag, n):
     return (64 + 8 * n) * E32 * mag
 
 
+@pytest.mark.parametrize("lens", [[2000], [100, 300, 900]])
+def test_scan_state_keeps_fp32s_precision(lens):
+    """The state of bf16 tokens is an fp32 sum.  Its products are exact to 2^-25; the tensor cores truncate
+    its sums at 16 products a chunk (16 * 2^-25); the weights' exponentials are good to 2^-22."""
+    import torch
+    import paper_2110_06037_gb300 as sn
+    rng = np.random.default_rng(31)
+    h, p, g, n = 4, 64, 1, 128
+    a = -rng.uniform(1, 16, h).astype(np.float32)
+    x, dt = dev(rng.normal(size=(sum(lens), h * p + 2 * g * n)), "bf16"), dev(rng.normal(size=(sum(lens), h)) - 3, "bf16")
+    out = torch.empty(len(lens), h, p, n, device="cuda")
+    offs = np.concatenate(([0], np.cumsum(lens)))
+    sn.StateSpace(h, p, g, n, dev(a)).scan(x, dt, offsets=ints(offs), max_len=max(lens), state_out=out)
+    for b in range(len(lens)):
+        rows = slice(offs[b], offs[b + 1])
+        _, _, ref, _ = ob.scan(host(x[rows]), host(dt[rows]), (h, p, g, n), a, None, None, np.zeros((h, p, n)))
+        d = host(out[b]) - ref
+        assert np.sqrt((d * d).sum() / (ref * ref).sum()) < 1e-6
+
+
 @pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
 @pytest.mark.parametrize("lens, sizes", [
     ([1], (1, 1, 1, 1)), ([0, 5, 1], (2, 8, 1, 16)), ([17, 64, 0, 33], (4, 64, 2, 128)), ([65], (6, 48, 2, 40)),
