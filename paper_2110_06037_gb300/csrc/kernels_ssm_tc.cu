@@ -216,7 +216,8 @@ __device__ __forceinline__ Parts2 parts2(float a, float b) {
 // ------------------------------------------------------------------- scan
 constexpr uint32_t TILE64 = Q * 128;  // 128 rows of 64 bf16 values
 // C (two tiles) and x twice, X's and the state's first two parts once; B's two tiles, the
-// third part of X' and a tile of zeros: B once beside C, twice in the place of C
+// third part of X' and a tile of zeros once.  The pass for states alone has B and X'
+// twice, in the places of C and the state.
 constexpr uint32_t OFF_B = 0, OFF_C = 4 * TILE64, OFF_X = 8 * TILE64, OFF_XW = 10 * TILE64, OFF_H = 12 * TILE64, OFF_SHARED = 14 * TILE64;
 constexpr size_t SCAN_SMEM = OFF_SHARED + 2048;
 static_assert(SCAN_SMEM <= 227 * 1024, "shared memory of a block");
@@ -225,7 +226,7 @@ static_assert(SCAN_SMEM <= 227 * 1024, "shared memory of a block");
 // warps that have written or read what the name says.
 enum Bar {
     F_B, F_C = F_B + 2, F_X = F_C + 2, E_B = F_X + 2, E_C = E_B + 2, E_X = E_C + 2,
-    M_PAIRS = E_X + 2, M_CARRIED, M_MADE, M_INSIDE, A_XW, A_MADE, A_STATE, A_P, A_OUT, BARS
+    M_PAIRS = E_X + 2, M_CARRIED, M_INSIDE, M_MADE, A_XW = M_MADE + 2, A_MADE = A_XW + 2, A_STATE = A_MADE + 2, A_P, A_OUT, BARS
 };
 struct Shared {
     alignas(16) float as[2][Q];  // A_s - log2 d_s of a chunk
@@ -254,7 +255,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                        const __grid_constant__ CUtensorMap mC, const __grid_constant__ TcP p, __nv_bfloat16 *__restrict__ y) {
     extern __shared__ __align__(1024) uint8_t smem[];
     Shared &sh = *reinterpret_cast<Shared *>(smem + OFF_SHARED);
-    constexpr int B_STAGES = FULL ? 1 : 2;
+    constexpr int STAGES1 = FULL ? 1 : 2;  // of B, X' and the products with it
     constexpr uint32_t OFF_XW3 = FULL ? 2 * TILE64 : OFF_C;  // the third part of X', and zeros
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const int pb = blockIdx.x % p.pblocks, head = blockIdx.x / p.pblocks, seg = blockIdx.y, b = blockIdx.z;
@@ -273,7 +274,9 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
     }
     static_assert(BARS < 31, "one lane a barrier");
     for (uint32_t e = threadIdx.x; e < TILE64 / 16; e += blockDim.x)
-        reinterpret_cast<uint4 *>(smem + OFF_XW3 + TILE64)[e] = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int i = 0; i < STAGES1; ++i)
+            reinterpret_cast<uint4 *>(smem + OFF_XW3 + (2 * i + 1) * TILE64)[e] = make_uint4(0u, 0u, 0u, 0u);
     fence_proxy_async_smem();
     tc_fence_before();
     __syncthreads();
@@ -324,14 +327,14 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                 return ok;
             };
             for (int c = 0; c < nc && ok; ++c) {
-                const int st = c & 1, bs = c % B_STAGES;
+                const int st = c & 1, bs = c % STAGES1;
                 if (FULL) {
                     if (!freed(E_C + st, c >> 1)) break;
                     load(&mC, F_C + st, OFF_C + st * 2 * TILE64, c, 2, 0, grp);
                 }
                 if (!freed(E_X + st, c >> 1)) break;
                 load(&mX, F_X + st, OFF_X + st * TILE64, c, 1, p0, head);
-                if (!freed(E_B + bs, c / B_STAGES)) break;
+                if (!freed(E_B + bs, c / STAGES1)) break;
                 load(&mB, F_B + bs, OFF_B + bs * 2 * TILE64, c, 2, 0, grp);
             }
         }
@@ -399,19 +402,21 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                 commit_one<1>(one, &sh.bar[E_C + st]);
             };
             auto made = [&](int c) {
-                const uint32_t bs = c % B_STAGES;
-                if (!need(F_B + bs, (uint32_t)(c / B_STAGES) & 1u) || !need(A_XW, c & 1) || (c > 0 && !need(A_MADE, (c - 1) & 1))) return;
+                const uint32_t bs = c % STAGES1;
+                const uint32_t n = c / STAGES1;
+                if (!need(F_B + bs, n & 1u) || !need(A_XW + bs, n & 1u) || (n > 0 && !need(A_MADE + bs, (n - 1) & 1u))) return;
                 tc_fence_after();
-                const uint64_t db = b_mn + bs * STAGE2;
+                const uint64_t db = b_mn + bs * STAGE2, xw = xw_mn + bs * STAGE2, xw3 = xw3_mn + bs * STAGE2;
+                const uint32_t d = tmem + T_D + bs * 128;
                 // (N = 128: the products with two parts of X' side by side.  The third part, beside
                 // zeros, comes first, while the sums are small: they are truncated at every MMA)
 #pragma unroll
                 for (int k = 0; k < Q / 16; ++k)
-                    umma_one<1>(one, tmem + T_D, db + mn_major(k), xw3_mn + mn_major(k), FMT | N128 | A_MN | B_MN, k > 0);
+                    umma_one<1>(one, d, db + mn_major(k), xw3 + mn_major(k), FMT | N128 | A_MN | B_MN, k > 0);
 #pragma unroll
                 for (int k = 0; k < Q / 16; ++k)
-                    umma_one<1>(one, tmem + T_D, db + mn_major(k), xw_mn + mn_major(k), FMT | N128 | A_MN | B_MN, 1);
-                commit_one<1>(one, &sh.bar[M_MADE]);
+                    umma_one<1>(one, d, db + mn_major(k), xw + mn_major(k), FMT | N128 | A_MN | B_MN, 1);
+                commit_one<1>(one, &sh.bar[M_MADE + bs]);
                 commit_one<1>(one, &sh.bar[E_B + bs]);
                 if (!FULL) commit_one<1>(one, &sh.bar[E_X + (c & 1)]);
             };
@@ -429,17 +434,19 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
         const int tid = threadIdx.x - 64, t = tid / 2, j0 = 4 * (tid & 1);
         float w_next = nc > 0 ? __ldg(table(0) + 2 * Q + t) : 0.0f;
         auto weigh = [&](int c) {
-            const int st = c & 1, bs = c % B_STAGES, valid = min(Q, s.len - (chunks.x + c) * Q);  // tokens there are
+            const int st = c & 1, bs = c % STAGES1, valid = min(Q, s.len - (chunks.x + c) * Q);  // tokens there are
             const float w = w_next;
             if (c + 1 < nc) w_next = __ldg(table(c + 1) + 2 * Q + t);
             must(F_X + st, (uint32_t)(c >> 1) & 1u);
-            if (c > 0) must(M_MADE, (c - 1) & 1);  // the X' before has been read
+            const uint32_t n = c / STAGES1;
+            if (n > 0) must(M_MADE + bs, (n - 1) & 1u);  // the X' before has been read
             if (valid < Q) {
-                must(F_B + bs, (uint32_t)(c / B_STAGES) & 1u);
+                must(F_B + bs, n & 1u);
                 if (FULL) must(M_PAIRS, c & 1);
             }
             if (!ok) return;
-            uint8_t *xr = smem + OFF_X + st * TILE64 + t * 128, *wr = smem + OFF_XW + t * 128, *w3 = smem + OFF_XW3 + t * 128;
+            uint8_t *xr = smem + OFF_X + st * TILE64 + t * 128, *wr = smem + OFF_XW + bs * 2 * TILE64 + t * 128;
+            uint8_t *w3 = smem + OFF_XW3 + bs * 2 * TILE64 + t * 128;
 #pragma unroll 2
             for (int i = 0; i < 4; ++i) {
                 const uint32_t at = (uint32_t)((j0 + i) ^ (t & 7)) << 4;
@@ -480,7 +487,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                 }
             }
             fence_proxy_async_smem();
-            arrive(A_XW);
+            arrive(A_XW + bs);
         };
         if constexpr (!FULL) {
             for (int c = 0; c < nc && ok; ++c) weigh(c);
@@ -605,18 +612,19 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             }
             const float e = exp2f(total_next);
             if (c + 1 < nc) total_next = __ldg(p.total + tab0 + (int64_t)(c + 1) * q.H);
-            if (!must(M_MADE, c & 1)) break;
+            const uint32_t bs = c % STAGES1, d = tmem + lanes + T_D + bs * 128 + c0;
+            if (!must(M_MADE + bs, (uint32_t)(c / STAGES1) & 1u)) break;
             tc_fence_after();
 #pragma unroll
             for (int i = 0; i < HC; i += 16) {
                 uint32_t u[16], v[16];
                 __syncwarp();
-                tmem_ld16x2(tmem + lanes + T_D + c0 + i, u, tmem + lanes + T_D + PB + c0 + i, v);
+                tmem_ld16x2(d + i, u, d + PB + i, v);
 #pragma unroll
                 for (int j = 0; j < 16; ++j) h[i + j] = fmaf(h[i + j], e, __uint_as_float(u[j]) + __uint_as_float(v[j]));
             }
             tc_fence_before();
-            arrive(A_MADE);
+            arrive(A_MADE + bs);
         }
         float *out = FULL ? (seg == p.segs - 1 && q.s_out && srow >= 0 ? q.s_out + srow : nullptr) : part(seg + 1);
         if (ok && out) {
