@@ -25,8 +25,12 @@
 // Each product has warps of its own for what goes into and comes out of it, so that
 // only the state's one multiply-add a chunk runs from chunk to chunk: in one order, two
 // blocks an SM, a chunk took a block 17.9 thousand cycles of waiting for one step after
-// the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128), the MMAs 32 of
-// them.  So: 161 us.
+// the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128).  So: 153 us, of
+// which 7 are the time steps, 30 the first pass, 115 the second, 7000 cycles a chunk.
+// The tensor cores are busy in 45% of them, the busiest scheduler issues in 65%; what
+// bounds it is the way from the pairs to P and to the next pairs.  (Tried and no faster: the next
+// chunk's pairs ahead, in TMEM of their own, 163; X' by the state's warps, 163; P's
+// columns 32 at a time, 165.)
 // Non-finite x: 0 * NaN would reach tokens before it, so such an x goes into the
 // product as 0 and makes its channel NaN from its token on; into the state it goes as
 // it is.  Waits are bounded.
@@ -172,27 +176,27 @@ __device__ __forceinline__ void tmem_ld16(uint32_t ta, float (&a)[16]) {
         : "r"(ta)
         : "memory");
 }
-__device__ __forceinline__ void tmem_ld16x2(uint32_t ta, uint32_t (&a)[16], uint32_t tb, uint32_t (&b)[16]) {
+__device__ __forceinline__ void tmem_ld16x2(uint32_t ta, float (&a)[16], uint32_t tb, float (&b)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%32];\n\t"
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%33];\n\t"
         "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(a[4]), "=r"(a[5]), "=r"(a[6]), "=r"(a[7]),
-          "=r"(a[8]), "=r"(a[9]), "=r"(a[10]), "=r"(a[11]), "=r"(a[12]), "=r"(a[13]), "=r"(a[14]), "=r"(a[15]),
-          "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]), "=r"(b[4]), "=r"(b[5]), "=r"(b[6]), "=r"(b[7]),
-          "=r"(b[8]), "=r"(b[9]), "=r"(b[10]), "=r"(b[11]), "=r"(b[12]), "=r"(b[13]), "=r"(b[14]), "=r"(b[15])
+        : "=f"(a[0]), "=f"(a[1]), "=f"(a[2]), "=f"(a[3]), "=f"(a[4]), "=f"(a[5]), "=f"(a[6]), "=f"(a[7]),
+          "=f"(a[8]), "=f"(a[9]), "=f"(a[10]), "=f"(a[11]), "=f"(a[12]), "=f"(a[13]), "=f"(a[14]), "=f"(a[15]),
+          "=f"(b[0]), "=f"(b[1]), "=f"(b[2]), "=f"(b[3]), "=f"(b[4]), "=f"(b[5]), "=f"(b[6]), "=f"(b[7]),
+          "=f"(b[8]), "=f"(b[9]), "=f"(b[10]), "=f"(b[11]), "=f"(b[12]), "=f"(b[13]), "=f"(b[14]), "=f"(b[15])
         : "r"(ta), "r"(tb)
         : "memory");
 }
-__device__ __forceinline__ void tmem_ld16x3(uint32_t ta, uint32_t (&a)[16], uint32_t tb, uint32_t (&b)[16], uint32_t tc_, uint32_t (&c)[16]) {
+__device__ __forceinline__ void tmem_ld16x3(uint32_t ta, float (&a)[16], uint32_t tb, float (&b)[16], uint32_t tc_, float (&c)[16]) {
     asm volatile(
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%48];\n\t"
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%49];\n\t"
         "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%32, %33, %34, %35, %36, %37, %38, %39, %40, %41, %42, %43, %44, %45, %46, %47}, [%50];\n\t"
         "tcgen05.wait::ld.sync.aligned;"
-        : "=r"(a[0]), "=r"(a[1]), "=r"(a[2]), "=r"(a[3]), "=r"(a[4]), "=r"(a[5]), "=r"(a[6]), "=r"(a[7]), "=r"(a[8]), "=r"(a[9]), "=r"(a[10]), "=r"(a[11]), "=r"(a[12]), "=r"(a[13]), "=r"(a[14]), "=r"(a[15]),
-          "=r"(b[0]), "=r"(b[1]), "=r"(b[2]), "=r"(b[3]), "=r"(b[4]), "=r"(b[5]), "=r"(b[6]), "=r"(b[7]), "=r"(b[8]), "=r"(b[9]), "=r"(b[10]), "=r"(b[11]), "=r"(b[12]), "=r"(b[13]), "=r"(b[14]), "=r"(b[15]),
-          "=r"(c[0]), "=r"(c[1]), "=r"(c[2]), "=r"(c[3]), "=r"(c[4]), "=r"(c[5]), "=r"(c[6]), "=r"(c[7]), "=r"(c[8]), "=r"(c[9]), "=r"(c[10]), "=r"(c[11]), "=r"(c[12]), "=r"(c[13]), "=r"(c[14]), "=r"(c[15])
+        : "=f"(a[0]), "=f"(a[1]), "=f"(a[2]), "=f"(a[3]), "=f"(a[4]), "=f"(a[5]), "=f"(a[6]), "=f"(a[7]), "=f"(a[8]), "=f"(a[9]), "=f"(a[10]), "=f"(a[11]), "=f"(a[12]), "=f"(a[13]), "=f"(a[14]), "=f"(a[15]),
+          "=f"(b[0]), "=f"(b[1]), "=f"(b[2]), "=f"(b[3]), "=f"(b[4]), "=f"(b[5]), "=f"(b[6]), "=f"(b[7]), "=f"(b[8]), "=f"(b[9]), "=f"(b[10]), "=f"(b[11]), "=f"(b[12]), "=f"(b[13]), "=f"(b[14]), "=f"(b[15]),
+          "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]), "=f"(c[4]), "=f"(c[5]), "=f"(c[6]), "=f"(c[7]), "=f"(c[8]), "=f"(c[9]), "=f"(c[10]), "=f"(c[11]), "=f"(c[12]), "=f"(c[13]), "=f"(c[14]), "=f"(c[15])
         : "r"(ta), "r"(tb), "r"(tc_)
         : "memory");
 }
@@ -202,16 +206,44 @@ __device__ __forceinline__ float ex2(float v) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
     return r;
 }
-// two values as the large and small bf16 parts of each
-struct Parts2 {
-    uint32_t hi, lo;
-};
-__device__ __forceinline__ Parts2 parts2(float a, float b) {
-    Parts2 r;
-    r.hi = pack2<__nv_bfloat16>(a, b);
-    const float2 h = unpack2<__nv_bfloat16>(r.hi);
-    r.lo = pack2<__nv_bfloat16>(a - h.x, b - h.y);
+// two fp32 values in one register pair: one instruction for both
+using F2 = unsigned long long;
+__device__ __forceinline__ F2 f2(float a, float b) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
     return r;
+}
+__device__ __forceinline__ float2 floats(F2 v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ F2 mul_2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 add_2(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 fma_2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+// the large bf16 parts of two values, which keep the rest
+__device__ __forceinline__ uint32_t part_of(F2 &v) {
+    const float2 f = floats(v);
+    const uint32_t p = pack2<__nv_bfloat16>(f.x, f.y);
+    const float2 h = unpack2<__nv_bfloat16>(p);
+    v = fma_2(f2(h.x, h.y), f2(-1.0f, -1.0f), v);
+    return p;
+}
+__device__ __forceinline__ uint32_t rounded(F2 v) {
+    const float2 f = floats(v);
+    return pack2<__nv_bfloat16>(f.x, f.y);
 }
 // ------------------------------------------------------------------- scan
 constexpr uint32_t TILE64 = Q * 128;  // 128 rows of 64 bf16 values
@@ -240,10 +272,10 @@ static_assert(sizeof(Shared) <= 2048, "behind the tiles");
 // large and small parts' products apart; inside; P's small parts
 constexpr uint32_t T_S = 0, T_Y0 = 128, T_D = 256, T_Y1 = 384, T_LO = 448;
 
-// Warps: 0 copies, 1 issues the MMAs, 2 to 9 make P (FULL) and the next chunk's X' (two
+// Warps: 0 copies, 1 issues the MMAs; FULL: 2 to 9 make P and the next chunk's X' (two
 // threads a row), 10 to 17 carry the state (half of the columns each four), 18 to 21
-// (FULL) take the outputs.
-constexpr int FULL_THREADS = 22 * 32, STATE_THREADS = 18 * 32;
+// take the outputs; otherwise 2 to 17 make X' (four threads a row), 18 to 25 carry the state.
+constexpr int FULL_THREADS = 22 * 32, STATE_THREADS = 26 * 32;
 
 // FULL: the outputs; otherwise a segment's state from nothing (segment 0: from s_in).
 // The MMAs' order, chunk i: inside(i), pairs(i + 1), carried(i), made(i + 1).  The two
@@ -255,6 +287,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                        const __grid_constant__ CUtensorMap mC, const __grid_constant__ TcP p, __nv_bfloat16 *__restrict__ y) {
     extern __shared__ __align__(1024) uint8_t smem[];
     Shared &sh = *reinterpret_cast<Shared *>(smem + OFF_SHARED);
+    constexpr int XT = FULL ? 2 : 4, STATE0 = 2 + 4 * XT;  // threads a row of X'; the state's first warp
     constexpr int STAGES1 = FULL ? 1 : 2;  // of B, X' and the products with it
     constexpr uint32_t OFF_XW3 = FULL ? 2 * TILE64 : OFF_C;  // the third part of X', and zeros
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -266,7 +299,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
     if (warp == 0) {
         tmem_alloc<1>(&sh.tmem, 512);
     } else if (warp == 1) {
-        if (lane < BARS) mbar_init(&sh.bar[lane], lane < A_XW ? 1 : lane == A_OUT ? 4 : 8);
+        if (lane < BARS) mbar_init(&sh.bar[lane], lane < A_XW ? 1 : lane < A_MADE ? 4 * XT : lane == A_OUT ? 4 : 8);
         if (lane == 31) sh.abort = sh.any_bad[0] = sh.any_bad[1] = 0;
         fence_mbar_init();
     } else if (warp >= 2 && warp < 6) {
@@ -429,9 +462,9 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             }
         }
         __syncwarp();
-    } else if (warp < 10) {
-        // ---------------- X', two threads a row
-        const int tid = threadIdx.x - 64, t = tid / 2, j0 = 4 * (tid & 1);
+    } else if (warp < STATE0) {
+        // ---------------- X', XT threads a row
+        const int tid = threadIdx.x - 64, t = tid / XT, j0 = 8 / XT * (tid % XT);
         float w_next = nc > 0 ? __ldg(table(0) + 2 * Q + t) : 0.0f;
         auto weigh = [&](int c) {
             const int st = c & 1, bs = c % STAGES1, valid = min(Q, s.len - (chunks.x + c) * Q);  // tokens there are
@@ -447,8 +480,8 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             if (!ok) return;
             uint8_t *xr = smem + OFF_X + st * TILE64 + t * 128, *wr = smem + OFF_XW + bs * 2 * TILE64 + t * 128;
             uint8_t *w3 = smem + OFF_XW3 + bs * 2 * TILE64 + t * 128;
-#pragma unroll 2
-            for (int i = 0; i < 4; ++i) {
+#pragma unroll 1  // (two at a time: 157 us for 153)
+            for (int i = 0; i < 8 / XT; ++i) {
                 const uint32_t at = (uint32_t)((j0 + i) ^ (t & 7)) << 4;
                 uint4 xv = *reinterpret_cast<const uint4 *>(xr + at);
                 if (t >= valid) {  // rows of another sequence: nothing of them may count
@@ -464,10 +497,8 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                 for (int e = 0; e < 4; ++e) {
                     const float2 f = unpack2<__nv_bfloat16>(u[e]);
                     odd |= ((u[e] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-                    const float2 m = make_float2(f.x * w, f.y * w);
-                    const Parts2 v = parts2(m.x, m.y);
-                    const float2 h = unpack2<__nv_bfloat16>(v.hi), l = unpack2<__nv_bfloat16>(v.lo);
-                    hi[e] = v.hi, lo[e] = v.lo, lo2[e] = pack2<__nv_bfloat16>(m.x - h.x - l.x, m.y - h.y - l.y);
+                    F2 v = mul_2(f2(f.x, f.y), f2(w, w));
+                    hi[e] = part_of(v), lo[e] = part_of(v), lo2[e] = rounded(v);
                 }
                 *reinterpret_cast<uint4 *>(wr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
                 *reinterpret_cast<uint4 *>(wr + TILE64 + at) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
@@ -522,22 +553,29 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                         __syncwarp();
                         if (blk <= quarter) {
                             float f[16];
+                            F2 v[8];
                             tmem_ld16(tmem + lanes + T_S + c0, f);
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
                                 const float4 As = *reinterpret_cast<const float4 *>(&sh.as[par][c0 + 4 * j]);
-                                f[4 * j] *= ex2(At - As.x), f[4 * j + 1] *= ex2(At - As.y);
-                                f[4 * j + 2] *= ex2(At - As.z), f[4 * j + 3] *= ex2(At - As.w);
+                                const float2 a = floats(fma_2(f2(As.x, As.y), f2(-1.0f, -1.0f), f2(At, At)));
+                                const float2 b = floats(fma_2(f2(As.z, As.w), f2(-1.0f, -1.0f), f2(At, At)));
+                                v[2 * j] = mul_2(f2(f[4 * j], f[4 * j + 1]), f2(ex2(a.x), ex2(a.y)));
+                                v[2 * j + 1] = mul_2(f2(f[4 * j + 2], f[4 * j + 3]), f2(ex2(b.x), ex2(b.y)));
                             }
                             if (blk == quarter) {
                                 const int own = row - c0;  // the diagonal's place among these columns
 #pragma unroll
-                                for (int j = 0; j < 16; ++j) f[j] = j < own ? f[j] : j == own ? f[j] + skip : 0.0f;
+                                for (int j = 0; j < 8; ++j) {
+                                    const float2 m = floats(v[j]);
+                                    v[j] = f2(2 * j < own ? m.x : 2 * j == own ? m.x + skip : 0.0f,
+                                              2 * j + 1 < own ? m.y : 2 * j + 1 == own ? m.y + skip : 0.0f);
+                                }
                             }
 #pragma unroll
                             for (int j = 0; j < 8; ++j) {
-                                const Parts2 v = parts2(f[2 * j], f[2 * j + 1]);
-                                hi[j] = v.hi, lo[j] = v.lo;
+                                hi[j] = part_of(v[j]);
+                                lo[j] = rounded(v[j]);
                             }
                         } else {
 #pragma unroll
@@ -555,35 +593,43 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                 if (c + 1 < nc && ok) weigh(c + 1);
             }
         }
-    } else if (warp < 18) {
+    } else if (warp < STATE0 + 8) {
         // ---------------- the state, [p][n] with lane n, in fp32: columns c0 to c0 + 31
         constexpr int HC = PB / 2;
-        float h[HC];
-        const int c0 = (warp - 10) / 4 * HC;
+        F2 h[HC / 2];
+        const int c0 = (warp - STATE0) / 4 * HC;
         const int64_t srow = s.slot >= 0 ? (((int64_t)s.slot * q.H + head) * q.P + p0 + c0) * q.N + row : -1;
         auto live = [&](int i) { return c0 + i < np && row < q.N; };
         auto part = [&](int j) { return p.part + part0 + ((int64_t)j * PB + c0) * q.N + row; };  // before segment 0, after fine segment j - 1
+        auto load = [&](const float *from) {
 #pragma unroll
-        for (int i = 0; i < HC; ++i) {
-            h[i] = 0.0f;
-            if (!live(i)) continue;
-            if (FULL && p.segs > 1) h[i] = part(seg > 0 ? 1 : 0)[(int64_t)i * q.N];
-            else if (seg == 0 && q.s_in && srow >= 0) h[i] = q.s_in[srow + (int64_t)i * q.N];
-        }
+            for (int i = 0; i < HC; i += 2)
+                h[i / 2] = f2(live(i) ? from[(int64_t)i * q.N] : 0.0f, live(i + 1) ? from[(int64_t)(i + 1) * q.N] : 0.0f);
+        };
+        auto store = [&](float *to) {
+#pragma unroll
+            for (int i = 0; i < HC; i += 2) {
+                const float2 v = floats(h[i / 2]);
+                if (live(i)) to[(int64_t)i * q.N] = v.x;
+                if (live(i + 1)) to[(int64_t)(i + 1) * q.N] = v.y;
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < HC / 2; ++i) h[i] = f2(0.0f, 0.0f);
+        if (FULL && p.segs > 1) load(part(seg > 0 ? 1 : 0));
+        else if (seg == 0 && q.s_in && srow >= 0) load(q.s_in + srow);
         if (FULL) {
             for (int j = 1; j < seg * p.fine; ++j) {
                 const int2 ch = segment(s.len, p.segs * p.fine, j);
                 float sum = 0.0f;
                 for (int c = ch.x; c < ch.y; ++c) sum += p.total[chunk_at(s, b, c) * q.H + head];
-                const float e = exp2f(sum);
+                const float e = exp2f(sum), *next = part(j + 1);
 #pragma unroll
-                for (int i = 0; i < HC; ++i)
-                    if (live(i)) h[i] = fmaf(h[i], e, part(j + 1)[(int64_t)i * q.N]);
+                for (int i = 0; i < HC; i += 2)
+                    h[i / 2] = fma_2(h[i / 2], f2(e, e), f2(live(i) ? next[(int64_t)i * q.N] : 0.0f, live(i + 1) ? next[(int64_t)(i + 1) * q.N] : 0.0f));
             }
         } else if (seg == 0) {  // the second pass may store over s_in: it reads this copy
-#pragma unroll
-            for (int i = 0; i < HC; ++i)
-                if (live(i)) part(0)[(int64_t)i * q.N] = h[i];
+            store(part(0));
         }
         auto put_state = [&]() {  // its two bf16 parts as an operand: rows n, 64 p
             uint8_t *hr = smem + OFF_H + row * 128;
@@ -593,8 +639,8 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     // (an infinite state's small part is NaN, as its sums over B's signs are)
-                    const Parts2 v = parts2(h[8 * i + 2 * e], h[8 * i + 2 * e + 1]);
-                    hi[e] = v.hi, lo[e] = v.lo;
+                    F2 v = h[4 * i + e];
+                    hi[e] = part_of(v), lo[e] = rounded(v);
                 }
                 const uint32_t at = (uint32_t)((c0 / 8 + i) ^ (row & 7)) << 4;
                 *reinterpret_cast<uint4 *>(hr + at) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
@@ -617,24 +663,21 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             tc_fence_after();
 #pragma unroll
             for (int i = 0; i < HC; i += 16) {
-                uint32_t u[16], v[16];
+                float u[16], v[16];
                 __syncwarp();
                 tmem_ld16x2(d + i, u, d + PB + i, v);
 #pragma unroll
-                for (int j = 0; j < 16; ++j) h[i + j] = fmaf(h[i + j], e, __uint_as_float(u[j]) + __uint_as_float(v[j]));
+                for (int j = 0; j < 16; j += 2)
+                    h[(i + j) / 2] = fma_2(h[(i + j) / 2], f2(e, e), add_2(f2(u[j], u[j + 1]), f2(v[j], v[j + 1])));
             }
             tc_fence_before();
             arrive(A_MADE + bs);
         }
         float *out = FULL ? (seg == p.segs - 1 && q.s_out && srow >= 0 ? q.s_out + srow : nullptr) : part(seg + 1);
-        if (ok && out) {
-#pragma unroll
-            for (int i = 0; i < HC; ++i)
-                if (live(i)) out[(int64_t)i * q.N] = h[i];
-        }
+        if (ok && out) store(out);
     } else {
         // ---------------- the outputs
-        const int t = threadIdx.x - 18 * 32;
+        const int t = threadIdx.x - (STATE0 + 8) * 32;
         float at_next = nc > 0 ? __ldg(table(0) + row) : 0.0f;
 #pragma unroll 1
         for (int c = 0; c < nc; ++c) {
@@ -649,7 +692,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             __nv_bfloat16 *yr = y + (s.first + (int64_t)(chunks.x + c) * Q + row) * q.ldy + (int64_t)head * q.P + p0;
 #pragma unroll 1
             for (int i = 0; i < PB; i += 16) {
-                uint32_t u[16], v[16], in[16];
+                float u[16], v[16], in[16];
                 __syncwarp();
                 tmem_ld16x3(tmem + lanes + T_Y0 + i, u, tmem + lanes + T_Y0 + PB + i, v, tmem + lanes + T_Y1 + i, in);
 #pragma unroll
@@ -657,14 +700,13 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                     uint32_t o[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        float f[2];
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            const int n = j + 2 * e + k;
-                            f[k] = fmaf(__uint_as_float(u[n]) + __uint_as_float(v[n]), et, __uint_as_float(in[n]));
-                            if (bad && row >= sh.bad[st][i + n]) f[k] = NAN;
+                        const int n = j + 2 * e;
+                        F2 f = fma_2(add_2(f2(u[n], u[n + 1]), f2(v[n], v[n + 1])), f2(et, et), f2(in[n], in[n + 1]));
+                        if (bad) {
+                            const float2 g = floats(f);
+                            f = f2(row >= sh.bad[st][i + n] ? NAN : g.x, row >= sh.bad[st][i + n + 1] ? NAN : g.y);
                         }
-                        o[e] = pack2<__nv_bfloat16>(f[0], f[1]);
+                        o[e] = rounded(f);
                     }
                     if (row < valid && i + j < np) *reinterpret_cast<uint4 *>(yr + i + j) = make_uint4(o[0], o[1], o[2], o[3]);
                 }
