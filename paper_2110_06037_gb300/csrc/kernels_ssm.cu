@@ -33,7 +33,19 @@ __global__ void __launch_bounds__(CONV_THREADS, CONV_BLOCKS)
     struct alignas(sizeof(T) * V) Piece {
         T v[V];
     };
-    float wt[V * W], b[V], h[W][V];  // h[j]: the input j + 1 - W tokens from the present one
+    // Two channels a register pair where there are two (arithmetic of single values: 41 us)
+    constexpr bool PAIRS = V % 2 == 0;
+    using L = typename std::conditional<PAIRS, F2, float>::type;
+    constexpr int VL = PAIRS ? V / 2 : V;
+    float wt[V * W], b[V];
+    L h[W][VL];  // h[j]: the input j + 1 - W tokens from the present one
+    auto unpack = [](const Piece &p, L(&to)[VL], bool have) {
+#pragma unroll
+        for (int v = 0; v < VL; ++v) {
+            if constexpr (PAIRS) to[v] = have ? f2(ldf(p.v + 2 * v), ldf(p.v + 2 * v + 1)) : f2(0.0f, 0.0f);
+            else to[v] = have ? ldf(p.v + v) : 0.0f;
+        }
+    };
     if constexpr (V % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < V * W / 4; ++i)
@@ -48,6 +60,17 @@ __global__ void __launch_bounds__(CONV_THREADS, CONV_BLOCKS)
 #pragma unroll
         for (int v = 0; v < V; ++v) b[v] = bias ? bias[c0 + v] : 0.0f;
     }
+    L wl[VL][W], bl[VL];
+#pragma unroll
+    for (int v = 0; v < VL; ++v) {
+        if constexpr (PAIRS) bl[v] = f2(b[2 * v], b[2 * v + 1]);
+        else bl[v] = b[v];
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            if constexpr (PAIRS) wl[v][j] = f2(wt[2 * v * W + j], wt[(2 * v + 1) * W + j]);
+            else wl[v][j] = wt[v * W + j];
+        }
+    }
     const T *xr = x + (s.first + t0) * ldx + c0;
     T *yr = y + (s.first + t0) * ldy + c0;
     T *kp = kept && s.slot >= 0 ? kept + (int64_t)s.slot * W * C + c0 : nullptr;
@@ -59,8 +82,7 @@ __global__ void __launch_bounds__(CONV_THREADS, CONV_BLOCKS)
         if (t0 >= back) p = *reinterpret_cast<const Piece *>(xr - back * ldx);
         else if (kp && s.pos + t0 >= back) p = *reinterpret_cast<const Piece *>(kp + (int64_t)((s.pos + t0 - back) % W) * C);
         else have = false;
-#pragma unroll
-        for (int v = 0; v < V; ++v) h[j][v] = have ? ldf(p.v + v) : 0.0f;
+        unpack(p, h[j], have);
     }
     const int n = (int)min((int64_t)len, s.len - t0);
     constexpr int U = 4;  // tokens at once; the next eight's loads are in flight meanwhile
@@ -70,15 +92,13 @@ __global__ void __launch_bounds__(CONV_THREADS, CONV_BLOCKS)
         if (u < n) raw[u / U][u % U] = *reinterpret_cast<const Piece *>(xr + u * ldx);
     xr += 2 * U * ldx;
     auto tokens = [&](Piece(&in)[U], int t) {
-        float win[W - 1 + U][V];  // inputs t + 1 - W to t + U - 1
+        L win[W - 1 + U][VL];  // inputs t + 1 - W to t + U - 1
 #pragma unroll
         for (int j = 0; j + 1 < W; ++j)
 #pragma unroll
-            for (int v = 0; v < V; ++v) win[j][v] = h[j + 1][v];
+            for (int v = 0; v < VL; ++v) win[j][v] = h[j + 1][v];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-#pragma unroll
-            for (int v = 0; v < V; ++v) win[W - 1 + u][v] = ldf(in[u].v + v);
+        for (int u = 0; u < U; ++u) unpack(in[u], win[W - 1 + u], true);
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (t + 2 * U + u < n) in[u] = *reinterpret_cast<const Piece *>(xr + u * ldx);
@@ -86,20 +106,33 @@ __global__ void __launch_bounds__(CONV_THREADS, CONV_BLOCKS)
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (t + u < n) {
-                float a[V];
+                L a[VL];
 #pragma unroll
-                for (int v = 0; v < V; ++v) {
-                    a[v] = b[v];
+                for (int v = 0; v < VL; ++v) {
+                    a[v] = bl[v];
 #pragma unroll
-                    for (int j = 0; j < W; ++j) a[v] = fmaf(wt[v * W + j], win[u + j][v], a[v]);
+                    for (int j = 0; j < W; ++j) {
+                        if constexpr (PAIRS) a[v] = fma_2(wl[v][j], win[u + j][v], a[v]);
+                        else a[v] = fmaf(wl[v][j], win[u + j][v], a[v]);
+                    }
                 }
                 if (act) {
 #pragma unroll
-                    for (int v = 0; v < V; ++v) a[v] = silu(a[v]);
+                    for (int v = 0; v < VL; ++v) {
+                        if constexpr (PAIRS) a[v] = silu_2(a[v]);
+                        else a[v] = silu(a[v]);
+                    }
                 }
                 Piece out;
 #pragma unroll
-                for (int v = 0; v < V; ++v) out.v[v] = cvt<T>(a[v]);
+                for (int v = 0; v < VL; ++v) {
+                    if constexpr (PAIRS) {
+                        const float2 f = floats(a[v]);
+                        out.v[2 * v] = cvt<T>(f.x), out.v[2 * v + 1] = cvt<T>(f.y);
+                    } else {
+                        out.v[v] = cvt<T>(a[v]);
+                    }
+                }
                 *reinterpret_cast<Piece *>(yr) = out;
             }
             yr += ldy;
@@ -107,7 +140,7 @@ __global__ void __launch_bounds__(CONV_THREADS, CONV_BLOCKS)
 #pragma unroll
         for (int j = 1; j < W; ++j)
 #pragma unroll
-            for (int v = 0; v < V; ++v) h[j][v] = win[U - 1 + j][v];
+            for (int v = 0; v < VL; ++v) h[j][v] = win[U - 1 + j][v];
     };
     for (int t = 0; t < n; t += 2 * U) {
         tokens(raw[0], t);

@@ -29,8 +29,50 @@ __device__ __forceinline__ Seq sequence(const SeqArgs &q, int b) {
     return s;
 }
 
+__device__ __forceinline__ float ex2(float v) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+// two fp32 values in one register pair: one instruction for both
+using F2 = unsigned long long;
+__device__ __forceinline__ F2 f2(float a, float b) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ float2 floats(F2 v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ F2 mul_2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 add_2(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 fma_2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
 // by the approximate exponential and division (2 ulp each; a denominator beyond 2^126 gives 0)
 __device__ __forceinline__ float silu(float v) { return __fdividef(v, 1.0f + __expf(-v)); }
+// the same of two values
+__device__ __forceinline__ F2 silu_2(F2 v) {
+    constexpr float LOG2E = 1.4426950408889634f;
+    const float2 t = floats(mul_2(v, f2(-LOG2E, -LOG2E)));
+    const float2 d = floats(add_2(f2(ex2(t.x), ex2(t.y)), f2(1.0f, 1.0f)));
+    float a, b;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(d.x));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(d.y));
+    return mul_2(v, f2(a, b));
+}
 // log(1 + e^v) without overflow, and exact where e^v is small
 __device__ __forceinline__ float softplus(float v) { return fmaxf(v, 0.0f) + log1pf(expf(-fabsf(v))); }
 
