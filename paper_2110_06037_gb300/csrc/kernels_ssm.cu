@@ -216,7 +216,8 @@ cudaError_t conv_width(int W, const SeqArgs &q, const T *x, int64_t ldx, T *y, i
 // tokens' sums are exchanged together.  What bounds it is the chain of a row's
 // tokens, so few rows are spread over segments of the sequence: a first pass makes
 // every segment's state from nothing, the second starts from the joined ones.
-// (Six sequences, 1030 tokens the longest, 6 heads of 48 x 40: in one piece 256 us.)
+// Six sequences, 1030 tokens the longest, 6 heads of 48 x 40: in one piece 256 us, cut
+// all alike 45, each by its own length 36; the two passes' latencies are what is left.
 constexpr int RT = 16, SEG_MIN = 64;  // tokens of a run, and of a segment at least
 
 struct RecP {
@@ -224,6 +225,8 @@ struct RecP {
     int32_t segs;
     float *part, *total;  // [batch][H][segs][P][N] states: before segment 0, then after segment j; [batch][H][segs]: sums of d a
 };
+// segments of one sequence: of SEG_MIN tokens at least, as many as `most`
+__device__ __forceinline__ int rec_own(int len, int most) { return max(1, min(most, (len + RT - 1) / RT / (SEG_MIN / RT))); }
 __device__ __forceinline__ int2 rec_segment(int len, int segs, int g) {  // tokens [first, last), whole runs
     const int runs = (len + RT - 1) / RT;
     return make_int2(min(len, (int)((int64_t)runs * g / segs) * RT), min(len, (int)((int64_t)runs * (g + 1) / segs) * RT));
@@ -242,7 +245,9 @@ __global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant
     const int pblocks = (q.P + 31) / 32, head = blockIdx.x / pblocks, p0 = blockIdx.x % pblocks * 32, seg = blockIdx.y;
     const int tid = threadIdx.x, row = p0 + tid / 8, l = tid % 8, b = blockIdx.z;
     const Seq s = sequence(q.q, b);
-    const int2 tok = rec_segment(s.len, p.segs, seg);
+    const int segs = rec_own(s.len, p.segs);
+    if (seg >= (FULL ? segs : segs - 1)) return;
+    const int2 tok = rec_segment(s.len, segs, seg);
     const int grp = head / (q.H / q.G), np = min(32, q.P - p0);
     const float a = q.a[head], dskip = q.d ? q.d[head] : 0.0f, dtb = q.dt_bias ? q.dt_bias[head] : 0.0f;
     const int64_t part0 = ((int64_t)b * q.H + head) * p.segs, srow = s.slot >= 0 ? (((int64_t)s.slot * q.H + head) * q.P + row) * q.N : -1;
@@ -254,7 +259,7 @@ __global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant
         const int n = value(i);
         st[i] = 0.0f;
         if (row >= q.P || n >= q.N) continue;
-        if (FULL && p.segs > 1) st[i] = state_at(seg > 0 ? 1 : 0)[n];
+        if (FULL && segs > 1) st[i] = state_at(seg > 0 ? 1 : 0)[n];
         else if (seg == 0 && q.s_in && srow >= 0) st[i] = q.s_in[srow + n];
     }
     if (FULL) {
@@ -359,7 +364,7 @@ __global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant
             }
         }
     }
-    float *out = FULL ? (seg == p.segs - 1 && q.s_out && srow >= 0 ? q.s_out + srow : nullptr) : state_at(seg + 1);
+    float *out = FULL ? (seg == segs - 1 && q.s_out && srow >= 0 ? q.s_out + srow : nullptr) : state_at(seg + 1);
     if (out && row < q.P) {
 #pragma unroll
         for (int i = 0; i < NL; ++i)

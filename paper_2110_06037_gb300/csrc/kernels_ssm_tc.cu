@@ -25,7 +25,7 @@
 // Each product has warps of its own for what goes into and comes out of it, so that
 // only the state's one multiply-add a chunk runs from chunk to chunk: in one order, two
 // blocks an SM, a chunk took a block 17.9 thousand cycles of waiting for one step after
-// the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128).  So: 153 us, of
+// the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128).  So: 151 us, of
 // which 7 are the time steps, 30 the first pass, 115 the second, 7000 cycles a chunk.
 // The tensor cores are busy in 45% of them, the busiest scheduler issues in 65%; what
 // bounds it is the way from the pairs to P and to the next pairs.  (Tried and no faster: the next
@@ -65,6 +65,8 @@ struct TcP {
 // index of a chunk's table: unique for chunk c of sequence b, since each sequence
 // before it has at most its tokens / Q + 1 chunks
 __device__ __forceinline__ int64_t chunk_at(const Seq &s, int b, int c) { return s.first / Q + b + c; }
+// segments of one sequence: of four chunks at least, as many as `most`
+__device__ __forceinline__ int own_segments(int len, int most) { return max(1, min(most, (len + Q - 1) / Q / 4)); }
 // segment g of a sequence: chunks [first, last)
 __device__ __forceinline__ int2 segment(int len, int segs, int g) {
     const int chunks = (len + Q - 1) / Q;
@@ -287,7 +289,9 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
     griddep_wait();
     const SsmP &q = p.s;
     const Seq s = sequence(q.q, b);
-    const int2 chunks = FULL ? segment(s.len, p.segs, seg) : segment(s.len, p.segs * p.fine, seg);
+    const int segs = own_segments(s.len, p.segs);
+    const bool used = seg < (FULL ? segs : (segs - 1) * p.fine);  // (a shorter sequence has fewer segments)
+    const int2 chunks = used ? segment(s.len, FULL ? segs : segs * p.fine, seg) : make_int2(0, 0);
     const int nc = chunks.y - chunks.x, grp = head / (q.H / q.G);
     const int p0 = pb * PB, np = min(PB, q.P - p0);
     const int64_t part0 = (((int64_t)b * q.H + head) * p.pblocks + pb) * (p.segs * p.fine) * PB * q.N;
@@ -448,7 +452,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             if (!ok) return;
             uint8_t *xr = smem + OFF_X + st * TILE64 + t * 128, *wr = smem + OFF_XW + bs * 2 * TILE64 + t * 128;
             uint8_t *w3 = smem + OFF_XW3 + bs * 2 * TILE64 + t * 128;
-#pragma unroll 1  // (two at a time: 157 us for 153)
+#pragma unroll 1  // (two at a time: 4 us more for 8192 tokens)
             for (int i = 0; i < 8 / XT; ++i) {
                 const uint32_t at = (uint32_t)((j0 + i) ^ (t & 7)) << 4;
                 uint4 xv = *reinterpret_cast<const uint4 *>(xr + at);
@@ -584,11 +588,12 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
         };
 #pragma unroll
         for (int i = 0; i < HC / 2; ++i) h[i] = f2(0.0f, 0.0f);
-        if (FULL && p.segs > 1) load(part(seg > 0 ? 1 : 0));
-        else if (seg == 0 && q.s_in && srow >= 0) load(q.s_in + srow);
-        if (FULL) {
+        if (used && FULL && segs > 1) load(part(seg > 0 ? 1 : 0));
+        else if (used && seg == 0 && q.s_in && srow >= 0) load(q.s_in + srow);
+        if (!used) {
+        } else if (FULL) {
             for (int j = 1; j < seg * p.fine; ++j) {
-                const int2 ch = segment(s.len, p.segs * p.fine, j);
+                const int2 ch = segment(s.len, segs * p.fine, j);
                 float sum = 0.0f;
                 for (int c = ch.x; c < ch.y; ++c) sum += p.total[chunk_at(s, b, c) * q.H + head];
                 const float e = exp2f(sum), *next = part(j + 1);
@@ -641,7 +646,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             tc_fence_before();
             arrive(A_MADE + bs);
         }
-        float *out = FULL ? (seg == p.segs - 1 && q.s_out && srow >= 0 ? q.s_out + srow : nullptr) : part(seg + 1);
+        float *out = !used ? nullptr : !FULL ? part(seg + 1) : seg == segs - 1 && q.s_out && srow >= 0 ? q.s_out + srow : nullptr;
         if (ok && out) store(out);
     } else {
         // ---------------- the outputs
