@@ -13,7 +13,8 @@
 // unaligned rows, or up to 8192 values: a block (or a warp) a row, straight from
 // global memory.  Longer rows: a block a row, the row read again for each statistic.
 // 8190 x 4096, bf16 with an fp32 residual: the block a row took 208 us (the loads of
-// a block wait while it reduces, and the weights go through L1 for every row).
+// a block wait while it reduces, and the weights go through L1 for every row), the ring
+// takes 82: 5700 GB/s, 84% of a copy's.
 #include <algorithm>
 
 #include "tc_common.cuh"

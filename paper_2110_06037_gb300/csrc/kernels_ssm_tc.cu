@@ -27,7 +27,7 @@
 // blocks an SM, a chunk took a block 17.9 thousand cycles of waiting for one step after
 // the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128).  So: 151 us, of
 // which 7 are the time steps, 30 the first pass, 115 the second, 7000 cycles a chunk.
-// The tensor cores are busy in 45% of them, the busiest scheduler issues in 65%; what
+// The tensor cores are busy in 38% of them, the busiest scheduler issues in 55%; what
 // bounds it is the way from the pairs to P and to the next pairs.  (Tried and no faster: the next
 // chunk's pairs ahead, in TMEM of their own, 163; X' by the state's warps, 163; P's
 // columns 32 at a time, 165.)
