@@ -217,7 +217,9 @@ cudaError_t conv_width(int W, const SeqArgs &q, const T *x, int64_t ldx, T *y, i
 // tokens, so few rows are spread over segments of the sequence: a first pass makes
 // every segment's state from nothing, the second starts from the joined ones.
 // Six sequences, 1030 tokens the longest, 6 heads of 48 x 40: in one piece 256 us, cut
-// all alike 45, each by its own length 36; the two passes' latencies are what is left.
+// all alike 45, each by its own length 36, the blocks with work first 32; the two
+// passes' latencies are what is left.  (Segments of 32 tokens: 31, but 98 for 61 for one
+// sequence of 2048 tokens and 4 heads of 64 x 128, whose segments are joined longer.)
 constexpr int RT = 16, SEG_MIN = 64;  // tokens of a run, and of a segment at least
 
 struct RecP {
@@ -232,6 +234,37 @@ __device__ __forceinline__ int2 rec_segment(int len, int segs, int g) {  // toke
     return make_int2(min(len, (int)((int64_t)runs * g / segs) * RT), min(len, (int)((int64_t)runs * (g + 1) / segs) * RT));
 }
 
+// What block `id` works on: each sequence has its own segments but the `but` last, and
+// `blocks` blocks to each.  The blocks that have work so are the first of the grid and
+// spread over the multiprocessors evenly.  Called by whole warps.
+struct Place {
+    int b, seg, block;  // b < 0: nothing
+};
+__device__ __forceinline__ Place rec_place(const SeqArgs &q, int most, int but, int blocks, int id) {
+    const int lane = threadIdx.x % 32;
+    int rest = id / blocks;  // the segment's number among all
+    if (!q.offsets || most == 1) {  // all alike
+        const int n = (q.offsets ? 1 : rec_own((int)q.max_len, most)) - but;
+        return n > 0 && rest / n < q.batch ? Place{rest / n, rest % n, id % blocks} : Place{-1, 0, 0};
+    }
+    for (int b0 = 0; b0 < q.batch; b0 += 32) {
+        const int n = b0 + lane < q.batch ? rec_own(sequence(q, b0 + lane).len, most) - but : 0;
+        int up = n;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int v = __shfl_up_sync(0xffffffffu, up, o);
+            if (lane >= o) up += v;
+        }
+        const uint32_t in = __ballot_sync(0xffffffffu, rest < up);
+        if (in) {
+            const int k = __ffs(in) - 1;
+            return Place{b0 + k, rest - (__shfl_sync(0xffffffffu, up, k) - __shfl_sync(0xffffffffu, n, k)), id % blocks};
+        }
+        rest -= __shfl_sync(0xffffffffu, up, 31);
+    }
+    return Place{-1, 0, 0};
+}
+
 // FULL: the outputs; otherwise a segment's state from nothing (segment 0: from s_in)
 template <typename T, int NL, bool FULL>
 __global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant__ RecP p, const T *__restrict__ xbc,
@@ -242,11 +275,12 @@ __global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant
     griddep_launch();
     griddep_wait();
     const SsmP &q = p.s;
-    const int pblocks = (q.P + 31) / 32, head = blockIdx.x / pblocks, p0 = blockIdx.x % pblocks * 32, seg = blockIdx.y;
-    const int tid = threadIdx.x, row = p0 + tid / 8, l = tid % 8, b = blockIdx.z;
+    const int pblocks = (q.P + 31) / 32, blocks = q.H * pblocks, tid = threadIdx.x, l = tid % 8;
+    const Place at = rec_place(q.q, p.segs, FULL ? 0 : 1, blocks, blockIdx.x);
+    if (at.b < 0) return;
+    const int b = at.b, seg = at.seg, head = at.block / pblocks, p0 = at.block % pblocks * 32, row = p0 + tid / 8;
     const Seq s = sequence(q.q, b);
     const int segs = rec_own(s.len, p.segs);
-    if (seg >= (FULL ? segs : segs - 1)) return;
     const int2 tok = rec_segment(s.len, segs, seg);
     const int grp = head / (q.H / q.G), np = min(32, q.P - p0);
     const float a = q.a[head], dskip = q.d ? q.d[head] : 0.0f, dtb = q.dt_bias ? q.dt_bias[head] : 0.0f;
@@ -391,13 +425,13 @@ int64_t rec_workspace(const SsmP &p) {
 
 template <typename T, int NL>
 cudaError_t launch_rec(const RecP &p, const T *xbc, const T *dtv, T *y, cudaStream_t st) {
-    const unsigned heads = (unsigned)(p.s.H * ((p.s.P + 31) / 32)), batch = (unsigned)p.s.q.batch;
+    const int64_t blocks = (int64_t)p.s.H * ((p.s.P + 31) / 32) * p.s.q.batch;
+    if (blocks * p.segs > INT32_MAX) return cudaErrorInvalidValue;
     if (p.segs > 1) {
-        const cudaError_t e = launch_pdl(ssm_scan_rec_kernel<T, NL, false>, dim3(heads, (unsigned)(p.segs - 1), batch), dim3(256), 0, st, p, xbc,
-                                         dtv, y);
+        const cudaError_t e = launch_pdl(ssm_scan_rec_kernel<T, NL, false>, dim3((unsigned)(blocks * (p.segs - 1))), dim3(256), 0, st, p, xbc, dtv, y);
         if (e != cudaSuccess) return e;
     }
-    return launch_pdl(ssm_scan_rec_kernel<T, NL, true>, dim3(heads, (unsigned)p.segs, batch), dim3(256), 0, st, p, xbc, dtv, y);
+    return launch_pdl(ssm_scan_rec_kernel<T, NL, true>, dim3((unsigned)(blocks * p.segs)), dim3(256), 0, st, p, xbc, dtv, y);
 }
 
 template <typename T>
