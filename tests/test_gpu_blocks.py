@@ -463,6 +463,31 @@ def test_scan_of_long_prompts_with_few_heads(dt, lens, sizes):
     assert torch.equal(again, y) and torch.equal(state, out)
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("lens, apart", [([5, 0, 70] * 12 + [900, 1, 300], True), ([700, 700], False)])
+def test_scan_cuts_each_sequence_by_its_own_length(dt, lens, apart):
+    """More sequences than a warp looks over at once, few of them long; and a batch of equal ones."""
+    import torch
+    import paper_2110_06037_gb300 as sn
+    h, p, g, n = sizes = 1, 32, 1, 16
+    rng = np.random.default_rng(len(lens))
+    a, d, b = ssm_weights(rng, h)
+    rows, c = sum(lens), h * p + 2 * g * n
+    xbc, step = dev(rng.normal(size=(rows, c)), dt), dev(rng.normal(size=(rows, h)) - 2, dt)
+    state = dev(rng.normal(size=(len(lens), h, p, n)))
+    slots = list(range(len(lens)))
+    ref, my, sref, ms = run_scan(host(xbc), host(step), lens, sizes, a, d, b, host(state), slots)
+    ssm = sn.StateSpace(h, p, g, n, dev(a), dev(d), dev(b))
+    out = torch.empty_like(state)
+    if apart:
+        off = ints(np.concatenate(([0], np.cumsum(lens))).tolist())
+        y = ssm.scan(xbc, step, offsets=off, max_len=max(lens), state_in=state, state_out=out)
+    else:
+        y = ssm.scan(xbc.unflatten(0, (len(lens), -1)), step.unflatten(0, (len(lens), -1)), state_in=state, state_out=out).flatten(0, 1)
+    close(y, ref, scan_bound(my, max(lens)) + (2.0 ** -14 * my if dt != "f32" else 0), dt)
+    close(out, sref, scan_bound(ms, max(lens)), "f32")
+
+
 @pytest.mark.parametrize("lens, sizes", [
     ([16], (1, 64, 1, 128)), ([127, 0, 1, 130, 64], (3, 64, 3, 64)), ([129], (8, 64, 2, 128)), ([385, 5], (2, 32, 1, 96)),
     ([256, 256], (2, 40, 2, 24)), ([300], (2, 8, 1, 8)), ([40, 500], (2, 136, 1, 104)), ([128] * 9, (4, 64, 1, 16)),
