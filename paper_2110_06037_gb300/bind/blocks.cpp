@@ -62,14 +62,18 @@ Rows rows_of(const Tensor &t, int64_t width, const char *what, std::optional<at:
     r.p = t.data_ptr();
     r.n = 1;
     // leading axes of more than one entry, from the last: each a multiple of the one behind it
+    // (an expanded axis, of stride 0, is none: its rows are not apart)
     int64_t expect = 0;
+    bool seen = false;
     for (int64_t i = d - 2; i >= 0; --i) {
-        const int64_t n = t.size(i);
+        const int64_t n = t.size(i), stride = t.stride(i);
         r.n *= n;
         if (n == 1 || t.numel() == 0) continue;
-        if (expect == 0) r.ld = t.stride(i);
-        else if (t.stride(i) != expect) refuse(std::string("the leading axes of ") + what + " do not collapse to evenly spaced rows");
-        expect = t.stride(i) * n;
+        if (stride == 0) refuse(std::string("the rows of ") + what + " lie on one another (an expanded axis)");
+        if (!seen) r.ld = stride;
+        else if (stride != expect) refuse(std::string("the leading axes of ") + what + " do not collapse to evenly spaced rows");
+        seen = true;
+        expect = stride * n;
     }
     if (r.n <= 1) r.ld = std::max(r.ld, width);
     return r;
