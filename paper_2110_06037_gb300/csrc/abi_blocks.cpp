@@ -136,6 +136,7 @@ sn_status sn_q4_dense(const sn_q4_weights *w, int32_t dtype, int64_t rows, const
         if (rows > kMaxRows) return fail(SN_EUNSUPPORTED, "sn_q4_dense: more than 2^31 - 1 rows");
         if (sn_status rc = rows_of(name, x, x_stride, w->k, dtype, "x")) return rc;
         if (sn_status rc = rows_of(name, y, y_stride, w->n, dtype, "y")) return rc;
+        SN_NEED(y != x, "y over x");
         const int64_t need = (int64_t)k::q4_workspace(*w, dtype, rows, x, x_stride);
         SN_NEED(need == 0 || (work && aligned(work, 256) && work_bytes >= need),
                 "needs " + std::to_string(need) + " bytes of scratch aligned to 256 (sn_q4_workspace)");
