@@ -4,7 +4,8 @@ Every translation unit under csrc/ is compiled by nvcc in parallel for
 sm_103a only, then linked with the static CUDA runtime into libsn.so next to
 this file.  Host code is portable C++17 (x86_64 here, aarch64 on the GPU host).
 bind/blocks.cpp, the tensor front end of the block operators, is compiled beside
-them against PyTorch's headers and linked to libsn.so as the module _blocks.
+them against PyTorch's headers and linked to libsn.so as the module _blocks, where
+PyTorch is installed: the library itself needs nvcc alone.
 """
 from __future__ import annotations
 
@@ -57,7 +58,7 @@ def _compile(src, verbose):
 
 def _torch_dir():
     spec = importlib.util.find_spec("torch")  # found, not imported
-    return os.path.dirname(spec.origin)
+    return os.path.dirname(spec.origin) if spec is not None and spec.origin else None
 
 
 def _compile_bind():
@@ -88,11 +89,11 @@ def build(verbose: bool = False, jobs: int | None = None) -> str:
     os.makedirs(BUILD, exist_ok=True)
     srcs = _sources()
     with cf.ThreadPoolExecutor(max_workers=jobs or min(16, os.cpu_count() or 4)) as ex:
-        bind = ex.submit(_compile_bind)
+        bind = ex.submit(_compile_bind) if _torch_dir() else None
         objs = list(ex.map(lambda s: _compile(s, verbose), srcs))
-        bind = bind.result()
-    _link(objs)
-    _link_bind(bind)
+        _link(objs)  # first: what becomes of the front end does not touch the library
+        if bind is not None:
+            _link_bind(bind.result())
     return LIB
 
 
