@@ -92,6 +92,22 @@ void *whole(const Opt &t, at::IntArrayRef shape, at::ScalarType dtype, const cha
 const int32_t *index_of(const Opt &t, int64_t n, const char *what) {
     return static_cast<const int32_t *>(whole(t, {n}, at::kInt, what));
 }
+// what a call takes beside its first tensor: on the same device (a handle's weights are on
+// `handle`, -1 where it has none)
+struct Device {
+    int index;
+    Device(const Tensor &first, int handle) : index(first.is_cuda() ? first.get_device() : -1) {
+        if (handle >= 0 && index >= 0 && handle != index)
+            refuse("the handle's weights are on device " + std::to_string(handle) + ", the call's tensors on " + std::to_string(index));
+    }
+    void same(const Tensor &t, const char *what) const {
+        if (index >= 0 && (!t.is_cuda() || t.get_device() != index))
+            refuse(std::string(what) + " is on " + t.device().str() + ", the call's first tensor on device " + std::to_string(index));
+    }
+    void same(const Opt &t, const char *what) const {
+        if (t) same(*t, what);
+    }
+};
 // an output: the caller's, or a new one
 Tensor output(const Opt &out, at::IntArrayRef shape, at::ScalarType dtype, const Tensor &like, const char *what) {
     if (!out) return at::empty(shape, like.options().dtype(dtype));
@@ -106,10 +122,11 @@ at::DimVector shape_with(const Tensor &t, int64_t last) {
 void *stream_of(const Tensor &t) { return c10::cuda::getCurrentCUDAStream(t.get_device()).stream(); }
 Tensor scratch(int64_t bytes, const Tensor &like) { return at::empty({bytes}, like.options().dtype(at::kByte)); }
 
-Tensor dense_q4(intptr_t handle, const Tensor &x, const Opt &out) {
+Tensor dense_q4(intptr_t handle, int device, const Tensor &x, const Opt &out) {
     const auto *w = reinterpret_cast<const sn_q4_weights *>(handle);
     const int dt = dtype_of(x.scalar_type(), "x");
     const Rows r = rows_of(x, w->k, "x");
+    Device(x, device).same(out, "out");
     const c10::cuda::CUDAGuard guard(x.device());
     Tensor y = output(out, shape_with(x, w->n), x.scalar_type(), x, "out");
     const Rows o = rows_of(y, w->n, "out");
@@ -121,7 +138,7 @@ Tensor dense_q4(intptr_t handle, const Tensor &x, const Opt &out) {
     return y;
 }
 
-py::tuple block_norm(intptr_t handle, const Opt &y, const Opt &residual, const Opt &gate, int64_t per, const Opt &out,
+py::tuple block_norm(intptr_t handle, int device, const Opt &y, const Opt &residual, const Opt &gate, int64_t per, const Opt &out,
                      const Opt &out_normed, const std::optional<at::ScalarType> &dtype) {
     const auto *p = reinterpret_cast<const sn_norm_params *>(handle);
     if (!y && !residual) refuse("neither y nor residual");
@@ -129,6 +146,8 @@ py::tuple block_norm(intptr_t handle, const Opt &y, const Opt &residual, const O
     const at::ScalarType type = y || !dtype ? first.scalar_type() : *dtype;
     const int64_t d = p->dim;
     const int dt = dtype_of(type, "rows");
+    const Device on(first, device);
+    on.same(residual, "residual"), on.same(gate, "gate"), on.same(out, "out"), on.same(out_normed, "out_normed");
     Rows ry, rr, rg, rs, rn;
     int rdt = dt;
     int64_t rows = 0;
@@ -181,6 +200,9 @@ Tensor causal_conv(const Tensor &x, const Tensor &weight, const Opt &bias, bool 
     if (weight.dim() != 2) refuse("weight must be [channels, width]");
     const int64_t c = weight.size(0), width = weight.size(1);
     const int dt = dtype_of(x.scalar_type(), "x");
+    const Device on(x, -1);
+    on.same(weight, "weight"), on.same(bias, "bias"), on.same(offsets, "offsets"), on.same(kept, "kept");
+    on.same(slots, "slots"), on.same(pos, "pos"), on.same(out, "out");
     const Batch b = batch_of(x, offsets, max_len);
     const Rows r = rows_of(x, c, "x");
     const int64_t n = kept ? kept->size(0) : b.n;
@@ -209,10 +231,13 @@ States states_of(const sn_ssm_params *p, const Opt &in, const Opt &out, int64_t 
 }
 int64_t channels_of(const sn_ssm_params *p) { return (int64_t)p->heads * p->head_dim + 2LL * p->groups * p->state; }
 
-Tensor scan(intptr_t handle, const Tensor &xbc, const Tensor &dt, const Opt &offsets, const std::optional<int64_t> &max_len,
+Tensor scan(intptr_t handle, int device, const Tensor &xbc, const Tensor &dt, const Opt &offsets, const std::optional<int64_t> &max_len,
             const Opt &state_in, const Opt &state_out, const Opt &slots, const Opt &out) {
     const auto *p = reinterpret_cast<const sn_ssm_params *>(handle);
     const int code = dtype_of(xbc.scalar_type(), "xbc");
+    const Device on(xbc, device);
+    on.same(dt, "dt"), on.same(offsets, "offsets"), on.same(state_in, "state_in"), on.same(state_out, "state_out");
+    on.same(slots, "slots"), on.same(out, "out");
     const Batch b = batch_of(xbc, offsets, max_len);
     const Rows r = rows_of(xbc, channels_of(p), "xbc"), rd = rows_of(dt, p->heads, "dt", xbc.scalar_type());
     if (rd.n != b.tokens) refuse("dt and xbc have different tokens");
@@ -230,10 +255,13 @@ Tensor scan(intptr_t handle, const Tensor &xbc, const Tensor &dt, const Opt &off
     return y;
 }
 
-Tensor step(intptr_t handle, const Tensor &xbc, const Tensor &dt, const Tensor &kept, const Tensor &state, const Opt &pos, const Opt &state_out,
+Tensor step(intptr_t handle, int device, const Tensor &xbc, const Tensor &dt, const Tensor &kept, const Tensor &state, const Opt &pos, const Opt &state_out,
             const Opt &slots, const Opt &out) {
     const auto *p = reinterpret_cast<const sn_ssm_params *>(handle);
     const int code = dtype_of(xbc.scalar_type(), "xbc");
+    const Device on(xbc, device);
+    on.same(dt, "dt"), on.same(kept, "kept"), on.same(state, "state"), on.same(pos, "pos"), on.same(state_out, "state_out");
+    on.same(slots, "slots"), on.same(out, "out");
     const Rows r = rows_of(xbc, channels_of(p), "xbc"), rd = rows_of(dt, p->heads, "dt", xbc.scalar_type());
     if (rd.n != r.n) refuse("dt and xbc have different rows");
     const States s = states_of(p, state, state_out ? state_out : Opt(state), r.n, slots.has_value());

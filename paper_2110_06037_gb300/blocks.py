@@ -13,7 +13,8 @@ Tensors are CUDA tensors of fp32, fp16 or bf16; rows may lie apart (a slice of a
 wider projection), the values of a row are contiguous.  Weights of norms,
 convolutions and scans and all states are fp32.  Calls run on `stream` (default:
 PyTorch's current one) and return without waiting; what they allocate is allocated
-for that stream.  Bad arguments raise SnError with the library's status.
+for that stream.  They run on the device of their tensors, which is one for all of a
+call's tensors and its handle's.  Bad arguments raise SnError with the library's status.
 
 Handles (Q4Weights, BlockNorm, StateSpace) keep their weight tensors alive and hold
 nothing else between calls.  The calls themselves go through the native module
@@ -52,6 +53,21 @@ def _refuse(msg):
 def _on(stream):
     """Context in which PyTorch's current stream, whose allocations and launches these are, is `stream`."""
     return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+
+
+@contextlib.contextmanager
+def _beside(t, stream):
+    """The same for a handle's setting up, on the device of `t`."""
+    with _torch().cuda.device(t.device if t.is_cuda else None), _on(stream):
+        yield
+
+
+def _device_of(*tensors):
+    """Index of the one device that the tensors (None: no tensor) are on, -1 without any."""
+    found = sorted({t.get_device() for t in tensors if t is not None})
+    if len(found) > 1:
+        _refuse(f"a handle's weights are on several devices: {found}")
+    return found[0] if found else -1
 
 
 def _dtype_code(dtype, what):
@@ -93,11 +109,11 @@ def quantize_q4(w, group=64, scale_dtype=None, stream=None):
     if scale_dtype not in (torch.float16, torch.bfloat16):
         _refuse("scale_dtype must be torch.float16 or torch.bfloat16")
     dt, ptr = _dtype_code(w.dtype, "w"), _whole(w, (n, k), w.dtype, "w")
-    with _on(stream):
+    with _beside(w, stream):
         codes = torch.empty((n, (k + 1) // 2), dtype=torch.uint8, device=w.device)
         scales = torch.empty((n, -(-k // group)), dtype=scale_dtype, device=w.device)
-    check(lib().sn_q4_quantize(ptr, dt, n, k, group, _dtype_code(scale_dtype, "scales"), codes.data_ptr(), scales.data_ptr(),
-                               _stream_ptr(stream)))
+        check(lib().sn_q4_quantize(ptr, dt, n, k, group, _dtype_code(scale_dtype, "scales"), codes.data_ptr(), scales.data_ptr(),
+                                   _stream_ptr(stream)))
     return codes, scales
 
 
@@ -118,21 +134,22 @@ class Q4Weights:
         cp = _whole(codes, (n, (k + 1) // 2), torch.uint8, "codes")
         sp = _whole(scales, (n, -(-k // group)), scales.dtype, "scales")
         bp = _whole(bias, (n,), torch.float32, "bias")
-        with _on(stream):
+        self.device = _device_of(codes, scales, bias)
+        with _beside(codes, stream):
             self.packed = torch.empty((nbytes.value,), dtype=torch.uint8, device=codes.device)
-        self.bias, self.n, self.k, self.group, self.act = bias, n, k, group, act
-        self._c = _sn.sn_q4_weights(n, k, group, _dtype_code(scales.dtype, "scales"), _sn.SN_ACT[act], self.packed.data_ptr(), bp)
-        self._at = C.addressof(self._c)
-        check(lib().sn_q4_pack(cp, sp, C.byref(self._c), _stream_ptr(stream)))
+            self.bias, self.n, self.k, self.group, self.act = bias, n, k, group, act
+            self._c = _sn.sn_q4_weights(n, k, group, _dtype_code(scales.dtype, "scales"), _sn.SN_ACT[act], self.packed.data_ptr(), bp)
+            self._at = C.addressof(self._c)
+            check(lib().sn_q4_pack(cp, sp, C.byref(self._c), _stream_ptr(stream)))
         self._dense = _load().dense_q4
 
 
 def dense_q4(x, w, out=None, stream=None):
     """y = act(x W^T + bias) with 4-bit weights: x [..., k] -> [..., n] of x's type, for any number of rows."""
     if stream is None:
-        return w._dense(w._at, x, out)
+        return w._dense(w._at, w.device, x, out)
     with _on(stream):
-        return w._dense(w._at, x, out)
+        return w._dense(w._at, w.device, x, out)
 
 
 # ------------------------------------------------------------------- norms
@@ -154,6 +171,7 @@ class BlockNorm:
         f32 = _torch().float32
         ptrs = [_whole(t, (self.dim,), f32, what)
                 for t, what in zip(self.weights, ("post", "post_bias", "pre", "pre_bias", "scale"))]
+        self.device = _device_of(*self.weights)
         self._c = _sn.sn_norm_params(self.dim, NORM_KINDS[kind], GATES[gate], int(gate_at == "after"), eps, *ptrs)
         self._at = C.addressof(self._c)
         self._norm = _load().block_norm
@@ -163,9 +181,9 @@ class BlockNorm:
         without pre weights.  y None: total is the residual itself (a block's first norm), and normed has
         the type `dtype` (default: the residual's).  out may be residual or y, out_normed may be y."""
         if stream is None:
-            return self._norm(self._at, y, residual, gate, rows_per_gate, out, out_normed, dtype)
+            return self._norm(self._at, self.device, y, residual, gate, rows_per_gate, out, out_normed, dtype)
         with _on(stream):
-            return self._norm(self._at, y, residual, gate, rows_per_gate, out, out_normed, dtype)
+            return self._norm(self._at, self.device, y, residual, gate, rows_per_gate, out, out_normed, dtype)
 
 
 # --------------------------------------------------- convolution and scan
@@ -206,6 +224,7 @@ class StateSpace:
             _whole(d, (self.heads,), f32, "d"), _whole(dt_bias, (self.heads,), f32, "dt_bias"),
             _whole(conv_weight, (self.channels, self.width), f32, "conv_weight"),
             _whole(conv_bias, (self.channels,), f32, "conv_bias"))
+        self.device = _device_of(*self.weights)
         self._at = C.addressof(self._c)
         self._scan, self._step = _load().scan, _load().step
 
@@ -216,15 +235,15 @@ class StateSpace:
         [entries, heads, head_dim, state]; state_in None: from zero; state_out (which may be state_in)
         receives the last ones."""
         if stream is None:
-            return self._scan(self._at, xbc, dt, offsets, max_len, state_in, state_out, slots, out)
+            return self._scan(self._at, self.device, xbc, dt, offsets, max_len, state_in, state_out, slots, out)
         with _on(stream):
-            return self._scan(self._at, xbc, dt, offsets, max_len, state_in, state_out, slots, out)
+            return self._scan(self._at, self.device, xbc, dt, offsets, max_len, state_in, state_out, slots, out)
 
     def step(self, xbc, dt, kept, state, pos, state_out=None, slots=None, out=None, stream=None):
         """One token of every sequence: xbc [batch, channels] before the convolution, dt [batch, heads],
         pos int32 [batch] (tokens that each sequence has had).  kept (as in causal_conv) is brought up to
         date in place, and so is state unless state_out is given."""
         if stream is None:
-            return self._step(self._at, xbc, dt, kept, state, pos, state_out, slots, out)
+            return self._step(self._at, self.device, xbc, dt, kept, state, pos, state_out, slots, out)
         with _on(stream):
-            return self._step(self._at, xbc, dt, kept, state, pos, state_out, slots, out)
+            return self._step(self._at, self.device, xbc, dt, kept, state, pos, state_out, slots, out)

@@ -7,6 +7,7 @@
 
 #include <cstdint>
 
+#include "per_device.h"
 #include "sn_internal.h"
 
 namespace sn {
@@ -79,6 +80,15 @@ inline int num_sms() {
         if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) n = 1;
     }
     return n;
+}
+
+// the kernel's limit of dynamic shared memory, once on each device; `set` is the kernel's own
+template <typename K>
+inline cudaError_t allow_smem(PerDevice &set, K *kern, size_t bytes) {
+    int dev = 0;
+    const cudaError_t e = cudaGetDevice(&dev);
+    if (e != cudaSuccess) return e;
+    return set.once(dev, [&] { return cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes); });
 }
 
 inline unsigned grid_for(int64_t n, int block, int64_t cap = 152LL * 64) {

@@ -481,12 +481,8 @@ __global__ void __launch_bounds__(256, 2) block_norm_ring_kernel(const __grid_co
 template <typename T, typename R, int NP>
 cudaError_t launch_ring_np(const RingP &q, int threads, cudaStream_t st) {
     const int per_sm = 512 / threads, room = 220 * 1024 / per_sm;  // blocks a multiprocessor, shared memory of each
-    static bool set = false;          // (idempotent)
-    if (!set) {
-        const cudaError_t e = cudaFuncSetAttribute(block_norm_ring_kernel<T, R, NP>, cudaFuncAttributeMaxDynamicSharedMemorySize, 110 * 1024);
-        if (e != cudaSuccess) return e;
-        set = true;
-    }
+    static PerDevice set;
+    if (const cudaError_t e = allow_smem(set, block_norm_ring_kernel<T, R, NP>, 110 * 1024)) return e;
     RingP p = q;
     p.stages = std::min(RING_MAX, room / q.stage_bytes);
     const int64_t blocks = std::min<int64_t>(q.n.a.rows, (int64_t)per_sm * num_sms());

@@ -578,12 +578,8 @@ Shape4 choose(int64_t rows, int n, int64_t steps, int widest) {
 template <typename T, typename X, int G>
 cudaError_t launch_prompt(const CUtensorMap &mX, PromptP &p, X *y, cudaStream_t st) {
     auto kern = q4_prompt_kernel<T, X, G>;
-    static bool set = false;  // (idempotent)
-    if (!set) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)Q4_SMEM);
-        if (e != cudaSuccess) return e;
-        set = true;
-    }
+    static PerDevice set;
+    if (const cudaError_t e = allow_smem(set, kern, Q4_SMEM)) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.blockDim = dim3(Q4_THREADS);
     cfg.dynamicSmemBytes = Q4_SMEM;

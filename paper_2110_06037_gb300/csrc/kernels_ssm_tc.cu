@@ -763,14 +763,9 @@ cudaError_t ssm_tc_scan(const SsmP &s, const __nv_bfloat16 *xbc, const __nv_bflo
         !tma_encode(&mB, SN_BF16, 3, xb, dim_b, str_b, box, CU_TENSOR_MAP_SWIZZLE_128B) ||
         !tma_encode(&mC, SN_BF16, 3, xc, dim_b, str_b, box, CU_TENSOR_MAP_SWIZZLE_128B))
         return cudaErrorInvalidValue;
-    static bool set = false;  // (idempotent)
-    if (!set) {
-        cudaError_t e = cudaFuncSetAttribute(ssm_scan_tc_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SCAN_SMEM);
-        if (e == cudaSuccess)
-            e = cudaFuncSetAttribute(ssm_scan_tc_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)SCAN_SMEM);
-        if (e != cudaSuccess) return e;
-        set = true;
-    }
+    static PerDevice set_full, set_states;
+    if (const cudaError_t e = allow_smem(set_full, ssm_scan_tc_kernel<true>, SCAN_SMEM)) return e;
+    if (const cudaError_t e = allow_smem(set_states, ssm_scan_tc_kernel<false>, SCAN_SMEM)) return e;
     const unsigned chunks = (unsigned)((s.q.max_len + Q - 1) / Q), heads = (unsigned)(s.H * p.pblocks);
     const int vec = s.H % 8 == 0 && s.lddt % 8 == 0 && reinterpret_cast<uintptr_t>(dtv) % 16 == 0;
     cudaError_t e = launch_pdl(ssm_steps_kernel, dim3(chunks, (unsigned)((s.H + 7) / 8), (unsigned)s.q.batch), dim3(256), 0, st, p, dtv, vec);

@@ -306,13 +306,8 @@ cudaError_t launch_few(const Q4P &q, int rows, const X *x, int64_t ldx, X *y, in
     size_t smem = (size_t)WARPS * 16 * NC * 8 * 4;
     smem += std::max((size_t)rows * PL * (p.phase * 64 + 32) * 2, (size_t)WARPS / p.wk * 16 * rows * 4);
     auto kern = q4_few_kernel<T, X, NC, GLOG, SB>;
-    static bool set = false;  // (idempotent)
-    if (!set) {
-        cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                             (int)(X_SMEM + WARPS * 16 * NC * 8 * 4 + 1024));
-        if (e != cudaSuccess) return e;
-        set = true;
-    }
+    static PerDevice set;
+    if (const cudaError_t e = allow_smem(set, kern, X_SMEM + WARPS * 16 * NC * 8 * 4 + 1024)) return e;
     const int wn = WARPS / p.wk;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)((q.nt + wn - 1) / wn * p.s));

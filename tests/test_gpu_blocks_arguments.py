@@ -40,3 +40,56 @@ def test_rows_that_lie_on_one_another_are_refused(what, axis):
     with pytest.raises(sn.SnError):
         calls(what, t)()
     calls(what, t.contiguous())()  # the same values in rows of their own
+
+
+def test_a_handle_of_another_device_is_refused():
+    import torch
+    import paper_2110_06037_gb300 as sn
+    x = torch.zeros(2, 64, device="cuda")
+    w = sn.Q4Weights(*sn.quantize_q4(torch.randn(64, 64, device="cuda")), 64, 64)
+    norm = sn.BlockNorm(64, post=torch.ones(64, device="cuda"))
+    c = 32 + 2 * 16
+    ssm = sn.StateSpace(1, 32, 1, 16, torch.zeros(1, device="cuda"), conv_weight=torch.zeros(c, 4, device="cuda"))
+    kept, state = torch.zeros(2, 4, c, device="cuda"), torch.zeros(2, 1, 32, 16, device="cuda")
+    uses = [(w, lambda: sn.dense_q4(x, w)), (norm, lambda: norm(x)), (ssm, lambda: ssm.scan(x[None], x[None, :, :1])),
+            (ssm, lambda: ssm.step(x, x[:, :1], kept, state, None))]
+    for handle, use in uses:
+        assert handle.device == x.get_device()
+        use()
+        handle.device += 1
+        with pytest.raises(sn.SnError, match="device"):
+            use()
+        handle.device -= 1
+
+
+def test_handles_are_set_up_on_the_device_of_their_tensors(monkeypatch):
+    import contextlib
+    import torch
+    import paper_2110_06037_gb300 as sn
+    entered = []
+
+    def device(d):
+        entered.append(d)
+        return contextlib.nullcontext()
+
+    t = torch.randn(8, 64, device="cuda")
+    monkeypatch.setattr(torch.cuda, "device", device)
+    codes, scales = sn.quantize_q4(t)
+    sn.Q4Weights(codes, scales, 64, 64)
+    assert entered == [t.device, t.device]
+
+
+def test_tensors_of_the_host_are_refused():
+    import torch
+    import paper_2110_06037_gb300 as sn
+    norm = sn.BlockNorm(64, post=torch.ones(64, device="cuda"), pre=torch.ones(64, device="cuda"), gate="silu")
+    x, h = torch.zeros(2, 64, device="cuda"), torch.zeros(2, 64)
+    for kw in ({"residual": h, "gate": x}, {"gate": h}, {"gate": x, "out": h}, {"gate": x, "out_normed": h}):
+        with pytest.raises(sn.SnError):
+            norm(x, **kw)
+    with pytest.raises(sn.SnError):
+        norm(h, gate=x)
+    with pytest.raises(sn.SnError):
+        sn.quantize_q4(h)
+    with pytest.raises(sn.SnError):
+        sn.causal_conv(x[None], torch.zeros(64, 4))
