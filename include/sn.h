@@ -490,9 +490,10 @@ SN_API sn_status sn_conv2d_wino_noalloc(const void *x_dev, sn_schema schema, con
  * last group of a row may be cut off); scales fp16 or bf16.
  * packed holds the weights in the kernels' own layout (sn_q4_bytes bytes of
  * device memory aligned to 256, filled by sn_q4_pack).
- * Numerics: for few rows codes times inputs are summed exactly (fp32 inputs in
- * three parts) and each group's sum is scaled in fp32; for many rows the scaled
- * weight is rounded to x's 16-bit type first (fp32 x: two parts, no rounding). */
+ * Numerics, for any number of rows: products of codes and inputs are exact (fp32
+ * inputs in three parts of 24 bits in all), a group's are added on the tensor cores,
+ * whose sums of fp32 are truncated, and each group's sum is multiplied by its scale
+ * and added in fp32.  No weight is rounded. */
 typedef struct {
     int32_t n, k, group;  /* output features, input features, weights per scale */
     int32_t scale_dtype;  /* SN_F16 or SN_BF16 */

@@ -76,26 +76,13 @@ __global__ void __launch_bounds__(256) q4_pack_kernel(const uint8_t *__restrict_
     out[id] = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// a warp a row: its scales into place, and its power of two
-__global__ void __launch_bounds__(128) q4_pack_scales_kernel(const uint16_t *__restrict__ scales, int bf16, int64_t n,
-                                                             int64_t groups, int64_t kg, int64_t nt,
-                                                             uint16_t *__restrict__ out, float *__restrict__ row_pow) {
-    const int64_t row = (int64_t)blockIdx.x * 4 + threadIdx.x / 32;
-    const int lane = threadIdx.x % 32, r = (int)(row % 16);
-    if (row >= nt * 16) return;
-    float m = 0.0f;
-    for (int64_t i = lane; i < kg; i += 32) {
-        const uint16_t s = row < n && i < groups ? scales[row * groups + i] : 0;
-        out[(row / 16 * kg + i) * 16 + (r % 8) * 2 + r / 8] = s;
-        const float v = bf16 ? __uint_as_float((uint32_t)s << 16) : __half2float(*reinterpret_cast<const __half *>(&s));
-        m = fmaxf(m, fabsf(v));
-    }
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (lane == 0) {
-        int e = 0;
-        if (m > 0.0f && m < INFINITY) frexpf(m, &e);
-        row_pow[row] = ldexpf(1.0f, max(-126, min(126, e)));
-    }
+// the scales into place, a value a thread; zeros behind the last row and group
+__global__ void __launch_bounds__(256) q4_pack_scales_kernel(const uint16_t *__restrict__ scales, int64_t n, int64_t groups,
+                                                             int64_t kg, int64_t total, uint16_t *__restrict__ out) {
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (id >= total) return;
+    const int64_t grp = id / 16 % kg, row = id / 16 / kg * 16 + id % 16 / 2 + id % 2 * 8;
+    out[id] = row < n && grp < groups ? scales[row * groups + grp] : 0;
 }
 
 // rows that fill the columns of the few-row kernel; more go to the tensor-core tiles
@@ -121,10 +108,9 @@ cudaError_t q4_pack(const uint8_t *codes, const void *scales, const sn_q4_weight
     q4_pack_kernel<<<(unsigned)((total + 255) / 256), 256, 0, st>>>(codes, w.n, w.k, l.kb, total, reinterpret_cast<uint4 *>(out));
     cudaError_t e = cudaGetLastError();
     if (e != cudaSuccess) return e;
-    q4_pack_scales_kernel<<<(unsigned)(l.nt * 4), 128, 0, st>>>(static_cast<const uint16_t *>(scales), w.scale_dtype == SN_BF16,
-                                                                w.n, groups, l.kg, l.nt,
-                                                                reinterpret_cast<uint16_t *>(out + l.scales_at),
-                                                                reinterpret_cast<float *>(out + l.pow_at));
+    const int64_t values = l.nt * l.kg * 16;
+    q4_pack_scales_kernel<<<(unsigned)((values + 255) / 256), 256, 0, st>>>(static_cast<const uint16_t *>(scales), w.n, groups, l.kg,
+                                                                            values, reinterpret_cast<uint16_t *>(out + l.scales_at));
     e = cudaGetLastError();
     return e != cudaSuccess ? e : cudaStreamSynchronize(st);
 }

@@ -12,8 +12,7 @@
 // holds q + 8.
 //
 // Scales follow: for each 16 rows and each group of columns 16 values, row g and
-// g + 8 next to each other; then a power of two for each row, at least its largest
-// |scale| (by which fp16 operands are divided so that they stay in range).
+// g + 8 next to each other.
 #pragma once
 
 #include "tc_common.cuh"
@@ -24,14 +23,13 @@ namespace k {
 struct Q4P {
     const uint4 *codes;       // [nt][kb][32]
     const uint32_t *scales;   // [nt][kg][8] pairs
-    const float *row_pow;     // [nt * 16]
     int32_t n, k, nt, kb, kg, glog;  // tiles of 16 rows, tiles of 64 columns, groups a row, log2 of the group
     int32_t scale_bf16, act;
     const float *bias;
 };
 
 struct Q4Layout {
-    int64_t nt, kb, kg, scales_at, pow_at, bytes;
+    int64_t nt, kb, kg, scales_at, bytes;
 };
 inline Q4Layout q4_layout(int64_t n, int64_t k, int group) {
     Q4Layout l;
@@ -40,15 +38,14 @@ inline Q4Layout q4_layout(int64_t n, int64_t k, int group) {
     l.kg = (l.kb * 64 + group - 1) / group;
     auto up = [](int64_t v) { return (v + 255) / 256 * 256; };
     l.scales_at = up(l.nt * l.kb * 512);
-    l.pow_at = l.scales_at + up(l.nt * l.kg * 32);
-    l.bytes = l.pow_at + up(l.nt * 64);
+    l.bytes = l.scales_at + up(l.nt * l.kg * 32);
     return l;
 }
 inline Q4P q4_params(const sn_q4_weights &w) {
     const Q4Layout l = q4_layout(w.n, w.k, w.group);
     const char *p = static_cast<const char *>(w.packed);
     return Q4P{reinterpret_cast<const uint4 *>(p), reinterpret_cast<const uint32_t *>(p + l.scales_at),
-               reinterpret_cast<const float *>(p + l.pow_at), w.n, w.k, (int32_t)l.nt, (int32_t)l.kb, (int32_t)l.kg,
+               w.n, w.k, (int32_t)l.nt, (int32_t)l.kb, (int32_t)l.kg,
                w.group == 32 ? 5 : w.group == 64 ? 6 : 7, w.scale_dtype == SN_BF16, w.act, w.bias};
 }
 

@@ -282,6 +282,16 @@ __device__ __forceinline__ void umma_one(uint32_t one, uint32_t d, uint64_t a, u
             ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
             : "memory");
 }
+// umma_one with A from TMEM: a lane's row, two bf16 values a column
+__device__ __forceinline__ void umma_ts_one(uint32_t one, uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "setp.ne.b32 q, %5, 0;\n\t"
+        "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"(acc), "r"(one)
+        : "memory");
+}
 template <int G>
 __device__ __forceinline__ void commit_one(uint32_t one, uint64_t *bar) {
     if constexpr (G == 2)
