@@ -11,7 +11,8 @@
 //   inside  P X         128 x P,   K = 128     P (the pairs, weighted) in two parts, from TMEM
 //   made    B^T X'      N x P,     K = 128     X' = weighted X in three parts
 // x, B and C are bf16, exact operands; what is computed goes in as bf16 parts: two for
-// the outputs, which are bf16 (2^-18 is lost), three for the state, which goes on in
+// the outputs, which are bf16 (2^-18 of a factor is lost, and by the decays up to 2^-14 of a
+// term, see TABLE), three for the state, which goes on in
 // fp32 (off by 9e-8 of itself; with two parts 2.4e-6, and 9 us less for 8192 tokens).
 // It stays in registers: each chunk's product is added by an fp32 multiply-add, since
 // the tensor core's own sums do not round to nearest.
@@ -25,8 +26,8 @@
 // Each product has warps of its own for what goes into and comes out of it, so that
 // only the state's one multiply-add a chunk runs from chunk to chunk: in one order, two
 // blocks an SM, a chunk took a block 17.9 thousand cycles of waiting for one step after
-// the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128).  So: 151 us, of
-// which 7 are the time steps, 30 the first pass, 115 the second, 7000 cycles a chunk.
+// the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128).  So: 156 us, of
+// which 7 are the time steps, 31 the first pass, 118 the second, 7200 cycles a chunk.
 // The tensor cores are busy in 38% of them, the busiest scheduler issues in 55%; what
 // bounds it is the way from the pairs to P and to the next pairs.  (Tried and no faster: the next
 // chunk's pairs ahead, in TMEM of their own, 163; X' by the state's warps, 163; P's
@@ -50,8 +51,13 @@ constexpr int Q = 128;          // tokens a chunk
 constexpr int PB = 64;          // channels a block
 constexpr float LOG2E = 1.4426950408889634f;
 
-// per chunk and head: A_t (inclusive, in units of log 2), A_s - log2 d_s, weights d_s e^{A_127 - A_s}
-constexpr int TABLE = 3 * Q;
+// Per chunk and head, in units of log 2, v_t = d_t a: A_t, the sum of v from the chunk's start to t;
+// weights for the state d_s e^{A_127 - A_s}; and for the pairs' weights, by blocks of 16 tokens:
+// R_t, the sum from the block's start to t; log2 d_s - R_s; d; what lies between blocks.  A pair's decay is
+// R_t - R_s and the sums of the blocks from s's to t's: a difference of sums of 16 steps, those
+// below -126 as -126 (nothing passes them).  It is off by 2^-24 of such sums; a difference A_t - A_s is by
+// that of a chunk's, 1e-3 where steps with a = -16 are 20, and the diagonal's weight, d_t, with it.
+constexpr int TAB_W = Q, TAB_F = 2 * Q, TAB_R = 3 * Q, TAB_D = 4 * Q, TAB_S = 5 * Q, TABLE = 5 * Q + 64;
 
 struct TcP {
     SsmP s;
@@ -123,19 +129,47 @@ __global__ void __launch_bounds__(256) ssm_steps_kernel(const __grid_constant__ 
         float before = __shfl_up_sync(0xffffffffu, up, 1), behind = __shfl_down_sync(0xffffffffu, down, 1);
         if (lane == 0) before = 0.0f;
         if (lane == 31) behind = 0.0f;
-        float4 A, B, W;
+        float4 A, W;
         A.x = before + v[0], A.y = A.x + v[1], A.z = A.y + v[2], A.w = A.z + v[3];
-        B = make_float4(A.x - log2f(d[0]), A.y - log2f(d[1]), A.z - log2f(d[2]), A.w - log2f(d[3]));
         float r = behind;
         W.w = d[3] * exp2f(r), r += v[3];
         W.z = d[2] * exp2f(r), r += v[2];
         W.y = d[1] * exp2f(r), r += v[1];
         W.x = d[0] * exp2f(r);
+        // the sums inside blocks of 16 tokens, four lanes each
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = v[i] < -126.0f ? -126.0f : v[i];  // (NaN stays)
+        const float low = (v[0] + v[1]) + (v[2] + v[3]);
+        up = low;
+#pragma unroll
+        for (int o = 1; o < 4; o *= 2) {
+            const float x = __shfl_up_sync(0xffffffffu, up, o, 4);
+            if (lane % 4 >= o) up += x;
+        }
+        before = __shfl_up_sync(0xffffffffu, up, 1, 4);
+        if (lane % 4 == 0) before = 0.0f;
+        float4 R;
+        R.x = before + v[0], R.y = R.x + v[1], R.z = R.y + v[2], R.w = R.z + v[3];
         const int64_t at = chunk_at(s, b, c) * p.s.H + head;
-        float4 *out = reinterpret_cast<float4 *>(p.table + at * TABLE);
-        out[lane] = A;
-        out[Q / 4 + lane] = B;
-        out[Q / 2 + lane] = W;
+        float *tab = p.table + at * TABLE;
+        auto put = [&](int which, const float4 &f) { *reinterpret_cast<float4 *>(tab + which + 4 * lane) = f; };
+        put(0, A);
+        put(TAB_W, W);
+        put(TAB_F, make_float4(log2f(d[0]) - R.x, log2f(d[1]) - R.y, log2f(d[2]) - R.z, log2f(d[3]) - R.w));
+        put(TAB_R, R);
+        put(TAB_D, make_float4(d[0], d[1], d[2], d[3]));
+        // the sums of the blocks from kb to t's, for t in block e / 8 and the four kb of each half of P's warps
+        float between[2] = {0.0f, 0.0f};
+#pragma unroll
+        for (int k = 0; k < Q / 16; ++k) {
+            const float sum = __shfl_sync(0xffffffffu, R.w, 4 * k + 3);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int e = lane + 32 * i, kb = 4 * (e % 4 / 2) + 2 * (e / 4 % 2) + e % 2;
+                between[i] += k >= kb && k < e / 8 ? sum : 0.0f;
+            }
+        }
+        tab[TAB_S + lane] = between[0], tab[TAB_S + 32 + lane] = between[1];
         if (lane == 31) p.total[at] = A.w;
     }
 }
@@ -221,7 +255,7 @@ enum Bar {
     M_PAIRS = E_X + 2, M_CARRIED, M_INSIDE, M_MADE, A_XW = M_MADE + 2, A_MADE = A_XW + 2, A_STATE = A_MADE + 2, A_P, A_OUT, BARS
 };
 struct Shared {
-    alignas(16) float as[2][Q];  // A_s - log2 d_s of a chunk
+    alignas(16) float fs[2][Q];  // TAB_F of a chunk
     uint64_t bar[BARS];
     uint32_t tmem;
     int abort, any_bad[2];
@@ -378,7 +412,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                 for (int part = 0; part < 2; ++part)
 #pragma unroll
                     for (int k = 0; k < Q / 16; ++k)
-                        umma_ts_one(one, tmem + T_Y1, tmem + (part ? T_LO + k * 8 : T_S + (k / 2) * 32 + (k % 2) * 8), dx + mn_major(k),
+                        umma_ts_one(one, tmem + T_Y1, tmem + (part ? T_LO + k * 8 : T_S + k * 16), dx + mn_major(k),
                                     FMT | N64 | B_MN, part > 0 || k > 0);
                 commit_one<1>(one, &sh.bar[M_INSIDE]);
                 commit_one<1>(one, &sh.bar[E_X + st]);
@@ -427,11 +461,11 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
     } else if (warp < STATE0) {
         // ---------------- X', XT threads a row
         const int tid = threadIdx.x - 64, t = tid / XT, j0 = 8 / XT * (tid % XT);
-        float w_next = nc > 0 ? __ldg(table(0) + 2 * Q + t) : 0.0f;
+        float w_next = nc > 0 ? __ldg(table(0) + TAB_W + t) : 0.0f;
         auto weigh = [&](int c) {
             const int st = c & 1, bs = c % STAGES1, valid = min(Q, s.len - (chunks.x + c) * Q);  // tokens there are
             const float w = w_next;
-            if (c + 1 < nc) w_next = __ldg(table(c + 1) + 2 * Q + t);
+            if (c + 1 < nc) w_next = __ldg(table(c + 1) + TAB_W + t);
             must(F_X + st, (uint32_t)(c >> 1) & 1u);
             const uint32_t n = c / STAGES1;
             if (n > 0) must(M_MADE + bs, (n - 1) & 1u);  // the X' before has been read
@@ -489,19 +523,24 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             // the factor of x itself, joins the diagonal.  After it the next chunk's X'
             const int quarter = warp % 4, half = (warp - 2) / 4;
             const float skip = q.d ? q.d[head] : 0.0f;
-            float at_next = 0.0f, as_next = 0.0f;  // of the next chunk: A of this row, A_s - log2 d_s of token tid (tid < 128)
+            // of the next chunk: this row's TAB_R and TAB_D; TAB_F of token tid (tid < 128)
+            float r_next = 0.0f, d_next = 0.0f, f_next = 0.0f;
             auto fetch = [&](int c) {
                 if (c >= nc) return;
-                at_next = __ldg(table(c) + row);
-                if (tid < Q) as_next = __ldg(table(c) + Q + tid);
+                const float *tab = table(c);
+                r_next = __ldg(tab + TAB_R + row), d_next = __ldg(tab + TAB_D + row);
+                if (tid < Q) f_next = __ldg(tab + TAB_F + tid);
             };
             fetch(0);
 #pragma unroll 1
             for (int c = -1; c < nc; ++c) {
                 if (c >= 0) {
                     const uint32_t par = c & 1;
-                    const float At = at_next;
-                    if (tid < Q) sh.as[par][tid] = as_next;  // (its last readers, two chunks ago, have passed the barrier since)
+                    const float dt = d_next;
+                    // R_t and what lies between, for the four times 16 columns at hand
+                    float4 base = __ldg(reinterpret_cast<const float4 *>(table(c) + TAB_S) + row / 16 * 2 + half);
+                    base.x += r_next, base.y += r_next, base.z += r_next, base.w += r_next;
+                    if (tid < Q) sh.fs[par][tid] = f_next;  // (its last readers, two chunks ago, have passed the barrier since)
                     fetch(c + 1);
                     if (bar_red_or(1, 256, !ok)) break;  // (the group leaves together)
                     if (!must(M_PAIRS, par)) continue;
@@ -517,21 +556,22 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                             float f[16];
                             F2 v[8];
                             tmem_ld16(tmem + lanes + T_S + c0, f);
+                            const float from = i == 0 ? base.x : i == 1 ? base.y : i == 2 ? base.z : base.w;
 #pragma unroll
                             for (int j = 0; j < 4; ++j) {
-                                const float4 As = *reinterpret_cast<const float4 *>(&sh.as[par][c0 + 4 * j]);
-                                const float2 a = floats(fma_2(f2(As.x, As.y), f2(-1.0f, -1.0f), f2(At, At)));
-                                const float2 b = floats(fma_2(f2(As.z, As.w), f2(-1.0f, -1.0f), f2(At, At)));
+                                const float4 t = *reinterpret_cast<const float4 *>(&sh.fs[par][c0 + 4 * j]);
+                                const float2 a = floats(add_2(f2(t.x, t.y), f2(from, from)));
+                                const float2 b = floats(add_2(f2(t.z, t.w), f2(from, from)));
                                 v[2 * j] = mul_2(f2(f[4 * j], f[4 * j + 1]), f2(ex2(a.x), ex2(a.y)));
                                 v[2 * j + 1] = mul_2(f2(f[4 * j + 2], f[4 * j + 3]), f2(ex2(b.x), ex2(b.y)));
                             }
                             if (blk == quarter) {
-                                const int own = row - c0;  // the diagonal's place among these columns
+                                const int own = row - c0;  // the diagonal's place among these columns: its weight is d
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) {
                                     const float2 m = floats(v[j]);
-                                    v[j] = f2(2 * j < own ? m.x : 2 * j == own ? m.x + skip : 0.0f,
-                                              2 * j + 1 < own ? m.y : 2 * j + 1 == own ? m.y + skip : 0.0f);
+                                    v[j] = f2(2 * j < own ? m.x : 2 * j == own ? fmaf(f[2 * j], dt, skip) : 0.0f,
+                                              2 * j + 1 < own ? m.y : 2 * j + 1 == own ? fmaf(f[2 * j + 1], dt, skip) : 0.0f);
                                 }
                             }
 #pragma unroll
@@ -544,7 +584,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
                             for (int j = 0; j < 8; ++j) hi[j] = lo[j] = 0u;
                         }
                         __syncwarp();
-                        tmem_st8(tmem + lanes + T_S + 32 * blk + 8 * (i % 2), hi);  // (these columns' pairs have been read)
+                        tmem_st8(tmem + lanes + T_S + c0, hi);  // (these columns' pairs have been read)
                         tmem_st8(tmem + lanes + T_LO + c0 / 2, lo);
                     }
                     tmem_wait_st();

@@ -95,3 +95,53 @@ def test_dense_with_scales_at_the_ends_of_bf16(dt, rows, size):
     y = sn.dense_q4(x, w)
     close(y, pre, sums_bound(mag, 128, 64) + 2.0 ** -126, dt)
     assert bool((y[0] == 0).all())
+
+
+# -------------------------------------------------------------------- scan
+def half_spacing(ref, dt):
+    """Half the distance of a type's values around ref: what one rounding may be off."""
+    bits = {"f16": 11, "bf16": 8}[dt]
+    _, e = np.frexp(ref)  # |ref| in [2^(e - 1), 2^e)
+    return np.maximum(np.ldexp(1.0, e - bits - 1), 2.0 ** -25 if dt == "f16" else 1e-37)
+
+
+def ramps(rng, kind, t, h):
+    if kind == "erase":  # one step far beyond the others, then small ones, again and again
+        raw = rng.normal(size=(t, h)) - 3
+        raw[5::37] = 3000.0
+        raw[20::53] = 1e4
+        return raw
+    return float(kind) * rng.uniform(0.9, 1.1, (t, h))
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("kind", ["0.1", "1", "5", "20", "60", "erase"])
+@pytest.mark.parametrize("lens, sizes", [([300], (2, 64, 1, 16)), ([127, 64, 130], (3, 32, 1, 8)), ([1100], (1, 64, 1, 64))])
+def test_scan_keeps_its_precision_whatever_the_steps(dt, kind, lens, sizes):
+    """y is rounded once; what it is made of is good to 2^-14 of the terms' sizes (two 16-bit parts of each
+    factor, exponents that matter, up to 32, to 2^-21 of themselves), also where every step times a is
+    large, or one step before them was.  A decay taken as the difference of two running sums is off by
+    2^-24 of those sums."""
+    import torch
+    import paper_2110_06037_gb300 as sn
+    h, p, g, n = sizes
+    rng = np.random.default_rng(sum(lens))
+    a = -rng.uniform(12, 16, h).astype(np.float32)
+    xbc = dev(rng.normal(size=(sum(lens), h * p + 2 * g * n)), dt)
+    step = dev(ramps(rng, kind, sum(lens), h), dt)
+    if dt == "f16":
+        step = step.clamp(max=1e4)
+    ssm = sn.StateSpace(h, p, g, n, dev(a))
+    out = torch.empty(len(lens), h, p, n, device="cuda")
+    at = np.concatenate(([0], np.cumsum(lens)))
+    y = ssm.scan(xbc, step, offsets=torch.tensor(at, dtype=torch.int32, device="cuda"), max_len=max(lens), state_out=out)
+    sn.check_device()
+    for i, (s, e) in enumerate(zip(at, at[1:])):
+        ref, my, sref, ms = ob.scan(host(xbc)[s:e], host(step)[s:e], sizes, a, None, None, np.zeros((h, p, n)))
+        got = host(y)[s:e]
+        # a value that rounds to none of fp16's is infinite
+        beyond = (np.abs(ref) + 2.0 ** -14 * my >= 65520) & (got == np.copysign(np.inf, ref)) if dt == "f16" else np.zeros(ref.shape, bool)
+        err = np.where(beyond, 0, np.abs(np.where(beyond, ref, got) - ref))
+        # (a state is the last few steps' where steps are large: 64 roundings and exponents to 2^-19)
+        assert (np.abs(host(out)[i] - sref) <= 2.0 ** -18 * ms + 1e-37).all()
+        assert (err <= half_spacing(ref, dt) + 2.0 ** -14 * my).all(), float((err / (half_spacing(ref, dt) + 2.0 ** -14 * my)).max())
