@@ -224,45 +224,16 @@ constexpr int RT = 16, SEG_MIN = 64;  // tokens of a run, and of a segment at le
 
 struct RecP {
     SsmP s;
-    int32_t segs;
-    float *part, *total;  // [batch][H][segs][P][N] states: before segment 0, then after segment j; [batch][H][segs]: sums of d a
+    int32_t segs, step;   // segments of a sequence at most, tokens of a segment at least
+    float *part, *total;  // [tokens / step][H][P][N] states: before segment 0, then after segment j; [tokens / step][H]: sums of d a
 };
-// segments of one sequence: of SEG_MIN tokens at least, as many as `most`
-__device__ __forceinline__ int rec_own(int len, int most) { return max(1, min(most, (len + RT - 1) / RT / (SEG_MIN / RT))); }
+// segments of one sequence, and the place of the first of their states: a sequence of two and more
+// has as many as it has steps, or fewer, so that those of the sequences before it end there
+__device__ __forceinline__ int rec_own(int len, int most, int step) { return max(1, min(most, len / step)); }
+__device__ __forceinline__ int64_t rec_first(const Seq &s, int step) { return s.first / step; }
 __device__ __forceinline__ int2 rec_segment(int len, int segs, int g) {  // tokens [first, last), whole runs
     const int runs = (len + RT - 1) / RT;
     return make_int2(min(len, (int)((int64_t)runs * g / segs) * RT), min(len, (int)((int64_t)runs * (g + 1) / segs) * RT));
-}
-
-// What block `id` works on: each sequence has its own segments but the `but` last, and
-// `blocks` blocks to each.  The blocks that have work so are the first of the grid and
-// spread over the multiprocessors evenly.  Called by whole warps.
-struct Place {
-    int b, seg, block;  // b < 0: nothing
-};
-__device__ __forceinline__ Place rec_place(const SeqArgs &q, int most, int but, int blocks, int id) {
-    const int lane = threadIdx.x % 32;
-    int rest = id / blocks;  // the segment's number among all
-    if (!q.offsets || most == 1) {  // all alike
-        const int n = (q.offsets ? 1 : rec_own((int)q.max_len, most)) - but;
-        return n > 0 && rest / n < q.batch ? Place{rest / n, rest % n, id % blocks} : Place{-1, 0, 0};
-    }
-    for (int b0 = 0; b0 < q.batch; b0 += 32) {
-        const int n = b0 + lane < q.batch ? rec_own(sequence(q, b0 + lane).len, most) - but : 0;
-        int up = n;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const int v = __shfl_up_sync(0xffffffffu, up, o);
-            if (lane >= o) up += v;
-        }
-        const uint32_t in = __ballot_sync(0xffffffffu, rest < up);
-        if (in) {
-            const int k = __ffs(in) - 1;
-            return Place{b0 + k, rest - (__shfl_sync(0xffffffffu, up, k) - __shfl_sync(0xffffffffu, n, k)), id % blocks};
-        }
-        rest -= __shfl_sync(0xffffffffu, up, 31);
-    }
-    return Place{-1, 0, 0};
 }
 
 // FULL: the outputs; otherwise a segment's state from nothing (segment 0: from s_in)
@@ -276,16 +247,16 @@ __global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant
     griddep_wait();
     const SsmP &q = p.s;
     const int pblocks = (q.P + 31) / 32, blocks = q.H * pblocks, tid = threadIdx.x, l = tid % 8;
-    const Place at = rec_place(q.q, p.segs, FULL ? 0 : 1, blocks, blockIdx.x);
+    const Place at = place_of(q.q, p.segs == 1, [&](int len) { return rec_own(len, p.segs, p.step) - (FULL ? 0 : 1); }, blocks, blockIdx.x);
     if (at.b < 0) return;
     const int b = at.b, seg = at.seg, head = at.block / pblocks, p0 = at.block % pblocks * 32, row = p0 + tid / 8;
     const Seq s = sequence(q.q, b);
-    const int segs = rec_own(s.len, p.segs);
+    const int segs = rec_own(s.len, p.segs, p.step);
     const int2 tok = rec_segment(s.len, segs, seg);
     const int grp = head / (q.H / q.G), np = min(32, q.P - p0);
     const float a = q.a[head], dskip = q.d ? q.d[head] : 0.0f, dtb = q.dt_bias ? q.dt_bias[head] : 0.0f;
-    const int64_t part0 = ((int64_t)b * q.H + head) * p.segs, srow = s.slot >= 0 ? (((int64_t)s.slot * q.H + head) * q.P + row) * q.N : -1;
-    auto state_at = [&](int j) { return p.part + ((part0 + j) * q.P + row) * q.N; };
+    const int64_t part0 = rec_first(s, p.step) * q.H + head, srow = s.slot >= 0 ? (((int64_t)s.slot * q.H + head) * q.P + row) * q.N : -1;
+    auto state_at = [&](int j) { return p.part + ((part0 + (int64_t)j * q.H) * q.P + row) * q.N; };
     float st[NL];
     auto value = [&](int i) { return ((i / 4) * 8 + l) * 4 + i % 4; };
 #pragma unroll
@@ -299,7 +270,7 @@ __global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant
     if (FULL) {
 #pragma unroll 4
         for (int j = 1; j < seg; ++j) {
-            const float e = expf(p.total[part0 + j]);
+            const float e = expf(p.total[part0 + (int64_t)j * q.H]);
 #pragma unroll
             for (int i = 0; i < NL; ++i)
                 if (row < q.P && value(i) < q.N) st[i] = fmaf(st[i], e, state_at(j + 1)[value(i)]);
@@ -408,7 +379,7 @@ __global__ void __launch_bounds__(256) ssm_scan_rec_kernel(const __grid_constant
         if (tid >= RT) sum = 0.0f;
 #pragma unroll
         for (int o = RT / 2; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-        if (tid == 0) p.total[part0 + seg] = sum;
+        if (tid == 0) p.total[part0 + (int64_t)seg * q.H] = sum;
     }
 }
 
@@ -418,26 +389,30 @@ int rec_segments(const SsmP &p) {
     const int64_t blocks = std::max<int64_t>(full * p.H * ((p.P + 31) / 32), 1);
     return (int)std::max<int64_t>(1, std::min<int64_t>({3LL * num_sms() / blocks, 64, p.q.max_len / SEG_MIN}));
 }
+int64_t rec_step(const SsmP &p, int64_t segs) { return std::max<int64_t>(SEG_MIN, p.q.max_len / segs); }
 int64_t rec_workspace(const SsmP &p) {
     const int64_t segs = rec_segments(p);
-    return segs > 1 ? ((int64_t)p.q.batch * p.H * segs * ((int64_t)p.P * p.N + 1) * 4 + 255) / 256 * 256 : 0;
+    return segs > 1 ? (p.q.tokens / rec_step(p, segs) * p.H * ((int64_t)p.P * p.N + 1) * 4 + 255) / 256 * 256 : 0;
 }
 
 template <typename T, int NL>
 cudaError_t launch_rec(const RecP &p, const T *xbc, const T *dtv, T *y, cudaStream_t st) {
-    const int64_t blocks = (int64_t)p.s.H * ((p.s.P + 31) / 32) * p.s.q.batch;
-    if (blocks * p.segs > INT32_MAX) return cudaErrorInvalidValue;
-    if (p.segs > 1) {
-        const cudaError_t e = launch_pdl(ssm_scan_rec_kernel<T, NL, false>, dim3((unsigned)(blocks * (p.segs - 1))), dim3(256), 0, st, p, xbc, dtv, y);
+    const int64_t heads = (int64_t)p.s.H * ((p.s.P + 31) / 32), steps = p.s.q.tokens / p.step, batch = p.s.q.batch;
+    // segments that there can be: one of each sequence, and one more for each step
+    const int64_t most = std::min(batch * p.segs, batch + steps), states = std::min(batch * (p.segs - 1), steps);
+    if (heads * most > INT32_MAX) return cudaErrorInvalidValue;
+    if (states > 0) {
+        const cudaError_t e = launch_pdl(ssm_scan_rec_kernel<T, NL, false>, dim3((unsigned)(heads * states)), dim3(256), 0, st, p, xbc, dtv, y);
         if (e != cudaSuccess) return e;
     }
-    return launch_pdl(ssm_scan_rec_kernel<T, NL, true>, dim3((unsigned)(blocks * p.segs)), dim3(256), 0, st, p, xbc, dtv, y);
+    return launch_pdl(ssm_scan_rec_kernel<T, NL, true>, dim3((unsigned)(heads * most)), dim3(256), 0, st, p, xbc, dtv, y);
 }
 
 template <typename T>
 cudaError_t launch_scan(const SsmP &s, const T *xbc, const T *dtv, T *y, void *work, cudaStream_t st) {
-    RecP p{s, s.q.tokens ? rec_segments(s) : 1, static_cast<float *>(work), nullptr};
-    p.total = p.part + (int64_t)s.q.batch * s.H * p.segs * s.P * s.N;
+    RecP p{s, s.q.tokens ? rec_segments(s) : 1, 0, static_cast<float *>(work), nullptr};
+    p.step = (int32_t)rec_step(s, p.segs);
+    p.total = p.part + s.q.tokens / p.step * s.H * s.P * s.N;
     if (s.N <= 32) return launch_rec<T, 4>(p, xbc, dtv, y, st);
     if (s.N <= 64) return launch_rec<T, 8>(p, xbc, dtv, y, st);
     if (s.N <= 128) return launch_rec<T, 16>(p, xbc, dtv, y, st);

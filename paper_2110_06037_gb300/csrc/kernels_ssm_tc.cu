@@ -26,8 +26,8 @@
 // Each product has warps of its own for what goes into and comes out of it, so that
 // only the state's one multiply-add a chunk runs from chunk to chunk: in one order, two
 // blocks an SM, a chunk took a block 17.9 thousand cycles of waiting for one step after
-// the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128).  So: 156 us, of
-// which 7 are the time steps, 31 the first pass, 118 the second, 7200 cycles a chunk.
+// the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128).  So: 159 us, of
+// which 7 are the time steps, 32 the first pass, 118 the second, 7300 cycles a chunk.
 // The tensor cores are busy in 38% of them, the busiest scheduler issues in 55%; what
 // bounds it is the way from the pairs to P and to the next pairs.  (Tried and no faster: the next
 // chunk's pairs ahead, in TMEM of their own, 163; X' by the state's warps, 163; P's
@@ -61,9 +61,10 @@ constexpr int TAB_W = Q, TAB_F = 2 * Q, TAB_R = 3 * Q, TAB_D = 4 * Q, TAB_S = 5 
 
 struct TcP {
     SsmP s;
-    int32_t segs, fine;      // segments a sequence; finer ones of the first pass in each
+    int32_t segs, step;      // segments a sequence at most; chunks of a segment at least
+    int32_t fine;            // finer ones of the first pass in each
     float *table, *total;    // [chunks][H][TABLE], [chunks][H]: A_127
-    float *part;             // [batch][H][p blocks][segs * fine][64][N]: state before the first, then after fine segment j
+    float *part;             // [tokens / Q / step * fine][H][p blocks][64][N]: state before the first, then after fine segment j
     int32_t pblocks;
     int *err;
 };
@@ -71,8 +72,9 @@ struct TcP {
 // index of a chunk's table: unique for chunk c of sequence b, since each sequence
 // before it has at most its tokens / Q + 1 chunks
 __device__ __forceinline__ int64_t chunk_at(const Seq &s, int b, int c) { return s.first / Q + b + c; }
-// segments of one sequence: of four chunks at least, as many as `most`
-__device__ __forceinline__ int own_segments(int len, int most) { return max(1, min(most, (len + Q - 1) / Q / 4)); }
+// segments of one sequence; one of two and more has as many as it has steps, or fewer, so that the
+// states of sequences before it end where its own begin, at first / Q / step
+__device__ __forceinline__ int own_segments(int len, const TcP &p) { return max(1, min(p.segs, len / Q / p.step)); }
 // segment g of a sequence: chunks [first, last)
 __device__ __forceinline__ int2 segment(int len, int segs, int g) {
     const int chunks = (len + Q - 1) / Q;
@@ -254,11 +256,15 @@ enum Bar {
     F_B, F_C = F_B + 2, F_X = F_C + 2, E_B = F_X + 2, E_C = E_B + 2, E_X = E_C + 2,
     M_PAIRS = E_X + 2, M_CARRIED, M_INSIDE, M_MADE, A_XW = M_MADE + 2, A_MADE = A_XW + 2, A_STATE = A_MADE + 2, A_P, A_OUT, BARS
 };
+struct Work {  // what a block works on: a sequence (b < 0: none), its segment's chunks, the place of its states
+    int first, len, slot, b, seg, segs, chunk0, chunks, part0;
+};
 struct Shared {
     alignas(16) float fs[2][Q];  // TAB_F of a chunk
     uint64_t bar[BARS];
     uint32_t tmem;
     int abort, any_bad[2];
+    Work w;
     int bad[2][PB];              // first token of a chunk whose x is not finite, by channel
 };
 static_assert(sizeof(Shared) <= 2048, "behind the tiles");
@@ -285,7 +291,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
     constexpr int STAGES1 = FULL ? 1 : 2;  // of B, X' and the products with it
     constexpr uint32_t OFF_XW3 = FULL ? 2 * TILE64 : OFF_C;  // the third part of X', and zeros
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const int pb = blockIdx.x % p.pblocks, head = blockIdx.x / p.pblocks, seg = blockIdx.y, b = blockIdx.z;
+    const int pb = blockIdx.x % p.pblocks, head = blockIdx.x / p.pblocks;  // (blockIdx.x: head * p.pblocks + pb)
     if (su32(smem) & 1023) {  // (the swizzled tiles need it; uniform over the block)
         if (threadIdx.x == 0) atomicOr(p.err, ERR_TMA_WAIT);
         return;
@@ -312,17 +318,28 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
     griddep_launch();  // (behind the allocation: see tmem_alloc)
     griddep_wait();
     const SsmP &q = p.s;
-    const Seq s = sequence(q.q, b);
-    const int segs = own_segments(s.len, p.segs);
-    const bool used = seg < (FULL ? segs : (segs - 1) * p.fine);  // (a shorter sequence has fewer segments)
-    const int2 chunks = used ? segment(s.len, FULL ? segs : segs * p.fine, seg) : make_int2(0, 0);
-    const int nc = chunks.y - chunks.x, grp = head / (q.H / q.G);
+    if (warp == 0) {  // what the block works on
+        const Place place = place_of(q.q, p.segs == 1, [&](int len) { return FULL ? own_segments(len, p) : (own_segments(len, p) - 1) * p.fine; },
+                                     1, (int)(blockIdx.y + blockIdx.z * gridDim.y));
+        const Seq s = sequence(q.q, max(place.b, 0));
+        const int segs = own_segments(s.len, p);
+        const int2 chunks = place.b >= 0 ? segment(s.len, FULL ? segs : segs * p.fine, place.seg) : make_int2(0, 0);
+        if (lane == 0)
+            sh.w = Work{(int)s.first, s.len, s.slot, place.b, place.seg, segs, chunks.x, chunks.y - chunks.x, (int)(s.first / Q / p.step) * p.fine};
+    }
+    __syncthreads();
+    // (by a reduction: in uniform registers, of which there are enough; as loaded, 165 us for 159)
+    auto uniform = [](int v) { return __reduce_max_sync(0xffffffffu, v); };
+    const bool used = uniform(sh.w.b) >= 0;
+    Seq s;
+    s.first = uniform(sh.w.first), s.len = uniform(sh.w.len), s.slot = uniform(sh.w.slot);
+    const int b = max(uniform(sh.w.b), 0), seg = uniform(sh.w.seg), segs = uniform(sh.w.segs), part0 = uniform(sh.w.part0);
+    const int chunk0 = uniform(sh.w.chunk0), nc = uniform(sh.w.chunks), grp = head / (q.H / q.G);
     const int p0 = pb * PB, np = min(PB, q.P - p0);
-    const int64_t part0 = (((int64_t)b * q.H + head) * p.pblocks + pb) * (p.segs * p.fine) * PB * q.N;
     const uint32_t base = su32(smem);
     const int row = (warp % 4) * 32 + lane;  // token t, or n of the state, by the warp's TMEM lanes
     const uint32_t lanes = (uint32_t)((warp % 4) * 32) << 16;
-    const int64_t tab0 = chunk_at(s, b, chunks.x) * q.H + head;
+    const int64_t tab0 = chunk_at(s, b, chunk0) * q.H + head;
     auto table = [&](int c) { return p.table + (tab0 + (int64_t)c * q.H) * TABLE; };
     bool ok = true;
     auto gave_up = [&](int code) {
@@ -346,7 +363,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
             auto load = [&](const CUtensorMap *m, int bar, uint32_t off, int c, int boxes, int x0, int g) {
                 mbar_expect_tx(&sh.bar[bar], boxes * TILE64);
                 for (int i = 0; i < boxes; ++i)
-                    tma_3d<1>(base + off + i * TILE64, m, su32(&sh.bar[bar]), x0 + 64 * i, g, (int)(s.first + (int64_t)(chunks.x + c) * Q));
+                    tma_3d<1>(base + off + i * TILE64, m, su32(&sh.bar[bar]), x0 + 64 * i, g, (int)(s.first + (int64_t)(chunk0 + c) * Q));
             };
             auto freed = [&](int i, int n) {  // the n-th chunk in a stage waits until the one before has been read
                 if (ok && n > 0 && !mbar_wait(&sh.bar[i], (uint32_t)(n - 1) & 1u)) {
@@ -463,7 +480,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
         const int tid = threadIdx.x - 64, t = tid / XT, j0 = 8 / XT * (tid % XT);
         float w_next = nc > 0 ? __ldg(table(0) + TAB_W + t) : 0.0f;
         auto weigh = [&](int c) {
-            const int st = c & 1, bs = c % STAGES1, valid = min(Q, s.len - (chunks.x + c) * Q);  // tokens there are
+            const int st = c & 1, bs = c % STAGES1, valid = min(Q, s.len - (chunk0 + c) * Q);  // tokens there are
             const float w = w_next;
             if (c + 1 < nc) w_next = __ldg(table(c + 1) + TAB_W + t);
             must(F_X + st, (uint32_t)(c >> 1) & 1u);
@@ -602,7 +619,7 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
         const int c0 = (warp - STATE0) / 4 * HC;
         const int64_t srow = s.slot >= 0 ? (((int64_t)s.slot * q.H + head) * q.P + p0 + c0) * q.N + row : -1;
         auto live = [&](int i) { return c0 + i < np && row < q.N; };
-        auto part = [&](int j) { return p.part + part0 + ((int64_t)j * PB + c0) * q.N + row; };  // before segment 0, after fine segment j - 1
+        auto part = [&](int j) { return p.part + (((int64_t)(part0 + j) * q.H * p.pblocks + blockIdx.x) * PB + c0) * q.N + row; };  // before segment 0, after fine segment j - 1
         auto load = [&](const float *from) {
 #pragma unroll
             for (int i = 0; i < HC; i += 2)
@@ -686,13 +703,13 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
         for (int c = 0; c < nc; ++c) {
             const float et = ex2(at_next);
             if (c + 1 < nc) at_next = __ldg(table(c + 1) + row);
-            const int st = c & 1, valid = min(Q, s.len - (chunks.x + c) * Q);
+            const int st = c & 1, valid = min(Q, s.len - (chunk0 + c) * Q);
             must(M_INSIDE, c & 1);
             must(M_CARRIED, c & 1);
             if (bar_red_or(2, 128, !ok)) break;  // (the group leaves together)
             tc_fence_after();
             const bool bad = *reinterpret_cast<volatile int *>(&sh.any_bad[st]);
-            __nv_bfloat16 *yr = y + (s.first + (int64_t)(chunks.x + c) * Q + row) * q.ldy + (int64_t)head * q.P + p0;
+            __nv_bfloat16 *yr = y + (s.first + (int64_t)(chunk0 + c) * Q + row) * q.ldy + (int64_t)head * q.P + p0;
 #pragma unroll 1
             for (int i = 0; i < PB; i += 16) {
                 float u[16], v[16], in[16];
@@ -741,13 +758,14 @@ __global__ void __launch_bounds__(FULL ? FULL_THREADS : STATE_THREADS, 1)
 // Segments that a sequence is cut into: as many as fill the SMs, of four chunks at
 // least; and the first pass's, which leaves the last segment out
 struct Cut {
-    int segs, fine;
+    int segs, step, fine;
 };
 Cut cut_of(const SsmP &p) {
     const int64_t full = (p.q.tokens + p.q.max_len - 1) / std::max<int64_t>(p.q.max_len, 1);  // sequences, counted by length
     const int64_t blocks = std::max<int64_t>(full * p.H * ((p.P + PB - 1) / PB), 1), chunks = (p.q.max_len + Q - 1) / Q;
     Cut c;
     c.segs = (int)std::max<int64_t>(1, std::min<int64_t>({num_sms() / blocks, 64, chunks / 4}));
+    c.step = (int)std::max<int64_t>(4, p.q.max_len / Q / c.segs);
     c.fine = c.segs == 1 ? 1 : (int)std::max<int64_t>(1, std::min<int64_t>(num_sms() / (blocks * (c.segs - 1)), chunks / c.segs / 2));
     return c;
 }
@@ -762,7 +780,7 @@ TcWork work_of(const SsmP &p) {
     w.total = w.table + up(w.chunks * p.H * TABLE * 4);
     w.part = w.total + up(w.chunks * p.H * 4);
     const Cut c = cut_of(p);
-    w.bytes = w.part + (c.segs > 1 ? up((int64_t)p.q.batch * p.H * ((p.P + PB - 1) / PB) * c.segs * c.fine * PB * p.N * 4) : 0);
+    w.bytes = w.part + (c.segs > 1 ? up(p.q.tokens / Q / c.step * c.fine * p.H * ((p.P + PB - 1) / PB) * PB * p.N * 4) : 0);
     return w;
 }
 
@@ -781,7 +799,7 @@ cudaError_t ssm_tc_scan(const SsmP &s, const __nv_bfloat16 *xbc, const __nv_bflo
     const TcWork w = work_of(s);
     char *base = static_cast<char *>(work);
     const Cut cut = cut_of(s);
-    TcP p{s, cut.segs, cut.fine, reinterpret_cast<float *>(base + w.table), reinterpret_cast<float *>(base + w.total),
+    TcP p{s, cut.segs, cut.step, cut.fine, reinterpret_cast<float *>(base + w.table), reinterpret_cast<float *>(base + w.total),
           reinterpret_cast<float *>(base + w.part), (s.P + PB - 1) / PB, device_error_word()};
     // xbc's rows as [heads][P] of x and [groups][N] of B and C: what lies behind a head's or group's end reads as 0
     CUtensorMap mX, mB, mC;
@@ -796,17 +814,23 @@ cudaError_t ssm_tc_scan(const SsmP &s, const __nv_bfloat16 *xbc, const __nv_bflo
     static PerDevice set_full, set_states;
     if (const cudaError_t e = allow_smem(set_full, ssm_scan_tc_kernel<true>, SCAN_SMEM)) return e;
     if (const cudaError_t e = allow_smem(set_states, ssm_scan_tc_kernel<false>, SCAN_SMEM)) return e;
-    const unsigned chunks = (unsigned)((s.q.max_len + Q - 1) / Q), heads = (unsigned)(s.H * p.pblocks);
+    const unsigned chunks = (unsigned)((s.q.max_len + Q - 1) / Q);
     const int vec = s.H % 8 == 0 && s.lddt % 8 == 0 && reinterpret_cast<uintptr_t>(dtv) % 16 == 0;
     cudaError_t e = launch_pdl(ssm_steps_kernel, dim3(chunks, (unsigned)((s.H + 7) / 8), (unsigned)s.q.batch), dim3(256), 0, st, p, dtv, vec);
     if (e != cudaSuccess) return e;
-    if (p.segs > 1) {
-        e = launch_pdl(ssm_scan_tc_kernel<false>, dim3(heads, (unsigned)((p.segs - 1) * p.fine), (unsigned)s.q.batch), dim3(STATE_THREADS), SCAN_SMEM, st,
-                       mX, mB, mC, p, y);
+    // segments that there can be: one of each sequence, and one more for each step
+    const int64_t heads = (int64_t)s.H * p.pblocks, steps = s.q.tokens / Q / p.step, batch = s.q.batch;
+    const int64_t most = std::min(batch * p.segs, batch + steps), states = std::min(batch * (p.segs - 1), steps) * p.fine;
+    if (std::max(most, states) > INT32_MAX) return cudaErrorInvalidValue;
+    auto grid = [&](int64_t n) {  // head and channels, segment's number
+        const int64_t z = (n + 65534) / 65535;
+        return dim3((unsigned)heads, (unsigned)((n + z - 1) / z), (unsigned)z);
+    };
+    if (states > 0) {
+        e = launch_pdl(ssm_scan_tc_kernel<false>, grid(states), dim3(STATE_THREADS), SCAN_SMEM, st, mX, mB, mC, p, y);
         if (e != cudaSuccess) return e;
     }
-    return launch_pdl(ssm_scan_tc_kernel<true>, dim3(heads, (unsigned)p.segs, (unsigned)s.q.batch), dim3(FULL_THREADS), SCAN_SMEM, st, mX, mB,
-                      mC, p, y);
+    return launch_pdl(ssm_scan_tc_kernel<true>, grid(most), dim3(FULL_THREADS), SCAN_SMEM, st, mX, mB, mC, p, y);
 }
 
 }  // namespace k

@@ -29,6 +29,39 @@ __device__ __forceinline__ Seq sequence(const SeqArgs &q, int b) {
     return s;
 }
 
+// What block `id` of a scan works on: each sequence has `own(length)` segments, each
+// segment `blocks` blocks.  The blocks that have work so are the first of the grid and
+// spread over the multiprocessors evenly.  Called by whole warps; alike: every sequence
+// has own(its length) = own(max_len).
+struct Place {
+    int b, seg, block;  // b < 0: nothing
+};
+template <typename Own>
+__device__ __forceinline__ Place place_of(const SeqArgs &q, bool alike, Own own, int blocks, int id) {
+    const int lane = threadIdx.x % 32;
+    int rest = id / blocks;  // the segment's number among all
+    if (!q.offsets || alike) {
+        const int n = own((int)q.max_len);
+        return n > 0 && rest / n < q.batch ? Place{rest / n, rest % n, id % blocks} : Place{-1, 0, 0};
+    }
+    for (int b0 = 0; b0 < q.batch; b0 += 32) {
+        const int n = b0 + lane < q.batch ? own(sequence(q, b0 + lane).len) : 0;
+        int up = n;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int v = __shfl_up_sync(0xffffffffu, up, o);
+            if (lane >= o) up += v;
+        }
+        const uint32_t in = __ballot_sync(0xffffffffu, rest < up);
+        if (in) {
+            const int k = __ffs(in) - 1;
+            return Place{b0 + k, rest - (__shfl_sync(0xffffffffu, up, k) - __shfl_sync(0xffffffffu, n, k)), id % blocks};
+        }
+        rest -= __shfl_sync(0xffffffffu, up, 31);
+    }
+    return Place{-1, 0, 0};
+}
+
 __device__ __forceinline__ float ex2(float v) {
     float r;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
