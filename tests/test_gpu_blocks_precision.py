@@ -145,3 +145,84 @@ def test_scan_keeps_its_precision_whatever_the_steps(dt, kind, lens, sizes):
         # (a state is the last few steps' where steps are large: 64 roundings and exponents to 2^-19)
         assert (np.abs(host(out)[i] - sref) <= 2.0 ** -18 * ms + 1e-37).all()
         assert (err <= half_spacing(ref, dt) + 2.0 ** -14 * my).all(), float((err / (half_spacing(ref, dt) + 2.0 ** -14 * my)).max())
+
+
+# ------------------------------------------------------------------- norms
+def norm_bound(v, ev, kind, eps, w, b):
+    """(norm of v, what it may be off) per element, v [rows, d] off by ev each.
+
+    To first order: the centred value is off by ev and by the mean's error (its own roundings, and the mean
+    of ev); 1 / sqrt(mean square + eps) relatively by half the mean square's error, at most the root mean
+    square of the centred values' errors over sqrt(mean square + eps).  Sums of a row are trees of at
+    most 64 roundings, rsqrtf and the products a few more."""
+    m = v.mean(1, keepdims=True) if kind == "layer" else 0.0
+    c = v - m
+    ec = ev + ((ev.mean(1, keepdims=True) + 64 * E32 * np.abs(v).mean(1, keepdims=True)) if kind == "layer" else 0.0) + E32 * np.abs(c)
+    r = 1 / np.sqrt((c * c).mean(1, keepdims=True) + eps)
+    er = np.sqrt((ec * ec).mean(1, keepdims=True)) * r + 40 * E32  # relative
+    out = c * r * w
+    bound = np.abs(w) * r * ec + np.abs(out) * (er + 4 * E32)
+    return (out, bound) if b is None else (out + b, bound + E32 * np.abs(out + b))
+
+
+def block_norm_bound(y, res, g, per, kind, eps, use, gate, at):
+    """(total, bound, normed or None, bound) of fp64 inputs."""
+    zero = np.zeros(y.shape)
+    gv = np.ones(y.shape) if g is None else ob.act(g, gate)[np.arange(len(y)) // per]
+    # __expf is good to 2 + 1.173 |g| ulp, __fdividef to 2 (an ulp is at most 2 E32), and the sum and product
+    eg = zero if g is None else np.abs(gv) * (12 + 3 * np.abs(g[np.arange(len(y)) // per])) * E32
+    t, e = (y * gv, np.abs(y) * eg + E32 * np.abs(y * gv)) if at == "before" else (y, zero)
+    if "post" in use:
+        t, e = norm_bound(t, e, kind, eps, use["post"].astype(np.float64), use["post_bias"] if "post_bias" in use else None)
+    if at == "after":
+        t, e = t * gv, e * np.abs(gv) + np.abs(t) * eg + E32 * np.abs(t * gv)
+    if "scale" in use:  # (which may be multiplied into the weight, and into the bias)
+        t, e = t * use["scale"], e * np.abs(use["scale"]) + 4 * E32 * np.abs(t * use["scale"])
+        if "post_bias" in use:
+            e = e + 4 * E32 * np.abs(use["scale"] * use["post_bias"] * (gv if at == "after" else 1.0))
+    if res is not None:
+        e = e + E32 * np.abs(res + t) + E32 * np.abs(t)
+        t = res + t
+    if "pre" not in use:
+        return t, e, None, None
+    n, en = norm_bound(t, e, kind, eps, use["pre"].astype(np.float64), use["pre_bias"] if "pre_bias" in use else None)
+    return t, e, n, en
+
+
+@pytest.mark.parametrize("dt, rdt", [("f32", "f32"), ("f16", "f32"), ("bf16", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("rows, d", [(5, 31), (4, 512), (3, 1024), (2, 4104), (2, 20001), (1301, 4096), (700, 512), (650, 1096)])
+@pytest.mark.parametrize("kind", ["rms", "layer"])
+@pytest.mark.parametrize("eps", [1e-5, 0.5])
+def test_norms_are_off_by_their_roundings(dt, rdt, rows, d, kind, eps):
+    """A norm with another eps, without its bias, or with sums in 16 bits would be far outside."""
+    import paper_2110_06037_gb300 as sn
+    rng = np.random.default_rng(rows + d)
+    w = {k: (1 + 0.2 * rng.normal(size=d)).astype(np.float32) for k in ("post", "pre", "scale")}
+    w |= {k: (0.1 * rng.normal(size=d)).astype(np.float32) for k in ("post_bias", "pre_bias")}
+    y, r = dev(rng.normal(size=(rows, d)) + 0.5, dt), dev(2 * rng.normal(size=(rows, d)), rdt)
+    for gate, at, per, names, with_res in (
+            ("none", "after", 1, w, True), ("sigmoid", "before", 3, w, True), ("silu", "after", 1, w, True),
+            ("silu", "before", 1, ("post", "pre"), True), ("linear", "after", 1, ("post", "post_bias", "scale"), False)):
+        g = None if gate == "none" else dev(2 * rng.normal(size=(-(-rows // per), d)), dt)
+        use = {k: w[k] for k in names}
+        norm = sn.BlockNorm(d, kind, eps, gate=gate, gate_at=at, **{k: dev(v) for k, v in use.items()})
+        total, normed = norm(y, residual=r if with_res else None, gate=g, rows_per_gate=per)
+        t, e, n, en = block_norm_bound(host(y), host(r) if with_res else None, None if g is None else host(g), per, kind, eps, use, gate, at)
+        close(total, t, e, rdt if with_res else dt)
+        if n is not None:
+            close(normed, n, en, dt)
+
+
+def test_the_norms_bound_sees_another_eps_and_a_missing_bias():
+    """Planted in the reference: what the bound is for."""
+    import paper_2110_06037_gb300 as sn
+    rng = np.random.default_rng(1)
+    rows, d = 1301, 4096
+    use = {k: (1 + 0.2 * rng.normal(size=d)).astype(np.float32) for k in ("post", "pre")}
+    use["pre_bias"] = (0.01 * rng.normal(size=d)).astype(np.float32)
+    y, r = dev(rng.normal(size=(rows, d))), dev(rng.normal(size=(rows, d)))
+    _, normed = sn.BlockNorm(d, "layer", 1e-3, **{k: dev(v) for k, v in use.items()})(y, residual=r)
+    for eps, names in ((1.1e-3, ("post", "pre", "pre_bias")), (1e-3, ("post", "pre"))):
+        _, _, n, en = block_norm_bound(host(y), host(r), None, 1, "layer", eps, {k: use[k] for k in names}, "none", "after")
+        with pytest.raises(AssertionError):
+            close(normed, n, en, "f32")
