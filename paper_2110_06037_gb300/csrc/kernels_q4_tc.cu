@@ -407,7 +407,7 @@ __global__ void __launch_bounds__(Q4_THREADS, 1)
                     }
                 };
                 if (p.q.act == SN_ACT_NONE) put([](float v) { return v; });
-                else put([&](float v) { return act_apply(v, p.q.act); });
+                else put([&](float v) { return q4_act(v, p.q.act); });
                 __syncwarp();
             }
         }

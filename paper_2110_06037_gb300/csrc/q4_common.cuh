@@ -72,6 +72,9 @@ __device__ __forceinline__ uint32_t code_pair<__half>(uint32_t w, int j) {
     return *reinterpret_cast<const uint32_t *>(&d);
 }
 
+// A layer's activation of one of its sums; a sum that is NaN stays so (max and min alone would hide it).
+__device__ __forceinline__ float q4_act(float v, int act) { return v != v ? v : act_apply(v, act); }
+
 // Three bf16 values that sum to an fp32 one (8 + 8 + 8 bits; the first rounded
 // towards zero, so that it cannot overflow; what is not finite stays in the first).
 struct Planes {

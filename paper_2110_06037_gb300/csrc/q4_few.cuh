@@ -271,7 +271,7 @@ __global__ void __launch_bounds__(WARPS * 32) q4_few_kernel(const __grid_constan
     };
     auto finish = [&](int o, float v) {
         const int j = (nt0 + o / 16 % wn) * 16 + o % 16, m = o / (16 * wn);
-        if (j < p.q.n) stf(y + m * p.ldy + j, act_apply(v + (p.q.bias ? p.q.bias[j] : 0.0f), p.q.act));
+        if (j < p.q.n) stf(y + m * p.ldy + j, q4_act(v + (p.q.bias ? p.q.bias[j] : 0.0f), p.q.act));
     };
     if (p.s == 1) {
         for (int o = threadIdx.x; o < outs; o += WARPS * 32) finish(o, block_sum(o));

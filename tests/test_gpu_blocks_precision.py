@@ -226,3 +226,17 @@ def test_the_norms_bound_sees_another_eps_and_a_missing_bias():
         _, _, n, en = block_norm_bound(host(y), host(r), None, 1, "layer", eps, {k: use[k] for k in names}, "none", "after")
         with pytest.raises(AssertionError):
             close(normed, n, en, "f32")
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows", [3, 70])
+@pytest.mark.parametrize("act", ["none", "relu", "relu6", "hswish", "hsigmoid"])
+def test_dense_activations_pass_nan_on(dt, rows, act):
+    import paper_2110_06037_gb300 as sn
+    w, _, _, _ = q4(np.random.default_rng(2), 40, 130, 64, "bf16", act=act)
+    x = dev(np.random.default_rng(3).normal(size=(rows, 130)), dt)
+    ref = host(sn.dense_q4(x, w))
+    x[1, 77] = float("nan")
+    got = host(sn.dense_q4(x, w))
+    assert np.isnan(got[1]).all()
+    assert np.array_equal(np.delete(got, 1, 0), np.delete(ref, 1, 0)) and not np.isnan(ref).any()
