@@ -89,6 +89,11 @@ void *whole(const Tensor &t, at::IntArrayRef shape, at::ScalarType dtype, const 
 void *whole(const Opt &t, at::IntArrayRef shape, at::ScalarType dtype, const char *what) {
     return t ? whole(*t, shape, dtype, what) : nullptr;
 }
+// entries of a buffer of them
+int64_t entries_of(const Tensor &t, const char *what) {
+    if (t.dim() == 0) refuse(std::string(what) + " has no axis of entries");
+    return t.size(0);
+}
 const int32_t *index_of(const Opt &t, int64_t n, const char *what) {
     return static_cast<const int32_t *>(whole(t, {n}, at::kInt, what));
 }
@@ -205,7 +210,7 @@ Tensor causal_conv(const Tensor &x, const Tensor &weight, const Opt &bias, bool 
     on.same(slots, "slots"), on.same(pos, "pos"), on.same(out, "out");
     const Batch b = batch_of(x, offsets, max_len);
     const Rows r = rows_of(x, c, "x");
-    const int64_t n = kept ? kept->size(0) : b.n;
+    const int64_t n = kept ? entries_of(*kept, "kept") : b.n;
     void *kp = kept ? whole(*kept, {n, width, c}, x.scalar_type(), "kept") : nullptr;
     if (kept && !slots && n < b.n) refuse("kept has fewer entries than there are sequences");
     const auto *w = static_cast<const float *>(whole(weight, {c, width}, at::kFloat, "weight"));
@@ -223,7 +228,7 @@ struct States {
     float *in, *out;
 };
 States states_of(const sn_ssm_params *p, const Opt &in, const Opt &out, int64_t batch, bool slots) {
-    const int64_t n = in ? in->size(0) : out ? out->size(0) : batch;
+    const int64_t n = in ? entries_of(*in, "state_in") : out ? entries_of(*out, "state_out") : batch;
     const int64_t shape[4] = {n, p->heads, p->head_dim, p->state};
     States s{n, static_cast<float *>(whole(in, shape, at::kFloat, "state_in")), static_cast<float *>(whole(out, shape, at::kFloat, "state_out"))};
     if (!slots && (in || out) && n < batch) refuse("fewer states than sequences");

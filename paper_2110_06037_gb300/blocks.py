@@ -124,6 +124,8 @@ class Q4Weights:
 
     def __init__(self, codes, scales, k, group, bias=None, act="none", stream=None):
         torch = _torch()
+        if codes.dim() != 2:
+            _refuse("codes must be [n, (k + 1) // 2]")
         n, k, group = int(codes.shape[0]), int(k), int(group)
         if act not in _sn.SN_ACT:
             _refuse(f"unknown act {act!r}")
@@ -215,6 +217,8 @@ class StateSpace:
         self.heads, self.head_dim, self.groups, self.state = int(heads), int(head_dim), int(groups), int(state)
         self.inner, self.channels = self.heads * self.head_dim, self.heads * self.head_dim + 2 * self.groups * self.state
         f32 = _torch().float32
+        if conv_weight is not None and conv_weight.dim() != 2:
+            _refuse("conv_weight must be [channels, width]")
         self.width = int(conv_weight.shape[1]) if conv_weight is not None else 0
         self.weights = (a, d, dt_bias, conv_weight, conv_bias)
         if a is None:

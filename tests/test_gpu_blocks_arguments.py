@@ -93,3 +93,31 @@ def test_tensors_of_the_host_are_refused():
         sn.quantize_q4(h)
     with pytest.raises(sn.SnError):
         sn.causal_conv(x[None], torch.zeros(64, 4))
+
+
+def test_buffers_without_an_axis_of_entries_are_refused():
+    import torch
+    import paper_2110_06037_gb300 as sn
+    one, x = torch.zeros((), device="cuda"), torch.zeros(1, 4, 64, device="cuda")
+    ssm = sn.StateSpace(1, 32, 1, 16, torch.zeros(1, device="cuda"), conv_weight=torch.zeros(64, 4, device="cuda"))
+    for use in (lambda: sn.causal_conv(x, torch.zeros(64, 4, device="cuda"), kept=one), lambda: ssm.scan(x, x[:, :, :1], state_in=one),
+                lambda: ssm.scan(x, x[:, :, :1], state_out=one), lambda: ssm.step(x[0], x[0, :, :1], one, one, None),
+                lambda: sn.StateSpace(1, 32, 1, 16, torch.zeros(1, device="cuda"), conv_weight=one),
+                lambda: sn.Q4Weights(one.to(torch.uint8), one.half(), 64, 64)):
+        with pytest.raises(sn.SnError):
+            use()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_a_scan_of_empty_sequences_hands_their_states_on(dt):
+    import torch
+    import paper_2110_06037_gb300 as sn
+    dtype = {"f32": torch.float32, "bf16": torch.bfloat16}[dt]
+    ssm = sn.StateSpace(2, 32, 1, 16, torch.zeros(2, device="cuda"))
+    x, step = torch.zeros(0, 96, dtype=dtype, device="cuda"), torch.zeros(0, 2, dtype=dtype, device="cuda")
+    off = torch.zeros(4, dtype=torch.int32, device="cuda")
+    state, out = torch.randn(3, 2, 32, 16, device="cuda"), torch.full((3, 2, 32, 16), 5.0, device="cuda")
+    assert ssm.scan(x, step, offsets=off, max_len=0, state_in=state, state_out=out).shape == (0, 64)
+    assert torch.equal(out, state)
+    ssm.scan(x, step, offsets=off, max_len=0, state_out=out)
+    assert bool((out == 0).all())
