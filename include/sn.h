@@ -474,7 +474,8 @@ SN_API sn_status sn_conv2d_wino_noalloc(const void *x_dev, sn_schema schema, con
  *     row's length; rows themselves are contiguous;
  *   - outputs may not overlap inputs unless the call says so;
  *   - calls are asynchronous on `stream` and allocate nothing; a call with no
- *     rows, tokens or sequences returns SN_OK and launches nothing;
+ *     rows, tokens or sequences returns SN_OK and launches nothing (but a scan of
+ *     sequences that are all empty still stores their states);
  *   - errors: SN_EINVAL (NULL pointer, bad size, stride, dtype or option),
  *     SN_EUNSUPPORTED (a size beyond the stated limits), SN_ECUDA.
  * Sequences: `batch` sequences lie one behind the other in the token rows;
