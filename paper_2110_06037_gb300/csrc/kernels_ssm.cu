@@ -217,7 +217,7 @@ cudaError_t conv_width(int W, const SeqArgs &q, const T *x, int64_t ldx, T *y, i
 // tokens, so few rows are spread over segments of the sequence: a first pass makes
 // every segment's state from nothing, the second starts from the joined ones.
 // Six sequences, 1030 tokens the longest, 6 heads of 48 x 40: in one piece 256 us, cut
-// all alike 45, each by its own length 36, the blocks with work first 32; the two
+// all alike 45, each by its own length 36, the blocks with work first 33; the two
 // passes' latencies are what is left.  (Segments of 32 tokens: 31, but 98 for 61 for one
 // sequence of 2048 tokens and 4 heads of 64 x 128, whose segments are joined longer.)
 constexpr int RT = 16, SEG_MIN = 64;  // tokens of a run, and of a segment at least

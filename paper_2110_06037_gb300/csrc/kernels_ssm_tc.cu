@@ -11,8 +11,8 @@
 //   inside  P X         128 x P,   K = 128     P (the pairs, weighted) in two parts, from TMEM
 //   made    B^T X'      N x P,     K = 128     X' = weighted X in three parts
 // x, B and C are bf16, exact operands; what is computed goes in as bf16 parts: two for
-// the outputs, which are bf16 (2^-18 of a factor is lost, and by the decays up to 2^-14 of a
-// term, see TABLE), three for the state, which goes on in
+// the outputs, which are bf16 (2^-18 of a factor is lost, and by the decays 2^-24 of sums of
+// 16 steps, see TABLE), three for the state, which goes on in
 // fp32 (off by 9e-8 of itself; with two parts 2.4e-6, and 9 us less for 8192 tokens).
 // It stays in registers: each chunk's product is added by an fp32 multiply-add, since
 // the tensor core's own sums do not round to nearest.
@@ -28,7 +28,7 @@
 // blocks an SM, a chunk took a block 17.9 thousand cycles of waiting for one step after
 // the other: 198 us for 8192 tokens of 64 heads (64 channels, N = 128).  So: 159 us, of
 // which 7 are the time steps, 32 the first pass, 118 the second, 7300 cycles a chunk.
-// The tensor cores are busy in 38% of them, the busiest scheduler issues in 55%; what
+// The tensor cores are busy in 38% of them, schedulers issue in 49%; what
 // bounds it is the way from the pairs to P and to the next pairs.  (Tried and no faster: the next
 // chunk's pairs ahead, in TMEM of their own, 163; X' by the state's warps, 163; P's
 // columns 32 at a time, 165.)

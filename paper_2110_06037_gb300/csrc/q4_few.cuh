@@ -20,7 +20,8 @@ namespace {
 // from global memory to registers in the operand's layout, eight tiles in flight; the
 // block's part of x lies in shared memory.  k is split over the WK warps of a
 // block that share a tile and over the S blocks of a cluster, whose sums meet in a
-// fixed order.  One bf16 row, 25088 -> 4096: 17 us, 3200 GB/s; then bound by the
+// fixed order.  One bf16 row, 25088 -> 4096: 17 us, 3200 GB/s; then bound by its 256
+// equal blocks, of which 104 multiprocessors have two and 48 one, and by the
 // instructions that unpack the codes.
 constexpr int WARPS = 8;
 
