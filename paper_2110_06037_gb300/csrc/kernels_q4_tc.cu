@@ -27,9 +27,10 @@
 // matrix product's measured rate), 227 with groups of 64, 389 with groups of 32; fp32 rows
 // 417 (weights scaled in two bf16 parts took five products for the three: 895).  Bound by
 // the hand-overs: a wait, an arrival and their instructions take a warp some 200 cycles
-// each, a pair of column blocks 1240 and a group about 800 in all, whatever BN is, where the
-// tensor core takes 512 for a pair.  (One column block a stage: 268 us.  x's rows as the
-// lanes, so that every column has a scale of its own: 256.)
+// each, and a pair of column blocks 1370 cycles (groups of 64: 2000, of 32: 3430), whatever BN
+// is, where the tensor core takes 512.  With no sums read, no codes expanded and half
+// of the MMAs it is 1200 (3000 of 32).  (One column block a stage: 268 us.  x's rows as the lanes,
+// so that every column has a scale of its own: 256.)
 #include <algorithm>
 
 #include "q4_common.cuh"
@@ -541,7 +542,7 @@ cudaError_t launch_prompt(const CUtensorMap &mX, const PromptP &p, X *y, cudaStr
     static PerDevice set;
     if (const cudaError_t e = allow_smem(set, kern, Q4_SMEM)) return e;
     const int64_t total = (int64_t)p.mtiles * p.ntiles;
-    if (total > INT32_MAX) return cudaErrorInvalidValue;
+    if (total > INT32_MAX / 2) return cudaErrorInvalidValue;  // (a block's next tile is counted in 32 bits)
     // codes as [nt][kb][8 row pairs][32 halfwords]: a box is eight tiles of two column blocks
     CUtensorMap mC;
     const uint64_t dims[4] = {32, 8, (uint64_t)p.q.kb, (uint64_t)p.q.nt}, strides[3] = {64, 512, (uint64_t)p.q.kb * 512};
