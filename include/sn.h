@@ -584,6 +584,102 @@ SN_API sn_status sn_ssm_step(const sn_ssm_params *p, int32_t dtype, int32_t batc
                              int64_t xbc_stride, const void *dt, int64_t dt_stride, void *kept,
                              const float *state_in, float *state_out, int32_t n_slots, const int32_t *slots,
                              const int32_t *pos, void *y, int64_t y_stride, void *stream);
+
+/* ---------------- operators of an attention layer --------------------------
+ * The serving form of the attention layers that stand between state-space blocks:
+ * norms of queries and keys with the position rotation, a paged cache of keys and
+ * values, attention over it, and the verification of drafted tokens.  What is said
+ * above of dtypes, sequences, offsets, slots, overlaps, streams and errors holds
+ * here too.  A token's heads are head_stride elements apart and tokens `stride`, in
+ * any order of the two; the values of a head are contiguous. */
+
+/* Norm and rotation of every head of q and k, in one pass: v' = norm(v) * weight over the
+ * head (fp32 statistics; SN_HEADS_NONE: v' = v, without weights), then its first 2 pairs
+ * values turn, (a, b) -> (a cos t - b sin t, a sin t + b cos t) with t = pos[axis[i]] f[i]
+ * for pair i: values i and i + pairs, or 2 i and 2 i + 1 (interleaved).  turns holds
+ * f[i] / 2 pi as sn_rope_turns makes them; a product with a position is exact modulo one
+ * turn, so that angles are as good at position 2^31 as at 1.  pos: device int32
+ * [tokens][axes]; axis: device int32 [pairs], each in [0, axes), NULL: axis 0 (others count
+ * as axis 0).  head_dim is even, up to 256.  q_heads or k_heads may be 0.  q_out may be q and
+ * k_out may be k, with equal strides. */
+typedef enum { SN_HEADS_RMS = 0, SN_HEADS_LAYER = 1, SN_HEADS_NONE = 2 } sn_heads_norm;
+typedef struct {
+    int32_t head_dim, pairs, axes, norm, interleaved;
+    float eps;
+    const uint64_t *turns;              /* device [pairs]; NULL when pairs is 0 */
+    const int32_t *axis;                /* device [pairs] or NULL */
+    const float *q_weight, *k_weight;   /* device fp32 [head_dim] or NULL (ones) */
+} sn_rope_params;
+/* Angles a position in radians (host, finite, magnitude up to 2^20) to turns (host): 64-bit fixed
+ * point, modulo one turn. */
+SN_API sn_status sn_rope_turns(const double *radians, int32_t n, uint64_t *turns);
+SN_API sn_status sn_head_rope(const sn_rope_params *p, int32_t dtype, int64_t tokens, int32_t q_heads, const void *q,
+                              int64_t q_stride, int64_t q_head_stride, void *q_out, int64_t q_out_stride,
+                              int64_t q_out_head_stride, int32_t k_heads, const void *k, int64_t k_stride,
+                              int64_t k_head_stride, void *k_out, int64_t k_out_stride, int64_t k_out_head_stride,
+                              const int32_t *pos, void *stream);
+
+/* Paged cache of keys and values: k and v are [pages][heads][page][head_dim], aligned to 16
+ * bytes, of dtype SN_F32, SN_F16, SN_BF16, or of codes (SN_QI8) with fp32 scales (aligned to 16 too)
+ * [pages][heads][page].  page is 16, 32, 64, 128 or 256; head_dim a multiple of 16 up to 256.
+ * Codes of a token's head: scale = max |v| / 127 (1 for zeros, at least 2^-149), code =
+ * clamp(rint(v / scale), -127, 127), both divisions in fp32; a head with a value that is not
+ * finite gets the scale NaN and codes 0.
+ * table (device int32 [n_slots][width]) lists the pages of each entry: position p of a sequence
+ * lies in page table[slot][p / page] at p % page.  pos (device int32 [batch], NULL: zeros) is the
+ * position of each sequence's first token here.  A position beyond the table, or whose page
+ * is outside [0, pages), has no place: nothing is stored for it, it reads as zeros, and
+ * attention leaves it out; so has a sequence without a slot.
+ * sn_kv_write stores the tokens' k and v; sn_kv_read returns those of the tokens' positions in
+ * `dtype` (that of the cache, or any for codes: code * scale, rounded once). */
+typedef struct {
+    int32_t dtype, pages, heads, page, head_dim;
+    void *k, *v;
+    float *k_scale, *v_scale;           /* SN_QI8 only */
+} sn_kv_cache;
+SN_API sn_status sn_kv_write(const sn_kv_cache *c, int32_t dtype, int64_t tokens, int32_t batch, int64_t max_len,
+                             const int32_t *offsets, const int32_t *pos, const int32_t *table, int32_t n_slots,
+                             int32_t width, const int32_t *slots, const void *k, int64_t k_stride,
+                             int64_t k_head_stride, const void *v, int64_t v_stride, int64_t v_head_stride,
+                             void *stream);
+SN_API sn_status sn_kv_read(const sn_kv_cache *c, int32_t dtype, int64_t tokens, int32_t batch, int64_t max_len,
+                            const int32_t *offsets, const int32_t *pos, const int32_t *table, int32_t n_slots,
+                            int32_t width, const int32_t *slots, void *k, int64_t k_stride, int64_t k_head_stride,
+                            void *v, int64_t v_stride, int64_t v_head_stride, void *stream);
+
+/* Attention of new tokens over the cache, which holds them already:
+ *   y = sum_j w_j v_j / sum_j w_j,   w_j = exp(scale q k_j),
+ * over the positions j of the query's own sequence up to its own (token i of a sequence is at
+ * pos + i).  q and y are dtype, [tokens][q_heads]; head h reads head h / (q_heads / heads) of the
+ * cache, whose dtype is `dtype` or SN_QI8.  max_context: at least every sequence's pos + length
+ * (positions from there on are left out).  A query without keys, or all of whose scores are -inf,
+ * gives zeros.  Keys and values that a query does not see do not reach it, whatever they are. */
+SN_API sn_status sn_attend_workspace(const sn_kv_cache *c, int32_t dtype, int32_t q_heads, int64_t tokens,
+                                     int32_t batch, int64_t max_len, int64_t max_context, int64_t *bytes);
+SN_API sn_status sn_attend(const sn_kv_cache *c, int32_t dtype, int32_t q_heads, float scale, int64_t tokens,
+                           int32_t batch, int64_t max_len, int64_t max_context, const int32_t *offsets,
+                           const int32_t *pos, const int32_t *table, int32_t n_slots, int32_t width,
+                           const int32_t *slots, const void *q, int64_t q_stride, int64_t q_head_stride, void *y,
+                           int64_t y_stride, int64_t y_head_stride, void *work, int64_t work_bytes, void *stream);
+
+/* Verification of drafted tokens.  Sequence b has drafted tokens x_i (device int32 [tokens]) with
+ * the drafting model's probabilities q_i (draft, [tokens] rows of vocab) and the target's p_i
+ * (target, [tokens + batch] rows: one more a sequence, behind its others).  Token x_i is accepted
+ * while accept[i] * q_i[x_i] < p_i[x_i].  The next token comes from the row of the first one that
+ * is not, by the weights max(p - q, 0) (p, where these are all zero), or from the last row of
+ * p: it is the first index whose cumulative weight exceeds sample[b] times their sum (the last
+ * index where none does).  out (int32 [batch][max_len + 1]): the accepted tokens, the next one, then
+ * -1; count (int32 [batch]): how many were accepted.
+ * Probabilities and sums are held in units of 2^-60, in integers, so that no order of additions
+ * matters: values outside [0, 1] count as the nearest of the two, NaN as 0, and a row sums to 8
+ * at most (of a larger sum the drawn index is in range, and nothing more is said).  accept and
+ * sample are fp32 in [0, 1).  A drafted token outside the vocabulary is not accepted.  vocab up to 2^24. */
+SN_API sn_status sn_verify_draft(int32_t dtype, int32_t vocab, int64_t tokens, int32_t batch, int64_t max_len,
+                                 const int32_t *offsets, const void *target, int64_t target_stride,
+                                 const void *draft, int64_t draft_stride, const int32_t *drafted,
+                                 const float *accept, const float *sample, int32_t *out, int32_t *count,
+                                 void *stream);
+
 /* Waits for `stream` and reports whether a bounded wait of one of the library's
  * kernels gave up since the last report (SN_ETIMEOUT, and the record is cleared). */
 SN_API sn_status sn_check_device(void *stream);

@@ -87,6 +87,18 @@ class sn_ssm_params(C.Structure):
                 ("conv_w", C.c_void_p), ("conv_b", C.c_void_p)]
 
 
+class sn_rope_params(C.Structure):
+    _fields_ = [("head_dim", C.c_int32), ("pairs", C.c_int32), ("axes", C.c_int32), ("norm", C.c_int32),
+                ("interleaved", C.c_int32), ("eps", C.c_float), ("turns", C.c_void_p), ("axis", C.c_void_p),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p)]
+
+
+class sn_kv_cache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("pages", C.c_int32), ("heads", C.c_int32), ("page", C.c_int32),
+                ("head_dim", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p),
+                ("v_scale", C.c_void_p)]
+
+
 ALLOC_FN = C.CFUNCTYPE(C.c_void_p, C.c_size_t, C.c_void_p)
 FREE_FN = C.CFUNCTYPE(None, C.c_void_p, C.c_void_p)
 
@@ -149,6 +161,21 @@ SIGNATURES = {
     "sn_ssm_step": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64,
                               C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p,
                               C.c_int64, C.c_void_p]),
+    "sn_rope_turns": (C.c_int, [C.c_void_p, C.c_int32, C.c_void_p]),
+    "sn_head_rope": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64]
+                     + 2 * [C.c_int32, C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64]
+                     + [C.c_void_p, C.c_void_p]),
+    "sn_kv_write": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                              C.c_int32, C.c_int32, C.c_void_p] + 2 * [C.c_void_p, C.c_int64, C.c_int64] + [C.c_void_p]),
+    "sn_kv_read": (C.c_int, [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_void_p,
+                             C.c_int32, C.c_int32, C.c_void_p] + 2 * [C.c_void_p, C.c_int64, C.c_int64] + [C.c_void_p]),
+    "sn_attend_workspace": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_int64,
+                                      C.POINTER(C.c_int64)]),
+    "sn_attend": (C.c_int, [C.c_void_p, C.c_int32, C.c_int32, C.c_float, C.c_int64, C.c_int32, C.c_int64, C.c_int64,
+                            C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p]
+                  + 2 * [C.c_void_p, C.c_int64, C.c_int64] + [C.c_void_p, C.c_int64, C.c_void_p]),
+    "sn_verify_draft": (C.c_int, [C.c_int32, C.c_int32, C.c_int64, C.c_int32, C.c_int64, C.c_void_p, C.c_void_p, C.c_int64,
+                                  C.c_void_p, C.c_int64] + 6 * [C.c_void_p]),
     "sn_check_device": (C.c_int, [C.c_void_p]),
     "sn_last_error": (C.c_char_p, []),
 }

@@ -3,9 +3,9 @@
 Every translation unit under csrc/ is compiled by nvcc in parallel for
 sm_103a only, then linked with the static CUDA runtime into libsn.so next to
 this file.  Host code is portable C++17 (x86_64 here, aarch64 on the GPU host).
-bind/blocks.cpp, the tensor front end of the block operators, is compiled beside
-them against PyTorch's headers and linked to libsn.so as the module _blocks, where
-PyTorch is installed: the library itself needs nvcc alone.
+bind/*.cpp, the tensor front end of the block and attention operators, is compiled
+beside them against PyTorch's headers and linked to libsn.so as the module _blocks,
+where PyTorch is installed: the library itself needs nvcc alone.
 """
 from __future__ import annotations
 
@@ -21,7 +21,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(CSRC, "_build")
 LIB = os.path.join(HERE, "libsn.so")
-BIND_SRC = os.path.join(HERE, "bind", "blocks.cpp")
+BIND_DIR = os.path.join(HERE, "bind")
 BIND = os.path.join(HERE, "_blocks.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
@@ -61,24 +61,30 @@ def _torch_dir():
     return os.path.dirname(spec.origin) if spec is not None and spec.origin else None
 
 
-def _compile_bind():
-    obj = os.path.join(BUILD, "bind_blocks.o")
-    if os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(f) for f in [BIND_SRC] + _headers()):
+def _compile_bind_file(src):
+    obj = os.path.join(BUILD, f"bind_{os.path.basename(src)[:-4]}.o")
+    deps = [src] + glob.glob(os.path.join(BIND_DIR, "*.h")) + _headers()
+    if os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(f) for f in deps):
         return obj
     inc = [os.path.join(_torch_dir(), "include"), os.path.join(_torch_dir(), "include", "torch", "csrc", "api", "include"),
            sysconfig.get_paths()["include"], os.path.join(os.path.dirname(os.path.dirname(NVCC)), "include"),
            os.path.join(HERE, "..", "include")]
-    cmd = ["g++", "-O2", "-std=c++20", "-fPIC", "-fvisibility=hidden", "-w", "-c", BIND_SRC, "-o", obj]
+    cmd = ["g++", "-O2", "-std=c++20", "-fPIC", "-fvisibility=hidden", "-w", "-c", src, "-o", obj]
     r = subprocess.run(cmd + [x for i in inc for x in ("-I", i)], capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError(f"g++ failed for {BIND_SRC}:\n{r.stdout}\n{r.stderr}")
+        raise RuntimeError(f"g++ failed for {src}:\n{r.stdout}\n{r.stderr}")
     return obj
 
 
-def _link_bind(obj):
-    if os.path.exists(BIND) and os.path.getmtime(BIND) >= max(os.path.getmtime(obj), os.path.getmtime(LIB)):
+def _compile_bind():
+    with cf.ThreadPoolExecutor() as ex:
+        return list(ex.map(_compile_bind_file, sorted(glob.glob(os.path.join(BIND_DIR, "*.cpp")))))
+
+
+def _link_bind(objs):
+    if os.path.exists(BIND) and os.path.getmtime(BIND) >= max(os.path.getmtime(f) for f in objs + [LIB]):
         return
-    cmd = ["g++", "-shared", obj, "-o", BIND, "-L", os.path.join(_torch_dir(), "lib"), "-ltorch", "-ltorch_cpu", "-ltorch_python",
+    cmd = ["g++", "-shared"] + objs + ["-o", BIND, "-L", os.path.join(_torch_dir(), "lib"), "-ltorch", "-ltorch_cpu", "-ltorch_python",
            "-lc10", "-lc10_cuda", "-L", HERE, "-l:libsn.so", "-Wl,-rpath,$ORIGIN"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:

@@ -1,31 +1,10 @@
 // extern "C" boundary of the state-space block's operators (declared in
 // include/sn.h): every argument is checked here, before anything is launched.
-#include <new>
-#include <string>
-
-#include "sn_internal.h"
+#include "abi_checks.h"
 
 using namespace sn;
 
-#define SN_GUARD(...)                                                    \
-    try {                                                                \
-        __VA_ARGS__                                                      \
-    } catch (const std::bad_alloc &) {                                   \
-        return fail(SN_ENOMEM, "host allocation failed");                \
-    } catch (const std::exception &ex) {                                 \
-        return fail(SN_EINVAL, std::string("internal error: ") + ex.what()); \
-    } catch (...) {                                                      \
-        return fail(SN_EINVAL, "internal error");                        \
-    }
-#define SN_NEED(cond, what) \
-    if (!(cond)) return fail(SN_EINVAL, std::string(name) + ": " + what)
-
 namespace {
-
-constexpr int64_t kMaxRows = INT32_MAX;
-
-bool float_type(int32_t dt) { return dt == SN_F32 || dt == SN_F16 || dt == SN_BF16; }
-bool aligned(const void *p, int64_t bytes) { return reinterpret_cast<uintptr_t>(p) % (uintptr_t)bytes == 0; }
 
 sn_status q4_sizes(const char *name, int64_t n, int64_t k, int32_t group) {
     SN_NEED(n >= 1 && k >= 1, "n and k must be positive");
@@ -41,24 +20,6 @@ sn_status q4_weights(const char *name, const sn_q4_weights *w) {
     SN_NEED(w->act >= SN_ACT_NONE && w->act <= SN_ACT_HSIGMOID, "bad act");
     SN_NEED(w->packed && aligned(w->packed, 256), "packed must be device memory aligned to 256 bytes");
     SN_NEED(aligned(w->bias, 4), "misaligned bias");
-    return SN_OK;
-}
-
-sn_status rows_of(const char *name, const void *p, int64_t stride, int64_t len, int32_t dt, const char *what) {
-    SN_NEED(p, std::string("NULL ") + what);
-    SN_NEED(stride >= len, std::string("the stride of ") + what + " is shorter than its rows");
-    SN_NEED(aligned(p, dtype_size(dt)), std::string("misaligned ") + what);
-    return SN_OK;
-}
-
-sn_status sequences(const char *name, int64_t tokens, int32_t batch, int64_t max_len, const int32_t *offsets,
-                    int32_t n_slots, const int32_t *slots, const int32_t *pos) {
-    SN_NEED(tokens >= 0 && batch >= 0 && max_len >= 0 && n_slots >= 0, "negative size");
-    if (batch > 65535) return fail(SN_EUNSUPPORTED, std::string(name) + ": more than 65535 sequences");
-    if (tokens > kMaxRows || max_len > kMaxRows) return fail(SN_EUNSUPPORTED, std::string(name) + ": more than 2^31 - 1 tokens");
-    SN_NEED(max_len <= tokens || batch == 0 || tokens == 0, "max_len beyond the tokens there are");
-    if (!offsets) SN_NEED((int64_t)batch * max_len == tokens, "without offsets there are batch * max_len tokens");
-    SN_NEED(aligned(offsets, 4) && aligned(slots, 4) && aligned(pos, 4), "misaligned offsets, slots or pos");
     return SN_OK;
 }
 

@@ -1,0 +1,340 @@
+// Attention of new tokens over a paged cache (sn_attend in include/sn.h): the form for every type by
+// multiply-adds in fp32, the join of split items, and the choice between the forms.
+//
+// A unit is 64 keys: scores of ROWS queries against them, their running maximum and sum, and the weighted
+// values, all in fp32; keys and values lie in shared memory as fp32 (codes times their scales).
+#include <algorithm>
+
+#include "attn_common.cuh"
+
+namespace sn {
+namespace k {
+
+namespace {
+
+constexpr int KEYS = 64;
+constexpr float LOG2E = 1.4426950408889634f;
+
+// four neighbours of a row of the cache
+template <typename C>
+__device__ __forceinline__ float4 row4(const C *p) {
+    if constexpr (sizeof(C) == 4) {
+        return *reinterpret_cast<const float4 *>(p);
+    } else if constexpr (sizeof(C) == 2) {
+        alignas(8) C t[4];
+        *reinterpret_cast<uint2 *>(t) = *reinterpret_cast<const uint2 *>(p);
+        return make_float4(ldf(t), ldf(t + 1), ldf(t + 2), ldf(t + 3));
+    } else {
+        const char4 c = *reinterpret_cast<const char4 *>(p);
+        return make_float4((float)c.x, (float)c.y, (float)c.z, (float)c.w);
+    }
+}
+
+// thread (tr, tc) of 16 x 16 has rows tr + 16 i, keys tc + 16 j and values 4 tc + 64 j of a row
+template <typename T, typename C, int RPT, int DV>
+__global__ void __launch_bounds__(256) attend_kernel(const __grid_constant__ AttnP p) {
+    constexpr int ROWS = 16 * RPT;
+    extern __shared__ __align__(16) float sm[];
+    __shared__ int64_t sh[4];
+    const int d = p.c.head_dim, ld = d + 4, tid = threadIdx.x, tr = tid / 16, tc = tid % 16;
+    float *qs = sm, *ks = qs + ROWS * ld, *vs = ks + KEYS * ld, *ps = vs + KEYS * d;
+    __shared__ uint8_t there[KEYS];
+    griddep_launch();
+    griddep_wait();
+    Pieces pieces;
+    pieces.start(p, sh);
+    for (Piece w; pieces.next(p, w);) {
+        const Seq &s = w.past.s;
+        const int64_t row0 = (int64_t)w.tile * ROWS, all = (int64_t)s.len * p.group;
+        __syncthreads();
+        for (int i = tid; i < ROWS * d / 4; i += 256) {
+            const int r = i / (d / 4), e = i % (d / 4) * 4;
+            float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (row0 + r < all) {
+                const T *x = static_cast<const T *>(p.h.x) + (s.first + (row0 + r) / p.group) * p.h.ldx +
+                             ((int64_t)w.head * p.group + (row0 + r) % p.group) * p.h.hx + e;
+                f = make_float4(ldf(x), ldf(x + 1), ldf(x + 2), ldf(x + 3));
+            }
+            *reinterpret_cast<float4 *>(qs + r * ld + e) = f;
+        }
+        int last[RPT];
+        float m[RPT], l[RPT], o[RPT][4 * DV];
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            const int64_t row = row0 + tr + 16 * i;
+            last[i] = row < all ? last_key(p, w.past, row) : -1;
+            m[i] = -INFINITY, l[i] = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 4 * DV; ++j) o[i][j] = 0.0f;
+        }
+        const int end = last_key(p, w.past, min(row0 + ROWS, all) - 1);
+        const int u1 = min(w.u1, end / KEYS + 1);
+        for (int u = w.u0; u < u1; ++u) {
+            __syncthreads();
+            for (int i = tid; i < KEYS * d / 4; i += 256) {
+                const int r = i / (d / 4), e = i % (d / 4) * 4, key = u * KEYS + r;
+                const int64_t place = key < w.past.ctx ? place_in(p.c, p.t, s.slot, key) : -1;
+                float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f), g = f;
+                if (place >= 0) {
+                    const int64_t row = row_in(p.c, place, w.head), at = row * d + e;
+                    f = row4(static_cast<const C *>(p.c.k) + at), g = row4(static_cast<const C *>(p.c.v) + at);
+                    if constexpr (sizeof(C) == 1) {
+                        const float a = p.c.k_scale[row], b = p.c.v_scale[row];
+                        f.x *= a, f.y *= a, f.z *= a, f.w *= a;
+                        g.x *= b, g.y *= b, g.z *= b, g.w *= b;
+                    }
+                }
+                *reinterpret_cast<float4 *>(ks + r * ld + e) = f;
+                *reinterpret_cast<float4 *>(vs + r * d + e) = g;
+                if (e == 0) there[r] = place >= 0;
+            }
+            __syncthreads();
+            float a[RPT][4];
+#pragma unroll
+            for (int i = 0; i < RPT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) a[i][j] = 0.0f;
+#pragma unroll 2
+            for (int e = 0; e < d; e += 4) {
+                float4 x[RPT], y[4];
+#pragma unroll
+                for (int i = 0; i < RPT; ++i) x[i] = *reinterpret_cast<const float4 *>(qs + (tr + 16 * i) * ld + e);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4 *>(ks + (tc + 16 * j) * ld + e);
+#pragma unroll
+                for (int i = 0; i < RPT; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        a[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, a[i][j]))));
+            }
+#pragma unroll
+            for (int i = 0; i < RPT; ++i) {
+                float up = m[i];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int k = tc + 16 * j;
+                    a[i][j] = there[k] && u * KEYS + k <= last[i] ? a[i][j] * p.scale : -INFINITY;
+                    up = fmaxf(up, a[i][j]);
+                }
+#pragma unroll
+                for (int k = 8; k; k /= 2) up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, k));
+                const float base = up == -INFINITY ? 0.0f : up, old = exp2f(m[i] - base);
+                m[i] = up;
+                float sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float e = exp2f(a[i][j] - base);
+                    sum += e;
+                    ps[(tr + 16 * i) * (KEYS + 4) + tc + 16 * j] = e;
+                }
+#pragma unroll
+                for (int k = 8; k; k /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, k);
+                l[i] = fmaf(l[i], old, sum);
+#pragma unroll
+                for (int j = 0; j < 4 * DV; ++j) o[i][j] *= old;
+            }
+            __syncwarp();  // (a row's weights are written and read by the same half of a warp)
+            for (int k = 0; k < KEYS; k += 4) {
+                float4 x[RPT];
+#pragma unroll
+                for (int i = 0; i < RPT; ++i) x[i] = *reinterpret_cast<const float4 *>(ps + (tr + 16 * i) * (KEYS + 4) + k);
+#pragma unroll
+                for (int j = 0; j < DV; ++j) {
+                    const int e = 4 * tc + 64 * j;
+                    if (e >= d) break;
+                    float4 y[4];
+#pragma unroll
+                    for (int n = 0; n < 4; ++n) y[n] = *reinterpret_cast<const float4 *>(vs + (k + n) * d + e);
+#pragma unroll
+                    for (int i = 0; i < RPT; ++i) {
+                        float *f = o[i] + 4 * j;
+                        f[0] = fmaf(x[i].w, y[3].x, fmaf(x[i].z, y[2].x, fmaf(x[i].y, y[1].x, fmaf(x[i].x, y[0].x, f[0]))));
+                        f[1] = fmaf(x[i].w, y[3].y, fmaf(x[i].z, y[2].y, fmaf(x[i].y, y[1].y, fmaf(x[i].x, y[0].y, f[1]))));
+                        f[2] = fmaf(x[i].w, y[3].z, fmaf(x[i].z, y[2].z, fmaf(x[i].y, y[1].z, fmaf(x[i].x, y[0].z, f[2]))));
+                        f[3] = fmaf(x[i].w, y[3].w, fmaf(x[i].z, y[2].w, fmaf(x[i].y, y[1].w, fmaf(x[i].x, y[0].w, f[3]))));
+                    }
+                }
+            }
+        }
+        uint32_t again = 0;  // rows of this thread's that are not finite
+#pragma unroll
+        for (int i = 0; i < RPT; ++i) {
+            const int64_t row = row0 + tr + 16 * i;
+            if (w.slot >= 0) {
+                float *part = part_of_slot(p, w.slot);
+                const int r = tr + 16 * i;
+#pragma unroll
+                for (int j = 0; j < DV; ++j) {
+                    const int e = 4 * tc + 64 * j;
+                    if (e < d) *reinterpret_cast<float4 *>(part + r * d + e) = make_float4(o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]);
+                }
+                if (tc == 0) part[ROWS * d + r] = m[i], part[ROWS * d + ROWS + r] = l[i];
+            } else if (row < all) {
+                T *y = static_cast<T *>(p.h.y) + (s.first + row / p.group) * p.h.ldy + ((int64_t)w.head * p.group + row % p.group) * p.h.hy;
+                const float f = l[i] == 0.0f ? 0.0f : 1.0f / l[i];
+#pragma unroll
+                for (int j = 0; j < DV; ++j)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int e = 4 * tc + 64 * j + k;
+                        const float v = l[i] == 0.0f ? 0.0f : o[i][4 * j + k] * f;
+                        if (e < d) stf(y + e, v);
+                        if (!(fabsf(v) < INFINITY)) again |= 1u << i;
+                    }
+            }
+        }
+        if (w.slot < 0 && s.len > 1) {
+#pragma unroll
+            for (int i = 0; i < RPT; ++i) {
+                const uint32_t bad = __ballot_sync(0xffffffffu, again >> i & 1u);
+                for (int half = 0; half < 2; ++half)
+                    if (bad >> (16 * half) & 0xffffu) attend_again<T>(p, w.b, w.head, row0 + tid / 32 * 2 + half + 16 * i);
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------- join
+// a block takes a query's head: its warps the parts of it in turn, a lane eight values, and the warps' sums in order
+template <typename T>
+__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttnP p) {
+    constexpr int W = 4;
+    __shared__ float so[W][256], sm[W], sl[W];
+    griddep_launch();
+    griddep_wait();
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, d = p.c.head_dim;
+    const int64_t t = blockIdx.x / p.q_heads;
+    const int qh = (int)(blockIdx.x - t * p.q_heads), head = qh / p.group;
+    const int b = sequence_of(p.q, t);
+    if (b < 0) return;
+    const Past past = past_of(p, b);
+    const int64_t row = (t - past.s.first) * p.group + qh % p.group;
+    const int tile = (int)(row / p.rows), r = (int)(row % p.rows);
+    if (tile >= past.tiles) return;  // (not this launch's)
+    const Span span = span_of(p, b, -1);
+    const int64_t n = share_of(p, span.all), u0 = span.before + ((int64_t)head * past.tiles + tile) * past.units, u1 = u0 + past.units;
+    const int c0 = (int)(u0 / n), c1 = (int)((u1 - 1) / n);
+    if (c0 == c1) return;  // one block had all of it
+    auto part = [&](int c) { return part_of_slot(p, 2 * c + (c == c0 && u0 != c0 * n)); };
+    float m = -INFINITY;
+    for (int c = c0 + (int)threadIdx.x; c <= c1; c += 32 * W) m = fmaxf(m, part(c)[(int64_t)p.rows * d + r]);
+#pragma unroll
+    for (int o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if (lane == 0) sm[warp] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    const float base = m == -INFINITY ? 0.0f : m;
+    float o[8], l = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = 0.0f;
+#pragma unroll 4
+    for (int c = c0 + warp; c <= c1; c += W) {
+        const float *f = part(c);
+        const float w = exp2f(f[(int64_t)p.rows * d + r] - base);
+        l = fmaf(f[(int64_t)p.rows * d + p.rows + r], w, l);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int e = 4 * lane + 128 * i;
+            if (e < d) {
+                const float4 v = *reinterpret_cast<const float4 *>(f + r * d + e);
+                o[4 * i] = fmaf(v.x, w, o[4 * i]), o[4 * i + 1] = fmaf(v.y, w, o[4 * i + 1]);
+                o[4 * i + 2] = fmaf(v.z, w, o[4 * i + 2]), o[4 * i + 3] = fmaf(v.w, w, o[4 * i + 3]);
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) *reinterpret_cast<float4 *>(&so[warp][4 * lane + 128 * i]) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+    if (lane == 0) sl[warp] = l;
+    __syncthreads();
+    l = (sl[0] + sl[1]) + (sl[2] + sl[3]);
+    const float f = l == 0.0f ? 0.0f : 1.0f / l;
+    T *y = static_cast<T *>(p.h.y) + t * p.h.ldy + (int64_t)qh * p.h.hy;
+    bool bad = false;
+    for (int e = threadIdx.x; e < d; e += 32 * W) {
+        const float v = l == 0.0f ? 0.0f : ((so[0][e] + so[1][e]) + (so[2][e] + so[3][e])) * f;
+        stf(y + e, v);
+        bad |= !(fabsf(v) < INFINITY);
+    }
+    if (past.s.len > 1 && __syncthreads_or(bad) && warp == 0) attend_again<T>(p, b, head, row);
+}
+
+// ------------------------------------------------------------------ choice
+
+struct Plan {
+    AttnP p;
+    int64_t grid;
+};
+// how the sequences of more than lo and up to hi tokens are cut into items of `rows` rows and units of `keys` keys
+// for a grid of up to `room` blocks at once
+Plan plan_of(const sn_kv_cache &c, const AttendArgs &a, int lo, int hi, int rows, int keys, int room, int least) {
+    Plan r{};
+    AttnP &p = r.p;
+    p.q = a.q, p.c = c, p.t = a.t;
+    p.q_heads = a.h.heads, p.group = a.h.heads / c.heads;
+    p.max_ctx = (int32_t)a.max_context;
+    p.scale = a.scale * LOG2E;
+    p.h = a.h;
+    p.lo = lo, p.hi = hi, p.rows = rows, p.keys = keys, p.least = least;
+    p.err = device_error_word();
+    // items at most: a sequence's last one may be cut off
+    const int64_t seqs = lo ? std::min<int64_t>(a.q.batch, a.q.tokens / (lo + 1)) : a.q.batch;
+    const int64_t most = std::min<int64_t>(a.q.max_len, hi);
+    const int64_t items = c.heads * std::min(seqs * ((most * p.group + rows - 1) / rows), a.q.tokens * p.group / rows + seqs);
+    const int64_t units = std::max<int64_t>(1, (a.max_context + keys - 1) / keys);
+    r.grid = items;
+    if (units > least && items < 4 * (int64_t)room) {
+        p.blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(room, (items * units + least - 1) / least));
+        r.grid = p.blocks;
+    }
+    return r;
+}
+size_t part_bytes(const Plan &r) { return (size_t)r.p.blocks * 2 * r.p.rows * (r.p.c.head_dim + 2) * 4; }
+
+Plan simple_plan(const sn_kv_cache &c, const AttendArgs &a) {
+    const int rows = a.q.max_len * (a.h.heads / c.heads) <= 16 ? 16 : 64;
+    return plan_of(c, a, 0, INT32_MAX, rows, KEYS, 2 * num_sms(), 2);
+}
+
+template <typename T, typename C, int RPT, int DV>
+cudaError_t launch_simple(const Plan &r, cudaStream_t st) {
+    const int d = r.p.c.head_dim;
+    const size_t bytes = 4 * (size_t)(16 * RPT * (d + 4) + KEYS * (d + 4) + KEYS * d + 16 * RPT * (KEYS + 4));
+    static PerDevice set;
+    if (const cudaError_t e = allow_smem(set, attend_kernel<T, C, RPT, DV>, 224 * 1024)) return e;
+    return launch_pdl(attend_kernel<T, C, RPT, DV>, dim3((unsigned)r.grid), dim3(256), bytes, st, r.p);
+}
+template <typename T, typename C>
+cudaError_t simple_of(const Plan &r, cudaStream_t st) {
+    const int dv = (r.p.c.head_dim + 63) / 64;
+    if (r.p.rows == 16) {
+        if (dv == 1) return launch_simple<T, C, 1, 1>(r, st);
+        if (dv == 2) return launch_simple<T, C, 1, 2>(r, st);
+        return launch_simple<T, C, 1, 4>(r, st);
+    }
+    if (dv == 1) return launch_simple<T, C, 4, 1>(r, st);
+    if (dv == 2) return launch_simple<T, C, 4, 2>(r, st);
+    return launch_simple<T, C, 4, 4>(r, st);
+}
+
+template <typename T>
+cudaError_t join(const Plan &r, cudaStream_t st) {
+    if (!r.p.blocks) return cudaSuccess;
+    return launch_pdl(attend_join_kernel<T>, dim3((unsigned)(r.p.q.tokens * r.p.q_heads)), dim3(128), 0, st, r.p);
+}
+
+}  // namespace
+
+size_t attend_workspace(const sn_kv_cache &c, int dt, const AttendArgs &a) { return part_bytes(simple_plan(c, a)); }
+
+cudaError_t attend(const sn_kv_cache &c, int dt, const AttendArgs &a, void *work, cudaStream_t st) {
+    Plan r = simple_plan(c, a);
+    r.p.part = static_cast<float *>(work);
+    SN_DT_SWITCH(dt, T, {
+        const cudaError_t e = c.dtype == SN_QI8 ? simple_of<T, int8_t>(r, st) : simple_of<T, T>(r, st);
+        return e ? e : join<T>(r, st);
+    })
+    return cudaSuccess;
+}
+
+}  // namespace k
+}  // namespace sn

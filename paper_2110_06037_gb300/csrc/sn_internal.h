@@ -453,6 +453,43 @@ cudaError_t ssm_scan(const sn_ssm_params &p, int dt, const SeqArgs &q, const voi
                      int64_t lddt, const float *s_in, float *s_out, void *y, int64_t ldy, void *work, cudaStream_t st);
 cudaError_t ssm_step(const sn_ssm_params &p, int dt, const SeqArgs &q, const void *xbc, int64_t ldx, const void *dtv,
                      int64_t lddt, void *kept, const float *s_in, float *s_out, void *y, int64_t ldy, cudaStream_t st);
+// operators of an attention layer (declared in include/sn.h; arguments checked there)
+struct HeadsArgs {  // the heads of a tensor's tokens, read and written
+    int32_t heads;
+    const void *x;
+    int64_t ldx, hx;  // strides of tokens and heads, in elements
+    void *y;
+    int64_t ldy, hy;
+    const float *weight;
+};
+cudaError_t head_rope(const sn_rope_params &p, int dt, int64_t tokens, const HeadsArgs &q, const HeadsArgs &k, const int32_t *pos,
+                      cudaStream_t st);
+struct TableArgs {  // the pages of each entry
+    const int32_t *at;
+    int32_t width;
+};
+cudaError_t kv_write(const sn_kv_cache &c, int dt, const SeqArgs &q, const TableArgs &t, const HeadsArgs &k, const HeadsArgs &v,
+                     cudaStream_t st);
+cudaError_t kv_read(const sn_kv_cache &c, int dt, const SeqArgs &q, const TableArgs &t, const HeadsArgs &k, const HeadsArgs &v,
+                    cudaStream_t st);
+struct AttendArgs {
+    SeqArgs q;
+    TableArgs t;
+    int64_t max_context;
+    float scale;
+    HeadsArgs h;  // queries and outputs
+};
+size_t attend_workspace(const sn_kv_cache &c, int dt, const AttendArgs &a);
+cudaError_t attend(const sn_kv_cache &c, int dt, const AttendArgs &a, void *work, cudaStream_t st);
+struct VerifyArgs {
+    SeqArgs q;
+    const void *target, *draft;
+    int64_t ldt, ldd;
+    const int32_t *drafted;
+    const float *accept, *sample;
+    int32_t *out, *count;
+};
+cudaError_t verify_draft(int dt, int vocab, const VerifyArgs &a, cudaStream_t st);
 // running max |x| of a float blob into *out (fp32 bits; zero it first)
 cudaError_t absmax(const void *x, int dt, int64_t n, unsigned *out, cudaStream_t st);
 }  // namespace k
