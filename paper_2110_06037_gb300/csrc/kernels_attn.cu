@@ -5,7 +5,7 @@
 // values, all in fp32; keys and values lie in shared memory as fp32 (codes times their scales).
 #include <algorithm>
 
-#include "attn_common.cuh"
+#include "attn_few.cuh"
 
 namespace sn {
 namespace k {
@@ -264,9 +264,11 @@ struct Plan {
     AttnP p;
     int64_t grid;
 };
-// how the sequences of more than lo and up to hi tokens are cut into items of `rows` rows and units of `keys` keys
-// for a grid of up to `room` blocks at once
-Plan plan_of(const sn_kv_cache &c, const AttendArgs &a, int lo, int hi, int rows, int keys, int room, int least) {
+// How the sequences of more than lo and up to hi tokens are cut into items of `rows` rows and units of `keys` keys
+// for a grid of up to `room` blocks at once: split, unless every item is short or there are items for `waves` waves.
+// (A prompt's items have their diagonals in different places, which a split into equal numbers of units does not see.)
+// A split costs the join's launch (2 us); `least` units of a block are worth as much.
+Plan plan_of(const sn_kv_cache &c, const AttendArgs &a, int lo, int hi, int rows, int keys, int room, int least, int waves) {
     Plan r{};
     AttnP &p = r.p;
     p.q = a.q, p.c = c, p.t = a.t;
@@ -282,7 +284,7 @@ Plan plan_of(const sn_kv_cache &c, const AttendArgs &a, int lo, int hi, int rows
     const int64_t items = c.heads * std::min(seqs * ((most * p.group + rows - 1) / rows), a.q.tokens * p.group / rows + seqs);
     const int64_t units = std::max<int64_t>(1, (a.max_context + keys - 1) / keys);
     r.grid = items;
-    if (units > least && items < 4 * (int64_t)room) {
+    if (units > 2 * least && items < waves * (int64_t)room) {
         p.blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(room, (items * units + least - 1) / least));
         r.grid = p.blocks;
     }
@@ -290,9 +292,36 @@ Plan plan_of(const sn_kv_cache &c, const AttendArgs &a, int lo, int hi, int rows
 }
 size_t part_bytes(const Plan &r) { return (size_t)r.p.blocks * 2 * r.p.rows * (r.p.c.head_dim + 2) * 4; }
 
-Plan simple_plan(const sn_kv_cache &c, const AttendArgs &a) {
-    const int rows = a.q.max_len * (a.h.heads / c.heads) <= 16 ? 16 : 64;
-    return plan_of(c, a, 0, INT32_MAX, rows, KEYS, 2 * num_sms(), 2);
+// sequences of up to this many tokens go to the form for few queries
+int few_tokens(int group) { return std::max(1, 64 / group); }
+
+struct Few {
+    few::Shape (*shape)(int, int64_t);
+    cudaError_t (*launch)(const AttnP &, int64_t, cudaStream_t);
+};
+Few few_of(int dt, int cache) {
+    if (cache == SN_QI8)
+        return dt == SN_F16 ? Few{few_shape_f16_q8, attend_few_f16_q8} : dt == SN_BF16 ? Few{few_shape_bf16_q8, attend_few_bf16_q8}
+                                                                                 : Few{few_shape_f32_q8, attend_few_f32_q8};
+    if (dt == SN_F32) return Few{nullptr, nullptr};
+    return dt == SN_F16 ? Few{few_shape_f16, attend_few_f16} : Few{few_shape_bf16, attend_few_bf16};
+}
+
+// the launches of a call: sequences of few tokens, the others; either may have nothing to do (grid 0)
+struct Plans {
+    Few few;
+    Plan a, b;
+};
+Plans plans_of(const sn_kv_cache &c, int dt, const AttendArgs &a) {
+    Plans r{few_of(dt, c.dtype), Plan{}, Plan{}};
+    const int group = a.h.heads / c.heads, n = r.few.launch ? few_tokens(group) : 0;
+    if (n) {
+        const few::Shape s = r.few.shape(c.head_dim, std::min<int64_t>(a.q.max_len, n) * group);
+        r.a = plan_of(c, a, 0, n, s.rows, few::UNIT, s.blocks * num_sms(), 4, 16);
+        if (!a.q.offsets && a.q.max_len > n) r.a.grid = 0;
+    }
+    if (a.q.max_len > n) r.b = plan_of(c, a, n, INT32_MAX, a.q.max_len * group <= 16 ? 16 : 64, KEYS, 2 * num_sms(), 2, 1);
+    return r;
 }
 
 template <typename T, typename C, int RPT, int DV>
@@ -324,14 +353,23 @@ cudaError_t join(const Plan &r, cudaStream_t st) {
 
 }  // namespace
 
-size_t attend_workspace(const sn_kv_cache &c, int dt, const AttendArgs &a) { return part_bytes(simple_plan(c, a)); }
+size_t attend_workspace(const sn_kv_cache &c, int dt, const AttendArgs &a) {
+    const Plans r = plans_of(c, dt, a);
+    return std::max(part_bytes(r.a), part_bytes(r.b));
+}
 
 cudaError_t attend(const sn_kv_cache &c, int dt, const AttendArgs &a, void *work, cudaStream_t st) {
-    Plan r = simple_plan(c, a);
-    r.p.part = static_cast<float *>(work);
+    Plans r = plans_of(c, dt, a);
+    r.a.p.part = r.b.p.part = static_cast<float *>(work);  // (one after the other)
     SN_DT_SWITCH(dt, T, {
-        const cudaError_t e = c.dtype == SN_QI8 ? simple_of<T, int8_t>(r, st) : simple_of<T, T>(r, st);
-        return e ? e : join<T>(r, st);
+        if (r.a.grid) {
+            if (const cudaError_t e = r.few.launch(r.a.p, r.a.grid, st)) return e;
+            if (const cudaError_t e = join<T>(r.a, st)) return e;
+        }
+        if (r.b.grid) {
+            if (const cudaError_t e = c.dtype == SN_QI8 ? simple_of<T, int8_t>(r.b, st) : simple_of<T, T>(r.b, st)) return e;
+            if (const cudaError_t e = join<T>(r.b, st)) return e;
+        }
     })
     return cudaSuccess;
 }

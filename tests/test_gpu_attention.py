@@ -166,8 +166,14 @@ class Case:
 
 def attend_bound(ref, dim, dt):
     """A score of dim products and two factors is off by es; a weight by that (its sum too), its exponential's 4 ulp and,
-    where it goes to the tensor cores in 16 bits, by its rounding; the sums by one rounding a key and 64 more."""
+    where it goes to the tensor cores in 16 bits, by its rounding; the sums by one rounding a key and 64 more.
+    Added after a first run in which a query's one large weight met a value of 0: a weight in fp16 (codes, fp16) below the
+    normal range is off by half the spacing there, 2^-25, not by a part of itself; the largest being 2^14, that is 2^-39
+    of the largest, a key, times its value (of these tests' values none is beyond 16; the sum of weights is the largest's
+    at least)."""
     _, mag, es, seen = ref
+    if dt != "f32":
+        mag = mag + (seen * 16.0 * 2.0 ** -39)[..., None] / U[dt]
     rel = 2 * (dim + 8) * 2 * E32 * es + 2 * 8 * E32 + (seen + 64) * 2 * E32 + U[dt]
     return mag * rel[..., None]
 
