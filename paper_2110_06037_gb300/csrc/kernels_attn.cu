@@ -6,6 +6,7 @@
 #include <algorithm>
 
 #include "attn_few.cuh"
+#include "attn_prompt.cuh"
 
 namespace sn {
 namespace k {
@@ -310,17 +311,25 @@ Few few_of(int dt, int cache) {
 // the launches of a call: sequences of few tokens, the others; either may have nothing to do (grid 0)
 struct Plans {
     Few few;
+    bool tensor;  // b by attn_prompt.cuh
     Plan a, b;
 };
 Plans plans_of(const sn_kv_cache &c, int dt, const AttendArgs &a) {
-    Plans r{few_of(dt, c.dtype), Plan{}, Plan{}};
-    const int group = a.h.heads / c.heads, n = r.few.launch ? few_tokens(group) : 0;
+    Plans r{few_of(dt, c.dtype), dt != SN_F32 && c.dtype != SN_QI8, Plan{}, Plan{}};
+    const int group = a.h.heads / c.heads, n = !r.few.launch ? 0 : r.tensor ? few_tokens(group) : INT32_MAX;
     if (n) {
         const few::Shape s = r.few.shape(c.head_dim, std::min<int64_t>(a.q.max_len, n) * group);
         r.a = plan_of(c, a, 0, n, s.rows, few::UNIT, s.blocks * num_sms(), 4, 16);
         if (!a.q.offsets && a.q.max_len > n) r.a.grid = 0;
     }
-    if (a.q.max_len > n) r.b = plan_of(c, a, n, INT32_MAX, a.q.max_len * group <= 16 ? 16 : 64, KEYS, 2 * num_sms(), 2, 1);
+    if (a.q.max_len > n && r.tensor) {
+        // two tiles of rows a block, unless one each makes more blocks busy (heads beyond 128 values: one)
+        const int keys = c.head_dim > 128 ? 64 : 128, sms = num_sms();
+        r.b = plan_of(c, a, n, INT32_MAX, 256, keys, sms, 4, 1);
+        if (c.head_dim > 128 || r.b.p.blocks) r.b = plan_of(c, a, n, INT32_MAX, 128, keys, sms, 4, 1);
+    } else if (a.q.max_len > n) {
+        r.b = plan_of(c, a, n, INT32_MAX, a.q.max_len * group <= 16 ? 16 : 64, KEYS, 2 * num_sms(), 2, 1);
+    }
     return r;
 }
 
@@ -367,7 +376,8 @@ cudaError_t attend(const sn_kv_cache &c, int dt, const AttendArgs &a, void *work
             if (const cudaError_t e = join<T>(r.a, st)) return e;
         }
         if (r.b.grid) {
-            if (const cudaError_t e = c.dtype == SN_QI8 ? simple_of<T, int8_t>(r.b, st) : simple_of<T, T>(r.b, st)) return e;
+            if (const cudaError_t e = r.tensor ? (dt == SN_F16 ? attend_prompt_f16 : attend_prompt_bf16)(r.b.p, r.b.grid, st) : simple_of<float, float>(r.b, st))
+                return e;
             if (const cudaError_t e = join<T>(r.b, st)) return e;
         }
     })
