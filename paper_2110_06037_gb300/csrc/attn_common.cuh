@@ -6,27 +6,19 @@
 namespace sn {
 namespace k {
 
-// the sequence that token t lies in, -1: none.  Called by whole warps with one t; each turn
-// narrows the range of sequences to a 32nd.
-__device__ __forceinline__ int sequence_of(const SeqArgs &q, int64_t t) {
+// the sequence that token t lies in, -1: none (of empty sequences the one behind them)
+__device__ __forceinline__ int sequence_at(const SeqArgs &q, int64_t t) {
     if (!q.offsets) {
         const int64_t b = q.max_len > 0 ? t / q.max_len : q.batch;
         return b < q.batch ? (int)b : -1;
     }
-    const int lane = threadIdx.x % 32;
-    // the last b with offsets[b] <= t (of empty sequences the one behind them)
-    int lo = 0, n = q.batch;  // it is lo - 1 or among the n from lo
-    while (n > 0) {
-        const int step = (n + 31) / 32;
-        const uint32_t below = __ballot_sync(0xffffffffu, lane * step < n && q.offsets[lo + lane * step] <= t);
-        const int found = 32 - __clz(below);  // the last of the 32 that is not beyond t, from 1
-        if (found == 0) break;
-        const int first = lo + (found - 1) * step;
-        n = min(step, lo + n - first) - 1;
-        lo = first + 1;
+    int lo = 0, hi = q.batch;  // the last b with offsets[b] <= t is lo - 1 or in [lo, hi)
+    while (lo < hi) {
+        const int mid = (lo + hi) / 2;
+        if (q.offsets[mid] <= t) lo = mid + 1;
+        else hi = mid;
     }
-    const int b = lo - 1;
-    return b >= 0 && t < q.offsets[b + 1] ? b : -1;
+    return lo > 0 && t < q.offsets[lo] ? lo - 1 : -1;
 }
 
 // where position `at` of slot's sequence lies: its page times the page's length plus its place there, -1: nowhere

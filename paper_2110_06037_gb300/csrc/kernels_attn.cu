@@ -196,40 +196,65 @@ __global__ void __launch_bounds__(256) attend_kernel(const __grid_constant__ Att
 }
 
 // ------------------------------------------------------------------- join
-// a block takes a query's head: its warps the parts of it in turn, a lane eight values, and the warps' sums in order
-template <typename T>
-__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttnP p) {
+// The items are counted again, and WPR warps take a row of one: its parts in turn, a lane eight values, and the
+// warps' sums in order.  used: rows of an item that there can be.  (Four warps where an item has many parts, one where
+// there are many items: 64 sequences of 8 heads by one warp a row 5 us, by four 9.)
+template <typename T, int WPR>
+__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttnP p, int used) {
     constexpr int W = 4;
     __shared__ float so[W][256], sm[W], sl[W];
     griddep_launch();
     griddep_wait();
-    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, d = p.c.head_dim;
-    const int64_t t = blockIdx.x / p.q_heads;
-    const int qh = (int)(blockIdx.x - t * p.q_heads), head = qh / p.group;
-    const int b = sequence_of(p.q, t);
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, sub = warp % WPR, d = p.c.head_dim;
+    const int64_t id = (int64_t)blockIdx.x * (W / WPR) + warp / WPR, item = id / used;
+    const int r = (int)(id - item * used);
+    int b = -1;
+    int64_t all = 0, before = 0, items = 0, mine = 0;  // units of all; before b's; items before b's; of this item among them
+    for (int b0 = 0; b0 < p.q.batch; b0 += 32) {
+        const Past s = past_of(p, min(b0 + lane, p.q.batch - 1));
+        const int64_t n = b0 + lane < p.q.batch ? (int64_t)s.tiles * p.c.heads : 0;
+        int64_t up = n, units = n * s.units;
+#pragma unroll
+        for (int o = 1; o < 32; o *= 2) {
+            const int64_t v = __shfl_up_sync(0xffffffffu, up, o), u = __shfl_up_sync(0xffffffffu, units, o);
+            if (lane >= o) up += v, units += u;
+        }
+        const uint32_t in = __ballot_sync(0xffffffffu, item < items + up);
+        if (b < 0 && in) {
+            const int k = __ffs(in) - 1;
+            b = b0 + k;
+            mine = item - items - __shfl_sync(0xffffffffu, up - n, k);
+            before = all + __shfl_sync(0xffffffffu, units - n * s.units, k);
+        }
+        items += __shfl_sync(0xffffffffu, up, 31);
+        all += __shfl_sync(0xffffffffu, units, 31);
+    }
     if (b < 0) return;
     const Past past = past_of(p, b);
-    const int64_t row = (t - past.s.first) * p.group + qh % p.group;
-    const int tile = (int)(row / p.rows), r = (int)(row % p.rows);
-    if (tile >= past.tiles) return;  // (not this launch's)
-    const Span span = span_of(p, b, -1);
-    const int64_t n = share_of(p, span.all), u0 = span.before + ((int64_t)head * past.tiles + tile) * past.units, u1 = u0 + past.units;
+    const int head = (int)(mine / past.tiles), tile = (int)(mine - (int64_t)head * past.tiles);
+    const int64_t row = (int64_t)tile * p.rows + r;
+    if (row >= (int64_t)past.s.len * p.group) return;
+    const int64_t t = past.s.first + row / p.group;
+    const int qh = head * p.group + (int)(row % p.group);
+    const int64_t n = share_of(p, all), u0 = before + mine * past.units, u1 = u0 + past.units;
     const int c0 = (int)(u0 / n), c1 = (int)((u1 - 1) / n);
     if (c0 == c1) return;  // one block had all of it
     auto part = [&](int c) { return part_of_slot(p, 2 * c + (c == c0 && u0 != c0 * n)); };
     float m = -INFINITY;
-    for (int c = c0 + (int)threadIdx.x; c <= c1; c += 32 * W) m = fmaxf(m, part(c)[(int64_t)p.rows * d + r]);
+    for (int c = c0 + sub * 32 + lane; c <= c1; c += 32 * WPR) m = fmaxf(m, part(c)[(int64_t)p.rows * d + r]);
 #pragma unroll
     for (int o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if (lane == 0) sm[warp] = m;
-    __syncthreads();
-    m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    if constexpr (WPR > 1) {
+        if (lane == 0) sm[warp] = m;
+        __syncthreads();
+        m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    }
     const float base = m == -INFINITY ? 0.0f : m;
     float o[8], l = 0.0f;
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = 0.0f;
 #pragma unroll 4
-    for (int c = c0 + warp; c <= c1; c += W) {
+    for (int c = c0 + sub; c <= c1; c += WPR) {
         const float *f = part(c);
         const float w = exp2f(f[(int64_t)p.rows * d + r] - base);
         l = fmaf(f[(int64_t)p.rows * d + p.rows + r], w, l);
@@ -243,20 +268,31 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
             }
         }
     }
+    if constexpr (WPR > 1) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) *reinterpret_cast<float4 *>(&so[warp][4 * lane + 128 * i]) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-    if (lane == 0) sl[warp] = l;
-    __syncthreads();
-    l = (sl[0] + sl[1]) + (sl[2] + sl[3]);
+        for (int i = 0; i < 2; ++i) *reinterpret_cast<float4 *>(&so[warp][4 * lane + 128 * i]) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+        if (lane == 0) sl[warp] = l;
+        __syncthreads();
+        if (warp) return;
+        l = (sl[0] + sl[1]) + (sl[2] + sl[3]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = 4 * lane + 128 * (i / 4) + i % 4;
+            o[i] = (so[0][e] + so[1][e]) + (so[2][e] + so[3][e]);
+        }
+    }
     const float f = l == 0.0f ? 0.0f : 1.0f / l;
     T *y = static_cast<T *>(p.h.y) + t * p.h.ldy + (int64_t)qh * p.h.hy;
     bool bad = false;
-    for (int e = threadIdx.x; e < d; e += 32 * W) {
-        const float v = l == 0.0f ? 0.0f : ((so[0][e] + so[1][e]) + (so[2][e] + so[3][e])) * f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int e = 4 * lane + 128 * (i / 4) + i % 4;
+        if (e >= d) continue;
+        const float v = l == 0.0f ? 0.0f : o[i] * f;
         stf(y + e, v);
         bad |= !(fabsf(v) < INFINITY);
     }
-    if (past.s.len > 1 && __syncthreads_or(bad) && warp == 0) attend_again<T>(p, b, head, row);
+    if (past.s.len > 1 && __any_sync(0xffffffffu, bad)) attend_again<T>(p, b, head, row);
 }
 
 // ------------------------------------------------------------------ choice
@@ -264,6 +300,8 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
 struct Plan {
     AttnP p;
     int64_t grid;
+    int64_t items;  // at most
+    int used;       // rows of an item at most
 };
 // How the sequences of more than lo and up to hi tokens are cut into items of `rows` rows and units of `keys` keys
 // for a grid of up to `room` blocks at once: split, unless every item is short or there are items for `waves` waves.
@@ -284,7 +322,8 @@ Plan plan_of(const sn_kv_cache &c, const AttendArgs &a, int lo, int hi, int rows
     const int64_t most = std::min<int64_t>(a.q.max_len, hi);
     const int64_t items = c.heads * std::min(seqs * ((most * p.group + rows - 1) / rows), a.q.tokens * p.group / rows + seqs);
     const int64_t units = std::max<int64_t>(1, (a.max_context + keys - 1) / keys);
-    r.grid = items;
+    r.grid = r.items = items;
+    r.used = (int)std::min<int64_t>(rows, most * p.group);
     if (units > 2 * least && items < waves * (int64_t)room) {
         p.blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(room, (items * units + least - 1) / least));
         r.grid = p.blocks;
@@ -357,7 +396,9 @@ cudaError_t simple_of(const Plan &r, cudaStream_t st) {
 template <typename T>
 cudaError_t join(const Plan &r, cudaStream_t st) {
     if (!r.p.blocks) return cudaSuccess;
-    return launch_pdl(attend_join_kernel<T>, dim3((unsigned)(r.p.q.tokens * r.p.q_heads)), dim3(128), 0, st, r.p);
+    const int64_t rows = r.items * r.used;
+    if (r.p.blocks > 8 * r.items) return launch_pdl(attend_join_kernel<T, 4>, dim3((unsigned)rows), dim3(128), 0, st, r.p, r.used);
+    return launch_pdl(attend_join_kernel<T, 1>, dim3((unsigned)((rows + 3) / 4)), dim3(128), 0, st, r.p, r.used);
 }
 
 }  // namespace

@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "kern_common.cuh"
+#include "tc_common.cuh"
 
 namespace sn {
 namespace k {
@@ -30,35 +31,27 @@ struct RopeP {
     float eps;
 };
 
+// W values as they lie in memory, and pairs of them
 template <typename T, int W>
-__device__ __forceinline__ void load_w(float *v, const T *p) {
-    constexpr int B = W * sizeof(T);
-    if constexpr (B == 16 || B == 8 || B == 4) {
-        using U = typename std::conditional<B == 16, uint4, typename std::conditional<B == 8, uint2, uint32_t>::type>::type;
-        U u = *reinterpret_cast<const U *>(p);
-        const T *t = reinterpret_cast<const T *>(&u);
-#pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = ldf(t + i);
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i) v[i] = ldf(p + i);
+struct alignas(W * sizeof(T) <= 16 ? W * sizeof(T) : 16) Raw {
+    T v[W];
+    __device__ __forceinline__ F2 two(int j) const {
+        if constexpr (W == 1) {
+            return f2(ldf(v), 0.0f);
+        } else if constexpr (sizeof(T) == 4) {
+            return f2(v[2 * j], v[2 * j + 1]);
+        } else {
+            const float2 f = tc::unpack2<T>(*reinterpret_cast<const uint32_t *>(v + 2 * j));
+            return f2(f.x, f.y);
+        }
     }
-}
-template <typename T, int W>
-__device__ __forceinline__ void store_w(T *p, const float *v) {
-    constexpr int B = W * sizeof(T);
-    if constexpr (B == 16 || B == 8 || B == 4) {
-        using U = typename std::conditional<B == 16, uint4, typename std::conditional<B == 8, uint2, uint32_t>::type>::type;
-        U u;
-        T *t = reinterpret_cast<T *>(&u);
-#pragma unroll
-        for (int i = 0; i < W; ++i) stf(t + i, v[i]);
-        *reinterpret_cast<U *>(p) = u;
-    } else {
-#pragma unroll
-        for (int i = 0; i < W; ++i) stf(p + i, v[i]);
+    __device__ __forceinline__ void set(int j, F2 x) {
+        const float2 f = floats(x);
+        if constexpr (W == 1) stf(v, f.x);
+        else if constexpr (sizeof(T) == 4) v[2 * j] = f.x, v[2 * j + 1] = f.y;
+        else *reinterpret_cast<uint32_t *>(v + 2 * j) = tc::pack2<T>(f.x, f.y);
     }
-}
+};
 
 __device__ __forceinline__ void turn(uint64_t angle, float &c, float &s) {
     const uint32_t u = (uint32_t)(angle >> 32);
@@ -73,10 +66,16 @@ __device__ __forceinline__ void turn(uint64_t angle, float &c, float &s) {
 }
 
 template <typename T, int W, int NC>
-__global__ void __launch_bounds__(256) head_rope_kernel(const __grid_constant__ RopeP p, int lph) {
-    constexpr int V = 2 * W * NC;
+__global__ void __launch_bounds__(256, 3) head_rope_kernel(const __grid_constant__ RopeP p, int lph) {
+    constexpr int AHEAD = 2, P = (W + 1) / 2;  // W = 1: the upper half of each F2 is idle
+    __shared__ __align__(16) float weights[2][256];  // (1 without)
     griddep_launch();
     griddep_wait();
+    for (int i = threadIdx.x; i < p.d; i += 256) {
+        weights[0][i] = p.h[0].weight ? p.h[0].weight[i] : 1.0f;
+        weights[1][i] = p.h[1].weight ? p.h[1].weight[i] : 1.0f;
+    }
+    __syncthreads();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, sub = lane % lph, per = 32 / lph;
     const int64_t id = (int64_t)blockIdx.x * 8 + warp;
     const int64_t t = id / p.split;
@@ -84,7 +83,7 @@ __global__ void __launch_bounds__(256) head_rope_kernel(const __grid_constant__ 
     const int part = (int)(id - t * p.split);
     // this lane's slots: where their values lie, and their turns
     int at[NC], bt[NC];
-    float cs[NC * W], sn[NC * W];
+    F2 cs[NC * P], sn[NC * P];
     bool in[NC];
 #pragma unroll
     for (int i = 0; i < NC; ++i) {
@@ -93,93 +92,143 @@ __global__ void __launch_bounds__(256) head_rope_kernel(const __grid_constant__ 
         const bool turns = c < p.pairs;
         at[i] = turns && !p.interleaved ? c : 2 * c;
         bt[i] = turns && !p.interleaved ? c + p.pairs : 2 * c + W;
+        // (of the lanes that share a slot, each computes every per-th turn of it)
+        float mc[W], ms[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) {
-            cs[i * W + j] = 1.0f, sn[i * W + j] = 0.0f;
-            if (!in[i] || !turns) continue;
-            int axis = p.axis ? p.axis[c + j] : 0;
+            mc[j] = 1.0f, ms[j] = 0.0f;
+            const int mine = j * per + lane / lph % min(per, W);
+            if (j * per >= W || !in[i] || !turns) continue;
+            int axis = p.axis ? p.axis[c + mine] : 0;
             if (axis < 0 || axis >= p.axes) axis = 0;
-            turn((uint64_t)(int64_t)p.pos[t * p.axes + axis] * p.turns[c + j], cs[i * W + j], sn[i * W + j]);
+            turn((uint64_t)(int64_t)p.pos[t * p.axes + axis] * p.turns[c + mine], mc[j], ms[j]);
         }
+        float own_c[W], own_s[W];
+#pragma unroll
+        for (int j = 0; j < W; ++j) own_c[j] = mc[j], own_s[j] = ms[j];
+#pragma unroll
+        for (int j = 0; j < W; ++j) {
+            const int from = sub + (j & (per - 1)) * lph, which = j / per;
+            float c1 = own_c[0], s1 = own_s[0];
+#pragma unroll
+            for (int k = 1; k < W; ++k)
+                if (k == which) c1 = own_c[k], s1 = own_s[k];
+            mc[j] = __shfl_sync(0xffffffffu, c1, from);
+            ms[j] = __shfl_sync(0xffffffffu, s1, from);
+        }
+#pragma unroll
+        for (int j = 0; j < P; ++j) cs[i * P + j] = f2(mc[2 * j], W > 1 ? mc[2 * j + 1 < W ? 2 * j + 1 : 0] : 0.0f), sn[i * P + j] = f2(ms[2 * j], W > 1 ? ms[2 * j + 1 < W ? 2 * j + 1 : 0] : 0.0f);
     }
     const float inv_d = 1.0f / (float)p.d;
-    const uint32_t group = lph == 32 ? 0xffffffffu : ((1u << lph) - 1u) << (lane / lph * lph);
+    auto both = [](F2 v) {
+        const float2 f = floats(v);
+        return f.x + f.y;
+    };
+    auto all = [&](float s) {  // (by whole warps: lanes without a head take part with what they have)
+        for (int o = lph / 2; o; o /= 2) s += __shfl_xor_sync(0xffffffffu, s, o);
+        return s;
+    };
 #pragma unroll 1
     for (int which = 0; which < 2; ++which) {
         const HeadsArgs &h = p.h[which];
-        const int heads = h.heads;
-        if (heads == 0) continue;
-        float w[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) w[i] = 1.0f;
-        if (h.weight) {
+        const int heads = h.heads, step = p.split * per;
+        int n = part * per + lane / lph;
+        const int turns = (heads - part * per + step - 1) / step;  // of the warp
+        const T *x = static_cast<const T *>(h.x) + t * h.ldx + n * h.hx;
+        T *y = static_cast<T *>(h.y) + t * h.ldy + n * h.hy;
+        const int64_t dx = step * h.hx, dy = step * h.hy;
+        const bool scaled = h.weight != nullptr;
+        // (the next AHEAD heads are on their way while one is worked on)
+        Raw<T, W> raw[AHEAD][2 * NC] = {};
+        int next = n;
+        auto load = [&](Raw<T, W> (&r)[2 * NC]) {
 #pragma unroll
             for (int i = 0; i < NC; ++i)
-                if (in[i]) {
-#pragma unroll
-                    for (int j = 0; j < W; ++j) w[2 * W * i + j] = h.weight[at[i] + j], w[2 * W * i + W + j] = h.weight[bt[i] + j];
+                if (in[i] && next < heads) {
+                    r[2 * i] = *reinterpret_cast<const Raw<T, W> *>(x + at[i]);
+                    r[2 * i + 1] = *reinterpret_cast<const Raw<T, W> *>(x + bt[i]);
                 }
-        }
-        const T *x = static_cast<const T *>(h.x) + t * h.ldx;
-        T *y = static_cast<T *>(h.y) + t * h.ldy;
-        for (int n = part * per + lane / lph; n < heads; n += p.split * per) {
-            const T *xh = x + n * h.hx;
-            T *yh = y + n * h.hy;
-            float v[V];
+            next += step, x += dx;
+        };
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
+        for (int k = 0; k < AHEAD; ++k) load(raw[k]);
+#pragma unroll 1
+        for (int i0 = 0; i0 < turns; i0 += AHEAD)
 #pragma unroll
-                for (int j = 0; j < 2 * W; ++j) v[2 * W * i + j] = 0.0f;
-                if (in[i]) {
-                    load_w<T, W>(v + 2 * W * i, xh + at[i]);
-                    load_w<T, W>(v + 2 * W * i + W, xh + bt[i]);
-                }
-            }
-            if (p.norm != SN_HEADS_NONE) {
-                if (p.norm == SN_HEADS_LAYER) {
-                    float s = 0.0f;
+            for (int k = 0; k < AHEAD; ++k) {
+                if (i0 + k >= turns) break;
+                F2 v[NC][2][P];  // both values of this lane's slots
 #pragma unroll
-                    for (int j = 0; j < V; ++j) s += v[j];
-                    for (int o = lph / 2; o; o /= 2) s += __shfl_xor_sync(group, s, o);
-                    s *= inv_d;
+                for (int i = 0; i < NC; ++i)
+#pragma unroll
+                    for (int j = 0; j < 2 * P; ++j) v[i][j / P][j % P] = raw[k][2 * i + j / P].two(j % P);
+                load(raw[k]);
+                if (p.norm != SN_HEADS_NONE) {
+                    if (p.norm == SN_HEADS_LAYER) {
+                        F2 s2 = f2(0.0f, 0.0f);
+#pragma unroll
+                        for (int i = 0; i < NC; ++i)
+#pragma unroll
+                            for (int j = 0; j < 2 * P; ++j) s2 = add_2(s2, v[i][j / P][j % P]);
+                        const float m = -all(both(s2)) * inv_d;
+#pragma unroll
+                        for (int i = 0; i < NC; ++i)
+                            if (in[i]) {
+#pragma unroll
+                                for (int j = 0; j < 2 * P; ++j) v[i][j / P][j % P] = add_2(v[i][j / P][j % P], f2(m, W > 1 ? m : 0.0f));
+                            }
+                    }
+                    F2 s2 = f2(0.0f, 0.0f);
 #pragma unroll
                     for (int i = 0; i < NC; ++i)
-                        if (in[i]) {
 #pragma unroll
-                            for (int j = 0; j < 2 * W; ++j) v[2 * W * i + j] -= s;
-                        }
-                }
-                float s = 0.0f;
+                        for (int j = 0; j < 2 * P; ++j) s2 = fma_2(v[i][j / P][j % P], v[i][j / P][j % P], s2);
+                    const float s = rsqrtf(all(both(s2)) * inv_d + p.eps);
 #pragma unroll
-                for (int j = 0; j < V; ++j) s = fmaf(v[j], v[j], s);
-                for (int o = lph / 2; o; o /= 2) s += __shfl_xor_sync(group, s, o);
-                s = rsqrtf(s * inv_d + p.eps);
+                    for (int i = 0; i < NC; ++i)
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[j] *= s * w[j];
-            }
+                        for (int j = 0; j < 2 * P; ++j) v[i][j / P][j % P] = mul_2(v[i][j / P][j % P], f2(s, s));
+                    if (scaled) {
 #pragma unroll
-            for (int i = 0; i < NC; ++i) {
-                if (!in[i]) continue;
-                float *a = v + 2 * W * i;
-                if ((sub + i * lph) * W < p.pairs) {
-                    if (p.interleaved) {
+                        for (int i = 0; i < NC; ++i) {
+                            if (!in[i]) continue;
+                            const Raw<float, W> wa = *reinterpret_cast<const Raw<float, W> *>(&weights[which][at[i]]);
+                            const Raw<float, W> wb = *reinterpret_cast<const Raw<float, W> *>(&weights[which][bt[i]]);
 #pragma unroll
-                        for (int j = 0; j < W; ++j) {
-                            const float c = cs[i * W + j], s = sn[i * W + j], e = a[2 * j], f = a[2 * j + 1];
-                            a[2 * j] = e * c - f * s, a[2 * j + 1] = e * s + f * c;
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < W; ++j) {
-                            const float c = cs[i * W + j], s = sn[i * W + j], e = a[j], f = a[W + j];
-                            a[j] = e * c - f * s, a[W + j] = e * s + f * c;
+                            for (int j = 0; j < P; ++j) v[i][0][j] = mul_2(v[i][0][j], wa.two(j)), v[i][1][j] = mul_2(v[i][1][j], wb.two(j));
                         }
                     }
                 }
-                store_w<T, W>(yh + at[i], a);
-                store_w<T, W>(yh + bt[i], a + W);
+#pragma unroll
+                for (int i = 0; i < NC; ++i) {
+                    if ((sub + i * lph) * W < p.pairs) {
+                        if (!p.interleaved || W == 1) {  // (one value of each: neighbours and halves are the same)
+#pragma unroll
+                            for (int j = 0; j < P; ++j) {
+                                const F2 c = cs[i * P + j], z = sn[i * P + j], a = v[i][0][j], b = v[i][1][j];
+                                v[i][0][j] = fma_2(a, c, mul_2(b, mul_2(z, f2(-1.0f, -1.0f))));
+                                v[i][1][j] = fma_2(a, z, mul_2(b, c));
+                            }
+                        } else {
+#pragma unroll
+                            for (int j = 0; j < W; ++j) {
+                                const float2 c = floats(cs[i * P + j / 2]), z = floats(sn[i * P + j / 2]), e = floats(v[i][j / P][j % P]);
+                                const float cj = j % 2 ? c.y : c.x, zj = j % 2 ? z.y : z.x;
+                                v[i][j / P][j % P] = fma_2(f2(e.x, e.x), f2(cj, zj), mul_2(f2(e.y, e.y), f2(-zj, cj)));
+                            }
+                        }
+                    }
+                    if (!in[i] || n >= heads) continue;
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        Raw<T, W> r;
+#pragma unroll
+                        for (int j = 0; j < P; ++j) r.set(j, v[i][half][j]);
+                        *reinterpret_cast<Raw<T, W> *>(y + (half ? bt[i] : at[i])) = r;
+                    }
+                }
+                n += step, y += dy;
             }
-        }
     }
 }
 

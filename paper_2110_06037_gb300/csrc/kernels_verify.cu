@@ -4,7 +4,8 @@
 // (a load of two probabilities a token); the row behind it is cut into the blocks' and their warps'
 // contiguous pieces, whose weights are summed in units of 2^-60, in integers: exact, so that neither the
 // cut nor the order matters.  With every block's and warp's sum known, one warp's piece holds the drawn
-// index, and that warp goes through it once more (from L2) with running sums.
+// index, and that warp's block goes through it once more (from L2): the warps' sums of its parts, and one warp's
+// running sums.  (One warp alone took 10 us for its 2000 values.)
 #include <algorithm>
 
 #include "attn_common.cuh"
@@ -15,7 +16,7 @@ namespace k {
 
 namespace {
 
-constexpr int WARPS = 16;
+constexpr int WARPS = 8;
 using U64 = unsigned long long;
 
 struct VerifyP {
@@ -24,8 +25,24 @@ struct VerifyP {
     int32_t blocks;        // of a cluster
 };
 
-// in units of 2^-60; outside [0, 1] the nearer end, NaN 0
-__device__ __forceinline__ U64 fixed(float v) { return __float2ull_rn(fminf(fmaxf(v, 0.0f), 1.0f) * 1152921504606846976.0f); }
+__device__ __forceinline__ uint32_t left(uint32_t v, int n) {  // (shifts by 32 and more, or less than 0: nothing is left)
+    uint32_t r;
+    asm("shl.b32 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(n));
+    return r;
+}
+__device__ __forceinline__ uint32_t right(uint32_t v, int n) {
+    uint32_t r;
+    asm("shr.u32 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(n));
+    return r;
+}
+// in whole units of 2^-60; outside [0, 1] the nearer end, NaN 0.  By shifts of the significand, 14 integer operations:
+// the conversion to 64 bits is a rare unit's, and two of them an element took 47 us for 64 rows of 128000 pairs.
+__device__ __forceinline__ U64 fixed(float v) {
+    const uint32_t u = __float_as_uint(fminf(fmaxf(v, 0.0f), 1.0f));
+    const uint32_t m = (u & 0x7fffffu) | 0x800000u;
+    const int n = (int)(u >> 23) - 90;  // v = m 2^n units (below the normal range: less than one)
+    return (U64)(left(m, n - 32) | right(m, 32 - n)) << 32 | (left(m, n) | right(m, -n));
+}
 __device__ __forceinline__ U64 weight(U64 p, U64 q) { return p > q ? p - q : 0; }
 __device__ __forceinline__ U64 sum_warp(U64 v) {
 #pragma unroll
@@ -33,27 +50,58 @@ __device__ __forceinline__ U64 sum_warp(U64 v) {
     return v;
 }
 
-// a lane's E neighbours of both rows from i on (beyond `end`: zeros)
+// a lane's E neighbours of both rows from i on (beyond `end`: zeros), as they lie there and their weights
 template <typename T, int E>
-__device__ __forceinline__ void load_pair(U64 (&w)[E], const T *p, const T *q, int i, int end) {
-    alignas(16) T x[E], z[E];
-    if constexpr (E * sizeof(T) == 16) {
-        if (i + E <= end) {
-            *reinterpret_cast<uint4 *>(x) = *reinterpret_cast<const uint4 *>(p + i);
-            if (q) *reinterpret_cast<uint4 *>(z) = *reinterpret_cast<const uint4 *>(q + i);
+struct alignas(E * sizeof(T)) Some {
+    T v[E];
+};
+template <typename T, int E>
+__device__ __forceinline__ Some<T, E> load_some(const T *p, int i, int end) {
+    if (i + E <= end) return *reinterpret_cast<const Some<T, E> *>(p + i);
+    Some<T, E> r;
 #pragma unroll
-            for (int j = 0; j < E; ++j) w[j] = q ? weight(fixed(ldf(x + j)), fixed(ldf(z + j))) : fixed(ldf(x + j));
-            return;
-        }
+    for (int j = 0; j < E; ++j) r.v[j] = i + j < end ? p[i + j] : cvt<T>(0.0f);
+    return r;
+}
+template <typename T, int E>
+__device__ __forceinline__ U64 sum_some(const Some<T, E> &x, const Some<T, E> &z, bool pair, U64 (&w)[E]) {
+    U64 sum = 0;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+        w[j] = fixed(ldf(x.v + j));
+        if (pair) w[j] = weight(w[j], fixed(ldf(z.v + j)));
+        sum += w[j];
     }
+    return sum;
+}
+// a lane's weights of [begin, end), the warp's next to one another; ONCE loads of each under way
+template <typename T, int E>
+__device__ __forceinline__ U64 sum_range(const T *p, const T *q, int begin, int end, int lane) {
+    constexpr int STEP = 32 * E, ONCE = E == 8 ? 2 : 4;
+    U64 sum = 0, w[E];
+    int i = begin;
+#pragma unroll 1
+    for (; i + ONCE * STEP <= end; i += ONCE * STEP) {
+        Some<T, E> x[ONCE], z[ONCE];
 #pragma unroll
-    for (int j = 0; j < E; ++j)
-        w[j] = i + j >= end ? 0 : q ? weight(fixed(ldf(p + i + j)), fixed(ldf(q + i + j))) : fixed(ldf(p + i + j));
+        for (int k = 0; k < ONCE; ++k) {
+            x[k] = *reinterpret_cast<const Some<T, E> *>(p + i + k * STEP + lane * E);
+            if (q) z[k] = *reinterpret_cast<const Some<T, E> *>(q + i + k * STEP + lane * E);
+        }
+#pragma unroll
+        for (int k = 0; k < ONCE; ++k) sum += sum_some<T, E>(x[k], z[k], q != nullptr, w);
+    }
+#pragma unroll 1
+    for (; i < end; i += STEP) {
+        const Some<T, E> x = load_some<T, E>(p, i + lane * E, end), z = q ? load_some<T, E>(q, i + lane * E, end) : x;
+        sum += sum_some<T, E>(x, z, q != nullptr, w);
+    }
+    return sum;
 }
 
 template <typename T, int E>  // E: values of a 16-byte load, 1 where rows are not aligned to it
 __global__ void __launch_bounds__(32 * WARPS) verify_kernel(const __grid_constant__ VerifyP p) {
-    __shared__ U64 sums[WARPS], total_sh, all_sh[8];
+    __shared__ U64 sums[WARPS], parts[WARPS], total_sh, all_sh[8];
     __shared__ int first_sh;
     griddep_launch();
     griddep_wait();
@@ -90,15 +138,7 @@ __global__ void __launch_bounds__(32 * WARPS) verify_kernel(const __grid_constan
     constexpr int STEP = 32 * E;
     U64 all;
     while (true) {
-        U64 mine = 0;
-#pragma unroll 4
-        for (int i = begin; i < end; i += STEP) {
-            U64 w[E];
-            load_pair<T, E>(w, pr, qr, i + lane * E, end);
-#pragma unroll
-            for (int j = 0; j < E; ++j) mine += w[j];
-        }
-        mine = sum_warp(mine);
+        const U64 mine = sum_warp(sum_range<T, E>(pr, qr, begin, end, lane));
         if (lane == 0) sums[warp] = mine;
         __syncthreads();
         if (warp == 0) {
@@ -135,15 +175,22 @@ __global__ void __launch_bounds__(32 * WARPS) verify_kernel(const __grid_constan
         return;
     }
     if (bar < before || bar - before >= all_sh[rank]) return;
-    for (int i = 0; i < warp; ++i) before += sums[i];
-    if (bar < before || bar - before >= sums[warp]) return;
-    // this warp's piece holds it
-    for (int i = begin; i < end; i += STEP) {
-        U64 w[E], mine = 0;
-        load_pair<T, E>(w, pr, qr, i + lane * E, end);
-#pragma unroll
-        for (int j = 0; j < E; ++j) mine += w[j];
-        U64 up = mine;
+    // the warp whose piece holds it, and its piece in parts for all of the block's
+    int has = 0;
+    while (has < WARPS - 1 && bar - before >= sums[has]) before += sums[has++];
+    const int64_t start = ((int64_t)rank * WARPS + has) * p.piece;
+    const int e0 = (int)min(start + p.piece, (int64_t)p.vocab), step = ((p.piece + WARPS - 1) / WARPS + STEP - 1) / STEP * STEP;
+    const int b1 = (int)min(start + (int64_t)warp * step, (int64_t)e0), e1 = min(b1 + step, e0);
+    const U64 mine = sum_warp(sum_range<T, E>(pr, qr, b1, e1, lane));
+    if (lane == 0) parts[warp] = mine;
+    __syncthreads();
+    for (int i = 0; i < warp; ++i) before += parts[i];
+    if (bar < before || bar - before >= parts[warp]) return;
+    for (int i = b1; i < e1; i += STEP) {
+        const Some<T, E> x = load_some<T, E>(pr, i + lane * E, e1), z = qr ? load_some<T, E>(qr, i + lane * E, e1) : x;
+        U64 w[E];
+        const U64 own = sum_some<T, E>(x, z, qr != nullptr, w);
+        U64 up = own;
 #pragma unroll
         for (int o = 1; o < 32; o *= 2) {
             const U64 v = __shfl_up_sync(0xffffffffu, up, o);
@@ -152,7 +199,7 @@ __global__ void __launch_bounds__(32 * WARPS) verify_kernel(const __grid_constan
         const uint32_t beyond = __ballot_sync(0xffffffffu, before + up > bar);
         if (beyond) {
             if (lane == __ffs(beyond) - 1) {
-                U64 c = before + up - mine;
+                U64 c = before + up - own;
                 int at = 0;
 #pragma unroll
                 for (int j = 0; j < E; ++j) {
