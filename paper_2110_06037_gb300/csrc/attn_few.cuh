@@ -1,20 +1,28 @@
-// Attention of few queries over a long cache of 16-bit values or 8-bit codes (sn_attend in include/sn.h).
+// Attention of few queries over a long cache, and of fp32 queries in any number (sn_attend in include/sn.h).
 //
 // What bounds it is the cache, read once.  A block's warps take 16 keys each in turn, with a ring of their own in
 // shared memory (cp.async: keys and values of the next tiles are on their way while one is worked on) and sums of their
 // own in registers; no warp waits for another before the end of an item, where their sums are joined.  A tile is two
-// products by mma.sync of 16 queries (the heads that share the cache's head, and a sequence's few tokens):
-//   S = Q K^T (16 x 16),   O += P V (16 x D),   P = 2^(S - m).
-// tcgen05 has no form below 64 rows, of which a token's few heads would use a tenth, and its operands go through
-// barriers of the whole block; with 16 rows the tensor pipe is at a quarter of its rate where memory is at its own.
-// P goes in as two 16-bit parts, so that no weight is rounded to less than 16 bits; with fp16 the largest is brought
-// to 2^14, so that a weight is off by 2^-22 of itself or 2^-39 of the largest.
+// products by mma.sync, with keys and dims as the rows and 8 queries (the heads that share the cache's head, and a
+// sequence's few tokens) as the columns, so that a token's few heads fill the product:
+//   S = K Q^T (16 x 8),   O += V^T P (D x 8),   P = 2^(S - m).
+// (tcgen05 has no form below 64 rows, its operands go through barriers of the whole block.)  m is the largest
+// score so far only up to a factor of 2^THR: one vote a tile says whether it has to grow, and the maximum across
+// lanes and the sums' scaling are rare.  P is transposed from the first product's layout to the second's by movmatrix.
+// 16-bit values: P goes in as two 16-bit parts, so that no weight is rounded to less than 16 bits; with fp16 the largest
+// is brought to 2^14, so that a weight is off by 2^-22 of itself or 2^-39 of the largest.
 //
 // Codes: q and codes go in as fp16 (codes exact; q times a power of two that brings a row's largest to 2^10, what is
 // below 2^-34 of that is lost; fp32 queries as two parts).  The keys' scales are factors of the scores.  A value's scale
 // is 2^e f, f in [1, 2): e goes into the exponent and f into the weight,
 //   P_j = 2^(s_j + e_j - m) f_j,   sum of weights += 2^(s_j + e_j - m) 2^-e_j,
-// so that P is within fp16's range whatever the scales are.
+// so that P is within fp16's range whatever the scales are.  What bounds codes is the issue of instructions: to
+// make fp16 of a tile's codes takes half of them.  For bf16 queries P is one part, off by 2^-11 of itself, an eighth of
+// the output's rounding.
+//
+// fp32 values: products in tf32 of two parts each, hi hi + hi lo + lo hi: off by 2^-21 of a product.  With fp32 queries
+// the products of 16 dims, or of a tile's keys, are summed apart and added to the sums in fp32: the tensor cores truncate what they add
+// to, which over a row of 10000 keys is 3e-6 of it.
 #pragma once
 
 #include <algorithm>
@@ -26,7 +34,7 @@ namespace sn {
 namespace k {
 namespace few {
 
-constexpr int WARPS = 4, TILE = 16, UNIT = 64;  // keys of a warp's tile and of a unit of work
+constexpr int TILE = 16, UNIT = 64;  // keys of a warp's tile and of a unit of work
 
 __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool there) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
@@ -49,10 +57,25 @@ __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint3
         asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    else
+    else if constexpr (std::is_same<M, __nv_bfloat16>::value)
         asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
             : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// an 8 x 8 matrix of 16-bit values, a lane's two neighbours of row lane / 4: the same of its transpose
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+// the tf32 part of a value, to nearest, and the rest
+__device__ __forceinline__ void split(uint32_t &hi, uint32_t &lo, float v) {
+    asm("cvt.rna.tf32.f32 %0, %1;" : "=r"(hi) : "f"(v));
+    lo = __float_as_uint(v - __uint_as_float(hi));
 }
 // two codes in offset binary (bytes lo and hi of x) as fp16: 1024 + c + 128 - 1152
 __device__ __forceinline__ uint32_t codes_f16(uint32_t x, uint32_t select) {
@@ -61,46 +84,57 @@ __device__ __forceinline__ uint32_t codes_f16(uint32_t x, uint32_t select) {
     return *reinterpret_cast<const uint32_t *>(&h);
 }
 
-// T: queries; C: cache (T, or int8_t); DT: head_dim at most; MT: 16-row tiles of an item
-template <typename T, typename C, int DT, int MT>
+// T: queries; C: cache (T, or int8_t); DT: head_dim at most; NB: blocks of 8 queries of an item
+template <typename T, typename C, int DT, int NB>
 struct Form {
-    static constexpr bool CODES = sizeof(C) == 1;
+    static constexpr bool CODES = sizeof(C) == 1, WIDE = sizeof(C) == 4;
     using M = typename std::conditional<CODES, __half, T>::type;  // the products' type
-    static constexpr int QP = CODES && sizeof(T) == 4 ? 2 : 1;      // parts of a query
-    static constexpr bool QREG = DT * MT * QP <= 128;               // queries in registers
-    static constexpr float TOP = std::is_same<M, __half>::value ? 14.0f : 0.0f;  // log2 of the largest weight
-    static constexpr int STAGES = CODES ? 5 : 3;
-    static constexpr int ROWS = 16 * MT;
-    // bytes of a row of the tile (its number of 16 bytes odd, so that eight rows are in different banks)
-    __host__ __device__ static constexpr int stride(int d) { return CODES ? (d / 16 % 2 ? d + 32 : d + 16) : 2 * d + 16; }
-    __host__ __device__ static constexpr int stage(int d) { return 2 * TILE * stride(d) + (CODES ? 2 * TILE * 4 : 0); }
+    static constexpr bool HALF = std::is_same<M, __half>::value;
+    static constexpr int QP = CODES && sizeof(T) == 4 ? 2 : 1;    // parts of a query in shared memory
+    static constexpr bool LO = !(CODES && std::is_same<T, __nv_bfloat16>::value);  // weights in two parts
+    static constexpr int STEP = WIDE ? 8 : 16;                    // dims of a product
+    static constexpr int QR = WIDE ? 4 : 2 * QP;                  // registers of 8 queries of a step
+    static constexpr bool QREG = NB * (DT / STEP) * QR <= 64 && NB * DT <= 256;  // queries in registers
+    // log2 of the largest weight when m is the largest score, and how far a score may be above m
+    // (codes: times the values' f, below 2)
+    static constexpr float TOP = HALF ? 14.0f : 0.0f, THR = HALF ? (CODES ? 0.95f : 1.5f) : 8.0f;
+    static constexpr int STAGES = 3;
+    static constexpr int ROWS = 8 * NB;
+    static constexpr int WARPS = WIDE && DT > 128 ? 2 : 4;
+    // blocks of an SM, by registers
+    static constexpr int BLOCKS = DT * NB <= 128 ? (WIDE ? 2 : 4) : DT * NB <= 256 ? 2 : 1;
+    // bytes of a row of a tile.  16-bit and codes: its number of 16 bytes odd, so that eight rows are in different
+    // banks.  fp32: keys are read two rows, 64 bytes each, at a time; values four rows 2 t, 32 bytes each
+    __host__ __device__ static constexpr int pad(int n, int to) { return n + (to - n % 128 + 128) % 128; }
+    __host__ __device__ static constexpr int k_row(int d) { return CODES ? (d / 16 % 2 ? d + 32 : d + 16) : WIDE ? pad(4 * d, 64) : 2 * d + 16; }
+    __host__ __device__ static constexpr int v_row(int d) { return WIDE ? pad(4 * d, 16) : k_row(d); }
+    __host__ __device__ static constexpr int stage(int d) { return TILE * (k_row(d) + v_row(d)) + (CODES ? 2 * TILE * 4 : 0); }
     // a warp's ring, which at the end holds its sums
     __host__ __device__ static constexpr int ring(int d) {
         const int a = STAGES * stage(d), b = ROWS * d * 4;
         return a > b ? a : b;
     }
-    __host__ __device__ static constexpr int bytes(int d) { return WARPS * ring(d) + QP * ROWS * (2 * d + 16) + ROWS * 4; }
+    __host__ __device__ static constexpr int q_row(int d) { return WIDE ? k_row(d) : 2 * d + 16; }
+    __host__ __device__ static constexpr int bytes(int d) { return WARPS * ring(d) + QP * ROWS * q_row(d) + ROWS * 4; }
 };
 
-template <typename T, typename C, int DT, int MT>
-__global__ void __launch_bounds__(32 * WARPS) attend_few_kernel(const __grid_constant__ AttnP p) {
-    using F = Form<T, C, DT, MT>;
+template <typename T, typename C, int DT, int NB>
+__global__ void __launch_bounds__(32 * Form<T, C, DT, NB>::WARPS, Form<T, C, DT, NB>::BLOCKS) attend_few_kernel(const __grid_constant__ AttnP p) {
+    using F = Form<T, C, DT, NB>;
     using M = typename F::M;
-    constexpr bool CODES = F::CODES;
-    constexpr int ROWS = F::ROWS, S = F::STAGES, QP = F::QP;
+    constexpr bool CODES = F::CODES, WIDE = F::WIDE;
+    constexpr int ROWS = F::ROWS, S = F::STAGES, QP = F::QP, WARPS = F::WARPS, KS = DT / F::STEP;
     extern __shared__ __align__(128) uint8_t sm[];
     __shared__ int64_t sh[4];
     __shared__ float sh_m[WARPS][ROWS], sh_l[WARPS][ROWS];
     const int d = p.c.head_dim, tid = threadIdx.x, warp = tid / 32, lane = tid % 32, g = lane / 4, t4 = lane % 4;
-    const int stride = F::stride(d), stage = F::stage(d), ring_bytes = F::ring(d);
-    uint8_t *ring = sm + warp * ring_bytes;
+    const int k_row = F::k_row(d), v_row = F::v_row(d), stage = F::stage(d), ring_bytes = F::ring(d), q_row = F::q_row(d);
+    uint8_t *ring = sm + warp * ring_bytes, *qs = sm + WARPS * ring_bytes;
     const uint32_t ring_at = tc::su32(ring);
-    M *qs = reinterpret_cast<M *>(sm + WARPS * ring_bytes);
-    const int qld = d + 8;
-    float *rf = reinterpret_cast<float *>(qs + QP * ROWS * qld);  // codes: factors of the queries' rows
-    // 16-byte pieces of a tile: they lie end to end in the cache, and 16 or 32 bytes further a row in the ring
+    float *rf = reinterpret_cast<float *>(qs + QP * ROWS * q_row);  // codes: factors of the queries
+    // 16-byte pieces of a tile: they lie end to end in the cache
     const int per_row = d * (int)sizeof(C) / 16, pieces = TILE * per_row;
-    const uint32_t inv = 65536u / (uint32_t)per_row + 1;  // (exact for numbers below 512 and rows of up to 32)
+    const uint32_t inv = 65536u / (uint32_t)per_row + 1;  // (exact for numbers up to 1024 and rows of up to 64: checked for all)
     griddep_launch();
     griddep_wait();
     Pieces work;
@@ -126,13 +160,12 @@ __global__ void __launch_bounds__(32 * WARPS) attend_few_kernel(const __grid_con
                 const char *kp = static_cast<const char *>(p.c.k) + row * d * (int)sizeof(C), *vp = static_cast<const char *>(p.c.v) + row * d * (int)sizeof(C);
                 const uint32_t to = ring_at + at * stage;
                 for (int i = lane; i < pieces; i += 32) {
-                    const int r = (int)((uint32_t)i * inv >> 16);
-                    const uint32_t o = to + r * stride + (i - r * per_row) * 16;
-                    cp16(o, kp + i * 16, r < keep);
-                    cp16(o + TILE * stride, vp + i * 16, r < keep);
+                    const int r = (int)((uint32_t)i * inv >> 16), x = (i - r * per_row) * 16;
+                    cp16(to + r * k_row + x, kp + i * 16, r < keep);
+                    cp16(to + TILE * k_row + r * v_row + x, vp + i * 16, r < keep);
                 }
                 if constexpr (CODES) {
-                    if (lane < 8) cp16(to + 2 * TILE * stride + lane * 16, (lane < 4 ? p.c.k_scale : p.c.v_scale) + row + lane % 4 * 4, ok);
+                    if (lane < 8) cp16(to + TILE * (k_row + v_row) + lane * 16, (lane < 4 ? p.c.k_scale : p.c.v_scale) + row + lane % 4 * 4, ok);
                 }
                 next += WARPS;
                 if (next < tile1) page = pages[next * TILE >> shift];
@@ -162,216 +195,296 @@ __global__ void __launch_bounds__(32 * WARPS) attend_few_kernel(const __grid_con
                     if (lane + 32 * i >= d) continue;
                     const float x0 = v[i] * f;
                     const __half hi = __float2half_rn(x0);
-                    qs[r * qld + lane + 32 * i] = hi;
-                    if constexpr (QP == 2) qs[(ROWS + r) * qld + lane + 32 * i] = __float2half_rn(x0 - __half2float(hi));
+                    reinterpret_cast<__half *>(qs + r * q_row)[lane + 32 * i] = hi;
+                    if constexpr (QP == 2) reinterpret_cast<__half *>(qs + (ROWS + r) * q_row)[lane + 32 * i] = __float2half_rn(x0 - __half2float(hi));
                 }
             }
         } else {
-            for (int i = tid; i < ROWS * d; i += 32 * WARPS) {
-                const int r = i / d, e = i - r * d;
-                qs[r * qld + e] = r < rows ? static_cast<const T *>(p.h.x)[(s.first + (row0 + r) / p.group) * p.h.ldx +
-                                                                           ((int64_t)w.head * p.group + (row0 + r) % p.group) * p.h.hx + e]
-                                           : cvt<T>(0.0f);
+            for (int r = warp; r < ROWS; r += WARPS) {
+                const T *x = static_cast<const T *>(p.h.x) + (s.first + (row0 + r) / p.group) * p.h.ldx + ((int64_t)w.head * p.group + (row0 + r) % p.group) * p.h.hx;
+                for (int e = lane; e < d; e += 32) reinterpret_cast<T *>(qs + r * q_row)[e] = r < rows ? x[e] : cvt<T>(0.0f);
             }
         }
         __syncthreads();
-        // a step of 16 dims of the queries: as ldmatrix lays them out, or for codes with a lane's four neighbours of a row
-        // (dims 4 t .. 4 t + 3) in its two registers, as the codes' bytes come
-        auto query = [&](uint32_t (&a)[4], int part, int mt, int k) {
-            const M *q = qs + (part * ROWS + 16 * mt) * qld + 16 * k;
-            if constexpr (CODES) {
-                const uint2 x = *reinterpret_cast<const uint2 *>(q + g * qld + 4 * t4), y = *reinterpret_cast<const uint2 *>(q + (g + 8) * qld + 4 * t4);
-                a[0] = x.x, a[2] = x.y, a[1] = y.x, a[3] = y.y;
+        // a step's 16 (8) dims of 8 queries, as the product's columns.  The order of dims is that of the keys' registers: for
+        // codes and fp32 a lane's four neighbours, as they come from one load
+        auto query = [&](uint32_t (&b)[F::QR], int n, int k) {
+            const uint8_t *q = qs + (8 * n + g) * q_row;
+            if constexpr (WIDE) {
+                const float2 x = *reinterpret_cast<const float2 *>(q + 64 * (k / 2) + 16 * t4 + 8 * (k % 2));
+                split(b[0], b[2], x.x), split(b[1], b[3], x.y);
+            } else if constexpr (CODES) {
+#pragma unroll
+                for (int i = 0; i < QP; ++i) {
+                    const uint2 x = *reinterpret_cast<const uint2 *>(q + i * ROWS * q_row + 32 * k + 8 * t4);
+                    b[2 * i] = x.x, b[2 * i + 1] = x.y;
+                }
             } else {
-                ldsm4(a, tc::su32(q + (lane % 16) * qld + lane / 16 * 8));
+                b[0] = *reinterpret_cast<const uint32_t *>(q + 32 * k + 4 * t4), b[1] = *reinterpret_cast<const uint32_t *>(q + 32 * k + 4 * t4 + 16);
             }
         };
-        constexpr int KS = DT / 16;
-        uint32_t qa[F::QREG ? QP * MT * KS : 1][4];
+        uint32_t qa[F::QREG ? NB * KS : 1][F::QR];
         if constexpr (F::QREG) {
 #pragma unroll
-            for (int i = 0; i < QP * MT; ++i)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
                 for (int k = 0; k < KS; ++k)
-                    if (16 * k < d) query(qa[i * KS + k], i / MT, i % MT, k);
+                    if (F::STEP * k < d) query(qa[n * KS + k], n, k);
         }
-        float factor[2 * MT];
-        int last[2 * MT];
+        // a lane's queries: 8 n + 2 t and the next
+        float factor[NB][2], m[NB][2], l[NB][2], o[NB][DT / 16][4];
+        int last[NB][2];
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
-            const int r = 8 * i + g;
-            factor[i] = p.scale * (CODES ? rf[r] : 1.0f);
-            last[i] = r < rows ? last_key(p, w.past, row0 + r) : -1;
+        for (int n = 0; n < NB; ++n) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = 8 * n + 2 * t4 + i;
+                factor[n][i] = p.scale * (CODES ? rf[r] : 1.0f);
+                last[n][i] = r < rows ? last_key(p, w.past, row0 + r) : INT32_MAX;  // (behind the queries: zeros, written nowhere)
+                m[n][i] = -INFINITY, l[n][i] = 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < DT / 16; ++j)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) o[n][j][k] = 0.0f;
         }
-        float m[2 * MT], l[2 * MT], o[MT][DT / 8][4];
-#pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) m[i] = -INFINITY, l[i] = 0.0f;
-#pragma unroll
-        for (int i = 0; i < MT; ++i)
-#pragma unroll
-            for (int j = 0; j < DT / 8; ++j)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) o[i][j][k] = 0.0f;
         int now = 0;  // place in the ring of the tile worked on
+#pragma unroll 1
         for (int tile = w.u0 * (UNIT / TILE) + warp; tile < tile1; tile += WARPS) {
             asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
             __syncwarp();
             const bool ok = there >> now & 1u;
             load();
-            const uint8_t *st = ring + now * stage;
-            const uint32_t sa = ring_at + now * stage, va = sa + TILE * stride;
+            const uint8_t *kt = ring + now * stage, *vt = kt + TILE * k_row;
+            const uint32_t ka = ring_at + now * stage, va = ka + TILE * k_row;
             now = now + 1 == S ? 0 : now + 1;
-            float c[MT][2][4];
+            // scores of keys g (0, 1) and g + 8 (2, 3)
+            float c[NB][4];
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int j = 0; j < 8; ++j) c[i][j / 4][j % 4] = 0.0f;
-            if constexpr (CODES) {
+                for (int j = 0; j < 4; ++j) c[n][j] = 0.0f;
+            auto with_query = [&](int n, int k, auto body) {
+                if constexpr (F::QREG) {
+                    body(qa[n * KS + k]);
+                } else {
+                    uint32_t b[F::QR];
+                    query(b, n, k);
+                    body(b);
+                }
+            };
+            if constexpr (WIDE) {
+#pragma unroll
+                for (int k = 0; k < DT / 16; ++k) {
+                    if (16 * k >= d) break;
+                    const float4 x = *reinterpret_cast<const float4 *>(kt + g * k_row + 64 * k + 16 * t4);
+                    const float4 y = *reinterpret_cast<const float4 *>(kt + (g + 8) * k_row + 64 * k + 16 * t4);
+                    uint32_t hi[2][4], lo[2][4];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        split(hi[e][0], lo[e][0], e ? x.z : x.x), split(hi[e][1], lo[e][1], e ? y.z : y.x);
+                        split(hi[e][2], lo[e][2], e ? x.w : x.y), split(hi[e][3], lo[e][3], e ? y.w : y.y);
+                    }
+#pragma unroll
+                    for (int n = 0; n < NB; ++n) {
+                        float some[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                        with_query(n, 2 * k, [&](const uint32_t (&b)[F::QR]) {
+                            with_query(n, 2 * k + 1, [&](const uint32_t (&b1)[F::QR]) {
+                                mma<float>(some, lo[0], b[0], b[1]);
+                                mma<float>(some, hi[0], b[2 % F::QR], b[3 % F::QR]);
+                                mma<float>(some, lo[1], b1[0], b1[1]);
+                                mma<float>(some, hi[1], b1[2 % F::QR], b1[3 % F::QR]);
+                                mma<float>(some, hi[0], b[0], b[1]);
+                                mma<float>(some, hi[1], b1[0], b1[1]);
+                            });
+                        });
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) c[n][j] += some[j];
+                    }
+                }
+            } else if constexpr (CODES) {
 #pragma unroll
                 for (int k = 0; k < KS; k += 2) {
                     if (16 * k >= d) break;
-                    uint32_t b[4];
-                    ldsm4(b, sa + (lane / 16 * 8 + lane % 8) * stride + 16 * k + lane / 8 % 2 * 16);
+                    uint32_t u[4];  // rows g, g + 8 of 16 dims, and of the next 16
+                    ldsm4(u, ka + (lane % 16) * k_row + 16 * k + lane / 16 * 16);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) b[e] ^= 0x80808080u;
+                    for (int e = 0; e < 4; ++e) u[e] ^= 0x80808080u;
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {  // (of the last 16 dims alone, half is behind the row)
                         if (16 * (k + e) >= d) break;
-                        const uint32_t b00 = codes_f16(b[e], 0x4140), b01 = codes_f16(b[e], 0x4342);
-                        const uint32_t b10 = codes_f16(b[e + 2], 0x4140), b11 = codes_f16(b[e + 2], 0x4342);
+                        const uint32_t a[4] = {codes_f16(u[2 * e], 0x4140), codes_f16(u[2 * e + 1], 0x4140), codes_f16(u[2 * e], 0x4342),
+                                               codes_f16(u[2 * e + 1], 0x4342)};
 #pragma unroll
-                        for (int i = 0; i < QP * MT; ++i) {
-                            uint32_t a[4];
-                            if constexpr (F::QREG) {
+                        for (int n = 0; n < NB; ++n)
+                            with_query(n, k + e, [&](const uint32_t (&b)[F::QR]) {
+                                if constexpr (QP == 2) {
+                                    float some[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                                    mma<M>(some, a, b[2], b[3]);
+                                    mma<M>(some, a, b[0], b[1]);
 #pragma unroll
-                                for (int x = 0; x < 4; ++x) a[x] = qa[i * KS + k + e][x];
-                            } else {
-                                query(a, i / MT, i % MT, k + e);
-                            }
-                            mma<M>(c[i % MT][0], a, b00, b01);
-                            mma<M>(c[i % MT][1], a, b10, b11);
-                        }
+                                    for (int j = 0; j < 4; ++j) c[n][j] += some[j];
+                                } else {
+                                    mma<M>(c[n], a, b[0], b[1]);
+                                }
+                            });
                     }
                 }
             } else {
 #pragma unroll
                 for (int k = 0; k < KS; ++k) {
                     if (16 * k >= d) break;
-                    uint32_t b[4];
-                    ldsm4(b, sa + (lane / 16 * 8 + lane % 8) * stride + 32 * k + lane / 8 % 2 * 16);
+                    uint32_t a[4];
+                    ldsm4(a, ka + (lane % 16) * k_row + 32 * k + lane / 16 * 16);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        uint32_t a[4];
-                        if constexpr (F::QREG) {
-#pragma unroll
-                            for (int x = 0; x < 4; ++x) a[x] = qa[i * KS + k][x];
-                        } else {
-                            query(a, 0, i, k);
-                        }
-                        mma<M>(c[i][0], a, b[0], b[1]);
-                        mma<M>(c[i][1], a, b[2], b[3]);
-                    }
+                    for (int n = 0; n < NB; ++n) with_query(n, k, [&](const uint32_t (&b)[F::QR]) { mma<M>(c[n], a, b[0], b[1]); });
                 }
             }
-            // this lane's four keys: 2 t, 2 t + 1, 8 + 2 t, 9 + 2 t; scales, and of the values' the power of two, its inverse, the rest
-            float ks[4], ve[4], vi[4], vf[4];
+            // the scales of this lane's two keys; of the values' the power of two, its inverse, the rest
+            float ks[2], ve[2], vi[2], vf[2];
             if constexpr (CODES) {
-                const float *f = reinterpret_cast<const float *>(st + 2 * TILE * stride);
+                const float *f = reinterpret_cast<const float *>(vt + TILE * v_row);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int key = 8 * (j / 2) + 2 * t4 + j % 2;
-                    ks[j] = f[key];
-                    const uint32_t u = __float_as_uint(f[TILE + key]), e = u >> 23 & 255u;
+                for (int j = 0; j < 2; ++j) {
+                    ks[j] = f[g + 8 * j];
+                    const uint32_t u = __float_as_uint(f[TILE + g + 8 * j]), e = u >> 23 & 255u;
                     // (below the normal range: 2^-126 and what is left; not finite: NaN)
                     ve[j] = (float)((int)(e ? e : 1u) - 127);
                     vi[j] = __uint_as_float((254u - min(max(e, 1u), 253u)) << 23);
                     vf[j] = e == 255u ? __int_as_float(0x7fc00000) : e ? __uint_as_float((u & 0x807fffffu) | 0x3f800000u)
-                                                                     : f[TILE + key] * 8.507059173023462e37f;
+                                                                     : f[TILE + g + 8 * j] * 8.507059173023462e37f;
                 }
             }
             const bool whole = ok && tile * TILE + TILE - 1 <= first;
-            uint32_t hi[MT][4], lo[MT][4];
+            bool grew = false;
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                float old[2];
-                bool grew = false;
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    const int n = 2 * i + r;
-                    float x[4], up = m[n];
+                for (int j = 0; j < 4; ++j) {
+                    float &x = c[n][j];
+                    x *= factor[n][j % 2];
+                    if constexpr (CODES) x = fmaf(x, ks[j / 2], ve[j / 2]);
+                    if (!whole && !(ok && tile * TILE + 8 * (j / 2) + g <= last[n][j % 2])) x = -INFINITY;
+                    grew |= x > m[n][j % 2] + F::THR;
+                }
+            if (__any_sync(0xffffffffu, grew)) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        x[j] = c[i][j / 2][2 * r + j % 2] * factor[n];
-                        if constexpr (CODES) x[j] = fmaf(x[j], ks[j], ve[j]);
-                        if (!whole && !(ok && tile * TILE + 8 * (j / 2) + 2 * t4 + j % 2 <= last[n])) x[j] = -INFINITY;
-                        up = fmaxf(up, x[j]);
+                for (int n = 0; n < NB; ++n)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float up = fmaxf(c[n][i], c[n][i + 2]);
+#pragma unroll
+                        for (int k = 4; k < 32; k *= 2) up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, k));
+                        up = fmaxf(up, m[n][i]);
+                        const float old = up == -INFINITY ? 1.0f : ex2(m[n][i] - up);
+                        m[n][i] = up;
+                        l[n][i] *= old;
+#pragma unroll
+                        for (int j = 0; j < DT / 16; ++j) o[n][j][i] *= old, o[n][j][i + 2] *= old;
                     }
-                    up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, 1));
-                    up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, 2));
-                    const float base = up == -INFINITY ? 0.0f : up, low = base - F::TOP;
-                    grew |= up > m[n];
-                    old[r] = ex2(m[n] - base);
-                    m[n] = up;
-                    float sum = 0.0f;
+            }
+            // the weights, as columns of the second product: keys 2 t, 2 t + 1 (b[0]) and 8 further (b[1]) of query g; small parts
+            uint32_t hi[NB][WIDE ? 4 : 2], lo[NB][WIDE ? 4 : 2];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        x[j] = ex2(x[j] - low);
-                        if constexpr (CODES) {
-                            sum = fmaf(x[j], vi[j], sum);
-                            x[j] *= x[j] == 0.0f && !whole ? 0.0f : vf[j];  // (a key that is not seen counts nothing, whatever its scale)
-                        } else {
-                            sum += x[j];
+            for (int n = 0; n < NB; ++n) {
+                float x[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float base = m[n][j % 2];
+                    x[j] = ex2(c[n][j] + (F::TOP - (base == -INFINITY ? 0.0f : base)));
+                    if constexpr (CODES) {
+                        l[n][j % 2] = fmaf(x[j], vi[j / 2], l[n][j % 2]);
+                        x[j] *= x[j] == 0.0f && !whole ? 0.0f : vf[j / 2];  // (a key that is not seen counts nothing, whatever its scale)
+                    } else {
+                        l[n][j % 2] += x[j];
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float a = x[2 * h], b = x[2 * h + 1];
+                    if constexpr (WIDE) {
+                        const uint32_t low = transposed(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x5410));
+                        const uint32_t high = transposed(__byte_perm(__float_as_uint(a), __float_as_uint(b), 0x7632));
+                        split(hi[n][2 * h], lo[n][2 * h], __uint_as_float(__byte_perm(low, high, 0x5410)));
+                        split(hi[n][2 * h + 1], lo[n][2 * h + 1], __uint_as_float(__byte_perm(low, high, 0x7632)));
+                    } else {
+                        const uint32_t u = tc::pack2<M>(a, b);
+                        hi[n][h] = transposed(u);
+                        if constexpr (F::LO) {
+                            const float2 f = tc::unpack2<M>(u);
+                            lo[n][h] = transposed(tc::pack2<M>(a - f.x, b - f.y));
                         }
                     }
-                    l[n] = fmaf(l[n], old[r], sum);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const uint32_t h = tc::pack2<M>(x[2 * j], x[2 * j + 1]);
-                        const float2 f = tc::unpack2<M>(h);
-                        hi[i][2 * j + r] = h;
-                        lo[i][2 * j + r] = tc::pack2<M>(x[2 * j] - f.x, x[2 * j + 1] - f.y);
-                    }
-                }
-                if (__any_sync(0xffffffffu, grew)) {
-#pragma unroll
-                    for (int j = 0; j < DT / 8; ++j) o[i][j][0] *= old[0], o[i][j][1] *= old[0], o[i][j][2] *= old[1], o[i][j][3] *= old[1];
                 }
             }
-            if constexpr (CODES) {
-                // a block of 32 dims: the n-th column of its j-th product is dim 4 n + j
-                const uint8_t *v = st + TILE * stride + 2 * t4 * stride + 4 * g;
+            if constexpr (WIDE) {
+                // a block of 32 dims: rows g and g + 8 of its product i are dims 4 g + 2 i and the next
+                const uint8_t *v = vt + 2 * t4 * v_row + 16 * g;
+#pragma unroll
+                for (int k = 0; k < DT / 32; ++k) {
+                    if (32 * k >= d) break;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t ah[2][4], al[2][4];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {  // keys 8 h + 2 t, and the next
+                            const float2 x = *reinterpret_cast<const float2 *>(v + 8 * h * v_row + 128 * k + 8 * i);
+                            const float2 y = *reinterpret_cast<const float2 *>(v + (8 * h + 1) * v_row + 128 * k + 8 * i);
+                            split(ah[h][0], al[h][0], x.x), split(ah[h][1], al[h][1], x.y);
+                            split(ah[h][2], al[h][2], y.x), split(ah[h][3], al[h][3], y.y);
+                        }
+#pragma unroll
+                        for (int n = 0; n < NB; ++n) {
+                            float some[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                mma<float>(some, al[h], hi[n][2 * h], hi[n][2 * h + 1]);
+                                mma<float>(some, ah[h], lo[n][2 * h], lo[n][2 * h + 1]);
+                            }
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) mma<float>(some, ah[h], hi[n][2 * h], hi[n][2 * h + 1]);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[n][2 * k + i][j] += some[j];
+                        }
+                    }
+                }
+            } else if constexpr (CODES) {
+                // a block of 32 dims: as for fp32
+                const uint8_t *v = vt + 2 * t4 * v_row + 4 * g;
 #pragma unroll
                 for (int k = 0; k < DT / 32; ++k) {
                     if (32 * k >= d) break;
                     uint32_t u[4];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) u[j] = *reinterpret_cast<const uint32_t *>(v + (8 * (j / 2) + j % 2) * stride + 32 * k) ^ 0x80808080u;
-                    uint32_t y[4];  // dims 0 and 1, 2 and 3 of keys 0 and 1; of keys 8 and 9
-                    y[0] = __byte_perm(u[0], u[1], 0x5140), y[1] = __byte_perm(u[0], u[1], 0x7362);
-                    y[2] = __byte_perm(u[2], u[3], 0x5140), y[3] = __byte_perm(u[2], u[3], 0x7362);
+                    for (int j = 0; j < 4; ++j) u[j] = *reinterpret_cast<const uint32_t *>(v + (8 * (j / 2) + j % 2) * v_row + 32 * k) ^ 0x80808080u;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t select = j % 2 ? 0x4342 : 0x4140;
-                        const uint32_t b0 = codes_f16(y[j / 2], select), b1 = codes_f16(y[2 + j / 2], select);
+                    for (int i = 0; i < 2; ++i) {  // dims 2 i and 2 i + 1 of keys 0 and 1; of keys 8 and 9
+                        const uint32_t y0 = __byte_perm(u[0], u[1], i ? 0x7362 : 0x5140), y1 = __byte_perm(u[2], u[3], i ? 0x7362 : 0x5140);
+                        const uint32_t a[4] = {codes_f16(y0, 0x4140), codes_f16(y0, 0x4342), codes_f16(y1, 0x4140), codes_f16(y1, 0x4342)};
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) {
-                            mma<M>(o[i][4 * k + j], hi[i], b0, b1);
-                            mma<M>(o[i][4 * k + j], lo[i], b0, b1);
+                        for (int n = 0; n < NB; ++n) {
+                            if constexpr (F::LO) {
+                                float some[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                                mma<M>(some, a, lo[n][0], lo[n][1]);
+                                mma<M>(some, a, hi[n][0], hi[n][1]);
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) o[n][2 * k + i][j] += some[j];
+                            } else {
+                                mma<M>(o[n][2 * k + i], a, hi[n][0], hi[n][1]);
+                            }
                         }
                     }
                 }
             } else {
 #pragma unroll
-                for (int k = 0; k < KS; ++k) {
+                for (int k = 0; k < DT / 16; ++k) {
                     if (16 * k >= d) break;
-                    uint32_t b[4];
-                    ldsm4_t(b, va + (lane % 16) * stride + 32 * k + lane / 16 * 16);
+                    uint32_t a[4];
+                    ldsm4_t(a, va + (lane / 16 * 8 + lane % 8) * v_row + 32 * k + lane / 8 % 2 * 16);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        mma<M>(o[i][2 * k], hi[i], b[0], b[1]);
-                        mma<M>(o[i][2 * k + 1], hi[i], b[2], b[3]);
-                        mma<M>(o[i][2 * k], lo[i], b[0], b[1]);
-                        mma<M>(o[i][2 * k + 1], lo[i], b[2], b[3]);
+                    for (int n = 0; n < NB; ++n) {
+                        mma<M>(o[n][k], a, hi[n][0], hi[n][1]);
+                        mma<M>(o[n][k], a, lo[n][0], lo[n][1]);
                     }
                 }
             }
@@ -381,24 +494,22 @@ __global__ void __launch_bounds__(32 * WARPS) attend_few_kernel(const __grid_con
         // the warps' sums, through their rings
         float *mine = reinterpret_cast<float *>(ring);
 #pragma unroll
-        for (int n = 0; n < 2 * MT; ++n) {
-            const int r = 8 * n + g;
-            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 1);
-            l[n] += __shfl_xor_sync(0xffffffffu, l[n], 2);
-            if (t4 == 0) sh_m[warp][r] = m[n], sh_l[warp][r] = l[n];
-            if (r >= rows) continue;
+        for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int j = 0; j < DT / 8; ++j) {
-                const float a = o[n / 2][j][2 * (n % 2)], b = o[n / 2][j][2 * (n % 2) + 1];
-                if constexpr (CODES) {
-                    const int e = 32 * (j / 4) + 8 * t4 + j % 4;
-                    if (e < d) mine[r * d + e] = a;
-                    if (e + 4 < d) mine[r * d + e + 4] = b;
-                } else {
-                    if (8 * j < d) *reinterpret_cast<float2 *>(mine + r * d + 8 * j + 2 * t4) = make_float2(a, b);
+            for (int i = 0; i < 2; ++i) {
+                const int r = 8 * n + 2 * t4 + i;
+#pragma unroll
+                for (int k = 4; k < 32; k *= 2) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], k);
+                if (g == 0) sh_m[warp][r] = m[n][i], sh_l[warp][r] = l[n][i];
+                if (r >= rows) continue;
+#pragma unroll
+                for (int j = 0; j < DT / 16; ++j) {
+                    // the dims of rows g and g + 8
+                    const int e = CODES || WIDE ? 32 * (j / 2) + 4 * g + 2 * (j % 2) : 16 * j + g, f = CODES || WIDE ? e + 1 : e + 8;
+                    if (e < d) mine[r * d + e] = o[n][j][i];
+                    if (f < d) mine[r * d + f] = o[n][j][i + 2];
                 }
             }
-        }
         __syncthreads();
         for (int r = warp; r < rows; r += WARPS) {
             float top = -INFINITY, f[WARPS], sum = 0.0f;
@@ -433,38 +544,48 @@ __global__ void __launch_bounds__(32 * WARPS) attend_few_kernel(const __grid_con
     }
 }
 
-template <typename T, typename C, int DT, int MT>
+template <typename T, typename C, int DT, int NB>
 cudaError_t launch(const AttnP &p, int64_t grid, cudaStream_t st) {
+    using F = Form<T, C, DT, NB>;
     static PerDevice set;
-    const size_t bytes = Form<T, C, DT, MT>::bytes(p.c.head_dim);
-    if (const cudaError_t e = allow_smem(set, attend_few_kernel<T, C, DT, MT>, Form<T, C, DT, MT>::bytes(DT))) return e;
-    return launch_pdl(attend_few_kernel<T, C, DT, MT>, dim3((unsigned)grid), dim3(32 * WARPS), bytes, st, p);
+    const size_t bytes = F::bytes(p.c.head_dim);
+    if (const cudaError_t e = allow_smem(set, attend_few_kernel<T, C, DT, NB>, F::bytes(DT))) return e;
+    return launch_pdl(attend_few_kernel<T, C, DT, NB>, dim3((unsigned)grid), dim3(32 * F::WARPS), bytes, st, p);
 }
-// blocks of an SM at once: by shared memory, and two by registers
-template <typename T, typename C>
-int blocks_of(int d, int rows) {
-    const bool two = rows > 16;
-    const int bytes = d <= 64 ? (two ? Form<T, C, 64, 2>::bytes(d) : Form<T, C, 64, 1>::bytes(d))
-                      : d <= 128 ? (two ? Form<T, C, 128, 2>::bytes(d) : Form<T, C, 128, 1>::bytes(d))
-                                 : Form<T, C, 256, 1>::bytes(d);
-    return std::max(1, std::min(d <= 64 && !two ? 3 : 2, 225 * 1024 / (bytes + 2048)));
-}
-template <typename T, typename C>
-cudaError_t launch_any(const AttnP &p, int64_t grid, cudaStream_t st) {
-    const int d = p.c.head_dim;
-    if (d > 128) return launch<T, C, 256, 1>(p, grid, st);
-    if (p.rows > 16) return d <= 64 ? launch<T, C, 64, 2>(p, grid, st) : launch<T, C, 128, 2>(p, grid, st);
-    return d <= 64 ? launch<T, C, 64, 1>(p, grid, st) : launch<T, C, 128, 1>(p, grid, st);
-}
-
 // how a launch is cut: rows of an item, blocks of an SM at once
 struct Shape {
     int rows, blocks;
 };
+template <typename F>
+Shape shape_of(int d) {
+    return Shape{F::ROWS, std::max(1, std::min(F::BLOCKS, 226 * 1024 / (F::bytes(d) + 2048)))};
+}
+// the form for heads of d values and items of `rows` rows: body(its Form, its launch)
+template <typename T, typename C, typename Body>
+auto with_form(int d, int64_t rows, Body body) {
+#define SN_FEW(DT, NB) return body(Form<T, C, DT, NB>{}, launch<T, C, DT, NB>)
+    if (d > 128) {
+        if constexpr (sizeof(C) < 4)  // (fp32: their products are the bound, and 16 queries' sums fill the registers)
+            if (rows > 8) SN_FEW(256, 2);
+        SN_FEW(256, 1);
+    }
+    if (d > 64) {
+        if (rows <= 8) SN_FEW(128, 1);
+        if (rows <= 16) SN_FEW(128, 2);
+        SN_FEW(128, 4);
+    }
+    if (rows <= 8) SN_FEW(64, 1);
+    if (rows <= 16) SN_FEW(64, 2);
+    SN_FEW(64, 4);
+#undef SN_FEW
+}
+template <typename T, typename C>
+cudaError_t launch_any(const AttnP &p, int64_t grid, cudaStream_t st) {
+    return with_form<T, C>(p.c.head_dim, p.rows, [&](auto, auto launch) { return launch(p, grid, st); });
+}
 template <typename T, typename C>
 Shape shape_any(int d, int64_t rows) {
-    const int n = rows > 16 && d <= 128 ? 32 : 16;
-    return Shape{n, blocks_of<T, C>(d, n)};
+    return with_form<T, C>(d, rows, [&](auto form, auto) { return shape_of<decltype(form)>(d); });
 }
 
 }  // namespace few
@@ -478,6 +599,8 @@ few::Shape few_shape_f16_q8(int d, int64_t rows);
 cudaError_t attend_few_f16_q8(const AttnP &p, int64_t grid, cudaStream_t st);
 few::Shape few_shape_bf16_q8(int d, int64_t rows);
 cudaError_t attend_few_bf16_q8(const AttnP &p, int64_t grid, cudaStream_t st);
+few::Shape few_shape_f32(int d, int64_t rows);
+cudaError_t attend_few_f32(const AttnP &p, int64_t grid, cudaStream_t st);
 few::Shape few_shape_f32_q8(int d, int64_t rows);
 cudaError_t attend_few_f32_q8(const AttnP &p, int64_t grid, cudaStream_t st);
 

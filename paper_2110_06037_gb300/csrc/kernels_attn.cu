@@ -1,8 +1,5 @@
-// Attention of new tokens over a paged cache (sn_attend in include/sn.h): the form for every type by
-// multiply-adds in fp32, the join of split items, and the choice between the forms.
-//
-// A unit is 64 keys: scores of ROWS queries against them, their running maximum and sum, and the weighted
-// values, all in fp32; keys and values lie in shared memory as fp32 (codes times their scales).
+// Attention of new tokens over a paged cache (sn_attend in include/sn.h): the choice between the forms for few
+// queries (attn_few.cuh) and for many (attn_prompt.cuh), how the work is cut, and the join of split items.
 #include <algorithm>
 
 #include "attn_few.cuh"
@@ -13,187 +10,7 @@ namespace k {
 
 namespace {
 
-constexpr int KEYS = 64;
 constexpr float LOG2E = 1.4426950408889634f;
-
-// four neighbours of a row of the cache
-template <typename C>
-__device__ __forceinline__ float4 row4(const C *p) {
-    if constexpr (sizeof(C) == 4) {
-        return *reinterpret_cast<const float4 *>(p);
-    } else if constexpr (sizeof(C) == 2) {
-        alignas(8) C t[4];
-        *reinterpret_cast<uint2 *>(t) = *reinterpret_cast<const uint2 *>(p);
-        return make_float4(ldf(t), ldf(t + 1), ldf(t + 2), ldf(t + 3));
-    } else {
-        const char4 c = *reinterpret_cast<const char4 *>(p);
-        return make_float4((float)c.x, (float)c.y, (float)c.z, (float)c.w);
-    }
-}
-
-// thread (tr, tc) of 16 x 16 has rows tr + 16 i, keys tc + 16 j and values 4 tc + 64 j of a row
-template <typename T, typename C, int RPT, int DV>
-__global__ void __launch_bounds__(256) attend_kernel(const __grid_constant__ AttnP p) {
-    constexpr int ROWS = 16 * RPT;
-    extern __shared__ __align__(16) float sm[];
-    __shared__ int64_t sh[4];
-    const int d = p.c.head_dim, ld = d + 4, tid = threadIdx.x, tr = tid / 16, tc = tid % 16;
-    float *qs = sm, *ks = qs + ROWS * ld, *vs = ks + KEYS * ld, *ps = vs + KEYS * d;
-    __shared__ uint8_t there[KEYS];
-    griddep_launch();
-    griddep_wait();
-    Pieces pieces;
-    pieces.start(p, sh);
-    for (Piece w; pieces.next(p, w);) {
-        const Seq &s = w.past.s;
-        const int64_t row0 = (int64_t)w.tile * ROWS, all = (int64_t)s.len * p.group;
-        __syncthreads();
-        for (int i = tid; i < ROWS * d / 4; i += 256) {
-            const int r = i / (d / 4), e = i % (d / 4) * 4;
-            float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-            if (row0 + r < all) {
-                const T *x = static_cast<const T *>(p.h.x) + (s.first + (row0 + r) / p.group) * p.h.ldx +
-                             ((int64_t)w.head * p.group + (row0 + r) % p.group) * p.h.hx + e;
-                f = make_float4(ldf(x), ldf(x + 1), ldf(x + 2), ldf(x + 3));
-            }
-            *reinterpret_cast<float4 *>(qs + r * ld + e) = f;
-        }
-        int last[RPT];
-        float m[RPT], l[RPT], o[RPT][4 * DV];
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-            const int64_t row = row0 + tr + 16 * i;
-            last[i] = row < all ? last_key(p, w.past, row) : -1;
-            m[i] = -INFINITY, l[i] = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4 * DV; ++j) o[i][j] = 0.0f;
-        }
-        const int end = last_key(p, w.past, min(row0 + ROWS, all) - 1);
-        const int u1 = min(w.u1, end / KEYS + 1);
-        for (int u = w.u0; u < u1; ++u) {
-            __syncthreads();
-            for (int i = tid; i < KEYS * d / 4; i += 256) {
-                const int r = i / (d / 4), e = i % (d / 4) * 4, key = u * KEYS + r;
-                const int64_t place = key < w.past.ctx ? place_in(p.c, p.t, s.slot, key) : -1;
-                float4 f = make_float4(0.0f, 0.0f, 0.0f, 0.0f), g = f;
-                if (place >= 0) {
-                    const int64_t row = row_in(p.c, place, w.head), at = row * d + e;
-                    f = row4(static_cast<const C *>(p.c.k) + at), g = row4(static_cast<const C *>(p.c.v) + at);
-                    if constexpr (sizeof(C) == 1) {
-                        const float a = p.c.k_scale[row], b = p.c.v_scale[row];
-                        f.x *= a, f.y *= a, f.z *= a, f.w *= a;
-                        g.x *= b, g.y *= b, g.z *= b, g.w *= b;
-                    }
-                }
-                *reinterpret_cast<float4 *>(ks + r * ld + e) = f;
-                *reinterpret_cast<float4 *>(vs + r * d + e) = g;
-                if (e == 0) there[r] = place >= 0;
-            }
-            __syncthreads();
-            float a[RPT][4];
-#pragma unroll
-            for (int i = 0; i < RPT; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) a[i][j] = 0.0f;
-#pragma unroll 2
-            for (int e = 0; e < d; e += 4) {
-                float4 x[RPT], y[4];
-#pragma unroll
-                for (int i = 0; i < RPT; ++i) x[i] = *reinterpret_cast<const float4 *>(qs + (tr + 16 * i) * ld + e);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) y[j] = *reinterpret_cast<const float4 *>(ks + (tc + 16 * j) * ld + e);
-#pragma unroll
-                for (int i = 0; i < RPT; ++i)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        a[i][j] = fmaf(x[i].w, y[j].w, fmaf(x[i].z, y[j].z, fmaf(x[i].y, y[j].y, fmaf(x[i].x, y[j].x, a[i][j]))));
-            }
-#pragma unroll
-            for (int i = 0; i < RPT; ++i) {
-                float up = m[i];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int k = tc + 16 * j;
-                    a[i][j] = there[k] && u * KEYS + k <= last[i] ? a[i][j] * p.scale : -INFINITY;
-                    up = fmaxf(up, a[i][j]);
-                }
-#pragma unroll
-                for (int k = 8; k; k /= 2) up = fmaxf(up, __shfl_xor_sync(0xffffffffu, up, k));
-                const float base = up == -INFINITY ? 0.0f : up, old = exp2f(m[i] - base);
-                m[i] = up;
-                float sum = 0.0f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float e = exp2f(a[i][j] - base);
-                    sum += e;
-                    ps[(tr + 16 * i) * (KEYS + 4) + tc + 16 * j] = e;
-                }
-#pragma unroll
-                for (int k = 8; k; k /= 2) sum += __shfl_xor_sync(0xffffffffu, sum, k);
-                l[i] = fmaf(l[i], old, sum);
-#pragma unroll
-                for (int j = 0; j < 4 * DV; ++j) o[i][j] *= old;
-            }
-            __syncwarp();  // (a row's weights are written and read by the same half of a warp)
-            for (int k = 0; k < KEYS; k += 4) {
-                float4 x[RPT];
-#pragma unroll
-                for (int i = 0; i < RPT; ++i) x[i] = *reinterpret_cast<const float4 *>(ps + (tr + 16 * i) * (KEYS + 4) + k);
-#pragma unroll
-                for (int j = 0; j < DV; ++j) {
-                    const int e = 4 * tc + 64 * j;
-                    if (e >= d) break;
-                    float4 y[4];
-#pragma unroll
-                    for (int n = 0; n < 4; ++n) y[n] = *reinterpret_cast<const float4 *>(vs + (k + n) * d + e);
-#pragma unroll
-                    for (int i = 0; i < RPT; ++i) {
-                        float *f = o[i] + 4 * j;
-                        f[0] = fmaf(x[i].w, y[3].x, fmaf(x[i].z, y[2].x, fmaf(x[i].y, y[1].x, fmaf(x[i].x, y[0].x, f[0]))));
-                        f[1] = fmaf(x[i].w, y[3].y, fmaf(x[i].z, y[2].y, fmaf(x[i].y, y[1].y, fmaf(x[i].x, y[0].y, f[1]))));
-                        f[2] = fmaf(x[i].w, y[3].z, fmaf(x[i].z, y[2].z, fmaf(x[i].y, y[1].z, fmaf(x[i].x, y[0].z, f[2]))));
-                        f[3] = fmaf(x[i].w, y[3].w, fmaf(x[i].z, y[2].w, fmaf(x[i].y, y[1].w, fmaf(x[i].x, y[0].w, f[3]))));
-                    }
-                }
-            }
-        }
-        uint32_t again = 0;  // rows of this thread's that are not finite
-#pragma unroll
-        for (int i = 0; i < RPT; ++i) {
-            const int64_t row = row0 + tr + 16 * i;
-            if (w.slot >= 0) {
-                float *part = part_of_slot(p, w.slot);
-                const int r = tr + 16 * i;
-#pragma unroll
-                for (int j = 0; j < DV; ++j) {
-                    const int e = 4 * tc + 64 * j;
-                    if (e < d) *reinterpret_cast<float4 *>(part + r * d + e) = make_float4(o[i][4 * j], o[i][4 * j + 1], o[i][4 * j + 2], o[i][4 * j + 3]);
-                }
-                if (tc == 0) part[ROWS * d + r] = m[i], part[ROWS * d + ROWS + r] = l[i];
-            } else if (row < all) {
-                T *y = static_cast<T *>(p.h.y) + (s.first + row / p.group) * p.h.ldy + ((int64_t)w.head * p.group + row % p.group) * p.h.hy;
-                const float f = l[i] == 0.0f ? 0.0f : 1.0f / l[i];
-#pragma unroll
-                for (int j = 0; j < DV; ++j)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int e = 4 * tc + 64 * j + k;
-                        const float v = l[i] == 0.0f ? 0.0f : o[i][4 * j + k] * f;
-                        if (e < d) stf(y + e, v);
-                        if (!(fabsf(v) < INFINITY)) again |= 1u << i;
-                    }
-            }
-        }
-        if (w.slot < 0 && s.len > 1) {
-#pragma unroll
-            for (int i = 0; i < RPT; ++i) {
-                const uint32_t bad = __ballot_sync(0xffffffffu, again >> i & 1u);
-                for (int half = 0; half < 2; ++half)
-                    if (bad >> (16 * half) & 0xffffu) attend_again<T>(p, w.b, w.head, row0 + tid / 32 * 2 + half + 16 * i);
-            }
-        }
-    }
-}
 
 // ------------------------------------------------------------------- join
 // The items are counted again, and WPR warps take a row of one: its parts in turn, a lane eight values, and the
@@ -332,9 +149,6 @@ Plan plan_of(const sn_kv_cache &c, const AttendArgs &a, int lo, int hi, int rows
 }
 size_t part_bytes(const Plan &r) { return (size_t)r.p.blocks * 2 * r.p.rows * (r.p.c.head_dim + 2) * 4; }
 
-// sequences of up to this many tokens go to the form for few queries
-int few_tokens(int group) { return std::max(1, 64 / group); }
-
 struct Few {
     few::Shape (*shape)(int, int64_t);
     cudaError_t (*launch)(const AttnP &, int64_t, cudaStream_t);
@@ -343,54 +157,30 @@ Few few_of(int dt, int cache) {
     if (cache == SN_QI8)
         return dt == SN_F16 ? Few{few_shape_f16_q8, attend_few_f16_q8} : dt == SN_BF16 ? Few{few_shape_bf16_q8, attend_few_bf16_q8}
                                                                                  : Few{few_shape_f32_q8, attend_few_f32_q8};
-    if (dt == SN_F32) return Few{nullptr, nullptr};
-    return dt == SN_F16 ? Few{few_shape_f16, attend_few_f16} : Few{few_shape_bf16, attend_few_bf16};
+    return dt == SN_F32 ? Few{few_shape_f32, attend_few_f32} : dt == SN_F16 ? Few{few_shape_f16, attend_few_f16} : Few{few_shape_bf16, attend_few_bf16};
 }
 
 // the launches of a call: sequences of few tokens, the others; either may have nothing to do (grid 0)
 struct Plans {
     Few few;
-    bool tensor;  // b by attn_prompt.cuh
     Plan a, b;
 };
 Plans plans_of(const sn_kv_cache &c, int dt, const AttendArgs &a) {
-    Plans r{few_of(dt, c.dtype), dt != SN_F32 && c.dtype != SN_QI8, Plan{}, Plan{}};
-    const int group = a.h.heads / c.heads, n = !r.few.launch ? 0 : r.tensor ? few_tokens(group) : INT32_MAX;
-    if (n) {
-        const few::Shape s = r.few.shape(c.head_dim, std::min<int64_t>(a.q.max_len, n) * group);
-        r.a = plan_of(c, a, 0, n, s.rows, few::UNIT, s.blocks * num_sms(), 4, 16);
-        if (!a.q.offsets && a.q.max_len > n) r.a.grid = 0;
-    }
-    if (a.q.max_len > n && r.tensor) {
+    Plans r{few_of(dt, c.dtype), Plan{}, Plan{}};
+    const int group = a.h.heads / c.heads, sms = num_sms();
+    const bool tensor = dt != SN_F32 && c.dtype != SN_QI8;
+    // sequences of up to 64 rows go to the form for few queries
+    const int n = tensor ? std::max(1, 64 / group) : INT32_MAX;
+    const few::Shape s = r.few.shape(c.head_dim, std::min<int64_t>(a.q.max_len, n) * group);
+    r.a = plan_of(c, a, 0, n, s.rows, few::UNIT, s.blocks * sms, 4, 16);
+    if (!a.q.offsets && a.q.max_len > n) r.a.grid = 0;  // (its scratch counts all the same: that is asked for without offsets)
+    if (a.q.max_len > n) {
         // two tiles of rows a block, unless one each makes more blocks busy (heads beyond 128 values: one)
-        const int keys = c.head_dim > 128 ? 64 : 128, sms = num_sms();
+        const int keys = c.head_dim > 128 ? 64 : 128;
         r.b = plan_of(c, a, n, INT32_MAX, 256, keys, sms, 4, 1);
         if (c.head_dim > 128 || r.b.p.blocks) r.b = plan_of(c, a, n, INT32_MAX, 128, keys, sms, 4, 1);
-    } else if (a.q.max_len > n) {
-        r.b = plan_of(c, a, n, INT32_MAX, a.q.max_len * group <= 16 ? 16 : 64, KEYS, 2 * num_sms(), 2, 1);
     }
     return r;
-}
-
-template <typename T, typename C, int RPT, int DV>
-cudaError_t launch_simple(const Plan &r, cudaStream_t st) {
-    const int d = r.p.c.head_dim;
-    const size_t bytes = 4 * (size_t)(16 * RPT * (d + 4) + KEYS * (d + 4) + KEYS * d + 16 * RPT * (KEYS + 4));
-    static PerDevice set;
-    if (const cudaError_t e = allow_smem(set, attend_kernel<T, C, RPT, DV>, 224 * 1024)) return e;
-    return launch_pdl(attend_kernel<T, C, RPT, DV>, dim3((unsigned)r.grid), dim3(256), bytes, st, r.p);
-}
-template <typename T, typename C>
-cudaError_t simple_of(const Plan &r, cudaStream_t st) {
-    const int dv = (r.p.c.head_dim + 63) / 64;
-    if (r.p.rows == 16) {
-        if (dv == 1) return launch_simple<T, C, 1, 1>(r, st);
-        if (dv == 2) return launch_simple<T, C, 1, 2>(r, st);
-        return launch_simple<T, C, 1, 4>(r, st);
-    }
-    if (dv == 1) return launch_simple<T, C, 4, 1>(r, st);
-    if (dv == 2) return launch_simple<T, C, 4, 2>(r, st);
-    return launch_simple<T, C, 4, 4>(r, st);
 }
 
 template <typename T>
@@ -417,8 +207,7 @@ cudaError_t attend(const sn_kv_cache &c, int dt, const AttendArgs &a, void *work
             if (const cudaError_t e = join<T>(r.a, st)) return e;
         }
         if (r.b.grid) {
-            if (const cudaError_t e = r.tensor ? (dt == SN_F16 ? attend_prompt_f16 : attend_prompt_bf16)(r.b.p, r.b.grid, st) : simple_of<float, float>(r.b, st))
-                return e;
+            if (const cudaError_t e = (dt == SN_F16 ? attend_prompt_f16 : attend_prompt_bf16)(r.b.p, r.b.grid, st)) return e;
             if (const cudaError_t e = join<T>(r.b, st)) return e;
         }
     })

@@ -293,6 +293,19 @@ def test_layouts_batches_and_rows_behind(dt, kind):
     assert c.cache.attend(q[:0], ints(c.table), offsets=ints([0, 0, 0]), max_len=0).shape == (0, 4, 64)
 
 
+@pytest.mark.parametrize("dt, kind", [("f32", "plain"), ("bf16", "plain"), ("f16", "q8")])
+def test_attend_tokens_beside_a_prompt(dt, kind):
+    """Long sequences of one token, whose keys are shared out and joined, in one call with a prompt; rows behind them."""
+    import torch
+    c = Case(dt, kind, [1, 150, 1, 0, 5], [3000, 10, 1700, 9, 2500], 2, 64, 32, seed=17)
+    q = c.queries(8)
+    y = c.cache.attend(q, ints(c.table), max_context=3001, **c.args())
+    c.check(q, y)
+    out = torch.full((c.tokens + 50, 8, 64), 7.0, dtype=q.dtype, device="cuda")
+    c.cache.attend(torch.cat((q, q[:50])), ints(c.table), out=out, max_context=3001, **c.args())
+    assert torch.equal(out[:c.tokens], y) and bool((out[c.tokens:] == 7).all())
+
+
 def test_attend_graphs_and_streams():
     """Two captured calls replayed on two streams at once, and eager calls between them."""
     import torch
