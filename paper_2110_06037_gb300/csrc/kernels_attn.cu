@@ -15,7 +15,7 @@ constexpr float LOG2E = 1.4426950408889634f;
 // ------------------------------------------------------------------- join
 // The items are counted again, and WPR warps take a row of one: its parts in turn, a lane eight values, and the
 // warps' sums in order.  used: rows of an item that there can be.  (Four warps where an item has many parts, one where
-// there are many items: 64 sequences of 8 heads by one warp a row 5 us, by four 9.)
+// there are many items: for 64 sequences of 8 heads, from cold caches, one warp a row takes 10.5 us, four take 15.5.)
 template <typename T, int WPR>
 __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttnP p, int used) {
     constexpr int W = 4;
@@ -171,8 +171,14 @@ Plans plans_of(const sn_kv_cache &c, int dt, const AttendArgs &a) {
     const bool tensor = dt != SN_F32 && c.dtype != SN_QI8;
     // sequences of up to 64 rows go to the form for few queries
     const int n = tensor ? std::max(1, 64 / group) : INT32_MAX;
-    const few::Shape s = r.few.shape(c.head_dim, std::min<int64_t>(a.q.max_len, n) * group);
-    r.a = plan_of(c, a, 0, n, s.rows, few::UNIT, s.blocks * sms, 4, 16);
+    // Items of as many rows as there can be, for then the cache is read once; of 8 beside prompts, whose single tokens these
+    // are, and where there is so little to do that more blocks matter more (5 sequences of up to 8 drafted tokens, 6 heads
+    // in fp32, 2500 keys: 48 us by 32 rows and 4 units a block, 24 us by 8 rows and single units)
+    int64_t rows = std::min<int64_t>(a.q.max_len, n) * group;
+    const int64_t units = std::max<int64_t>(1, a.max_context / few::UNIT);
+    if ((tensor && a.q.max_len > n) || a.q.tokens * group / 8 * c.heads * units < 16 * sms) rows = std::min<int64_t>(rows, std::max(group, 8));
+    const few::Shape s = r.few.shape(c.head_dim, rows);
+    r.a = plan_of(c, a, 0, n, s.rows, few::UNIT, s.blocks * sms, dt == SN_F32 && c.dtype != SN_QI8 ? 1 : 4, 16);
     if (!a.q.offsets && a.q.max_len > n) r.a.grid = 0;  // (its scratch counts all the same: that is asked for without offsets)
     if (a.q.max_len > n) {
         // two tiles of rows a block, unless one each makes more blocks busy (heads beyond 128 values: one)

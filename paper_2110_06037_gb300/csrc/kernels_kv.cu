@@ -4,7 +4,8 @@
 // What bounds it is memory, and next to it the chain of four loads from a token to its page.  A lane has 16
 // neighbours of a head, the lanes of a head are neighbours, and a warp has as many heads of a token at once (a turn;
 // keys and values alike).  A block of four warps takes a few tokens, finds their places at once, a lane each, and its
-// warps take the turns, two of them loaded before the first is worked on.
+// warps take the turns, two of them loaded before the first is worked on.  8333 tokens of 8 heads of 128, bf16 into codes
+// and back: 33 us (18 and 15, each 52 MB); with a warp a token and a division a value 50.
 // Codes: the largest |v| by integers (above those of finite values there are infinities and NaN), v / s by the
 // reciprocal, rounded by adding 1.5 * 2^23, whose low byte then is the code.
 #include <algorithm>

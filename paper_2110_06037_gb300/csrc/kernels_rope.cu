@@ -11,6 +11,10 @@
 // has W slots in a row (two loads of W values) NC times, LPH lanes a head, 32 / LPH heads a warp, so that
 // a pair's two values meet in one lane, its angle is computed once a lane and token and serves all heads
 // that the lane sees, and only the norm's sums cross lanes.
+//
+// What bounds a prompt is the issue of instructions and their latency, next to memory: 8192 tokens of 40 heads of 128 in bf16
+// take 40 us (4.1 TB/s, 61 % of a copy's rate) with pairs of values in one instruction and the next two heads
+// under way, 62 us without either.  A lane that shares its slots with others computes a part of their turns.
 #include <algorithm>
 
 #include "kern_common.cuh"

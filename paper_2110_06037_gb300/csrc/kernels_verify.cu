@@ -5,7 +5,8 @@
 // contiguous pieces, whose weights are summed in units of 2^-60, in integers: exact, so that neither the
 // cut nor the order matters.  With every block's and warp's sum known, one warp's piece holds the drawn
 // index, and that warp's block goes through it once more (from L2): the warps' sums of its parts, and one warp's
-// running sums.  (One warp alone took 10 us for its 2000 values.)
+// running sums.  64 sequences over 128000 tokens: 26 us (2.4 TB/s): a chain of five dependent reads before the rows,
+// two meetings of a cluster behind them.
 #include <algorithm>
 
 #include "attn_common.cuh"
