@@ -24,6 +24,7 @@
 #pragma once
 
 #include "attn_common.cuh"
+#include "attn_order.h"
 #include "tc_common.cuh"
 
 namespace sn {
@@ -381,7 +382,7 @@ __global__ void __launch_bounds__(Form<DT, NT>::THREADS, 1)
                 if (grew) f = ex2(m - up), m = up;
                 if (__any_sync(0xffffffffu, grew)) {
                     l2 = mul_2(l2, f2(f, f));
-                    if (j > 0) {
+                    if (j > 0) {  // (the product before that one is over: these scores were asked for behind it)
                         must(&sh.pv[t], (sums + j - 1) & 1u, ERR_EPI_WAIT);
                         tc_fence_after();
 #pragma unroll 1
@@ -416,7 +417,7 @@ __global__ void __launch_bounds__(Form<DT, NT>::THREADS, 1)
                 meet();
             }
             if (n) {
-                must(&sh.pv[t], (sums + n - 1) & 1u, ERR_EPI_WAIT);
+                for (int j = first_open_product(n, LA); j < n; ++j) must(&sh.pv[t], (sums + j) & 1u, ERR_EPI_WAIT);
                 tc_fence_after();
             }
             tiles += n, sums += n;

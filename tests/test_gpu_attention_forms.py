@@ -1,0 +1,123 @@
+"""Attention over a cache on the GPU, each of its kernels' instances by its sizes, against the definition in 64 bits.
+
+Error bounds, for terms of magnitudes that sum to M (the weights' values here): a score of dim products and eight
+factors and roundings is off by (dim + 8) 2^-24 of the magnitude of its products, and by as much again where the tensor
+cores truncate; a weight by that, and so is their sum; the exponential's argument and 2 ulp count 8 roundings, twice; the sums
+one a key and 64 more, twice for truncation.  What goes to the tensor cores in 16 bits is off by PART of itself (one part: half
+a step of its type; two parts: the square of that), in fp16 also by half the spacing of the smallest values, 2^-25, where the
+largest weight is 2^14.  The result is rounded once, by U of itself.
+"""
+import math
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+E32 = 2.0 ** -24
+U = {"f32": 0.0, "f16": 2.0 ** -11, "bf16": 2.0 ** -8}
+TINY = {"f32": 1e-37, "f16": 2.0 ** -24, "bf16": 1e-37}  # half the spacing of the smallest values
+
+
+def tdt(name):
+    import torch
+    return {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}[name]
+
+
+def ints(a):
+    import torch
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device="cuda")
+
+
+class Case:
+    """A cache of random pages, dealt to sequences of `new` tokens behind `before`, and their queries."""
+
+    def __init__(self, dt, kind, new, before, q_heads, heads, dim, page, seed=0):
+        import torch
+        import paper_2110_06037_gb300 as sn
+        self.g = g = torch.Generator(device="cuda").manual_seed(seed)
+        self.dt, self.new, self.before, self.dim, self.heads, self.page = dt, list(new), list(before), dim, heads, page
+        per = [-(-(a + b) // page) for a, b in zip(new, before)]
+        pages = sum(per) + 2
+        order = np.random.default_rng(seed).permutation(pages)
+        self.table = np.full((len(new), max([1] + per) + 1), -1, dtype=np.int32)
+        for i, n in enumerate(per):
+            self.table[i, :n] = order[sum(per[:i]):sum(per[:i + 1])]
+        self.offsets = np.concatenate(([0], np.cumsum(new))).astype(np.int32)
+        shape = (pages, heads, page, dim)
+        if kind == "q8":
+            kv = [torch.randint(-127, 128, shape, generator=g, device="cuda", dtype=torch.int8) for _ in range(2)]
+            scales = [(0.5 + torch.rand(shape[:3], generator=g, device="cuda")) / 64 for _ in range(2)]
+            self.t = kv + scales
+        else:
+            self.t = [torch.randn(shape, generator=g, device="cuda").to(tdt(dt)) for _ in range(2)]
+        self.cache = sn.KVCache(*self.t)
+        self.q = (1.5 * torch.randn(int(self.offsets[-1]), q_heads, dim, generator=g, device="cuda")).to(tdt(dt))
+        self.args = dict(offsets=ints(self.offsets), max_len=max(new), pos=ints(before), max_context=max(a + b for a, b in zip(new, before)))
+
+    def run(self, **kw):
+        return self.cache.attend(self.q, ints(self.table), **{**self.args, **kw})
+
+    def values(self):
+        """(keys, values) as fp64 [pages, heads, page, dim]."""
+        k, v = (t.double() for t in self.t[:2])
+        return (k, v) if len(self.t) == 2 else (k * self.t[2].double()[..., None], v * self.t[3].double()[..., None])
+
+    def reference(self):
+        """(y, magnitude of what is averaged, magnitude of a score's products, keys seen, largest value)."""
+        import torch
+        k, v = self.values()
+        scale, group = 1 / math.sqrt(self.dim), self.q.shape[1] // self.heads
+        y = torch.zeros(self.q.shape, dtype=torch.float64, device="cuda")
+        mag, es = torch.zeros_like(y), torch.zeros(y.shape[:2], dtype=torch.float64, device="cuda")
+        seen, top = torch.zeros_like(es), torch.zeros_like(es)
+        for b, (n, at) in enumerate(zip(self.new, self.before)):
+            if n == 0:
+                continue
+            ids = torch.from_numpy(self.table[b, :-(-(n + at) // self.page)]).long().cuda()
+            rows = slice(int(self.offsets[b]), int(self.offsets[b + 1]))
+            last = at + torch.arange(n, device="cuda")
+            unseen = torch.arange(n + at, device="cuda")[None, :] > last[:, None]
+            for h in range(self.q.shape[1]):
+                kk, vv = (t[ids, h // group].flatten(0, 1)[:n + at] for t in (k, v))
+                q = self.q[rows, h].double()
+                s = (q @ kk.T * scale).masked_fill(unseen, -math.inf)
+                w = torch.softmax(s, dim=1)
+                y[rows, h], mag[rows, h] = w @ vv, w @ vv.abs()
+                es[rows, h] = (q.abs() @ kk.abs().T * scale).masked_fill(unseen, 0).amax(dim=1)
+                seen[rows, h], top[rows, h] = (last + 1).double(), vv.abs().max()
+        return y, mag, es, seen, top
+
+    def check(self, got, part):
+        y, mag, es, seen, top = self.reference()
+        rel = 2 * (self.dim + 8) * 2 * E32 * es + 16 * E32 + (seen + 64) * 2 * E32 + part
+        bound = mag * rel[..., None]
+        if self.dt == "f16" or len(self.t) > 2:
+            bound = bound + (seen * top * 2.0 ** -39)[..., None]
+        err = (got.double() - y).abs() - (U[self.dt] * (y.abs() + bound) + bound + TINY[self.dt])
+        assert not got.isnan().any()
+        assert float(err.max()) <= 0, (float(err.max()), np.unravel_index(int(err.argmax()), tuple(err.shape)))
+
+
+# new, before, query heads, heads, dim, page: more than 64 rows a sequence, 16-bit values.  Heads beyond 128 values go by one tile
+# of 128 rows and 64 keys at a time; up to eight of these are one block's, and so are more where blocks are many
+PROMPTS = [
+    ([40], [0], 4, 2, 192, 16), ([65], [0], 1, 1, 256, 128), ([70], [0], 1, 1, 144, 16), ([130], [0], 2, 2, 256, 256), ([90], [60], 3, 1, 176, 32),
+    ([100, 1, 66], [100, 300, 60], 7, 1, 192, 32), ([80], [432], 4, 4, 256, 64), ([640], [560], 32, 8, 256, 128),
+    ([90, 70], [2000, 777], 4, 2, 256, 16), ([200], [3000], 8, 2, 144, 256), ([66, 65], [1000, 999], 2, 2, 240, 128),
+    # and where few rows have many keys, whose units are shared out and joined, heads of up to 128
+    ([90], [1100], 4, 2, 128, 16), ([130, 1, 70], [5000, 40, 2000], 8, 2, 96, 64), ([100], [2500], 2, 1, 80, 256), ([70], [3000], 3, 1, 64, 32),
+    ([66], [1500], 2, 2, 16, 128), ([300], [1000], 1, 1, 128, 256), ([129, 65], [1200, 4000], 5, 1, 48, 128),
+    # two tiles of rows a block
+    ([300, 17], [0, 5], 8, 2, 128, 256), ([260], [700], 4, 2, 64, 256), ([128, 257], [3, 0], 2, 2, 112, 128)]
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("new, before, q_heads, heads, dim, page", PROMPTS)
+def test_prompts(dt, new, before, q_heads, heads, dim, page):
+    import torch
+    c = Case(dt, "plain", new, before, q_heads, heads, dim, page, seed=dim + len(new))
+    y = c.run()
+    c.check(y, U[dt])
+    for _ in range(3):
+        assert torch.equal(c.run(), y)
