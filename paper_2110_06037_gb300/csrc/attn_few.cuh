@@ -538,7 +538,7 @@ __global__ void __launch_bounds__(32 * Form<T, C, DT, NB>::WARPS, Form<T, C, DT,
                 }
             }
             if (part && lane == 0) part[ROWS * d + r] = top, part[ROWS * d + ROWS + r] = sum;
-            if (!part && s.len > 1 && __any_sync(0xffffffffu, bad)) attend_again<T>(p, w.b, w.head, row0 + r);
+            if (!part && __any_sync(0xffffffffu, bad)) attend_again<T>(p, w.b, w.head, row0 + r);
         }
         __syncthreads();  // the rings and the queries are free
     }

@@ -109,7 +109,7 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
         stf(y + e, v);
         bad |= !(fabsf(v) < INFINITY);
     }
-    if (past.s.len > 1 && __any_sync(0xffffffffu, bad)) attend_again<T>(p, b, head, row);
+    if (__any_sync(0xffffffffu, bad)) attend_again<T>(p, b, head, row);
 }
 
 // ------------------------------------------------------------------ choice
