@@ -185,8 +185,8 @@ __device__ __forceinline__ int last_key(const AttnP &p, const Past &s, int64_t r
 }
 
 // An output that is not finite may have met values that its query does not see (0 times infinity), or infinities that
-// it sees but that came to the products in two parts (infinity less infinity): it is then computed again from what it sees,
-// by one whole warp, in fp32.
+// it sees but that came to the products in two parts (infinity less infinity), or codes with scales beyond the products'
+// range: it is then computed again from what it sees, by one whole warp, in fp32.
 template <typename T>
 __device__ __noinline__ void attend_again(const AttnP &p, int b, int head, int64_t row) {
     const int lane = threadIdx.x % 32, d = p.c.head_dim;

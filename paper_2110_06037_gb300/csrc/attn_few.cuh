@@ -16,7 +16,9 @@
 // below 2^-34 of that is lost; fp32 queries as two parts).  The keys' scales are factors of the scores.  A value's scale
 // is 2^e f, f in [1, 2): e goes into the exponent and f into the weight,
 //   P_j = 2^(s_j + e_j - m) f_j,   sum of weights += 2^(s_j + e_j - m) 2^-e_j,
-// so that P is within fp16's range whatever the scales are.  What bounds codes is the issue of instructions: to
+// so that P is within fp16's range.  With e from -76 to 24 no sum of weights is infinite, and what 2^(s_j + e_j - m) loses
+// below fp32's range is below 2^-40 of them; a key whose value has another scale makes the row NaN, and
+// attend_again computes it.  What bounds codes is the issue of instructions: to
 // make fp16 of a tile's codes takes half of them.  For bf16 queries P is one part, off by 2^-11 of itself, an eighth of
 // the output's rounding.
 //
@@ -348,11 +350,11 @@ __global__ void __launch_bounds__(32 * Form<T, C, DT, NB>::WARPS, Form<T, C, DT,
                 for (int j = 0; j < 2; ++j) {
                     ks[j] = f[g + 8 * j];
                     const uint32_t u = __float_as_uint(f[TILE + g + 8 * j]), e = u >> 23 & 255u;
-                    // (below the normal range: 2^-126 and what is left; not finite: NaN)
-                    ve[j] = (float)((int)(e ? e : 1u) - 127);
-                    vi[j] = __uint_as_float((254u - min(max(e, 1u), 253u)) << 23);
-                    vf[j] = e == 255u ? __int_as_float(0x7fc00000) : e ? __uint_as_float((u & 0x807fffffu) | 0x3f800000u)
-                                                                     : f[TILE + g + 8 * j] * 8.507059173023462e37f;
+                    const bool far = e - (127u - 76u) > 100u;  // (not finite too)
+                    const uint32_t n = far ? 127u : e;
+                    ve[j] = (float)((int)n - 127);
+                    vi[j] = __uint_as_float((254u - n) << 23);
+                    vf[j] = far ? __int_as_float(0x7fc00000) : __uint_as_float((u & 0x807fffffu) | 0x3f800000u);
                 }
             }
             const bool whole = ok && tile * TILE + TILE - 1 <= first;

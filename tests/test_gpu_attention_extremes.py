@@ -75,3 +75,37 @@ def test_fp32_value_that_rounds_to_infinity_in_fewer_bits():
     c.t[1][..., 3], c.t[1][..., 5] = torch.finfo(torch.float32).max, -torch.finfo(torch.float32).max
     n, i = at(c, 0, 0)
     assert torch.equal(c.run(), c.t[1][n, 0, i].expand_as(c.q))
+
+
+@pytest.mark.parametrize("new, before", SIZES + [([1, 3, 1], [2500, 40, 900])])
+@pytest.mark.parametrize("dt, far", [(dt, f) for dt in ("f32", "f16", "bf16") for f in (2.0 ** -100, 1e-36, 2.0 ** -149, 2.0 ** 40, 2.0 ** 100)
+                                     if dt != "f16" or f < 1])
+@pytest.mark.parametrize("where", ["first", "some", "all"])
+def test_codes_with_far_scales_of_values(dt, new, before, far, where):
+    """Values next to zero, or huge, beside others or alone, weigh what their scores say."""
+    import torch
+    c = Case(dt, "q8", new, before, 4, 2, 64, 16, seed=5)
+    scale = c.t[3]
+    if where == "first":
+        for b in range(len(new)):
+            scale[at(c, b, 0)[0], 0, :9] = far
+    elif where == "some":
+        scale[torch.rand(scale.shape, generator=c.g, device="cuda") < 0.3] = far
+    else:
+        scale.fill_(far)
+    # a weight over codes is one fp16 part for bf16, two for the others
+    c.check(c.run(), 2.0 ** (-11 if dt == "bf16" else -21))
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("new, before", SIZES)
+def test_codes_behind_what_is_seen_do_not_matter(dt, new, before):
+    """Scales of every kind in the places behind a sequence."""
+    import torch
+    c = Case(dt, "q8", new, before, 4, 2, 64, 256, seed=6)
+    want = c.run()
+    n, i = at(c, 0, new[0] + before[0] - 1)
+    for j, far in enumerate([0.0, 2.0 ** -149, 2.0 ** 127, math.inf, -math.inf, math.nan, -math.nan]):
+        if i + 1 + j < c.page:
+            c.t[2][n, :, i + 1 + j], c.t[3][n, :, i + 1 + j] = far, far
+    assert torch.equal(c.run(), want)
