@@ -141,7 +141,7 @@ Plan plan_of(const sn_kv_cache &c, const AttendArgs &a, int lo, int hi, int rows
     const int64_t units = std::max<int64_t>(1, (a.max_context + keys - 1) / keys);
     r.grid = r.items = items;
     r.used = (int)std::min<int64_t>(rows, most * p.group);
-    if (units > 2 * least && items < waves * (int64_t)room) {
+    if (items && units > 2 * least && items < waves * (int64_t)room) {  // (without items: grid 0, nothing is launched)
         p.blocks = (int32_t)std::max<int64_t>(1, std::min<int64_t>(room, (items * units + least - 1) / least));
         r.grid = p.blocks;
     }

@@ -121,3 +121,13 @@ def test_prompts(dt, new, before, q_heads, heads, dim, page):
     c.check(y, U[dt])
     for _ in range(3):
         assert torch.equal(c.run(), y)
+
+
+@pytest.mark.parametrize("dt, kind", [("f32", "plain"), ("bf16", "plain"), ("f16", "q8")])
+@pytest.mark.parametrize("context", [64, 4096])
+def test_rows_behind_empty_sequences_are_left(dt, kind, context):
+    import torch
+    c = Case(dt, kind, [9], [0], 4, 2, 64, 16)
+    out = torch.full_like(c.q, 7.0)
+    c.cache.attend(c.q, ints(np.zeros((3, 300))), offsets=ints([0, 0, 0, 0]), max_len=0, pos=ints([5, 0, 9]), max_context=context, out=out)
+    assert bool((out == 7).all())
