@@ -2,6 +2,7 @@
 #pragma once
 
 #include "ssm_common.cuh"
+#include "tc_common.cuh"
 
 namespace sn {
 namespace k {
@@ -143,6 +144,9 @@ struct Pieces {
             if (threadIdx.x == 0) sh[0] = from, sh[1] = to, sh[2] = s.before, sh[3] = s.b;
         }
         __syncthreads();
+        rewind(sh);
+    }
+    __device__ __forceinline__ void rewind(const int64_t *sh) {
         at = sh[0], end = sh[1], before = sh[2], b = (int)sh[3];
         first = true;
     }
@@ -174,6 +178,9 @@ struct Pieces {
         return true;
     }
 };
+// log2 of the weight of the largest score (fp16 products: so that small weights are within its range)
+template <typename T, bool CODES>
+constexpr float top_weight() { return CODES || std::is_same<T, __half>::value ? 14.0f : 0.0f; }
 __device__ __forceinline__ float *part_of_slot(const AttnP &p, int slot) {
     return p.part + (int64_t)slot * p.rows * (p.c.head_dim + 2);
 }
@@ -184,54 +191,148 @@ __device__ __forceinline__ int last_key(const AttnP &p, const Past &s, int64_t r
     return (int)(at < s.ctx ? at : s.ctx - 1);
 }
 
-// An output that is not finite may have met values that its query does not see (0 times infinity), or infinities that
+// A result that is not finite may have met values that its query does not see (0 times infinity), or infinities that
 // it sees but that came to the products in two parts (infinity less infinity), or codes with scales beyond the products'
-// range: it is then computed again from what it sees, by one whole warp, in fp32.
+// range: it is then computed again from what it sees, by one whole warp, in fp32.  Of a cut item that is the part that has
+// met them: its average, with a sum of weights of 1 (and its largest score changed accordingly).
+// Keys go ONCE at a time, a lane pairs of a head's values, all loads before what needs them (for they are what it waits
+// for), and the sums stay divided by that of the weights and within their type, so that roundings make no infinity.  A row ends
+// where what is not finite has become NaN, which nothing changes any more.
+// It is slow: a prompt of 4096 tokens, 32 heads of 128 over 8, all of whose rows see an infinite value from the start, takes
+// 57 ms for 0.19 in bf16, 91 for 1.1 over codes, 165 for 5.1 in fp32; with a NaN in its place 0.9, 1.4 and 5.7, with
+// one in the middle half of the infinity's; one token over 131072 keys 3.4 ms for 0.10, with a NaN 0.12.
+template <typename C>
+struct Pair {  // two neighbours as they lie in memory
+    using Raw = typename std::conditional<sizeof(C) == 4, float2, typename std::conditional<sizeof(C) == 2, uint32_t, char2>::type>::type;
+    static __device__ __forceinline__ Raw load(const void *p, int64_t at) { return *reinterpret_cast<const Raw *>(static_cast<const C *>(p) + at); }
+    static __device__ __forceinline__ float2 floats(Raw v) {
+        if constexpr (sizeof(C) == 4) return v;
+        else if constexpr (sizeof(C) == 2) return tc::unpack2<C>(v);
+        else return make_float2((float)v.x, (float)v.y);
+    }
+};
 template <typename T>
-__device__ __noinline__ void attend_again(const AttnP &p, int b, int head, int64_t row) {
+constexpr float largest_of() { return std::is_same<T, __nv_bfloat16>::value ? 3.38953138925e38f : 3.40282346639e38f; }
+template <typename T, typename C, int ONCE>
+__device__ __forceinline__ void compute_again(const AttnP &p, const Past &past, int head, int tile, int r, int u0, int u1, float *part) {
+    constexpr bool CODES = sizeof(C) == 1;
     const int lane = threadIdx.x % 32, d = p.c.head_dim;
-    const Past past = past_of(p, b);
-    const int64_t token = past.s.first + row / p.group, qh = (int64_t)head * p.group + row % p.group;
-    const int last = last_key(p, past, row);
+    const int64_t row = (int64_t)tile * p.rows + r, token = past.s.first + row / p.group, qh = (int64_t)head * p.group + row % p.group;
+    const T *x = static_cast<const T *>(p.h.x) + token * p.h.ldx + qh * p.h.hx;
+    T *y = static_cast<T *>(p.h.y) + token * p.h.ldy + qh * p.h.hy;
+    const int last = (int)min((int64_t)last_key(p, past, row), (int64_t)u1 * p.keys - 1);
     float q[8], o[8], m = -INFINITY, l = 0.0f;
+    uint32_t need = 0, infinite = 0;  // of this lane's values: not finite; averages of an infinity
+    __syncwarp();  // (others may have written them)
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
+        const int e = 64 * (i / 2) + 2 * lane + i % 2;
         o[i] = 0.0f;
-        q[i] = lane + 32 * i < d ? ldf(static_cast<const T *>(p.h.x) + token * p.h.ldx + qh * p.h.hx + lane + 32 * i) : 0.0f;
+        q[i] = e < d ? ldf(x + e) : 0.0f;
+        if (e < d && !(fabsf(part ? part[r * d + e] : ldf(y + e)) < INFINITY)) need |= 1u << i;
     }
-    for (int j = 0; j <= last; ++j) {
-        const int64_t place = place_in(p.c, p.t, past.s.slot, j);
-        if (place < 0) continue;
-        const int64_t r = row_in(p.c, place, head);
-        float s = 0.0f, v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int e = lane + 32 * i;
-            v[i] = 0.0f;
-            if (e >= d) continue;
-            if (p.c.dtype == SN_QI8) {
-                s = fmaf(q[i], (float)static_cast<const int8_t *>(p.c.k)[r * d + e], s);
-                v[i] = p.c.v_scale[r] * (float)static_cast<const int8_t *>(p.c.v)[r * d + e];
-            } else {
-                s = fmaf(q[i], ldf(static_cast<const T *>(p.c.k) + r * d + e), s);
-                v[i] = ldf(static_cast<const T *>(p.c.v) + r * d + e);
-            }
+    if (!__any_sync(0xffffffffu, need)) return;
+    bool open = true;
+#pragma unroll 1
+    for (int64_t j0 = (int64_t)u0 * p.keys; open && j0 <= last; j0 += 32) {
+        int64_t mine = -1;  // the row of key j0 + lane
+        if (j0 + lane <= last) {
+            const int64_t place = place_in(p.c, p.t, past.s.slot, j0 + lane);
+            if (place >= 0) mine = row_in(p.c, place, head);
         }
+        float ks = 1.0f, vs = 1.0f;
+        if (CODES && mine >= 0) ks = p.c.k_scale[mine], vs = p.c.v_scale[mine];
+#pragma unroll 1
+        for (int g = 0; open && g < 32 && j0 + g <= last; g += ONCE) {
+            float s[ONCE];
 #pragma unroll
-        for (int k = 16; k; k /= 2) s += __shfl_xor_sync(0xffffffffu, s, k);
-        s *= p.scale;
-        if (p.c.dtype == SN_QI8) s *= p.c.k_scale[r];
-        const float up = fmaxf(m, s), base = up == -INFINITY ? 0.0f : up;
-        const float old = exp2f(m - base), w = exp2f(s - base);
-        m = up;
-        l = fmaf(l, old, w);
+            for (int k = 0; k < ONCE; ++k) s[k] = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = fmaf(o[i], old, w * v[i]);
+            for (int i = 0; i < 8; i += 2) {
+                const int e = 32 * i + 2 * lane;
+                if (32 * i >= d) break;
+                typename Pair<C>::Raw v[ONCE];
+#pragma unroll
+                for (int k = 0; k < ONCE; ++k) {
+                    const int64_t r = __shfl_sync(0xffffffffu, mine, g + k);
+                    v[k] = Pair<C>::load(p.c.k, (r < 0 ? 0 : r) * d + (e < d ? e : 0));
+                }
+#pragma unroll
+                for (int k = 0; k < ONCE; ++k) {
+                    const float2 f = Pair<C>::floats(v[k]);
+                    const float z = CODES ? __shfl_sync(0xffffffffu, ks, g + k) : 1.0f;
+                    if (e < d) s[k] = fmaf(q[i], CODES ? f.x * z : f.x, fmaf(q[i + 1], CODES ? f.y * z : f.y, s[k]));
+                }
+            }
+            float up = m;
+#pragma unroll
+            for (int k = 0; k < ONCE; ++k) {
+#pragma unroll
+                for (int n = 16; n; n /= 2) s[k] += __shfl_xor_sync(0xffffffffu, s[k], n);
+                s[k] = __shfl_sync(0xffffffffu, (int)(mine < 0), g + k) ? -INFINITY : s[k] * p.scale;
+                up = fmaxf(up, s[k]);
+            }
+            const float base = up == -INFINITY ? 0.0f : up;
+            const float before = l * exp2f(m - base);
+            m = up, l = before;
+#pragma unroll
+            for (int k = 0; k < ONCE; ++k) {
+                s[k] = exp2f(s[k] - base);
+                l += s[k];
+            }
+            const float inv = l == 0.0f ? 0.0f : 1.0f / l, keep = before * inv;
+            bool any = false;
+#pragma unroll
+            for (int i = 0; i < 8; i += 2) {
+                const int e = 32 * i + 2 * lane;
+                if (32 * i >= d) break;
+                typename Pair<C>::Raw v[ONCE];
+#pragma unroll
+                for (int k = 0; k < ONCE; ++k) {
+                    const int64_t r = __shfl_sync(0xffffffffu, mine, g + k);
+                    v[k] = Pair<C>::load(p.c.v, (r < 0 ? 0 : r) * d + (e < d ? e : 0));
+                }
+                o[i] *= keep, o[i + 1] *= keep;
+#pragma unroll
+                for (int k = 0; k < ONCE; ++k) {
+                    float2 f = Pair<C>::floats(v[k]);
+                    const float z = CODES ? __shfl_sync(0xffffffffu, vs, g + k) : 1.0f;
+                    if (CODES) f.x *= z, f.y *= z;
+                    if (__shfl_sync(0xffffffffu, (int)(mine < 0), g + k)) f.x = f.y = 0.0f;
+                    o[i] = fmaf(s[k] * inv, f.x, o[i]), o[i + 1] = fmaf(s[k] * inv, f.y, o[i + 1]);
+                    infinite |= (uint32_t)(fabsf(f.x) == INFINITY) << i | (uint32_t)(fabsf(f.y) == INFINITY) << (i + 1);
+                }
+#pragma unroll
+                for (int h = i; h < i + 2; ++h) {
+                    if (fabsf(o[h]) == INFINITY && !(infinite >> h & 1u)) o[h] = copysignf(largest_of<T>(), o[h]);
+                    any |= (need >> h & 1u) && o[h] == o[h];
+                }
+            }
+            open = l == l && (l == 0.0f || __any_sync(0xffffffffu, any));
+        }
     }
+    const float bad = l != l ? l : 0.0f;
+    const bool all = part && (open || l != l);  // (a part's other values get its new factor, but beside NaN they stay)
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (lane + 32 * i < d)
-            stf(static_cast<T *>(p.h.y) + token * p.h.ldy + qh * p.h.hy + lane + 32 * i, l == 0.0f ? 0.0f : o[i] / l);
+    for (int i = 0; i < 8; ++i) {
+        const int e = 64 * (i / 2) + 2 * lane + i % 2;
+        if (e >= d || !(all || (need >> i & 1u))) continue;
+        const float v = l > 0.0f ? o[i] : bad;
+        if (part) part[r * d + e] = v;
+        else stf(y + e, v);
+    }
+    if (all && lane == 0) {
+        part[(int64_t)p.rows * d + r] = l > 0.0f ? m + log2f(l) + top_weight<T, CODES>() : m;
+        part[(int64_t)p.rows * d + p.rows + r] = l > 0.0f ? 1.0f : bad;
+    }
+}
+// row r of a piece of work
+template <typename T, int ONCE>
+__device__ __noinline__ void attend_again(const AttnP &p, int b, int head, int tile, int r, int u0, int u1, int slot) {
+    const Past past = past_of(p, b);
+    float *part = slot >= 0 ? part_of_slot(p, slot) : nullptr;
+    if (p.c.dtype == SN_QI8) compute_again<T, int8_t, ONCE>(p, past, head, tile, r, u0, u1, part);
+    else compute_again<T, T, ONCE>(p, past, head, tile, r, u0, u1, part);
 }
 
 }  // namespace k

@@ -99,7 +99,7 @@ struct Form {
     static constexpr bool QREG = NB * (DT / STEP) * QR <= 64 && NB * DT <= 256;  // queries in registers
     // log2 of the largest weight when m is the largest score, and how far a score may be above m
     // (codes: times the values' f, below 2)
-    static constexpr float TOP = HALF ? 14.0f : 0.0f, THR = HALF ? (CODES ? 0.95f : 1.5f) : 8.0f;
+    static constexpr float TOP = top_weight<T, CODES>(), THR = HALF ? (CODES ? 0.95f : 1.5f) : 8.0f;
     static constexpr int STAGES = 3;
     static constexpr int ROWS = 8 * NB;
     static constexpr int WARPS = WIDE && DT > 128 ? 2 : 4;
@@ -536,11 +536,11 @@ __global__ void __launch_bounds__(32 * Form<T, C, DT, NB>::WARPS, Form<T, C, DT,
                 } else {
                     v = sum == 0.0f ? 0.0f : v * inv_l;
                     stf(y + e, v);
-                    bad |= !(fabsf(v) < INFINITY);
                 }
+                bad |= !(fabsf(v) < INFINITY);
             }
             if (part && lane == 0) part[ROWS * d + r] = top, part[ROWS * d + ROWS + r] = sum;
-            if (!part && __any_sync(0xffffffffu, bad)) attend_again<T>(p, w.b, w.head, row0 + r);
+            if (__any_sync(0xffffffffu, bad)) attend_again<T, 4>(p, w.b, w.head, w.tile, r, w.u0, w.u1, w.slot);
         }
         __syncthreads();  // the rings and the queries are free
     }

@@ -52,7 +52,7 @@ struct Shared {
     uint64_t full[8], empty[8], s[2], pv[2];
     int64_t start[4];
     uint32_t tmem;
-    int abort;
+    int abort, again;  // a wait gave up; a result is not finite
 };
 static_assert(sizeof(Shared) <= 1024, "behind the ring");
 
@@ -141,7 +141,7 @@ __global__ void __launch_bounds__(Form<DT, NT>::THREADS, 1)
     using F = Form<DT, NT>;
     constexpr int KT = F::KT, LA = F::LA, GATE = 128 + 64;  // threads that meet at a named barrier: a tile's softmax, two warps
     constexpr uint32_t R = F::R;
-    constexpr float TOP = std::is_same<T, __half>::value ? 14.0f : 0.0f, THR = std::is_same<T, __half>::value ? 1.0f : 8.0f;
+    constexpr float TOP = top_weight<T, false>(), THR = std::is_same<T, __half>::value ? 1.0f : 8.0f;
     extern __shared__ __align__(1024) uint8_t smem[];
     Shared &sh = *reinterpret_cast<Shared *>(smem + F::OFF_SH);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -154,7 +154,7 @@ __global__ void __launch_bounds__(Form<DT, NT>::THREADS, 1)
         tmem_alloc<1>(&sh.tmem, 512);
     } else if (warp == 1) {
         if (lane < 20) mbar_init(&sh.full[0] + lane, 1);
-        if (lane == 31) sh.abort = 0;
+        if (lane == 31) sh.abort = sh.again = 0;
         fence_mbar_init();
     }
     tc_fence_before();
@@ -441,14 +441,12 @@ __global__ void __launch_bounds__(Form<DT, NT>::THREADS, 1)
                     float f[8];
 #pragma unroll
                     for (int k = 0; k < 8; ++k) f[k] = l == 0.0f ? 0.0f : __uint_as_float(o[i + k]) * (part_at ? 1.0f : inv);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) bad |= !(fabsf(f[k]) < INFINITY);
                     if (part_at) {
                         float4 *q = reinterpret_cast<float4 *>(part_at + (int64_t)pr * d + e + i);
                         q[0] = make_float4(f[0], f[1], f[2], f[3]), q[1] = make_float4(f[4], f[5], f[6], f[7]);
-                        continue;
-                    }
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) bad |= !(fabsf(f[k]) < INFINITY);
-                    if (vec_y) {
+                    } else if (vec_y) {
                         *reinterpret_cast<uint4 *>(y + e + i) = make_uint4(pack2<T>(f[0], f[1]), pack2<T>(f[2], f[3]), pack2<T>(f[4], f[5]), pack2<T>(f[6], f[7]));
                     } else {
 #pragma unroll
@@ -456,8 +454,16 @@ __global__ void __launch_bounds__(Form<DT, NT>::THREADS, 1)
                     }
                 }
             }
-            for (uint32_t again = __ballot_sync(0xffffffffu, bad && ok); again; again &= again - 1)
-                attend_again<T>(p, w.b, w.head, row - lane + __ffs(again) - 1);
+            if (bad) *reinterpret_cast<volatile int *>(&sh.again) = 1;
+        }
+        // such rows, when every piece of the block is done: no other warp waits for these then
+        bar_wait(1, 128 * NT);
+        if (*reinterpret_cast<volatile int *>(&sh.again) && ok) {
+            pieces.rewind(sh.start);
+            for (Piece w; pieces.next(p, w);) {
+                const int rows = (int)min((int64_t)128 * NT, (int64_t)w.past.s.len * p.group - (int64_t)w.tile * (128 * NT));
+                for (int i = warp; i < rows; i += 4 * NT) attend_again<T, 16>(p, w.b, w.head, w.tile, i, w.u0, w.u1, w.slot);
+            }
         }
     }
     tc_fence_before();

@@ -15,9 +15,11 @@ constexpr float LOG2E = 1.4426950408889634f;
 // ------------------------------------------------------------------- join
 // The items are counted again, and WPR warps take a row of one: its parts in turn, a lane eight values, and the
 // warps' sums in order.  used: rows of an item that there can be.  (Four warps where an item has many parts, one where
-// there are many items: for 64 sequences of 8 heads, from cold caches, one warp a row takes 10.5 us, four take 15.5.)
+// there are many items: for 64 sequences of 8 heads, from cold caches, one warp a row takes 10.5 us, four take 15.5.
+// 64 registers: two blocks of it then fit beside the three of the kernel before, and count the items while that one ends:
+// that case takes 186 us; with 72, of which one fits, 197.)
 template <typename T, int WPR>
-__global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant__ AttnP p, int used) {
+__global__ void __launch_bounds__(128, 8) attend_join_kernel(const __grid_constant__ AttnP p, int used) {
     constexpr int W = 4;
     __shared__ float so[W][256], sm[W], sl[W];
     griddep_launch();
@@ -57,24 +59,38 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
     const int c0 = (int)(u0 / n), c1 = (int)((u1 - 1) / n);
     if (c0 == c1) return;  // one block had all of it
     auto part = [&](int c) { return part_of_slot(p, 2 * c + (c == c0 && u0 != c0 * n)); };
-    float m = -INFINITY;
-    for (int c = c0 + sub * 32 + lane; c <= c1; c += 32 * WPR) m = fmaxf(m, part(c)[(int64_t)p.rows * d + r]);
-#pragma unroll
-    for (int o = 16; o; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if constexpr (WPR > 1) {
-        if (lane == 0) sm[warp] = m;
-        __syncthreads();
-        m = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    float m = -INFINITY, l = 0.0f;
+    for (int c = c0 + sub * 32 + lane; c <= c1; c += 32 * WPR) {
+        const float *f = part(c) + (int64_t)p.rows * d + r;
+        const float up = fmaxf(m, f[0]), base = up == -INFINITY ? 0.0f : up;
+        l = fmaf(l, exp2f(m - base), f[p.rows] * exp2f(f[0] - base));
+        m = up;
     }
-    const float base = m == -INFINITY ? 0.0f : m;
-    float o[8], l = 0.0f;
+    float top = m;
+#pragma unroll
+    for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    if constexpr (WPR > 1) {
+        if (lane == 0) sm[warp] = top;
+        __syncthreads();
+        top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
+    }
+    const float base = top == -INFINITY ? 0.0f : top;
+    l *= exp2f(m - base);
+#pragma unroll
+    for (int o = 16; o; o /= 2) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if constexpr (WPR > 1) {
+        if (lane == 0) sl[warp] = l;
+        __syncthreads();
+        l = (sl[0] + sl[1]) + (sl[2] + sl[3]);
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    float o[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = 0.0f;
 #pragma unroll 4
     for (int c = c0 + sub; c <= c1; c += WPR) {
         const float *f = part(c);
-        const float w = exp2f(f[(int64_t)p.rows * d + r] - base);
-        l = fmaf(f[(int64_t)p.rows * d + p.rows + r], w, l);
+        const float w = exp2f(f[(int64_t)p.rows * d + r] - base) * inv;  // (so that no sum is beyond the largest value)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int e = 4 * lane + 128 * i;
@@ -88,28 +104,26 @@ __global__ void __launch_bounds__(128) attend_join_kernel(const __grid_constant_
     if constexpr (WPR > 1) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) *reinterpret_cast<float4 *>(&so[warp][4 * lane + 128 * i]) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-        if (lane == 0) sl[warp] = l;
         __syncthreads();
         if (warp) return;
-        l = (sl[0] + sl[1]) + (sl[2] + sl[3]);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int e = 4 * lane + 128 * (i / 4) + i % 4;
             o[i] = (so[0][e] + so[1][e]) + (so[2][e] + so[3][e]);
         }
     }
-    const float f = l == 0.0f ? 0.0f : 1.0f / l;
     T *y = static_cast<T *>(p.h.y) + t * p.h.ldy + (int64_t)qh * p.h.hy;
-    bool bad = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int e = 4 * lane + 128 * (i / 4) + i % 4;
         if (e >= d) continue;
-        const float v = l == 0.0f ? 0.0f : o[i] * f;
-        stf(y + e, v);
-        bad |= !(fabsf(v) < INFINITY);
+        if (fabsf(o[i]) == INFINITY) {  // by rounding, where no part is: the largest value
+            bool infinite = false;
+            for (int c = c0; c <= c1; ++c) infinite |= fabsf(part(c)[r * d + e]) == INFINITY;
+            if (!infinite) o[i] = copysignf(largest_of<T>(), o[i]);
+        }
+        stf(y + e, l == 0.0f ? 0.0f : o[i]);
     }
-    if (__any_sync(0xffffffffu, bad)) attend_again<T>(p, b, head, row);
 }
 
 // ------------------------------------------------------------------ choice

@@ -3,7 +3,7 @@ import math
 
 import pytest
 
-from test_gpu_attention_forms import Case
+from test_gpu_attention_forms import Case, tdt
 
 pytestmark = pytest.mark.gpu
 
@@ -74,7 +74,12 @@ def test_fp32_value_that_rounds_to_infinity_in_fewer_bits():
     c = Case("f32", "plain", [1], [0], 2, 1, 32, 16, seed=4)
     c.t[1][..., 3], c.t[1][..., 5] = torch.finfo(torch.float32).max, -torch.finfo(torch.float32).max
     n, i = at(c, 0, 0)
-    assert torch.equal(c.run(), c.t[1][n, 0, i].expand_as(c.q))
+    y, v = c.run(), c.t[1][n, 0, i].expand_as(c.q)
+    assert torch.equal(y[..., 3], v[..., 3]) and torch.equal(y[..., 5], v[..., 5])
+    # The weight is 1.  A value goes in as its nearest tf32 (11 bits; the rest is at most 2^-11 of it) and that rest, of which the
+    # tensor cores take 11 bits: what they drop is below 2^-10 of the rest, 2^-21 of the value; the sum and its scaling are 3 roundings
+    # of 2^-24, one of them truncated: below 2^-21 too.
+    assert ((y - v).abs() <= 2.0 ** -20 * v.abs()).all()
 
 
 @pytest.mark.parametrize("new, before", SIZES + [([1, 3, 1], [2500, 40, 900])])
@@ -109,3 +114,66 @@ def test_codes_behind_what_is_seen_do_not_matter(dt, new, before):
         if i + 1 + j < c.page:
             c.t[2][n, :, i + 1 + j], c.t[3][n, :, i + 1 + j] = far, far
     assert torch.equal(c.run(), want)
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("new, before", SIZES)
+def test_the_largest_values(dt, new, before):
+    """An average of largest values is one, although their sum is beyond the range."""
+    import torch
+    top = torch.finfo(tdt(dt)).max
+    c = Case(dt, "plain", new, before, 4, 2, 64, 16, seed=7)
+    c.t[1][..., 3], c.t[1][..., 9] = top, -top
+    y = c.run()
+    # (weights, their sum and the division are off by some 2^-20 in all; in fp16 and bf16 a result next to the top rounds to it)
+    for at_, want in ((3, top), (9, -top)):
+        assert ((y[..., at_].double() - want).abs() <= top * (2.0 ** -18 if dt == "f32" else 0)).all()
+    assert y.isfinite().all()
+
+
+FORMS = [([90], [200], 4, 2, 64, 16), ([200], [0], 4, 2, 128, 128), ([90], [0], 2, 1, 256, 64), ([100, 70], [3000, 10], 4, 2, 256, 32),
+         ([130, 1, 90], [2500, 900, 300], 4, 1, 128, 64), ([6, 1], [2000, 90], 4, 2, 64, 16)]
+
+
+@pytest.mark.parametrize("dt, kind", [("f32", "plain"), ("f16", "plain"), ("bf16", "plain"), ("f16", "q8"), ("bf16", "q8"), ("f32", "q8")])
+@pytest.mark.parametrize("new, before, q_heads, heads, dim, page", FORMS)
+@pytest.mark.parametrize("what", ["key", "value", "late value"])
+def test_nan_reaches_those_that_see_it(dt, kind, new, before, q_heads, heads, dim, page, what):
+    """One NaN in a key or value of the first sequence: rows before it and other sequences and heads stay, those behind it are NaN (of a value:
+    in its place)."""
+    import torch
+    c = Case(dt, kind, new, before, q_heads, heads, dim, page, seed=8)
+    want = c.run()
+    j = before[0] + new[0] - 3 if what == "late value" else before[0] // 2 + 1
+    n, i = at(c, 0, j)
+    if kind == "q8":
+        c.t[2 if what == "key" else 3][n, 0, i] = math.nan
+    else:
+        c.t[0 if what == "key" else 1][n, 0, i, 5] = math.nan
+    y = c.run()
+    nan = torch.zeros_like(y, dtype=torch.bool)
+    rows = slice(max(0, j - before[0]), new[0])
+    nan[rows, :q_heads // heads, :] = True
+    if kind == "plain" and what != "key":
+        nan[rows, :q_heads // heads, :5] = nan[rows, :q_heads // heads, 6:] = False
+    assert torch.equal(y.isnan(), nan)
+    if kind == "plain":
+        c.t[0][n, 0, i, 5] = c.t[1][n, 0, i, 5] = 0  # (what the others do not see)
+    else:
+        c.t[2][n, 0, i] = c.t[3][n, 0, i] = 1
+    # (what was computed again is off by fp32's roundings, what was not by those that it had)
+    tol = 4 * 2.0 ** {"f32": -18, "f16": -10, "bf16": -7}[dt] * c.values()[1].abs().max()
+    assert ((y.double() - want.double()).abs()[~nan] <= tol).all()
+    assert torch.equal(y[new[0]:], want[new[0]:]) and torch.equal(y[:, q_heads // heads:], want[:, q_heads // heads:])
+
+
+@pytest.mark.parametrize("dt", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("new, before", SIZES)
+def test_a_value_of_infinity_or_nan_that_nothing_weighs(dt, new, before):
+    """Every score is -inf: zeros, whatever the values are."""
+    c = Case(dt, "plain", new, before, 4, 1, 64, 16, seed=9)
+    c.t[0].zero_()
+    c.t[0][:, :, :, 0] = -math.inf
+    c.q[..., 0] = 1.0
+    c.t[1][..., 2], c.t[1][..., 3] = math.nan, math.inf
+    assert not c.run().any()
