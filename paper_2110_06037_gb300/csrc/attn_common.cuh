@@ -74,7 +74,7 @@ __device__ __forceinline__ Past past_of(const AttnP &p, int b) {
     r.ctx = r.s.slot >= 0 ? (int32_t)ctx : 0;
     const bool mine = r.s.len > p.lo && r.s.len <= p.hi;
     r.tiles = mine ? (int32_t)(((int64_t)r.s.len * p.group + p.rows - 1) / p.rows) : 0;
-    r.units = max(1, (r.ctx + p.keys - 1) / p.keys);
+    r.units = max(1, (r.ctx - 1) / p.keys + 1);  // (a sum would leave 32 bits)
     return r;
 }
 // units of a sequence (whole: its items)

@@ -180,8 +180,9 @@ __global__ void __launch_bounds__(Form<DT, NT>::THREADS, 1)
     };
     // the page of this lane's part of a tile of keys, `of` keys, -1: none
     auto page_of = [&](const Piece &w, int j, int of) {
+        if (lane * of >= KT) return -1;
         const int key = (w.u0 + j) * KT + lane * of;
-        if (lane * of >= KT || key >= w.past.ctx) return -1;
+        if (key >= w.past.ctx) return -1;
         const int n = p.t.at[(int64_t)w.past.s.slot * p.t.width + (key >> shift)];
         return n >= 0 && n < p.c.pages ? n : -1;
     };

@@ -177,3 +177,27 @@ def test_a_value_of_infinity_or_nan_that_nothing_weighs(dt, new, before):
     c.q[..., 0] = 1.0
     c.t[1][..., 2], c.t[1][..., 3] = math.nan, math.inf
     assert not c.run().any()
+
+
+@pytest.mark.parametrize("dt, new", [("f32", 1), ("f16", 1), ("bf16", 1), ("bf16", 5), ("f16", 70), ("bf16", 70)])
+def test_positions_up_to_the_last(dt, new):
+    """A sequence that ends at position 2^31 - 2, of whose pages the first, one in the middle and the last two exist."""
+    import torch
+    import paper_2110_06037_gb300 as sn
+    width, page, dim = 1 << 23, 256, 64
+    g = torch.Generator(device="cuda").manual_seed(10)
+    k, v = (torch.randn(4, 1, page, dim, generator=g, device="cuda").to(tdt(dt)) for _ in range(2))
+    table = torch.full((1, width), -1, dtype=torch.int32, device="cuda")
+    there = [0, 5000001, width - 2, width - 1]
+    for n, i in enumerate(there):
+        table[0, i] = n
+    pos = 2 ** 31 - 1 - new
+    q = torch.randn(new, 1, dim, generator=g, device="cuda").to(tdt(dt))
+    y = sn.KVCache(k, v).attend(q, table, offsets=torch.tensor([0, new], dtype=torch.int32, device="cuda"), max_len=new,
+                                pos=torch.tensor([pos], dtype=torch.int32, device="cuda"))
+    at_ = torch.cat([i * page + torch.arange(page, device="cuda") for i in there])
+    s = q[:, 0].double() @ k[:, 0].flatten(0, 1).double().T / 8
+    s = s.masked_fill(at_[None] > pos + torch.arange(new, device="cuda")[:, None], -math.inf)
+    want = torch.softmax(s, dim=1) @ v[:, 0].flatten(0, 1).double()
+    # scores of some 5 in magnitudes, off by 2 (dim + 8) 2^-24 of these; weights and results rounded once (prompts: both)
+    assert ((y[:, 0].double() - want).abs() <= {"f32": 2.0 ** -14, "f16": 2.0 ** -9, "bf16": 2.0 ** -6}[dt] * v.abs().max()).all()
