@@ -13,7 +13,7 @@
 // is brought to 2^14, so that a weight is off by 2^-22 of itself or 2^-39 of the largest.
 //
 // Codes: q and codes go in as fp16 (codes exact; q times a power of two that brings a row's largest to 2^10, what is
-// below 2^-34 of that is lost; fp32 queries as two parts).  The keys' scales are factors of the scores.  A value's scale
+// below 2^-34 of that is lost, up to a power of 120; fp32 queries as two parts).  The keys' scales are factors of the scores.  A value's scale
 // is 2^e f, f in [1, 2): e goes into the exponent and f into the weight,
 //   P_j = 2^(s_j + e_j - m) f_j,   sum of weights += 2^(s_j + e_j - m) 2^-e_j,
 // so that P is within fp16's range.  With e from -76 to 24 no sum of weights is infinite, and what 2^(s_j + e_j - m) loses
@@ -189,7 +189,7 @@ __global__ void __launch_bounds__(32 * Form<T, C, DT, NB>::WARPS, Form<T, C, DT,
                 }
 #pragma unroll
                 for (int o = 16; o; o /= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                const int e = min(max(137 + 127 - (int)(__float_as_uint(top) >> 23), 1), 227);  // the factor's exponent, of 127 + 10 - (e - 127)
+                const int e = min(max(137 + 127 - (int)(__float_as_uint(top) >> 23), 1), 247);  // the factor's exponent, of 127 + 10 - (e - 127)
                 const float f = __uint_as_float((uint32_t)e << 23);
                 if (lane == 0) rf[r] = __uint_as_float((uint32_t)(254 - e) << 23);
 #pragma unroll

@@ -201,3 +201,14 @@ def test_positions_up_to_the_last(dt, new):
     want = torch.softmax(s, dim=1) @ v[:, 0].flatten(0, 1).double()
     # scores of some 5 in magnitudes, off by 2 (dim + 8) 2^-24 of these; weights and results rounded once (prompts: both)
     assert ((y[:, 0].double() - want).abs() <= {"f32": 2.0 ** -14, "f16": 2.0 ** -9, "bf16": 2.0 ** -6}[dt] * v.abs().max()).all()
+
+
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("new, before", SIZES)
+@pytest.mark.parametrize("power", [-121, -115, -100, 60, 110, 121])
+def test_codes_with_far_queries(dt, new, before, power):
+    """Queries near the ends of the range, and keys' scales that bring the scores back."""
+    c = Case(dt, "q8", new, before, 4, 2, 64, 16, seed=11)
+    c.q.mul_(2.0 ** power)
+    c.t[2].mul_(2.0 ** -power)
+    c.check(c.run(), 2.0 ** (-11 if dt == "bf16" else -21))
