@@ -123,6 +123,50 @@ def test_prompts(dt, new, before, q_heads, heads, dim, page):
         assert torch.equal(c.run(), y)
 
 
+# What weights (and fp32 values) are off by: two parts of 16 bits; in tf32 each of two factors by 2^-21 (what is dropped of its
+# second part) and the product of the second parts, 2^-22, left out; codes: two parts of fp16, one for bf16.
+FEW = {("f32", "plain"): 2.0 ** -19, ("f16", "plain"): 2.0 ** -22, ("bf16", "plain"): 2.0 ** -16, ("f32", "q8"): 2.0 ** -21, ("f16", "q8"): 2.0 ** -21,
+       ("bf16", "q8"): 2.0 ** -11}
+# Enough to do that items have more than 8 rows (tokens times the heads that share): up to 12 rows go by 16, up to 48 by 32.
+# 450 keys: a block takes whole items; 740: units are shared out
+ROWS = {12: [3, 3, 2, 1] * 12, 48: [12, 7, 9, 0, 5] * 4}
+
+
+@pytest.mark.parametrize("dt, kind", FEW)
+@pytest.mark.parametrize("dim, rows, context, heads", [
+    (48, 12, 450, 7), (64, 12, 740, 5), (64, 48, 450, 7), (16, 48, 740, 5), (112, 12, 740, 5), (128, 12, 450, 7), (128, 48, 740, 5), (80, 48, 450, 7),
+    (208, 12, 450, 7), (256, 12, 740, 5), (256, 48, 450, 7), (144, 48, 740, 5)])
+def test_few_rows(dt, kind, dim, rows, context, heads):
+    import torch
+    new = ROWS[rows]
+    c = Case(dt, kind, new, [max(0, context - n - 7 * i) for i, n in enumerate(new)], 4 * heads, heads, dim, 64, seed=dim + rows)
+    y = c.run()
+    c.check(y, FEW[dt, kind])
+    assert torch.equal(c.run(), y)
+
+
+@pytest.mark.parametrize("dt, kind", [k for k in FEW if k[0] == "f32" or k[1] == "q8"])
+@pytest.mark.parametrize("new, before, q_heads, heads, dim, page", [
+    ([100] * 14, list(range(14)), 16, 4, 128, 32), ([900, 300], [0, 77], 8, 2, 128, 64), ([700, 0, 133], [5, 9, 600], 12, 3, 64, 16),
+    ([333, 401], [100, 0], 8, 2, 256, 256), ([1100], [40], 5, 1, 96, 128)])
+def test_prompts_by_few_rows(dt, kind, new, before, q_heads, heads, dim, page):
+    """Prompts in fp32 and over codes."""
+    c = Case(dt, kind, new, before, q_heads, heads, dim, page, seed=dim + len(new))
+    c.check(c.run(), FEW[dt, kind])
+
+
+@pytest.mark.parametrize("dt, kind", FEW)
+@pytest.mark.parametrize("new, before, q_heads, heads, dim, page", [
+    # single tokens and drafts in items of 8 rows, short and shared out, alone and beside prompts; groups that do not divide 8
+    ([1, 1, 1], [0, 15, 700], 8, 8, 128, 16), ([1], [5000], 3, 1, 96, 64), ([2, 0, 3], [1000, 0, 70], 7, 1, 64, 256), ([1, 1], [2000, 30], 20, 1, 240, 32),
+    ([1, 200, 1, 9], [4000, 0, 63, 1500], 8, 2, 128, 128), ([1] * 33, list(range(33)), 4, 4, 32, 16), ([1], [3000], 200, 2, 128, 64)])
+def test_tokens(dt, kind, new, before, q_heads, heads, dim, page):
+    c = Case(dt, kind, new, before, q_heads, heads, dim, page, seed=dim + len(new))
+    y = c.run()
+    part = U[dt] if kind == "plain" and dt != "f32" and max(new) > 64 else FEW[dt, kind]  # (a prompt's weights are one part)
+    c.check(y, part)
+
+
 @pytest.mark.parametrize("dt, kind", [("f32", "plain"), ("bf16", "plain"), ("f16", "q8")])
 @pytest.mark.parametrize("context", [64, 4096])
 def test_rows_behind_empty_sequences_are_left(dt, kind, context):
