@@ -82,13 +82,13 @@ __device__ __forceinline__ int64_t units_of(const AttnP &p, const Past &r) {
     return (int64_t)r.tiles * p.c.heads * (p.blocks ? r.units : 1);
 }
 
-// by one whole warp: the units of all sequences, those before sequence `b` (b >= 0), or the sequence in
-// which unit `at` lies (at >= 0) and those before it
+// by one whole warp: the units of all sequences, and the sequence in which unit `at` lies (at >= 0; b < 0: none) and
+// those before it
 struct Span {
     int64_t all, before;
     int b;
 };
-__device__ __forceinline__ Span span_of(const AttnP &p, int b, int64_t at) {
+__device__ __forceinline__ Span span_of(const AttnP &p, int64_t at) {
     const int lane = threadIdx.x % 32;
     Span r{0, 0, -1};
     for (int b0 = 0; b0 < p.q.batch; b0 += 32) {
@@ -99,7 +99,6 @@ __device__ __forceinline__ Span span_of(const AttnP &p, int b, int64_t at) {
             const int64_t v = __shfl_up_sync(0xffffffffu, up, o);
             if (lane >= o) up += v;
         }
-        if (b >= b0 && b < b0 + 32) r.before = r.all + __shfl_sync(0xffffffffu, up - n, b - b0);
         if (at >= 0 && r.b < 0) {
             const uint32_t in = __ballot_sync(0xffffffffu, at < r.all + up);
             if (in) {
@@ -135,11 +134,11 @@ struct Pieces {
             Span s{0, 0, -1};
             int64_t from = blockIdx.x, to = from + 1;
             if (p.blocks) {
-                s = span_of(p, -1, -1);
+                s = span_of(p, -1);
                 const int64_t n = share_of(p, s.all);
                 from = min(n * (int64_t)blockIdx.x, s.all), to = min(from + n, s.all);
             }
-            if (from < to) s = span_of(p, -1, from);
+            if (from < to) s = span_of(p, from);
             if (s.b < 0) to = from;
             if (threadIdx.x == 0) sh[0] = from, sh[1] = to, sh[2] = s.before, sh[3] = s.b;
         }
