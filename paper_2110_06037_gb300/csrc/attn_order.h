@@ -1,4 +1,4 @@
-// What the end of a piece of prompt attention waits for (attn_prompt.cuh).  Host code too: no CUDA here.
+// When the softmax of prompt attention waits for products (attn_prompt.cuh).  Host code too: no CUDA here.
 #pragma once
 
 #ifdef __CUDACC__
@@ -10,10 +10,12 @@
 namespace sn {
 namespace k {
 
-// A wait by parity tells a phase from the one before it only, so it holds when that one is known to be over.  The last
-// scores of n tiles are asked for behind the product with values `ahead` tiles earlier: when they have come, products
-// 0 to n - 1 - ahead are over, and the next ones may not be.  The end so waits for each product from this one on.
-SN_HOST_DEVICE constexpr int first_open_product(int n, int ahead) { return n > ahead ? n - ahead : 0; }
+// A wait by parity tells a phase from its neighbours only: it holds where the phase before is known to be over and the one
+// after cannot be.  The scores of tile j are asked for behind the product with values `ahead` tiles earlier.  With one in
+// between, two products are open when a piece of n tiles ends, and a wait for the last alone might take the one before the
+// other for it; so the last weights are handed over behind the product before theirs.  (Later it might be too late: with
+// both over, a wait for the first lasts for ever.)
+SN_HOST_DEVICE constexpr bool waits_before_weights(int j, int n, int ahead) { return ahead > 1 && j > 0 && j == n - 1; }
 
 }  // namespace k
 }  // namespace sn

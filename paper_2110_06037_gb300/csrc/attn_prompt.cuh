@@ -18,9 +18,12 @@
 // A weight is rounded once, to the queries' type: off by half a step of the output's type, and independent from
 // key to key.  (fp16: the largest weight is between 2^14 and 2^15, so that one is off by 2^-11 of itself or 2^-39 of the largest.)
 // Products on different accumulators do not keep their order, so the S that takes P's place waits until P has been read.
-// Prompts of 4096 and 777 tokens, 32 heads of 128 over 8, bf16: 188 us, 820 TFLOP/s; a pair of tiles takes some 4800
-// cycles, in which the tensor cores are busy 2048: a tile of rows goes from S through its softmax (3000) to the
-// products before the next S (1700), and two of them side by side do not fill that.
+// A wait by parity holds only where the phase before is known to be over and the one after is not: see attn_order.h.
+// Prompts of 4096 and 777 tokens, 32 heads of 128 over 8, bf16: 187 us a call, 820 TFLOP/s, of which this kernel takes 164 (profiled) and
+// the launches for few rows before it, which find nothing to do there, the rest.  A pair of tiles of rows and a tile of keys take
+// some 4900 cycles of a multiprocessor, the tensor cores busy 46 % of them: a tile goes from S through its softmax to the
+// products before its next S, and two of them side by side do not fill that.  The instances with two tiles spill 164
+// bytes a thread: a row's 128 scores are live at once.
 #pragma once
 
 #include "attn_common.cuh"
@@ -414,11 +417,12 @@ __global__ void __launch_bounds__(Form<DT, NT>::THREADS, 1)
                 }
                 l2 = add_2(sum[0], sum[1]);
                 tmem_stored();
+                if (waits_before_weights(j, n, LA)) must(&sh.pv[t], (sums + j - 1) & 1u, ERR_EPI_WAIT);
                 tc_fence_before();
                 meet();
             }
             if (n) {
-                for (int j = first_open_product(n, LA); j < n; ++j) must(&sh.pv[t], (sums + j) & 1u, ERR_EPI_WAIT);
+                must(&sh.pv[t], (sums + n - 1) & 1u, ERR_EPI_WAIT);
                 tc_fence_after();
             }
             tiles += n, sums += n;

@@ -3,7 +3,7 @@ import math
 
 import pytest
 
-from test_gpu_attention_forms import Case, tdt
+from test_gpu_attention_forms import Case, no_wait_gave_up, tdt  # noqa: F401 (a fixture of every test)
 
 pytestmark = pytest.mark.gpu
 
