@@ -652,10 +652,12 @@ SN_API sn_status sn_kv_read(const sn_kv_cache *c, int32_t dtype, int64_t tokens,
  * over the positions j of the query's own sequence up to its own (token i of a sequence is at
  * pos + i).  q and y are dtype, [tokens][q_heads]; head h reads head h / (q_heads / heads) of the
  * cache, whose dtype is `dtype` or SN_QI8.  max_context: at least every sequence's pos + length
- * (positions from there on are left out; more than 2^31 - 1 count as that many).  A query without keys, or all of whose scores are -inf,
- * gives zeros.  Keys and values that a query does not see do not reach it, whatever they are.
- * A result that is not finite (NaN or infinities among what is seen, or beside it in a prompt), or that codes with scales of
- * values below 2^-76 or from 2^25 on go into, is computed again in fp32, which may take hundreds of times as long. */
+ * (positions from there on are left out; more than 2^31 - 1 count as that many).  A query without
+ * keys, or all of whose scores are -inf, gives zeros.  Keys and values that a query does not see do
+ * not reach it, whatever they are.
+ * A result that is not finite (NaN or infinities among what is seen, or behind it in a prompt), or
+ * that codes with scales of values below 2^-76 or from 2^25 on go into, is computed again in fp32:
+ * as good, but it may take hundreds of times as long. */
 SN_API sn_status sn_attend_workspace(const sn_kv_cache *c, int32_t dtype, int32_t q_heads, int64_t tokens,
                                      int32_t batch, int64_t max_len, int64_t max_context, int64_t *bytes);
 SN_API sn_status sn_attend(const sn_kv_cache *c, int32_t dtype, int32_t q_heads, float scale, int64_t tokens,

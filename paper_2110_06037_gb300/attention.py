@@ -145,7 +145,8 @@ class KVCache:
                stream=None):
         """Attention of the tokens' queries [..., q_heads, dim] over the keys of their sequences up to their own
         position (written before).  q_heads is a multiple of the cache's heads, in that order.  max_context: at least every
-        sequence's pos + length (default: all that the table has room for).  scale: default 1 / sqrt(dim)."""
+        sequence's pos + length (default: all that the table has room for).  scale: default 1 / sqrt(dim).  A result that is
+        not finite is computed again in fp32, which is slow."""
         if stream is None:
             return self._attend(self._at, self.device, q, table, offsets, max_len, pos, max_context, scale, slots, out)
         with _on(stream):

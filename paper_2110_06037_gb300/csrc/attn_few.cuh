@@ -18,9 +18,9 @@
 //   P_j = 2^(s_j + e_j - m) f_j,   sum of weights += 2^(s_j + e_j - m) 2^-e_j,
 // so that P is within fp16's range.  With e from -76 to 24 no sum of weights is infinite, and what 2^(s_j + e_j - m) loses
 // below fp32's range is below 2^-40 of them; a key whose value has another scale makes the row NaN, and
-// attend_again computes it.  What bounds codes is the issue of instructions: to
-// make fp16 of a tile's codes takes half of them.  For bf16 queries P is one part, off by 2^-11 of itself, an eighth of
-// the output's rounding.
+// attend_again computes it.  For bf16 queries P is one part, off by 2^-11 of itself, an eighth of the output's rounding.
+// What bounds codes is the issue of instructions: some 800 a tile of 16 keys, heads of 128 and 8 queries, of which some 200 load
+// the codes and make fp16 of them (20 for 32 dims of keys, 24 of values, and 16 loads of these).
 //
 // fp32 values: products in tf32 of two parts each, hi hi + hi lo + lo hi: off by 2^-21 of a product.  With fp32 queries
 // the products of 16 dims, or of a tile's keys, are summed apart and added to the sums in fp32: the tensor cores truncate what they add

@@ -186,8 +186,13 @@ Plans plans_of(const sn_kv_cache &c, int dt, const AttendArgs &a) {
     // sequences of up to 64 rows go to the form for few queries
     const int n = tensor ? std::max(1, 64 / group) : INT32_MAX;
     // Items of as many rows as there can be, for then the cache is read once; of 8 beside prompts, whose single tokens these
-    // are, and where there is so little to do that more blocks matter more (5 sequences of up to 8 drafted tokens, 6 heads
-    // in fp32, 2500 keys: 48 us by 32 rows and 4 units a block, 24 us by 8 rows and single units)
+    // are, and where there is so little to do that more blocks matter more.  Both, us by 8 rows and by as many as there can be:
+    // 5 sequences of up to 8 drafted tokens, 6 heads of 80 over 2 in fp32, 2500 keys, 28 and 42; 2 of 4 tokens, 16 heads of 128 over 2
+    // in bf16, 3000 keys, 23 and 38; 4 of 8 tokens, 32 over 8, 600 keys, 20 and 40; a prompt of 60 tokens over codes 6.7 and
+    // 13.8; beside a prompt of 2048 tokens, 32 single tokens with 3000 keys each 143 and 242, 3 sequences of 4 tokens 123 and
+    // 149, but one of 16 tokens with 60000 keys 339 and 286 (the rule sees the longest sequence alone).  Where the bound
+    // chooses the other: 16 tokens with 60000 keys, 8 heads over 2, 84 and 80, with 20000 40 and 51; 8 sequences of 5 tokens over
+    // codes, 32 heads over 8, 4000 keys, 69 and 94.
     int64_t rows = std::min<int64_t>(a.q.max_len, n) * group;
     const int64_t units = std::max<int64_t>(1, a.max_context / few::UNIT);
     if ((tensor && a.q.max_len > n) || a.q.tokens * group / 8 * c.heads * units < 16 * sms) rows = std::min<int64_t>(rows, std::max(group, 8));
