@@ -630,6 +630,8 @@ SN_API sn_status sn_head_rope(const sn_rope_params *p, int32_t dtype, int64_t to
  * position of each sequence's first token here.  A position beyond the table, or whose page
  * is outside [0, pages), has no place: nothing is stored for it, it reads as zeros, and
  * attention leaves it out; so has a sequence without a slot.
+ * Entries may share pages, but no two tokens of one sn_kv_write have the same place: which of them is
+ * then stored, of codes and scales each for itself, is not said.
  * sn_kv_write stores the tokens' k and v; sn_kv_read returns those of the tokens' positions in
  * `dtype` (that of the cache, or any for codes: code * scale, rounded once). */
 typedef struct {

@@ -183,3 +183,57 @@ def test_rows_behind_empty_sequences_are_left(dt, kind, context):
     out = torch.full_like(c.q, 7.0)
     c.cache.attend(c.q, ints(np.zeros((3, 300))), offsets=ints([0, 0, 0, 0]), max_len=0, pos=ints([5, 0, 9]), max_context=context, out=out)
     assert bool((out == 7).all())
+
+
+PROMPT_FORMS = [([200, 9, 70], [0, 30, 5], 8, 2, 128, 64), ([90, 1], [200, 0], 4, 2, 48, 16), ([70, 66], [0, 100], 4, 2, 256, 128),
+                ([80, 5], [2500, 3000], 4, 2, 128, 32)]
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("new, before, q_heads, heads, dim, page", PROMPT_FORMS)
+def test_prompt_layouts_and_rows_behind(dt, new, before, q_heads, heads, dim, page):
+    """Heads before tokens, strides that no vector load fits, rows behind the last sequence; scales of both signs and zero."""
+    import torch
+    c = Case(dt, "plain", new, before, q_heads, heads, dim, page, seed=21)
+    want, n = c.run(), len(c.q)
+    kw = dict(**c.args)
+    swapped = c.q.transpose(0, 1).contiguous().transpose(0, 1)
+    out = torch.full((q_heads, n, dim), 7.0, dtype=c.q.dtype, device="cuda").transpose(0, 1)
+    assert c.cache.attend(swapped, ints(c.table), out=out, **kw) is out and torch.equal(out, want)
+    for shift in (0, 1):
+        wide = torch.full((n + 3, q_heads, dim + 3), 7.0, dtype=c.q.dtype, device="cuda")
+        result = wide.clone()
+        wide[:n, :, shift:shift + dim] = c.q
+        c.cache.attend(wide[..., shift:shift + dim], ints(c.table), out=result[..., shift:shift + dim], **kw)
+        assert torch.equal(result[:n, :, shift:shift + dim], want)
+        result[:n, :, shift:shift + dim] = 7
+        assert bool((result == 7).all())
+    minus = c.cache.attend(-c.q, ints(c.table), scale=-1 / math.sqrt(dim), **kw)
+    assert torch.equal(minus, want)
+    c.q.zero_()
+    assert torch.equal(c.run(scale=0.0), c.run())
+
+
+@pytest.mark.parametrize("dt", ["f16", "bf16"])
+@pytest.mark.parametrize("new, before, q_heads, heads, dim, page", PROMPT_FORMS)
+def test_prompts_at_once_and_replayed(dt, new, before, q_heads, heads, dim, page):
+    """Two captured calls replayed on two streams, eager ones between them."""
+    import torch
+    cs = [Case(dt, "plain", new, before, q_heads, heads, dim, page, seed=s) for s in (22, 23)]
+    tables = [ints(c.table) for c in cs]
+    want = [c.run() for c in cs]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for c, t in zip(cs, tables):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(c.cache.attend(c.q, t, **c.args))
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(10):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        eager = cs[0].cache.attend(cs[0].q, tables[0], stream=streams[1], **cs[0].args)
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], want[0]) and torch.equal(outs[1], want[1]) and torch.equal(eager, want[0])
