@@ -63,7 +63,7 @@ __global__ void __launch_bounds__(128, 8) attend_join_kernel(const __grid_consta
     for (int c = c0 + sub * 32 + lane; c <= c1; c += 32 * WPR) {
         const float *f = part(c) + (int64_t)p.rows * d + r;
         const float up = fmaxf(m, f[0]), base = up == -INFINITY ? 0.0f : up;
-        l = fmaf(l, exp2f(m - base), f[p.rows] * exp2f(f[0] - base));
+        l = fmaf(l, ex2(m - base), f[p.rows] * ex2(f[0] - base));
         m = up;
     }
     float top = m;
@@ -75,7 +75,7 @@ __global__ void __launch_bounds__(128, 8) attend_join_kernel(const __grid_consta
         top = fmaxf(fmaxf(sm[0], sm[1]), fmaxf(sm[2], sm[3]));
     }
     const float base = top == -INFINITY ? 0.0f : top;
-    l *= exp2f(m - base);
+    l *= ex2(m - base);
 #pragma unroll
     for (int o = 16; o; o /= 2) l += __shfl_xor_sync(0xffffffffu, l, o);
     if constexpr (WPR > 1) {
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(128, 8) attend_join_kernel(const __grid_consta
 #pragma unroll 4
     for (int c = c0 + sub; c <= c1; c += WPR) {
         const float *f = part(c);
-        const float w = exp2f(f[(int64_t)p.rows * d + r] - base) * inv;  // (so that no sum is beyond the largest value)
+        const float w = ex2(f[(int64_t)p.rows * d + r] - base) * inv;  // (so that no sum is beyond the largest value)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int e = 4 * lane + 128 * i;
@@ -113,16 +113,25 @@ __global__ void __launch_bounds__(128, 8) attend_join_kernel(const __grid_consta
         }
     }
     T *y = static_cast<T *>(p.h.y) + t * p.h.ldy + (int64_t)qh * p.h.hy;
+    bool infinite = false;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const int e = 4 * lane + 128 * (i / 4) + i % 4;
         if (e >= d) continue;
-        if (fabsf(o[i]) == INFINITY) {  // by rounding, where no part is: the largest value
-            bool infinite = false;
-            for (int c = c0; c <= c1; ++c) infinite |= fabsf(part(c)[r * d + e]) == INFINITY;
-            if (!infinite) o[i] = copysignf(largest_of<T>(), o[i]);
-        }
         stf(y + e, l == 0.0f ? 0.0f : o[i]);
+        infinite |= fabsf(o[i]) == INFINITY;
+    }
+    if (!infinite) return;
+    // by rounding, where no part is: the largest value
+#pragma unroll 1
+    for (int i = 0; i < 8; ++i) {
+        const int e = 4 * lane + 128 * (i / 4) + i % 4;
+        if (e >= d) continue;
+        const float now = ldf(y + e);
+        if (fabsf(now) < INFINITY) continue;
+        bool any = false;
+        for (int c = c0; c <= c1; ++c) any |= !(fabsf(part(c)[r * d + e]) < INFINITY);
+        if (!any && now == now) stf(y + e, copysignf(largest_of<T>(), now));
     }
 }
 
